@@ -18,6 +18,14 @@
  *                          of consecutive sentences is not above a threshold.
  *   retrieval_metrics      P@k and MRR@k of retrieved index lists against one positive per
  *                          query.
+ * and the encoder's operators over the same packed sequences, in bf16 or fp16:
+ *   packed_attention_fwd, packed_attention_bwd
+ *                          softmax attention with grouped heads over packed sequences of
+ *                          different lengths, its gradients, and one-token calls over a cache.
+ *   adapter_linear_fwd, adapter_linear_bwd
+ *                          a shared projection with a low-rank adapter per request beside it,
+ *                          and its gradients.
+ *   rotary_apply           rotation of queries and keys by their position, and back.
  *
  * Conventions shared by every entry point
  *   Pointers.  Every array argument is a DEVICE pointer on the current HIP device, owned by
@@ -80,6 +88,11 @@ typedef int32_t hpr_status;
  *     longer document scores NaN, which makes the loss NaN).
  *   dense_ip_topk: dim % 8 == 0, 8 <= dim <= 8192; n < 2^31.
  *   semantic_chunk: dim % 8 == 0, 8 <= dim <= 4096; 1 <= n < 2^31.
+ *   packed_attention_*: dim % 8 == 0, 8 <= dim <= 128; heads a multiple of kv_heads, at most 32
+ *     heads per kv head; strides of q, k and v multiples of 8 in [0, 2^22); fewer than 2^31 rows.
+ *   adapter_linear_*: k % 8 == 0, m % 8 == 0, both <= 65536; 1 <= r <= 128; fewer than 2^31 rows.
+ *   rotary_apply: rot % 16 == 0, 16 <= rot <= dim, dim % 8 == 0, dim <= 1024; strides multiples of
+ *     8; fewer than 2^31 rows.
  */
 
 /* ---------------------------------------------------------------------------------------------
@@ -310,6 +323,131 @@ hpr_status hpr_scale_f32(float* x, int64_t n, const float* scale, void* stream);
 hpr_status hpr_scale_grads_bf16(const float* dq, int64_t n_q, uint16_t* dq_out, const float* dd,
                                 int64_t n_d, uint16_t* dd_out, const float* scale, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * packed_attention_fwd -- softmax attention with grouped heads over packed sequences.
+ *
+ * The attention of the encoder whose token embeddings the MaxSim calls score (Sec. 3.2.1 fine-tunes
+ * a causal encoder with grouped heads and a bidirectional one).  Sequence s has the query rows
+ * q_off[s] .. q_off[s+1]-1 and the first k_len[s] (NULL: all) of the key rows k_off[s] ..
+ * k_off[s+1]-1, lq and lk of them, which may differ: with lq < lk the queries are the last ones
+ * (a question after its cached context, or one new token: lq = 1).  Query head h reads kv head
+ * h / (heads / kv_heads); query i sees key j when
+ *     not causal, or  j <= i + lk - lq  and (window = 0 or j > i + lk - lq - window)
+ *     out[i] = sum_j softmax_j(scale <q_i, k_j>) v_j      over the keys that it sees
+ *     lse[i] = log sum_j exp(scale <q_i, k_j>)
+ * A row that sees no key gets out = 0 and lse = -inf.  Any sequence may be empty on either side.
+ * Arithmetic: 16-bit products accumulated in fp32 (MFMA); maxima, exponentials and sums in fp32; the
+ * exponentials are rounded to 16 bits as operands of the product with v, and out once at the end.
+ * Sums have a fixed order: results are bit-reproducible.
+ *
+ *   q [n_q, heads, dim], k and v [n_k, kv_heads, dim]: dtype HPR_BF16 or HPR_F16, each with its row
+ *     and head strides in elements (a head's values are contiguous), so that they can be views of
+ *     one projection's output
+ *   q_off, k_off int64 [n_seq + 1]; k_len int64 [n_seq] or NULL
+ *   out [n_q, heads, dim] dense; lse fp32 [n_q, heads] or NULL
+ *   ws     workspace of packed_attention_workspace_size(d) bytes (may be 0)
+ * Preconditions, like those above not checked on the device: both offsets start at 0, never fall
+ * and end at n_q and n_k; every row that some query sees is finite.  Key rows past k_len[s] are not
+ * read.
+ * ------------------------------------------------------------------------------------------- */
+#define HPR_BF16 0
+#define HPR_F16 1
+
+typedef struct {
+  int64_t n_q, n_k;                 /* query rows, key rows                                     */
+  int64_t q_row, q_head;            /* strides in elements                                      */
+  int64_t k_row, k_head;
+  int64_t v_row, v_head;
+  int32_t n_seq, heads, kv_heads, dim;
+  int32_t dtype, causal, window;    /* HPR_BF16 or HPR_F16; 0 or 1; 0: none, else needs causal  */
+  float scale;                      /* positive                                                 */
+} hpr_attention;
+
+size_t packed_attention_workspace_size(const hpr_attention* d);
+hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const uint16_t* k,
+                                const uint16_t* v, const int64_t* q_off, const int64_t* k_off,
+                                const int64_t* k_len, uint16_t* out, float* lse,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * packed_attention_bwd -- the gradients of packed_attention_fwd.
+ *
+ * With p the forward's probabilities (recomputed from lse), delta_i = <dout_i, out_i> and
+ * ds_ij = p_ij (<dout_i, v_j> - delta_i):
+ *     dv_j = sum_i p_ij dout_i;  dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i
+ * those of a kv head summed over its query heads.  p and ds are rounded to 16 bits as operands of the
+ * second products; all sums are fp32 with a fixed order (no atomics).  Rows that see no key and keys
+ * that no row sees get zeros.
+ *
+ *   dout [n_q, heads, dim] dense; out and lse as the forward wrote them
+ *   dq [n_q, heads, dim], dk and dv [n_k, kv_heads, dim], dense; dq, or dk and dv together, may be NULL
+ *   ws     workspace of packed_attention_bwd_workspace_size(d) bytes
+ * ------------------------------------------------------------------------------------------- */
+size_t packed_attention_bwd_workspace_size(const hpr_attention* d);
+hpr_status packed_attention_bwd(const hpr_attention* d, const uint16_t* dout, const uint16_t* q,
+                                const uint16_t* k, const uint16_t* v, const uint16_t* out,
+                                const float* lse, const int64_t* q_off, const int64_t* k_off,
+                                const int64_t* k_len, uint16_t* dq, uint16_t* dk, uint16_t* dv,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * adapter_linear_fwd -- a shared projection with a low-rank adapter per request beside it.
+ *
+ * The encoder is fine-tuned through low-rank adapters beside frozen weights (Sec. 3.2.1); one call
+ * may hold rows of many requests, each with its own adapter.  Row t of request s (req_off[s] <= t <
+ * req_off[s+1]) with adapter i = adapter[s] (negative, or not below n_ad: none):
+ *     h[t] = scale[i] A[i] x[t]        y[t] = W x[t] + B[i] h[t]
+ * Arithmetic: 16-bit products accumulated in fp32 (MFMA), h rounded once to 16 bits, y once.  Sums
+ * have a fixed order.  Requests may be empty; rows of no request get W x.
+ *
+ *   x [n, k], W [m, k], A [n_ad, r, k], B [n_ad, m, r]: dtype HPR_BF16 or HPR_F16, dense
+ *   scale fp32 [n_ad]; req_off int64 [n_req + 1] (starts at 0, never falls, ends at n); adapter
+ *   int32 [n_req]
+ *   h [n, r rounded up to 16]: output, the gradients need it; rows without an adapter unwritten
+ *   y [n, m]: output
+ * ------------------------------------------------------------------------------------------- */
+hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uint16_t* w, int32_t m,
+                              const uint16_t* a, const uint16_t* b, int32_t r, int32_t n_ad,
+                              const float* scale, const int64_t* req_off, const int32_t* adapter,
+                              int32_t n_req, int32_t dtype, uint16_t* h, uint16_t* y, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * adapter_linear_bwd -- the gradients of adapter_linear_fwd (W and scale are frozen).
+ *
+ *     g[t] = scale[i] B[i]^T dy[t]     dx[t] = W^T dy[t] + A[i]^T g[t]
+ *     dA[i] = sum_t g[t] x[t]^T        dB[i] = sum_t dy[t] h[t]^T      over the adapter's rows
+ * g is rounded once to 16 bits; the sums are fp32, in the order of the rows' blocks (no atomics).
+ * Adapters without a row get zeros.  dx, da and db may each be NULL.
+ *   ws     workspace of adapter_linear_bwd_workspace_size(...) bytes
+ * ------------------------------------------------------------------------------------------- */
+size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_t r, int32_t n_ad,
+                                         int32_t n_req);
+hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, int32_t k,
+                              const uint16_t* w, int32_t m, const uint16_t* a, const uint16_t* b,
+                              int32_t r, int32_t n_ad, const float* scale, const int64_t* req_off,
+                              const int32_t* adapter, int32_t n_req, int32_t dtype,
+                              const uint16_t* h, uint16_t* dx, uint16_t* da, uint16_t* db, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * rotary_apply -- rotation of queries and keys by their position.
+ *
+ * With c = cos[pos[t]] and s = sin[pos[t]] (tables fp32 [n_pos, rot / 2]; inverse: s negated, which
+ * is the gradient), values j and j + rot / 2 of every head of row t, j < rot / 2:
+ *     (x_j c_j - x_{j+rot/2} s_j,  x_{j+rot/2} c_j + x_j s_j)
+ * and values past rot are copied.  In fp32, rounded once.  A position outside [0, n_pos) makes the
+ * row's rotated values NaN.
+ *
+ *   q [n, q_heads, dim] and k [n, k_heads, dim] (k_heads may be 0) with row and head strides in
+ *   elements; dtype HPR_BF16 or HPR_F16; pos int32 [n]; q_out and k_out dense, not overlapping the
+ *   inputs
+ * ------------------------------------------------------------------------------------------- */
+hpr_status rotary_apply(const uint16_t* q, int64_t q_row, int64_t q_head, int32_t q_heads,
+                        const uint16_t* k, int64_t k_row, int64_t k_head, int32_t k_heads, int64_t n,
+                        int32_t dim, int32_t rot, const int32_t* pos, const float* cos_table,
+                        const float* sin_table, int64_t n_pos, int32_t inverse, int32_t dtype,
+                        uint16_t* q_out, uint16_t* k_out, void* stream);
+
 /* Calibration for benchmarks: what the device sustains, to report beside the published peaks.
  *   hpr_mfma_calibration  launches a kernel of 8 waves per CU, each running `iters` iterations
  *                         of four independent v_mfma_f32_32x32x16_bf16 on register operands (no
@@ -333,7 +471,8 @@ hpr_status hpr_read_calibration(const void* buf, int64_t bytes, uint32_t* sink, 
  * "infonce_pool" (the total loss: InfoNCE and the pooling in one launch), "contrastive", "grad_q",
  * "grad_d", "scale_grads", "dense_sample" (the sample's scores, or every score where they are all
  * stored), "dense_scan", "dense_merge", "dense_fallback", "semantic_chunk", "retrieval_metrics",
- * "mfma_calibration", "read_calibration"), returns the sum of their durations in milliseconds and
+ * "attn_fwd" and "attn_bwd" (all launches of a call), "adapter_shrink", "adapter_expand",
+ * "adapter_transpose", "adapter_outer", "rotary", "mfma_calibration", "read_calibration"), returns the sum of their durations in milliseconds and
  * the launch count (0 and 0 for any other name, such as "pool", which is no launch of its own any
  * more), and forgets them. */
 hpr_status hpr_kernel_timing(int32_t enable);

@@ -17,6 +17,17 @@ fallback: if the library is not built, or a call fails, an exception is raised.
     retrieval_metrics(idx, positive, k)           -> dict(p_at_k, mrr_at_k, ranks) on the device
     csr_validate(off, n_tok)                      -> (status name, first bad document or -1)
 
+The encoder's operators over the same packed sequences, in bf16 or fp16:
+
+    packed_attention(q, k, v, q_off, ...)         -> out like q, with autograd to q, k and v
+    packed_attention_fwd(q, k, v, q_off, ...)     -> dict(out, lse)
+    packed_attention_bwd(dout, q, k, v, out, lse, q_off, ...) -> dict(dq, dk, dv)
+    adapter_linear(x, W, A, B, scale, off, adapter) -> y [n, m], with autograd to x, A and B
+    adapter_linear_fwd(x, W, A, B, scale, off, adapter)       -> dict(y, h)
+    adapter_linear_bwd(dy, x, W, A, B, scale, off, adapter, h) -> dict(dx, da, db)
+    rotary(q, k, pos, cos, sin)                   -> (q, k) rotated, with autograd to q and k
+    rotary_apply(q, k, pos, cos, sin, inverse)    -> (q, k) rotated
+
 Q and D are bf16 CUDA tensors ([nq, lq, dim] and [n_tok, dim]); off is int64 [n_docs + 1];
 pos is int32 [nq]; Q and X of dense_ip_topk are fp16 [nq, dim] and [n, dim].  A valid CSR is a
 precondition of the MaxSim calls (the library never reads the offsets on the host); with the
@@ -76,6 +87,17 @@ _SIGNATURES = {
     "semantic_chunk": (_I32, [_P, _I64, _I32, _P, _I64, _F32, _P, _P, _P, _P, _SZ, _P]),
     "semantic_chunk_workspace_size": (_SZ, [_I64, _I32]),
     "retrieval_metrics": (_I32, [_P, _I32, _I32, _I32, _P, _P, _P, _P]),
+    "packed_attention_workspace_size": (_SZ, [_P]),
+    "packed_attention_bwd_workspace_size": (_SZ, [_P]),
+    "packed_attention_fwd": (_I32, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "packed_attention_bwd": (_I32, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "adapter_linear_fwd": (_I32, [_P, _I64, _I32, _P, _I32, _P, _P, _I32, _I32, _P, _P, _P, _I32, _I32,
+                                  _P, _P, _P]),
+    "adapter_linear_bwd_workspace_size": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I32]),
+    "adapter_linear_bwd": (_I32, [_P, _P, _I64, _I32, _P, _I32, _P, _P, _I32, _I32, _P, _P, _P, _I32,
+                                  _I32, _P, _P, _P, _P, _P, _SZ, _P]),
+    "rotary_apply": (_I32, [_P, _I64, _I64, _I32, _P, _I64, _I64, _I32, _I64, _I32, _I32, _P, _P, _P,
+                            _I64, _I32, _I32, _P, _P, _P]),
     "hpr_mfma_calibration": (_I32, [_I64, _I32, _P, ctypes.POINTER(ctypes.c_double), _P]),
     "hpr_read_calibration": (_I32, [_P, _I64, _P, _P]),
     "hpr_csr_validate": (_I32, [_P, _I64, _I64, _P, _P, _P]),
@@ -431,6 +453,300 @@ def retrieval_metrics(idx, positive, k=None):
     _launch(lib().retrieval_metrics, dev, _ptr(idx), nq, ld, k, _ptr(positive), _ptr(ranks),
             _ptr(metrics))
     return {"metrics": metrics, "ranks": ranks}
+
+
+# ---- the encoder's operators --------------------------------------------------------------
+
+_HALF_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+class _AttentionDesc(ctypes.Structure):
+    _fields_ = [(n, _I64) for n in ("n_q", "n_k", "q_row", "q_head", "k_row", "k_head", "v_row",
+                                    "v_head")] + \
+               [(n, _I32) for n in ("n_seq", "heads", "kv_heads", "dim", "dtype", "causal",
+                                    "window")] + [("scale", _F32)]
+
+
+def _need_heads(t, name, dtype, device):
+    """[rows, heads, dim] with contiguous values and 16-byte aligned rows and heads (views of a
+    projection's output are fine)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype or dtype not in _HALF_TYPES:
+        raise TypeError(f"{name} must be bfloat16 or float16, the same for every tensor, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have 3 dimensions, got {t.dim()}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.numel() and (t.stride(2) != 1 or any(x % 8 for x in _strides(t)) or t.data_ptr() % 16):
+        raise ValueError(f"{name} must have contiguous values, and rows and heads aligned to 16 bytes")
+
+
+def _strides(t):
+    # (a dimension of one row or head may carry any stride; it is never stepped over)
+    return (t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _attention_desc(q, k, v, q_off, k_off, k_len, causal, window, scale):
+    dtype = getattr(q, "dtype", None)
+    dev = getattr(q, "device", None)
+    _need_heads(q, "q", dtype, dev)
+    _need_heads(k, "k", dtype, dev)
+    _need_heads(v, "v", dtype, dev)
+    if k.shape != v.shape:
+        raise ValueError(f"k and v differ in shape: {tuple(k.shape)}, {tuple(v.shape)}")
+    n_q, heads, dim = q.shape
+    n_k, kv_heads, k_dim = k.shape
+    if dim != k_dim:
+        raise ValueError(f"k has dim {k_dim}, q has {dim}")
+    _need(q_off, "q_off", torch.int64, 1, dev)
+    if q_off.numel() < 1:
+        raise ValueError("q_off must hold n_seq + 1 offsets")
+    if k_off is None:
+        k_off = q_off
+        if n_k != n_q:
+            raise ValueError(f"k has {n_k} rows, q has {n_q}: pass k_off")
+    elif k_off is not q_off:
+        _need(k_off, "k_off", torch.int64, 1, dev)
+        if k_off.numel() != q_off.numel():
+            raise ValueError("k_off must hold as many offsets as q_off")
+    n_seq = q_off.numel() - 1
+    if k_len is not None:
+        _need(k_len, "k_len", torch.int64, 1, dev)
+        if k_len.numel() != n_seq:
+            raise ValueError("k_len must hold one length per sequence")
+    scale = dim ** -0.5 if scale is None and dim else scale
+    d = _AttentionDesc(n_q, n_k, *_strides(q), *_strides(k), *_strides(v), n_seq, heads, kv_heads, dim,
+                       _HALF_TYPES[dtype], bool(causal), int(window), float(scale or 0.0))
+    return dev, d, k_off
+
+
+def packed_attention_fwd(q, k, v, q_off, k_off=None, k_len=None, causal=True, window=0, scale=None,
+                         need_lse=True, out=None, ws=None):
+    """Attention over packed sequences: dict(out [n_q, heads, dim], lse fp32 [n_q, heads] or None).
+
+    q [n_q, heads, dim], k and v [n_k, kv_heads, dim], bf16 or fp16; sequence s has query rows
+    q_off[s]..q_off[s+1] and key rows k_off[s]..k_off[s+1] (int64; None: q_off), of which the first
+    k_len[s] count (int64 [n_seq]; None: all).  causal aligns the last query with the last key;
+    window > 0 also hides keys more than window - 1 before it.  scale defaults to dim ** -0.5.
+    """
+    dev, d, k_off = _attention_desc(q, k, v, q_off, k_off, k_len, causal, window, scale)
+    L = lib()
+    need = L.packed_attention_workspace_size(ctypes.byref(d))
+    if need and (ws is None or ws.numel() < need):
+        ws = _workspace(need, dev)
+    if out is None:
+        out = torch.empty((d.n_q, d.heads, d.dim), dtype=q.dtype, device=dev)
+    else:
+        _need(out, "out", q.dtype, 3, dev)
+        if out.shape != q.shape:
+            raise ValueError(f"out must be {tuple(q.shape)}")
+    lse = torch.empty((d.n_q, d.heads), dtype=torch.float32, device=dev) if need_lse else None
+    _launch(L.packed_attention_fwd, dev, ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(q_off),
+            _ptr(k_off), _ptr(k_len), _ptr(out), _ptr(lse), _ptr(ws) if need else None,
+            ws.numel() if need else 0)
+    return {"out": out, "lse": lse}
+
+
+def packed_attention_bwd(dout, q, k, v, out, lse, q_off, k_off=None, k_len=None, causal=True, window=0,
+                         scale=None, need_dq=True, need_dkv=True, ws=None):
+    """Gradients of packed_attention_fwd: dict(dq, dk, dv), dense and of the inputs' type; dq, or dk
+    and dv together, None where not needed.  out and lse are the forward's."""
+    dev, d, k_off = _attention_desc(q, k, v, q_off, k_off, k_len, causal, window, scale)
+    for t, name in ((dout, "dout"), (out, "out")):
+        _need(t, name, q.dtype, 3, dev)
+        if t.shape != q.shape:
+            raise ValueError(f"{name} must be {tuple(q.shape)}")
+    _need(lse, "lse", torch.float32, 2, dev)
+    if lse.shape != q.shape[:2]:
+        raise ValueError(f"lse must be {tuple(q.shape[:2])}")
+    L = lib()
+    need = L.packed_attention_bwd_workspace_size(ctypes.byref(d))
+    ws = ws if ws is not None and ws.numel() >= need else _workspace(need, dev)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=dev) if need_dq else None
+    dk = torch.empty(k.shape, dtype=q.dtype, device=dev) if need_dkv else None
+    dv = torch.empty(k.shape, dtype=q.dtype, device=dev) if need_dkv else None
+    _launch(L.packed_attention_bwd, dev, ctypes.byref(d), _ptr(dout), _ptr(q), _ptr(k), _ptr(v),
+            _ptr(out), _ptr(lse), _ptr(q_off), _ptr(k_off), _ptr(k_len), _ptr(dq), _ptr(dk), _ptr(dv),
+            _ptr(ws), ws.numel())
+    return {"dq": dq, "dk": dk, "dv": dv}
+
+
+class _PackedAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, q_off, k_off, k_len, causal, window, scale):
+        ctx.how = (causal, window, scale)
+        train = any(ctx.needs_input_grad[:3])
+        r = packed_attention_fwd(q.detach(), k.detach(), v.detach(), q_off, k_off, k_len, causal,
+                                 window, scale, need_lse=train)
+        if train:
+            ctx.save_for_backward(q, k, v, r["out"], r["lse"], q_off, k_off, k_len)
+        return r["out"]
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        q, k, v, out, lse, q_off, k_off, k_len = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        g = packed_attention_bwd(grad_out.contiguous(), q, k, v, out, lse, q_off, k_off, k_len,
+                                 *ctx.how, need_dq=need[0], need_dkv=need[1] or need[2])
+        return (g["dq"], g["dk"] if need[1] else None, g["dv"] if need[2] else None,
+                None, None, None, None, None, None)
+
+
+def packed_attention(q, k, v, q_off, k_off=None, k_len=None, causal=True, window=0, scale=None):
+    """packed_attention_fwd's out, differentiable (gradients reach q, k and v)."""
+    return _PackedAttention.apply(q, k, v, q_off, k_off, k_len, causal, window, scale)
+
+
+def _adapter_inputs(x, W, A, B, scale, off, adapter):
+    dtype = getattr(x, "dtype", None)
+    if dtype not in _HALF_TYPES:
+        raise TypeError(f"x must be a bfloat16 or float16 tensor, got {dtype or type(x).__name__}")
+    _need(x, "x", dtype, 2)
+    dev = x.device
+    _need(W, "W", dtype, 2, dev)
+    _need(A, "A", dtype, 3, dev)
+    _need(B, "B", dtype, 3, dev)
+    _need(scale, "scale", torch.float32, 1, dev)
+    _need(off, "off", torch.int64, 1, dev)
+    _need(adapter, "adapter", torch.int32, 1, dev)
+    n, k = x.shape
+    m = W.shape[0]
+    n_ad, r = A.shape[:2]
+    if W.shape[1] != k or A.shape[2] != k:
+        raise ValueError(f"x has {k} columns, W {W.shape[1]} and A {A.shape[2]}")
+    if B.shape != (n_ad, m, r):
+        raise ValueError(f"B must be {(n_ad, m, r)}, got {tuple(B.shape)}")
+    if scale.numel() != n_ad:
+        raise ValueError("scale must hold one factor per adapter")
+    if off.numel() != adapter.numel() + 1:
+        raise ValueError("off must hold one offset per request and one more")
+    return dev, n, k, m, r, n_ad, adapter.numel(), _HALF_TYPES[dtype]
+
+
+def adapter_linear_fwd(x, W, A, B, scale, off, adapter, out=None):
+    """A shared projection with a low-rank adapter per request beside it: dict(y [n, m], h).
+
+    x [n, k], W [m, k], A [n_ad, r, k], B [n_ad, m, r], bf16 or fp16; scale fp32 [n_ad].  Request s
+    has rows off[s]..off[s+1] (int64 [n_req + 1]) and adapter[s] (int32 [n_req], negative: none):
+    h_t = scale A x_t, y_t = W x_t + B h_t.  h [n, r rounded up to 16] is what the gradients read.
+    """
+    dev, n, k, m, r, n_ad, n_req, code = _adapter_inputs(x, W, A, B, scale, off, adapter)
+    h = torch.empty((n, (r + 15) // 16 * 16), dtype=x.dtype, device=dev)
+    if out is None:
+        out = torch.empty((n, m), dtype=x.dtype, device=dev)
+    else:
+        _need(out, "out", x.dtype, 2, dev)
+        if out.shape != (n, m):
+            raise ValueError(f"out must be {(n, m)}")
+    _launch(lib().adapter_linear_fwd, dev, _ptr(x), n, k, _ptr(W), m, _ptr(A), _ptr(B), r, n_ad,
+            _ptr(scale), _ptr(off), _ptr(adapter), n_req, code, _ptr(h), _ptr(out))
+    return {"y": out, "h": h}
+
+
+def adapter_linear_bwd(dy, x, W, A, B, scale, off, adapter, h, need_dx=True, need_da=True, need_db=True,
+                       ws=None):
+    """Gradients of adapter_linear_fwd's y: dict(dx, da, db), of the inputs' type, None where not
+    needed.  W and scale are frozen."""
+    dev, n, k, m, r, n_ad, n_req, code = _adapter_inputs(x, W, A, B, scale, off, adapter)
+    _need(dy, "dy", x.dtype, 2, dev)
+    if dy.shape != (n, m):
+        raise ValueError(f"dy must be {(n, m)}")
+    _need(h, "h", x.dtype, 2, dev)
+    if h.shape != (n, (r + 15) // 16 * 16):
+        raise ValueError("h must be the forward's")
+    L = lib()
+    need = L.adapter_linear_bwd_workspace_size(n, k, m, r, n_ad, n_req)
+    ws = ws if ws is not None and ws.numel() >= need else _workspace(need, dev)
+    dx = torch.empty_like(x) if need_dx else None
+    da = torch.empty_like(A) if need_da else None
+    db = torch.empty_like(B) if need_db else None
+    _launch(L.adapter_linear_bwd, dev, _ptr(dy), _ptr(x), n, k, _ptr(W), m, _ptr(A), _ptr(B), r, n_ad,
+            _ptr(scale), _ptr(off), _ptr(adapter), n_req, code, _ptr(h), _ptr(dx), _ptr(da), _ptr(db),
+            _ptr(ws), ws.numel())
+    return {"dx": dx, "da": da, "db": db}
+
+
+class _AdapterLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, W, A, B, scale, off, adapter):
+        r = adapter_linear_fwd(x.detach(), W.detach(), A.detach(), B.detach(), scale, off, adapter)
+        ctx.save_for_backward(x, W, A, B, scale, off, adapter, r["h"])
+        return r["y"]
+
+    @staticmethod
+    def backward(ctx, grad_y):
+        need = ctx.needs_input_grad
+        g = adapter_linear_bwd(grad_y.contiguous(), *ctx.saved_tensors, need_dx=need[0],
+                               need_da=need[2], need_db=need[3])
+        return g["dx"], None, g["da"], g["db"], None, None, None
+
+
+def adapter_linear(x, W, A, B, scale, off, adapter):
+    """adapter_linear_fwd's y, differentiable (gradients reach x, A and B; W and scale are frozen)."""
+    for t, name in ((W, "W"), (scale, "scale")):
+        if isinstance(t, torch.Tensor) and t.requires_grad:
+            raise ValueError(f"{name} is frozen: it must not require a gradient")
+    return _AdapterLinear.apply(x, W, A, B, scale, off, adapter)
+
+
+def rotary_apply(q, k, pos, cos, sin, inverse=False):
+    """q [n, heads, dim] and k [n, kv_heads, dim] (or None) rotated by their rows' positions.
+
+    pos int32 [n]; cos and sin fp32 [n_pos, rot / 2]: values j and j + rot / 2 of every head turn by
+    the position's angle j, values past rot are copied.  inverse turns back (the gradient).
+    """
+    dtype = getattr(q, "dtype", None)
+    dev = getattr(q, "device", None)
+    _need_heads(q, "q", dtype, dev)
+    n, heads, dim = q.shape
+    kv_heads = 0
+    if k is not None:
+        _need_heads(k, "k", dtype, dev)
+        kv_heads = k.shape[1]
+        if k.shape[0] != n or k.shape[2] != dim:
+            raise ValueError(f"k must be [{n}, kv_heads, {dim}], got {tuple(k.shape)}")
+    _need(pos, "pos", torch.int32, 1, dev)
+    if pos.numel() != n:
+        raise ValueError("pos must hold one position per row")
+    _need(cos, "cos", torch.float32, 2, dev)
+    _need(sin, "sin", torch.float32, 2, dev)
+    if cos.shape != sin.shape:
+        raise ValueError("cos and sin differ in shape")
+    q_out = torch.empty((n, heads, dim), dtype=dtype, device=dev)
+    k_out = torch.empty((n, kv_heads, dim), dtype=dtype, device=dev) if k is not None else None
+    _launch(lib().rotary_apply, dev, _ptr(q), *_strides(q), heads, _ptr(k),
+            *(_strides(k) if k is not None else (0, 0)), kv_heads, n, dim, 2 * cos.shape[1], _ptr(pos),
+            _ptr(cos), _ptr(sin), cos.shape[0], bool(inverse), _HALF_TYPES[dtype], _ptr(q_out),
+            _ptr(k_out))
+    return q_out, k_out
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, pos, cos, sin):
+        ctx.save_for_backward(pos, cos, sin)
+        return rotary_apply(q.detach(), k.detach() if k is not None else None, pos, cos, sin)
+
+    @staticmethod
+    def backward(ctx, gq, gk):
+        pos, cos, sin = ctx.saved_tensors
+        need_q, need_k = ctx.needs_input_grad[:2]
+        a, b = [g.contiguous() if g is not None and need else None
+                for g, need in ((gq, need_q), (gk, need_k))]
+        if a is None and b is None:
+            return None, None, None, None, None
+        if a is None:
+            return None, rotary_apply(b, None, pos, cos, sin, inverse=True)[0], None, None, None
+        dq, dk = rotary_apply(a, b, pos, cos, sin, inverse=True)
+        return dq, dk, None, None, None
+
+
+def rotary(q, k, pos, cos, sin):
+    """rotary_apply, differentiable (gradients reach q and k, by the rotation back)."""
+    return _Rotary.apply(q, k, pos, cos, sin)
 
 
 def calibrate(device="cuda:0", mfma_iters=20000, read_bytes=16 << 30, reps=3):

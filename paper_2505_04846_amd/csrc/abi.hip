@@ -311,6 +311,100 @@ hpr_status run_loss(const uint16_t* q, int32_t nq, int32_t lq, const uint16_t* d
   return HPR_OK;
 }
 
+// Shared checks of the attention calls; fills what both directions read.
+hpr_status check_attention(const hpr_attention* d, const uint16_t* q, const uint16_t* k,
+                           const uint16_t* v, const int64_t* q_off, const int64_t* k_off,
+                           const int64_t* k_len, AttnArgs* out) {
+  if (!d) return fail(HPR_ERR_INVALID_ARG, "the description must be non-NULL");
+  if (d->n_q < 0 || d->n_k < 0 || d->n_seq < 0)
+    return fail(HPR_ERR_INVALID_ARG, "n_q, n_k and n_seq must be >= 0");
+  if (d->n_seq == 0 && (d->n_q > 0 || d->n_k > 0))
+    return fail(HPR_ERR_INVALID_ARG, "rows without a sequence (n_seq = 0)");
+  if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0)
+    return fail(HPR_ERR_INVALID_ARG, "heads (%d) must be a positive multiple of kv_heads (%d)",
+                d->heads, d->kv_heads);
+  if (d->dtype != HPR_BF16 && d->dtype != HPR_F16)
+    return fail(HPR_ERR_INVALID_ARG, "dtype (%d) must be HPR_BF16 or HPR_F16", d->dtype);
+  if (d->window < 0 || (d->window > 0 && !d->causal))
+    return fail(HPR_ERR_INVALID_ARG, "window (%d) must be >= 0, and needs causal", d->window);
+  if (!(d->scale > 0.f) || d->scale > 3.0e38f)
+    return fail(HPR_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (d->dim < 8 || d->dim % 8 != 0 || d->dim > 128)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "attention needs dim %% 8 == 0 and 8 <= dim <= 128 (dim=%d)",
+                d->dim);
+  if (d->heads / d->kv_heads > kMaxGroup)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "more than %d heads per kv head", kMaxGroup);
+  // (the grids hold up to a tile per 4 rows and kv head, and 64 splits of those below one round)
+  if (d->n_q >= (int64_t(1) << 31) || d->n_k >= (int64_t(1) << 31) || d->kv_heads > 1024 ||
+      (d->n_q / 4 + d->n_k / 128 + d->n_seq) * d->kv_heads >= (int64_t(1) << 31))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "too many rows or heads");
+  const int64_t strides[6] = {d->q_row, d->q_head, d->k_row, d->k_head, d->v_row, d->v_head};
+  for (int64_t x : strides)
+    if (x < 0 || x % 8 != 0 || x >= (int64_t(1) << 22))
+      return fail(HPR_ERR_UNSUPPORTED_SHAPE, "strides must be multiples of 8 in [0, 2^22)");
+  if ((d->n_q > 0 && !q) || (d->n_k > 0 && (!k || !v)) || (d->n_seq > 0 && (!q_off || !k_off)))
+    return fail(HPR_ERR_INVALID_ARG, "q, k, v and the offsets must be non-NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_off) || !aligned16(k_off) ||
+      !aligned16(k_len))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  AttnArgs a = {};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_row = d->q_row;
+  a.q_head = d->q_head;
+  a.k_row = d->k_row;
+  a.k_head = d->k_head;
+  a.v_row = d->v_row;
+  a.v_head = d->v_head;
+  a.q_off = q_off;
+  a.k_off = k_off;
+  a.k_len = k_len;
+  a.n_q = d->n_q;
+  a.n_k = d->n_k;
+  a.n_seq = d->n_seq;
+  a.heads = d->heads;
+  a.kv_heads = d->kv_heads;
+  a.G = d->heads / d->kv_heads;
+  a.dim = d->dim;
+  a.window = d->window;
+  a.causal = d->causal != 0;
+  a.f16 = d->dtype == HPR_F16;
+  a.scale = d->scale;
+  a.c = d->scale * 1.4426950408889634f;
+  a.g_inv = 65536u / (uint32_t)a.G + 1u;
+  a.splits = 1;
+  *out = a;
+  return HPR_OK;
+}
+
+// Shared checks of the adapter calls.
+hpr_status check_adapters(const uint16_t* x, int64_t n, int32_t k, const uint16_t* w, int32_t m,
+                          const uint16_t* a, const uint16_t* b, int32_t r, int32_t n_ad,
+                          const float* scale, const int64_t* req_off, const int32_t* adapter,
+                          int32_t n_req, int32_t dtype) {
+  if (n < 0 || n_ad < 0 || n_req < 0)
+    return fail(HPR_ERR_INVALID_ARG, "n, n_ad and n_req must be >= 0");
+  if (k < 1 || m < 1 || r < 1)
+    return fail(HPR_ERR_INVALID_ARG, "k (%d), m (%d) and r (%d) must be >= 1", k, m, r);
+  if (dtype != HPR_BF16 && dtype != HPR_F16)
+    return fail(HPR_ERR_INVALID_ARG, "dtype (%d) must be HPR_BF16 or HPR_F16", dtype);
+  if (k % 8 != 0 || m % 8 != 0 || k > 65536 || m > 65536)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE,
+                "adapters need k and m multiples of 8 up to 65536 (k=%d, m=%d)", k, m);
+  if (r > kMaxRank) return fail(HPR_ERR_UNSUPPORTED_SHAPE, "r=%d exceeds %d", r, kMaxRank);
+  // (the grids hold up to a workgroup per 32 x 64 outputs, 64 x 64 weights, or 512 x 256 x 64)
+  if (n >= (int64_t(1) << 31) || (n / 32 + 1) * (int64_t)((m > k ? m : k) / 64 + 1) >= (int64_t(1) << 31) ||
+      (n / 512 + n_req) * (int64_t)((m > k ? m : k) / 256 + 1) * 2 >= (int64_t(1) << 31) || n_ad > 65535)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "too many rows, requests or adapters");
+  if ((n > 0 && !x) || !w || (n_ad > 0 && (!a || !b || !scale)) || (n_req > 0 && (!req_off || !adapter)))
+    return fail(HPR_ERR_INVALID_ARG, "x, w, the adapters, their scales and the requests must be non-NULL");
+  if (!aligned16(x) || !aligned16(w) || !aligned16(a) || !aligned16(b) || !aligned16(scale) ||
+      !aligned16(req_off) || !aligned16(adapter))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  return HPR_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -500,6 +594,197 @@ hpr_status retrieval_metrics(const int64_t* topk_idx, int32_t nq, int32_t ld, in
     return launch_retrieval_metrics(topk_idx, nq, ld, k, positive, ranks_out, metrics_out, s);
   });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "retrieval metrics launch");
+}
+
+size_t packed_attention_workspace_size(const hpr_attention* d) {
+  if (!d || d->n_q < 1 || d->n_seq < 1 || d->heads < 1 || d->kv_heads < 1 || d->dim < 1 ||
+      d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
+    return 0;
+  const int64_t splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
+  if (splits <= 1) return 0;
+  const size_t rows = (size_t)splits * d->n_q * d->heads;
+  return align_up(rows * d->dim * sizeof(float)) + align_up(rows * 2 * sizeof(float));
+}
+
+size_t packed_attention_bwd_workspace_size(const hpr_attention* d) {
+  if (!d || d->n_q < 1 || d->heads < 1) return 0;
+  return align_up((size_t)d->n_q * d->heads * sizeof(float));
+}
+
+hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const uint16_t* k,
+                                const uint16_t* v, const int64_t* q_off, const int64_t* k_off,
+                                const int64_t* k_len, uint16_t* out, float* lse, void* ws,
+                                size_t ws_bytes, void* stream) {
+  AttnArgs a;
+  hpr_status st = check_attention(d, q, k, v, q_off, k_off, k_len, &a);
+  if (st != HPR_OK) return st;
+  if (d->n_q == 0) return HPR_OK;
+  if (!out) return fail(HPR_ERR_INVALID_ARG, "out must be non-NULL");
+  if (!aligned16(out) || !aligned16(lse))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  const size_t need = packed_attention_workspace_size(d);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+  a.out = out;
+  a.lse = lse;
+  a.splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
+  if (a.splits > 1) {
+    Carver c(ws);
+    const size_t rows = (size_t)a.splits * d->n_q * d->heads;
+    a.part_o = c.take<float>(rows * d->dim * sizeof(float));
+    a.part_ml = c.take<float>(rows * 2 * sizeof(float));
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = timed("attn_fwd", s, [&] { return launch_attn_fwd(a, s); });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "attention launch");
+}
+
+hpr_status packed_attention_bwd(const hpr_attention* d, const uint16_t* dout, const uint16_t* q,
+                                const uint16_t* k, const uint16_t* v, const uint16_t* out,
+                                const float* lse, const int64_t* q_off, const int64_t* k_off,
+                                const int64_t* k_len, uint16_t* dq, uint16_t* dk, uint16_t* dv,
+                                void* ws, size_t ws_bytes, void* stream) {
+  AttnArgs a;
+  hpr_status st = check_attention(d, q, k, v, q_off, k_off, k_len, &a);
+  if (st != HPR_OK) return st;
+  if (d->n_q > 0 && (!dout || !out || !lse))
+    return fail(HPR_ERR_INVALID_ARG, "dout, out and lse must be non-NULL");
+  if (d->n_k > 0 && (!dk != !dv))
+    return fail(HPR_ERR_INVALID_ARG, "dk and dv are computed together: both or neither");
+  if (!aligned16(dout) || !aligned16(out) || !aligned16(lse) || !aligned16(dq) || !aligned16(dk) ||
+      !aligned16(dv))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  const size_t need = packed_attention_bwd_workspace_size(d);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+  a.out = const_cast<uint16_t*>(out);
+  a.lse = const_cast<float*>(lse);
+  a.dout = dout;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.delta = static_cast<float*>(ws);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = timed("attn_bwd", s, [&] { return launch_attn_bwd(a, s); });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "attention gradient launch");
+}
+
+hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uint16_t* w, int32_t m,
+                              const uint16_t* a, const uint16_t* b, int32_t r, int32_t n_ad,
+                              const float* scale, const int64_t* req_off, const int32_t* adapter,
+                              int32_t n_req, int32_t dtype, uint16_t* h, uint16_t* y, void* stream) {
+  hpr_status st = check_adapters(x, n, k, w, m, a, b, r, n_ad, scale, req_off, adapter, n_req, dtype);
+  if (st != HPR_OK) return st;
+  if (n == 0) return HPR_OK;
+  if (!h || !y) return fail(HPR_ERR_INVALID_ARG, "h and y must be non-NULL");
+  if (!aligned16(h) || !aligned16(y))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  const AdapterArgs g = {x, w, a, b, scale, req_off, adapter, n, k, m, r, n_ad, n_req,
+                         dtype == HPR_F16};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = timed("adapter_shrink", s, [&] { return launch_adapter_shrink(g, h, s); });
+  if (e == hipSuccess)
+    e = timed("adapter_expand", s, [&] { return launch_adapter_expand(g, h, y, s); });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "adapter launch");
+}
+
+size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_t r, int32_t n_ad,
+                                         int32_t n_req) {
+  if (n < 0 || k < 1 || m < 1 || r < 1 || n_ad < 0 || n_req < 0) return 0;
+  const size_t rp = (size_t)adapter_rank_pad(r), most = (size_t)(k > m ? k : m);
+  return align_up((size_t)m * k * 2) + align_up((size_t)n_ad * r * k * 2) +
+         align_up((size_t)n_ad * r * m * 2) + align_up((size_t)n * rp * 2) +
+         align_up((size_t)adapter_outer_parts(n, n_req) * rp * most * sizeof(float));
+}
+
+hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, int32_t k,
+                              const uint16_t* w, int32_t m, const uint16_t* a, const uint16_t* b,
+                              int32_t r, int32_t n_ad, const float* scale, const int64_t* req_off,
+                              const int32_t* adapter, int32_t n_req, int32_t dtype,
+                              const uint16_t* h, uint16_t* dx, uint16_t* da, uint16_t* db, void* ws,
+                              size_t ws_bytes, void* stream) {
+  hpr_status st = check_adapters(x, n, k, w, m, a, b, r, n_ad, scale, req_off, adapter, n_req, dtype);
+  if (st != HPR_OK) return st;
+  if (n > 0 && (!dy || !h)) return fail(HPR_ERR_INVALID_ARG, "dy and h must be non-NULL");
+  if (!aligned16(dy) || !aligned16(h) || !aligned16(dx) || !aligned16(da) || !aligned16(db))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  const size_t need = adapter_linear_bwd_workspace_size(n, k, m, r, n_ad, n_req);
+  if (!ws || ws_bytes < need)
+    return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const size_t rp = (size_t)adapter_rank_pad(r), most = (size_t)(k > m ? k : m);
+  Carver c(ws);
+  uint16_t* wt = c.take<uint16_t>((size_t)m * k * 2);
+  uint16_t* at = c.take<uint16_t>((size_t)n_ad * r * k * 2);
+  uint16_t* bt = c.take<uint16_t>((size_t)n_ad * r * m * 2);
+  uint16_t* g = c.take<uint16_t>((size_t)n * rp * 2);
+  float* part = c.take<float>((size_t)adapter_outer_parts(n, n_req) * rp * most * sizeof(float));
+  // g and dx: the forward's kernels on (dy, W^T, B^T, A^T)
+  const AdapterArgs f = {x, w, a, b, scale, req_off, adapter, n, k, m, r, n_ad, n_req,
+                         dtype == HPR_F16};
+  AdapterArgs t = f;
+  t.x = dy;
+  t.w = wt;
+  t.a = bt;
+  t.b = at;
+  t.k = m;
+  t.m = k;
+  hipError_t e = hipSuccess;
+  if (n > 0 && (dx || da)) {
+    e = timed("adapter_transpose", s, [&] {
+      hipError_t x1 = launch_transpose(b, bt, n_ad, m, r, s);
+      if (x1 == hipSuccess && dx) x1 = launch_transpose(a, at, n_ad, r, k, s);
+      if (x1 == hipSuccess && dx) x1 = launch_transpose(w, wt, 1, m, k, s);
+      return x1;
+    });
+    if (e == hipSuccess) e = timed("adapter_shrink", s, [&] { return launch_adapter_shrink(t, g, s); });
+    if (e == hipSuccess && dx)
+      e = timed("adapter_expand", s, [&] { return launch_adapter_expand(t, g, dx, s); });
+    if (e != hipSuccess) return hip_fail(e, "adapter gradient launch");
+  }
+  if (da)
+    e = timed("adapter_outer", s, [&] {
+      return launch_adapter_outer(f, g, x, k, false, part, da, s);
+    });
+  if (e == hipSuccess && db)
+    e = timed("adapter_outer", s, [&] {
+      return launch_adapter_outer(f, h, dy, m, true, part, db, s);
+    });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "adapter gradient launch");
+}
+
+hpr_status rotary_apply(const uint16_t* q, int64_t q_row, int64_t q_head, int32_t q_heads,
+                        const uint16_t* k, int64_t k_row, int64_t k_head, int32_t k_heads, int64_t n,
+                        int32_t dim, int32_t rot, const int32_t* pos, const float* cos_table,
+                        const float* sin_table, int64_t n_pos, int32_t inverse, int32_t dtype,
+                        uint16_t* q_out, uint16_t* k_out, void* stream) {
+  if (n < 0 || n >= (int64_t(1) << 31))
+    return fail(HPR_ERR_INVALID_ARG, "n (%lld) must satisfy 0 <= n < 2^31", (long long)n);
+  if (q_heads < 1 || k_heads < 0 || n_pos < 1)
+    return fail(HPR_ERR_INVALID_ARG, "q_heads (%d) and n_pos (%lld) must be >= 1, k_heads (%d) >= 0",
+                q_heads, (long long)n_pos, k_heads);
+  if (dtype != HPR_BF16 && dtype != HPR_F16)
+    return fail(HPR_ERR_INVALID_ARG, "dtype (%d) must be HPR_BF16 or HPR_F16", dtype);
+  if (dim < 1 || dim % 8 != 0 || dim > 1024 || rot < 16 || rot % 16 != 0 || rot > dim)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE,
+                "rotary needs dim %% 8 == 0, dim <= 1024, rot %% 16 == 0 and 16 <= rot <= dim "
+                "(dim=%d, rot=%d)", dim, rot);
+  if (q_heads > 4096 || k_heads > 4096)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "more than 4096 heads");
+  if (n == 0) return HPR_OK;
+  if (!q || !q_out || !pos || !cos_table || !sin_table || (k_heads > 0 && (!k || !k_out)))
+    return fail(HPR_ERR_INVALID_ARG, "q, k, pos, the tables and the outputs must be non-NULL");
+  if ((q_row | q_head | k_row | k_head) % 8 != 0 || q_row < 0 || q_head < 0 || k_row < 0 || k_head < 0)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "strides must be non-negative multiples of 8");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(pos) ||
+      !aligned16(cos_table) || !aligned16(sin_table))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  const RotaryArgs a = {{q, k}, {q_out, k_out}, {q_row, k_row}, {q_head, k_head}, {q_heads, k_heads},
+                        pos, cos_table, sin_table, n, n_pos, dim, rot, inverse != 0,
+                        dtype == HPR_F16};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = timed("rotary", s, [&] { return launch_rotary(a, s); });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "rotary launch");
 }
 
 hpr_status hpr_mfma_calibration(int64_t iters, int32_t operands, float* sink, double* flops,

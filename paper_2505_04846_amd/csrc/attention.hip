@@ -1,0 +1,707 @@
+// Attention over packed sequences with grouped heads: forward, gradients, and the join of calls
+// whose keys are split over workgroups.
+//
+// Sequence s holds query rows [q_off[s], q_off[s+1]) and key rows [k_off[s], k_off[s] + its key
+// count).  For query head h, its kv head h / G, token i of lq and key j of lk:
+//   visible(i, j):  j <= i + lk - lq (causal), j > i + lk - lq - window (window > 0)
+//   x_ij = scale <q_i, k_j>,  p_ij = softmax of x_i. over the visible keys,  o_i = sum_j p_ij v_j
+//   lse_i = log sum_j exp(x_ij)   (no visible key: o_i = 0, lse_i = -inf, no gradient)
+// and with g = dL/do, delta_i = <g_i, o_i>, ds_ij = p_ij (<g_i, v_j> - delta_i):
+//   dv_j = sum_i p_ij g_i,  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i
+// with the sums for a kv head over all query heads of its group.
+//
+// Slots.  The query rows of a kv head's whole group share its keys, so a tile's rows are (token,
+// head of the group) pairs, "slots": slot = token * G + head.  A tile takes TS = rows / G whole
+// tokens.  Tiles are found without a plan: sequence s owns the tile numbers from
+// q_off[s] / TS + s, which leaves every sequence at least ceil(lq / TS) of them, and a workgroup
+// searches the offsets for its own (numbers past the sequence's end exit at once).
+//
+// Products.  All of them are v_mfma_f32_32x32x16 with the 32 rows that a wave owns as the columns
+// of the result, so a lane holds 16 entries of one of its rows (the entries of the two half-waves
+// interleave by fours).  Row statistics are then per lane, and such a result, rounded to 16 bits,
+// is the right operand of the next product as it stands: the left operand follows its order of k
+// (see tr_frag).  Left operands are tiles in LDS, read by rows (row_frag) or by columns (tr_frag,
+// ds_read_b64_tr_b16).
+#include "common.h"
+#include "half.h"
+#include "kernels.h"
+#include "tiles.h"
+
+namespace hpr {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// Stands for the maximum of no key yet, finite so that differences with it stay numbers.
+constexpr float kNoMax = -1e30f;
+// A row's running maximum is raised only when a score passes it by this much (in powers of two):
+// the exponentials then stay below 2^8, harmless in fp32 sums and 16-bit products alike (their
+// relative rounding does not depend on it), and most tiles skip the rescaling of the output.
+constexpr float kRaise = 8.f;
+
+constexpr int kKeys = 64;  // keys per tile of the forward and dq kernels
+
+// max / sum over the two half-waves, in both of them
+__device__ __forceinline__ float half_max(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+struct Seq {
+  int64_t q0, k0;  // first rows
+  int lq, lk;
+};
+
+// Bounds of sequence s, inside the tensors whatever the offsets hold.
+__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int s) {
+  Seq r;
+  auto clamp = [](int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); };
+  r.q0 = clamp(a.q_off[s], 0, a.n_q);
+  r.lq = (int)(clamp(a.q_off[s + 1], r.q0, a.n_q) - r.q0);
+  r.k0 = clamp(a.k_off[s], 0, a.n_k);
+  int64_t lk = clamp(a.k_off[s + 1], r.k0, a.n_k) - r.k0;
+  if (a.k_len) lk = clamp(a.k_len[s], 0, lk);
+  r.lk = (int)lk;
+  return r;
+}
+
+// Keys [lo, hi) visible from token i (of lq, with lk keys).
+struct Span {
+  int lo, hi;
+};
+__device__ __forceinline__ Span span_of(const AttnArgs& a, const Seq& s, int i) {
+  Span r = {0, s.lk};
+  if (a.causal) {
+    const int64_t reach = (int64_t)i + s.lk - s.lq;  // the last visible key
+    r.hi = reach < 0 ? 0 : (int)reach + 1;
+    if (a.window > 0) {
+      const int64_t lo = reach - a.window + 1;
+      r.lo = lo < 0 ? 0 : (int)lo;
+    }
+  }
+  return r;
+}
+
+// The right operand's registers of one 32-slot column block: values [16 s, 16 s + 16) of the
+// lane's row, zero past dim.
+template <int D>
+__device__ __forceinline__ void load_cols(const uint16_t* row, int dim, int half, u32x4 (&f)[D / 16]) {
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const int d = 16 * s + 8 * half;
+    f[s] = u32x4{0u, 0u, 0u, 0u};
+    if (d < dim) f[s] = load16(row + d);
+  }
+}
+
+// A probability from the logarithm (base 2) of it.  An fp32 lse of enormous scores is off by more than
+// a power of two; the clamp (an output modifier, free) keeps such rows finite.
+__device__ __forceinline__ float prob(float x) {
+  return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f);
+}
+
+// ---- forward --------------------------------------------------------------------------------
+
+// One tile of NW * 32 slots of one kv head against a split of its visible keys, kKeys at a time
+// through two LDS stages.
+template <class T, int D, int NW>
+__device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
+  constexpr int kS = D / 16, kDb = D / 32;
+  constexpr int kTile = kKeys * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTile];
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % a.kv_heads;
+  const int64_t w = blockIdx.x / a.kv_heads;
+  const int split = (int)(w % a.splits);
+  const int64_t tile = a.tiles - 1 - w / a.splits;  // late tiles see the most keys: first
+  const int sq = find_seq(a.q_off, a.n_seq, a.ts, tile);
+  const Seq S = seq_of(a, sq);
+  const int64_t tok0 = (tile - (S.q0 / a.ts + sq)) * a.ts;
+  if (tok0 < 0 || tok0 >= S.lq) return;
+  const int t0 = (int)tok0;
+  const int n_tok = S.lq - t0 < a.ts ? S.lq - t0 : a.ts;
+
+  // this lane's slot
+  const int slot = wave * 32 + col;
+  const int n_slot = n_tok * a.G;
+  const bool live = slot < n_slot;
+  const bool wave_live = wave * 32 < n_slot;
+  const int cs = live ? slot : n_slot - 1;
+  const int tok = t0 + cs / a.G, head = kvh * a.G + cs % a.G;
+  const Span mine = span_of(a, S, tok);
+  const int last_slot = wave * 32 + 31 < n_slot ? wave * 32 + 31 : n_slot - 1;
+  const Span wfirst = span_of(a, S, t0 + (wave_live ? wave * 32 : 0) / a.G);
+  const Span wlast = span_of(a, S, t0 + last_slot / a.G);
+  const Span tfirst = span_of(a, S, t0), tlast = span_of(a, S, t0 + n_tok - 1);
+
+  // key tiles of this split
+  const int k_first = tfirst.lo / kKeys, k_end = (tlast.hi + kKeys - 1) / kKeys;
+  const int n_kt = k_end > k_first ? k_end - k_first : 0;
+  const int kt0 = k_first + (int)((int64_t)n_kt * split / a.splits);
+  const int kt1 = k_first + (int)((int64_t)n_kt * (split + 1) / a.splits);
+
+  u32x4 q[kS];
+  load_cols<D>(a.q + (S.q0 + tok) * a.q_row + head * a.q_head, a.dim, half, q);
+
+  f32x16 o[kDb];
+#pragma unroll
+  for (int db = 0; db < kDb; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+  float m = kNoMax, l = 0.f;
+
+  const TileReads<D> rd(lane);
+  const TileLoad<D, kKeys, NW> ld(wave, lane, a.dim / 8);
+  const uint16_t* kb = a.k + S.k0 * a.k_row + kvh * a.k_head;
+  const uint16_t* vb = a.v + S.k0 * a.v_row + kvh * a.v_head;
+  auto issue = [&](int buf, int kt) {
+    const int first = kt * kKeys;
+    const int last = S.lk - 1 - first;  // last valid row of the tile (>= 0)
+    const __amdgpu_buffer_rsrc_t rk = tile_rsrc(kb + (int64_t)first * a.k_row);
+    const __amdgpu_buffer_rsrc_t rv = tile_rsrc(vb + (int64_t)first * a.v_row);
+    unsigned char* st = smem + buf * 2 * kTile;
+#pragma unroll
+    for (int j = 0; j < ld.kLoads; ++j) {
+      const int r = ld.row[j] < last ? ld.row[j] : last;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(st + (wave * ld.kLoads + j) * 1024),
+                                               16, r * (int)a.k_row * 2 + ld.chunk[j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < ld.kLoads; ++j) {
+      const int r = ld.row[j] < last ? ld.row[j] : last;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rv, (lds_void_t*)(st + kTile + (wave * ld.kLoads + j) * 1024), 16,
+          r * (int)a.v_row * 2 + ld.chunk[j], 0, 0, 0);
+    }
+  };
+
+  if (kt0 < kt1) issue(0, kt0);
+#pragma unroll 1
+  for (int kt = kt0; kt < kt1; ++kt) {
+    const int buf = (kt - kt0) & 1;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    sync_lds();  // the tile has landed, and nobody reads the other stage any more
+    if (kt + 1 < kt1) issue(buf ^ 1, kt + 1);
+    const int first = kt * kKeys;
+    if (!wave_live || first >= wlast.hi || first + kKeys <= wfirst.lo) continue;
+    const unsigned char* ks = smem + buf * 2 * kTile;
+    const unsigned char* vs = ks + kTile;
+    f32x16 x[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kS; ++s) x[b] = T::mfma(rd.row_frag(ks, b, s), q[s], x[b]);
+    }
+    if (first + kKeys > wfirst.hi || first < wlast.lo) {  // some key is not every slot's
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = first + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
+          if (key >= mine.hi || key < mine.lo) x[b][r] = -__builtin_inff();
+        }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][r]);
+    top = half_max(top) * a.c;
+    if (__any(top > m + kRaise)) {
+      const float mn = fmaxf(m, top);
+      const float f = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < kDb; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= f;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      u32x4 p[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], a.c, -m));
+        l += x[b][r];
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[s][e] = T::pack(x[b][8 * s + 2 * e], x[b][8 * s + 2 * e + 1]);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) o[db] = T::mfma(rd.tr_frag(vs, b, s, db), p[s], o[db]);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  if (!live) return;
+  l = half_sum(l);
+  const int64_t row = (S.q0 + tok) * a.heads + head;
+  if (a.splits > 1) {
+    // unnormalised sums, their reference maximum and total: attn_join_kernel
+    const int64_t at = ((int64_t)split * a.n_q * a.heads + row);
+    float* dst = a.part_o + at * a.dim;
+#pragma unroll
+    for (int db = 0; db < kDb; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = 32 * db + 8 * g + 4 * half;
+        if (d < a.dim)
+          *reinterpret_cast<f32x4*>(dst + d) =
+              f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
+      }
+    if (half == 0) {
+      a.part_ml[2 * at] = m;
+      a.part_ml[2 * at + 1] = l;
+    }
+    return;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  uint16_t* dst = a.out + row * a.dim;
+#pragma unroll
+  for (int db = 0; db < kDb; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * db + 8 * g + 4 * half;
+      if (d < a.dim)
+        *reinterpret_cast<uint2*>(dst + d) =
+            uint2{T::pack(o[db][4 * g] * inv, o[db][4 * g + 1] * inv),
+                  T::pack(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv)};
+    }
+  if (a.lse && half == 0) a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
+}
+
+// out = the splits' sums joined under their common maximum.  A wave per (token, head), lane d.
+template <class T>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  const int64_t rows = a.n_q * a.heads;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  float m = kNoMax;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + row)]);
+  float l = 0.f, o0 = 0.f, o1 = 0.f;
+  const int d = 2 * lane;
+  for (int s = 0; s < a.splits; ++s) {
+    const int64_t at = s * rows + row;
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - m);
+    l += f * a.part_ml[2 * at + 1];
+    if (d < a.dim) {
+      const float2 v = *reinterpret_cast<const float2*>(a.part_o + at * a.dim + d);
+      o0 += f * v.x;
+      o1 += f * v.y;
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  if (d < a.dim)
+    *reinterpret_cast<uint32_t*>(a.out + row * a.dim + d) = T::pack(o0 * inv, o1 * inv);
+  if (a.lse && lane == 0) a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
+}
+
+// ---- gradients --------------------------------------------------------------------------------
+
+// dq of a tile of slots, over all their visible keys; also delta, which the dk/dv kernel reads.
+template <class T, int D, int NW>
+__device__ __forceinline__ void attn_dq(const AttnArgs& a) {
+  constexpr int kS = D / 16, kDb = D / 32;
+  constexpr int kTile = kKeys * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTile];
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % a.kv_heads;
+  const int64_t tile = a.tiles - 1 - blockIdx.x / a.kv_heads;
+  const int sq = find_seq(a.q_off, a.n_seq, a.ts, tile);
+  const Seq S = seq_of(a, sq);
+  const int64_t tok0 = (tile - (S.q0 / a.ts + sq)) * a.ts;
+  if (tok0 < 0 || tok0 >= S.lq) return;
+  const int t0 = (int)tok0;
+  const int n_tok = S.lq - t0 < a.ts ? S.lq - t0 : a.ts;
+  const int slot = wave * 32 + col;
+  const int n_slot = n_tok * a.G;
+  const bool live = slot < n_slot;
+  const bool wave_live = wave * 32 < n_slot;
+  const int cs = live ? slot : n_slot - 1;
+  const int tok = t0 + cs / a.G, head = kvh * a.G + cs % a.G;
+  const Span mine = span_of(a, S, tok);
+  const int last_slot = wave * 32 + 31 < n_slot ? wave * 32 + 31 : n_slot - 1;
+  const Span wfirst = span_of(a, S, t0 + (wave_live ? wave * 32 : 0) / a.G);
+  const Span wlast = span_of(a, S, t0 + last_slot / a.G);
+  const Span tfirst = span_of(a, S, t0), tlast = span_of(a, S, t0 + n_tok - 1);
+  const int kt0 = tfirst.lo / kKeys, kt1 = (tlast.hi + kKeys - 1) / kKeys;
+
+  const int64_t row = (S.q0 + tok) * a.heads + head;
+  u32x4 q[kS], g[kS];
+  load_cols<D>(a.q + (S.q0 + tok) * a.q_row + head * a.q_head, a.dim, half, q);
+  load_cols<D>(a.dout + row * a.dim, a.dim, half, g);
+  float delta = 0.f;
+  {
+    u32x4 o[kS];
+    load_cols<D>(a.out + row * a.dim, a.dim, half, o);
+#pragma unroll
+    for (int s = 0; s < kS; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        delta += T::lo(g[s][e]) * T::lo(o[s][e]) + T::hi(g[s][e]) * T::hi(o[s][e]);
+    delta = half_sum(delta);
+  }
+  if (live && half == 0) a.delta[row] = delta;
+  const float lse2 = a.lse[row] * kLog2e;
+
+  f32x16 dq[kDb];
+#pragma unroll
+  for (int db = 0; db < kDb; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
+
+  const TileReads<D> rd(lane);
+  const TileLoad<D, kKeys, NW> ld(wave, lane, a.dim / 8);
+  const uint16_t* kb = a.k + S.k0 * a.k_row + kvh * a.k_head;
+  const uint16_t* vb = a.v + S.k0 * a.v_row + kvh * a.v_head;
+  auto issue = [&](int buf, int kt) {
+    const int first = kt * kKeys;
+    const int last = S.lk - 1 - first;
+    const __amdgpu_buffer_rsrc_t rk = tile_rsrc(kb + (int64_t)first * a.k_row);
+    const __amdgpu_buffer_rsrc_t rv = tile_rsrc(vb + (int64_t)first * a.v_row);
+    unsigned char* st = smem + buf * 2 * kTile;
+#pragma unroll
+    for (int j = 0; j < ld.kLoads; ++j) {
+      const int r = ld.row[j] < last ? ld.row[j] : last;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(st + (wave * ld.kLoads + j) * 1024),
+                                               16, r * (int)a.k_row * 2 + ld.chunk[j], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rv, (lds_void_t*)(st + kTile + (wave * ld.kLoads + j) * 1024), 16,
+          r * (int)a.v_row * 2 + ld.chunk[j], 0, 0, 0);
+    }
+  };
+  if (kt0 < kt1) issue(0, kt0);
+#pragma unroll 1
+  for (int kt = kt0; kt < kt1; ++kt) {
+    const int buf = (kt - kt0) & 1;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    sync_lds();
+    if (kt + 1 < kt1) issue(buf ^ 1, kt + 1);
+    const int first = kt * kKeys;
+    if (!wave_live || first >= wlast.hi || first + kKeys <= wfirst.lo) continue;
+    const unsigned char* ks = smem + buf * 2 * kTile;
+    const unsigned char* vs = ks + kTile;
+    const bool partial = first + kKeys > wfirst.hi || first < wlast.lo;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      f32x16 x, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = 0.f, dp[r] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        x = T::mfma(rd.row_frag(ks, b, s), q[s], x);
+        dp = T::mfma(rd.row_frag(vs, b, s), g[s], dp);
+      }
+      u32x4 ds[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float p = prob(__builtin_fmaf(x[r], a.c, -lse2));
+        if (partial) {
+          const int key = first + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
+          if (key >= mine.hi || key < mine.lo) p = 0.f;
+        }
+        x[r] = p * (dp[r] - delta);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ds[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) dq[db] = T::mfma(rd.tr_frag(ks, b, s, db), ds[s], dq[db]);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  if (!live || !a.dq) return;
+  uint16_t* dst = a.dq + row * a.dim;
+#pragma unroll
+  for (int db = 0; db < kDb; ++db)
+#pragma unroll
+    for (int gq = 0; gq < 4; ++gq) {
+      const int d = 32 * db + 8 * gq + 4 * half;
+      if (d < a.dim)
+        *reinterpret_cast<uint2*>(dst + d) =
+            uint2{T::pack(dq[db][4 * gq] * a.scale, dq[db][4 * gq + 1] * a.scale),
+                  T::pack(dq[db][4 * gq + 2] * a.scale, dq[db][4 * gq + 3] * a.scale)};
+    }
+}
+
+// dk and dv of a tile of NW * 32 keys of one kv head, over all the slots that see them, kSlots
+// (whole tokens of G slots) at a time.  A wave owns 32 keys; the sum over the group's heads is
+// the sum over slots.
+constexpr int kSlots = 64;
+
+template <class T, int D, int NW>
+__device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
+  constexpr int kS = D / 16, kDb = D / 32;
+  constexpr int kTile = kSlots * D * 2;
+  constexpr int kStage = 2 * kTile + 2 * kSlots * 4;  // q, dout, lse, delta
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * kStage];
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % a.kv_heads;
+  const int64_t tile = blockIdx.x / a.kv_heads;  // early keys are seen by the most tokens: first
+  const int sq = find_seq(a.k_off, a.n_seq, NW * 32, tile);
+  Seq S = seq_of(a, sq);
+  const int64_t key0 = (tile - (S.k0 / (NW * 32) + sq)) * (NW * 32);
+  // gradient rows exist for the whole of the sequence's room, zero past its key count
+  const int64_t room_end = a.k_off[sq + 1] < a.n_k ? a.k_off[sq + 1] : a.n_k;
+  const int64_t room = room_end - S.k0;
+  if (key0 < 0 || key0 >= room) return;
+  const int key = (int)key0 + wave * 32 + col;
+  const bool live = key < room, seen = key < S.lk;
+  const int ck = seen ? key : S.lk - 1;
+
+  // tokens that see a key of the tile / of the wave: causal i >= key - (lk - lq), and with a
+  // window i < key - (lk - lq) + window
+  const int shift = S.lk - S.lq;
+  auto first_tok = [&](int k) {
+    const int t = a.causal ? k - shift : 0;
+    return t < 0 ? 0 : t;
+  };
+  auto end_tok = [&](int k) {
+    if (!(a.causal && a.window > 0)) return S.lq;
+    const int64_t t = (int64_t)k - shift + a.window;
+    return t < 0 ? 0 : (t < S.lq ? (int)t : S.lq);
+  };
+  const int kend = (int)key0 + NW * 32 - 1 < S.lk - 1 ? (int)key0 + NW * 32 - 1 : S.lk - 1;
+  const int ts = a.ts;
+  int st0 = 0, st1 = 0;  // stages of ts tokens
+  if ((int)key0 < S.lk) {
+    st0 = first_tok((int)key0) / ts;
+    st1 = (end_tok(kend) + ts - 1) / ts;
+  }
+  const int wk0 = (int)key0 + wave * 32;
+  const bool wave_live = wk0 < S.lk;
+  const int wk1 = wk0 + 31 < S.lk - 1 ? wk0 + 31 : S.lk - 1;
+  const int my_first = first_tok(key), my_end = seen ? end_tok(key) : 0;
+  const int w_first = first_tok(wk0), w_end = end_tok(wk1);            // any of the wave's keys
+  const int w_first_all = first_tok(wk1), w_end_all = end_tok(wk0);    // all of them
+
+  u32x4 k[kS], v[kS];
+#pragma unroll
+  for (int s = 0; s < kS; ++s) k[s] = v[s] = u32x4{0u, 0u, 0u, 0u};
+  if (wave_live) {
+    load_cols<D>(a.k + (S.k0 + ck) * a.k_row + kvh * a.k_head, a.dim, half, k);
+    load_cols<D>(a.v + (S.k0 + ck) * a.v_row + kvh * a.v_head, a.dim, half, v);
+  }
+  f32x16 dk[kDb], dv[kDb];
+#pragma unroll
+  for (int db = 0; db < kDb; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[db][r] = 0.f, dv[db][r] = 0.f;
+
+  const TileReads<D> rd(lane);
+  const TileLoad<D, kSlots, NW> ld(wave, lane, a.dim / 8);
+  const int used = ts * a.G;  // slots of a stage
+  int tok_of[ld.kLoads], head_of[ld.kLoads];
+#pragma unroll
+  for (int j = 0; j < ld.kLoads; ++j) {
+    const int r = ld.row[j] < used ? ld.row[j] : used - 1;
+    tok_of[j] = r / a.G;
+    head_of[j] = r % a.G;
+  }
+  const int lr = lane < used ? lane : used - 1;
+  const int l_tok = lr / a.G, l_head = lr % a.G;
+  const int64_t d_row = (int64_t)a.heads * a.dim;
+  const uint16_t* qb = a.q + S.q0 * a.q_row + kvh * a.G * a.q_head;
+  const uint16_t* gb = a.dout + S.q0 * d_row + kvh * a.G * a.dim;
+  auto issue = [&](int buf, int st) {
+    const int t = st * ts;
+    const int last = S.lq - 1 - t;  // last valid token of the stage
+    const __amdgpu_buffer_rsrc_t rq = tile_rsrc(qb + (int64_t)t * a.q_row);
+    const __amdgpu_buffer_rsrc_t rg = tile_rsrc(gb + (int64_t)t * d_row);
+    unsigned char* base = smem + buf * kStage;
+#pragma unroll
+    for (int j = 0; j < ld.kLoads; ++j) {
+      const int tk = tok_of[j] < last ? tok_of[j] : last;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rq, (lds_void_t*)(base + (wave * ld.kLoads + j) * 1024), 16,
+          (tk * (int)a.q_row + head_of[j] * (int)a.q_head) * 2 + ld.chunk[j], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rg, (lds_void_t*)(base + kTile + (wave * ld.kLoads + j) * 1024), 16,
+          (tk * a.heads + head_of[j]) * a.dim * 2 + ld.chunk[j], 0, 0, 0);
+    }
+    if (wave < 2) {  // statistics: wave 0 lse, wave 1 delta, a slot per lane
+      const int tk = l_tok < last ? l_tok : last;
+      const float* src = (wave == 0 ? a.lse : a.delta) + (S.q0 + t + tk) * a.heads + kvh * a.G + l_head;
+      __builtin_amdgcn_global_load_lds((glb_void_t*)src,
+                                       (lds_void_t*)(base + 2 * kTile + wave * kSlots * 4), 4, 0, 0);
+    }
+  };
+  if (st0 < st1) issue(0, st0);
+#pragma unroll 1
+  for (int st = st0; st < st1; ++st) {
+    const int buf = (st - st0) & 1;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    sync_lds();
+    if (st + 1 < st1) issue(buf ^ 1, st + 1);
+    const int t = st * ts;
+    if (!wave_live || t >= w_end || t + ts <= w_first) continue;
+    const unsigned char* qs = smem + buf * kStage;
+    const unsigned char* gs = qs + kTile;
+    const float* lse_s = reinterpret_cast<const float*>(qs + 2 * kTile);
+    const float* del_s = lse_s + kSlots;
+    // every slot of the stage holds a token that sees every key of the wave
+    const bool partial = used < kSlots || t + ts > S.lq || t < w_first_all || t + ts > w_end_all ||
+                         wk0 + 31 >= S.lk;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      f32x16 x, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = 0.f, dp[r] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        x = T::mfma(rd.row_frag(qs, b, s), k[s], x);
+        dp = T::mfma(rd.row_frag(gs, b, s), v[s], dp);
+      }
+      u32x4 p16[2], ds[2];
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + 32 * b + 8 * q4 + 4 * half);
+        const f32x4 dl = *reinterpret_cast<const f32x4*>(del_s + 32 * b + 8 * q4 + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * q4 + e;
+          float p = prob(__builtin_fmaf(x[r], a.c, -ls[e] * kLog2e));
+          if (partial) {
+            const int slot = 32 * b + 8 * q4 + 4 * half + e;
+            const int tk = t + (int)(((uint32_t)slot * a.g_inv) >> 16);
+            if (slot >= used || tk < my_first || tk >= my_end) p = 0.f;
+          }
+          x[r] = p;
+          dp[r] = p * (dp[r] - dl[e]);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p16[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
+          ds[s][e] = T::pack(dp[8 * s + 2 * e], dp[8 * s + 2 * e + 1]);
+        }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) {
+          dv[db] = T::mfma(rd.tr_frag(gs, b, s, db), p16[s], dv[db]);
+          dk[db] = T::mfma(rd.tr_frag(qs, b, s, db), ds[s], dk[db]);
+        }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  if (!live) return;
+  const int64_t row = ((S.k0 + key) * a.kv_heads + kvh) * a.dim;
+#pragma unroll
+  for (int db = 0; db < kDb; ++db)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      const int d = 32 * db + 8 * g4 + 4 * half;
+      if (d >= a.dim) continue;
+      const float f = seen ? a.scale : 0.f;
+      *reinterpret_cast<uint2*>(a.dk + row + d) =
+          uint2{T::pack(dk[db][4 * g4] * f, dk[db][4 * g4 + 1] * f),
+                T::pack(dk[db][4 * g4 + 2] * f, dk[db][4 * g4 + 3] * f)};
+      *reinterpret_cast<uint2*>(a.dv + row + d) =
+          uint2{T::pack(dv[db][4 * g4], dv[db][4 * g4 + 1]),
+                T::pack(dv[db][4 * g4 + 2], dv[db][4 * g4 + 3])};
+    }
+}
+
+// (The bodies are device functions: the host pass knows no buffer resources.)
+template <class T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_fwd_kernel(AttnArgs a) {
+  attn_fwd<T, D, NW>(a);
+}
+template <class T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(AttnArgs a) {
+  attn_dq<T, D, NW>(a);
+}
+template <class T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void attn_dkv_kernel(AttnArgs a) {
+  attn_dkv<T, D, NW>(a);
+}
+
+constexpr int kFwdWaves = 4, kBwdWaves = 4;
+
+template <class T, int D>
+hipError_t run_fwd(AttnArgs a, hipStream_t s) {
+  const int64_t grid = a.tiles * a.kv_heads * a.splits;
+  hipLaunchKernelGGL((attn_fwd_kernel<T, D, kFwdWaves>), dim3((unsigned)grid), dim3(64 * kFwdWaves),
+                     0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && a.splits > 1) {
+    const int64_t rows = a.n_q * a.heads;
+    hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+template <class T, int D>
+hipError_t run_bwd(AttnArgs a, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.n_q > 0) {
+    a.ts = 32 * kBwdWaves / a.G;
+    a.tiles = a.n_q / a.ts + a.n_seq;
+    hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves>), dim3((unsigned)(a.tiles * a.kv_heads)),
+                       dim3(64 * kBwdWaves), 0, s, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.dk && a.n_k > 0) {
+    a.ts = kSlots / a.G;
+    a.tiles = a.n_k / (32 * kBwdWaves) + a.n_seq;
+    hipLaunchKernelGGL((attn_dkv_kernel<T, D, kBwdWaves>), dim3((unsigned)(a.tiles * a.kv_heads)),
+                       dim3(64 * kBwdWaves), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+// Splits of the key axis: enough workgroups for four rounds of the chip's two per CU where the
+// tiles alone are fewer than one, and no fewer than 256 keys of the mean sequence each.
+int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
+  constexpr int n_cu = 256;
+  const int G = heads / kv_heads;
+  const int64_t ts = 32 * kFwdWaves / G;
+  // tiles that hold tokens, at most one a sequence more than the mean length takes
+  const int64_t wgs = (n_q / ts + (n_q < n_seq ? n_q : n_seq)) * kv_heads;
+  if (wgs >= 2 * n_cu || n_q == 0) return 1;
+  const int64_t mean = n_k / n_seq;
+  int64_t s = (8 * (int64_t)n_cu + wgs - 1) / wgs;
+  const int64_t most = mean / 256 < 1 ? 1 : mean / 256;
+  if (s > most) s = most;
+  return (int)(s > 64 ? 64 : s);
+}
+
+hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream) {
+  if (a.n_q == 0) return hipSuccess;
+  a.ts = 32 * kFwdWaves / a.G;
+  a.tiles = a.n_q / a.ts + a.n_seq;
+  if (a.f16) return a.dim <= 64 ? run_fwd<HalfF16, 64>(a, stream) : run_fwd<HalfF16, 128>(a, stream);
+  return a.dim <= 64 ? run_fwd<HalfBf16, 64>(a, stream) : run_fwd<HalfBf16, 128>(a, stream);
+}
+
+hipError_t launch_attn_bwd(AttnArgs a, hipStream_t stream) {
+  if (a.f16) return a.dim <= 64 ? run_bwd<HalfF16, 64>(a, stream) : run_bwd<HalfF16, 128>(a, stream);
+  return a.dim <= 64 ? run_bwd<HalfBf16, 64>(a, stream) : run_bwd<HalfBf16, 128>(a, stream);
+}
+
+}  // namespace hpr

@@ -245,6 +245,76 @@ hipError_t launch_retrieval_metrics(const int64_t* idx, int nq, int64_t ld, int 
                                     const int64_t* pos, int32_t* ranks, double* out,
                                     hipStream_t stream);
 
+// Attention over packed sequences (attention.hip, which states the definition).  Strides in
+// elements.  The launchers fill ts and tiles.
+struct AttnArgs {
+  const uint16_t *q, *k, *v;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  const int64_t *q_off, *k_off, *k_len;  // k_len may be null
+  int64_t n_q, n_k;
+  int n_seq, heads, kv_heads, G, dim;
+  int window;       // 0: none
+  bool causal, f16;
+  float scale, c;   // c = scale * log2(e)
+  uint32_t g_inv;   // 65536 / G + 1: (slot * g_inv) >> 16 = slot / G for slot < 64
+  uint16_t* out;    // [n_q, heads, dim] (the gradients read it)
+  float* lse;       // [n_q, heads], may be null in the forward
+  int splits;       // of the key axis; above 1 the parts go through
+  float* part_o;    // [splits, n_q, heads, dim] and
+  float* part_ml;   // [splits, n_q, heads, 2]
+  const uint16_t* dout;       // [n_q, heads, dim]
+  uint16_t *dq, *dk, *dv;     // dense; dq may be null, dk and dv together
+  float* delta;               // [n_q, heads] scratch
+  int ts;           // tokens of a tile or stage
+  int64_t tiles;    // per kv head
+};
+constexpr int kMaxGroup = 32;  // query heads of one kv head
+int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
+hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream);
+hipError_t launch_attn_bwd(AttnArgs a, hipStream_t stream);
+
+// Rotation by position (rotary.hip) of up to two tensors of n rows: x[i] [n, heads[i], dim] with
+// strides row[i], head[i] into out[i] (dense).
+struct RotaryArgs {
+  const uint16_t* x[2];
+  uint16_t* out[2];
+  int64_t row[2], head[2];
+  int heads[2];
+  const int32_t* pos;
+  const float *cosp, *sinp;  // [n_pos, rot / 2]
+  int64_t n, n_pos;
+  int dim, rot;
+  bool inverse, f16;
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+
+// Shared projection with low-rank adapters (adapters.hip).
+struct AdapterArgs {
+  const uint16_t *x, *w, *a, *b;  // [n, k], [m, k], [n_ad, r, k], [n_ad, m, r]
+  const float* scale;             // [n_ad]
+  const int64_t* off;             // [n_req + 1]
+  const int32_t* adapter;         // [n_req], negative: none
+  int64_t n;
+  int k, m, r, n_ad, n_req;
+  bool f16;
+};
+constexpr int kMaxRank = 128;
+inline int adapter_rank_pad(int r) { return (r + 15) / 16 * 16; }
+// h[n, rank_pad] = scale_a x A_a^T (zero past r), rows of requests without an adapter unwritten
+hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t stream);
+// y[n, m] = x W^T + h B_a^T
+hipError_t launch_adapter_expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y,
+                                 hipStream_t stream);
+// out[i] = in[i]^T for count matrices [rows, cols]
+hipError_t launch_transpose(const uint16_t* in, uint16_t* out, int64_t count, int rows, int cols,
+                            hipStream_t stream);
+// Sums over the rows of each adapter's requests, L[n, rank_pad] and M[n, cols]:
+//   out[a][j][c] = sum L[t, j] M[t, c], j < r (transposed: out[a][c][j])
+// through parts of adapter_outer_parts(n, n_req) * rank_pad * cols floats.
+int64_t adapter_outer_parts(int64_t n, int n_req);
+hipError_t launch_adapter_outer(const AdapterArgs& a, const uint16_t* L, const uint16_t* M, int cols,
+                                bool transposed, float* part, uint16_t* out, hipStream_t stream);
+
 // Calibration (calibration.hip): a pure-MFMA kernel of mfma_calibration_waves(n_cu) waves, each
 // running `iters` iterations of four v_mfma_f32_32x32x16_bf16 (sink: at least one float per
 // 4-wave workgroup); a pure streaming read of `bytes` (a multiple of 16) with `blocks`
