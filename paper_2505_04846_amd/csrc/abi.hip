@@ -601,14 +601,20 @@ size_t packed_attention_workspace_size(const hpr_attention* d) {
       d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
     return 0;
   const int64_t splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
-  if (splits <= 1) return 0;
+  const size_t plan = align_up((size_t)attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads) *
+                               sizeof(AttnTile));
+  if (splits <= 1) return plan;
   const size_t rows = (size_t)splits * d->n_q * d->heads;
-  return align_up(rows * d->dim * sizeof(float)) + align_up(rows * 2 * sizeof(float));
+  return plan + align_up(rows * d->dim * sizeof(float)) + align_up(rows * 2 * sizeof(float));
 }
 
 size_t packed_attention_bwd_workspace_size(const hpr_attention* d) {
-  if (!d || d->n_q < 1 || d->heads < 1) return 0;
-  return align_up((size_t)d->n_q * d->heads * sizeof(float));
+  if (!d || d->n_q < 0 || d->n_seq < 0 || d->heads < 1 || d->kv_heads < 1 ||
+      d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
+    return 0;
+  return align_up((size_t)d->n_q * d->heads * sizeof(float)) +
+         align_up((size_t)attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads) * sizeof(AttnTile)) +
+         align_up((size_t)attn_plan_key_tiles(d->n_k, d->n_seq, d->kv_heads) * sizeof(AttnTile));
 }
 
 hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const uint16_t* k,
@@ -628,8 +634,10 @@ hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const
   a.out = out;
   a.lse = lse;
   a.splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
+  Carver c(ws);
+  const int64_t plan = attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads);
+  if (plan > 0) a.q_plan = c.take<AttnTile>((size_t)plan * sizeof(AttnTile));
   if (a.splits > 1) {
-    Carver c(ws);
     const size_t rows = (size_t)a.splits * d->n_q * d->heads;
     a.part_o = c.take<float>(rows * d->dim * sizeof(float));
     a.part_ml = c.take<float>(rows * 2 * sizeof(float));
@@ -663,7 +671,12 @@ hpr_status packed_attention_bwd(const hpr_attention* d, const uint16_t* dout, co
   a.dq = dq;
   a.dk = dk;
   a.dv = dv;
-  a.delta = static_cast<float*>(ws);
+  Carver c(ws);
+  a.delta = c.take<float>((size_t)d->n_q * d->heads * sizeof(float));
+  const int64_t plan = attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads);
+  if (plan > 0) a.q_plan = c.take<AttnTile>((size_t)plan * sizeof(AttnTile));
+  const int64_t k_plan = attn_plan_key_tiles(d->n_k, d->n_seq, d->kv_heads);
+  if (k_plan > 0) a.k_plan = c.take<AttnTile>((size_t)k_plan * sizeof(AttnTile));
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = timed("attn_bwd", s, [&] { return launch_attn_bwd(a, s); });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "attention gradient launch");

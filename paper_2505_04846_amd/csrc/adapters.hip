@@ -361,8 +361,7 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
       int cc = c0 + 8 * c;
       if (cc >= cols) cc = cols - 8;
       const void* p = in ? (const void*)(M + (t + r) * cols + cc) : (const void*)kZero16;
-      __builtin_amdgcn_global_load_lds((glb_void_t*)p,
-                                       (lds_void_t*)(smem + (1 + wave) * kTile + j * 1024), 16, 0, 0);
+      load_lds16(p, LDS_ADDRESS(smem) + (1 + wave) * kTile + j * 1024);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -372,8 +371,7 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
       int cc = j0 + 8 * c;
       if (cc >= rp) cc = rp - 8;
       const void* p = in ? (const void*)(L + (t + r) * rp + cc) : (const void*)kZero16;
-      __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)(smem + (2 * wave + j) * 1024), 16,
-                                       0, 0);
+      load_lds16(p, LDS_ADDRESS(smem) + (2 * wave + j) * 1024);
     }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     sync_lds();

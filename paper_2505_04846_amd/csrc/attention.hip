@@ -12,9 +12,10 @@
 //
 // Slots.  The query rows of a kv head's whole group share its keys, so a tile's rows are (token,
 // head of the group) pairs, "slots": slot = token * G + head.  A tile takes TS = rows / G whole
-// tokens.  Tiles are found without a plan: sequence s owns the tile numbers from
-// q_off[s] / TS + s, which leaves every sequence at least ceil(lq / TS) of them, and a workgroup
-// searches the offsets for its own (numbers past the sequence's end exit at once).
+// tokens.  Sequence s owns the tile numbers from q_off[s] / TS + s, which leaves every sequence at
+// least ceil(lq / TS) of them (numbers past the sequence's end are no tiles).  In small calls a
+// workgroup searches the offsets for its tile; calls of many tiles have a first launch write
+// them down (plan_kernel).
 //
 // Products.  All of them are v_mfma_f32_32x32x16 with the 32 rows that a wave owns as the columns
 // of the result, so a lane holds 16 entries of one of its rows (the entries of the two half-waves
@@ -70,11 +71,42 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& a, int s) {
   return r;
 }
 
+// Tile `tile` of ts tokens a tile.  The whole wave searches.
+__device__ __forceinline__ AttnTile find_q_tile(const AttnArgs& a, uint32_t tile, int ts) {
+  const int s = find_seq(a.q_off, a.n_seq, ts, tile);
+  const Seq S = seq_of(a, s);
+  AttnTile r = {S.q0, S.k0, S.lq, S.lk, 0, 0};
+  const int64_t first = ((int64_t)tile - ((uint32_t)S.q0 / (uint32_t)ts + (uint32_t)s)) * ts;
+  if (first >= 0 && first < S.lq) {
+    r.first = (int)first;
+    r.n = S.lq - r.first < ts ? S.lq - r.first : ts;
+  }
+  return r;
+}
+// The same for tiles of `rows` key rows; the gradients' rows of a sequence are its whole room.
+__device__ __forceinline__ AttnTile find_k_tile(const AttnArgs& a, uint32_t tile, int rows) {
+  const int s = find_seq(a.k_off, a.n_seq, rows, tile);
+  const Seq S = seq_of(a, s);
+  AttnTile r = {S.q0, S.k0, S.lq, S.lk, 0, 0};
+  const int64_t end = a.k_off[s + 1] < a.n_k ? a.k_off[s + 1] : a.n_k;
+  const int64_t room = end - S.k0;
+  const int64_t first = ((int64_t)tile - ((uint32_t)S.k0 / (uint32_t)rows + (uint32_t)s)) * rows;
+  if (first >= 0 && first < room) {
+    r.first = (int)first;
+    r.n = room - first < rows ? (int)(room - first) : rows;
+  }
+  return r;
+}
+__device__ __forceinline__ AttnTile uniform_tile(const AttnTile* p) {
+  AttnTile r = *p;  // (a uniform address: scalar loads)
+  return r;
+}
+
 // Keys [lo, hi) visible from token i (of lq, with lk keys).
 struct Span {
   int lo, hi;
 };
-__device__ __forceinline__ Span span_of(const AttnArgs& a, const Seq& s, int i) {
+__device__ __forceinline__ Span span_of(const AttnArgs& a, const AttnTile& s, int i) {
   Span r = {0, s.lk};
   if (a.causal) {
     const int64_t reach = (int64_t)i + s.lk - s.lq;  // the last visible key
@@ -87,8 +119,8 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, const Seq& s, int i) 
   return r;
 }
 
-// The right operand's registers of one 32-slot column block: values [16 s, 16 s + 16) of the
-// lane's row, zero past dim.
+// The right operand's registers of one 32-row column block straight from memory: values
+// [16 s, 16 s + 16) of the lane's row, zero past dim.
 template <int D>
 __device__ __forceinline__ void load_cols(const uint16_t* row, int dim, int half, u32x4 (&f)[D / 16]) {
 #pragma unroll
@@ -99,11 +131,110 @@ __device__ __forceinline__ void load_cols(const uint16_t* row, int dim, int half
   }
 }
 
+// A wave's own 32 rows through its own 32 * D * 2 bytes of LDS, so that memory sees whole rows (by
+// lanes a row's pieces of 16 or 32 bytes would be requests of their own).
+template <int D>
+struct WaveRows {
+  static constexpr int kCh = D / 8, kRows = 64 / kCh, kLoads = 32 / kRows;
+  static constexpr int kBytes = 32 * D * 2;
+  // src(r): the address of row r of the 32
+  template <class F>
+  static __device__ __forceinline__ void load(F src, uint32_t lds, int lane, int chunks) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = j * kRows + lane / kCh;
+      const int c = (lane % kCh) ^ swz<D>(r);
+      load_lds16(src(r) + 8 * (c < chunks ? c : chunks - 1), lds + j * 1024);
+    }
+  }
+  // the loaded rows as right operands, zero past dim
+  static __device__ __forceinline__ void cols(const TileReads<D>& rd, const unsigned char* lds, int dim,
+                                              int half, u32x4 (&f)[D / 16]) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      f[s] = rd.row_frag(lds, 0, s);
+      if (16 * s + 8 * half >= dim) f[s] = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  // x, times the lane's factor, as 16-bit rows: dst(r) is row r's address, or null
+  template <class T, class F>
+  static __device__ __forceinline__ void store(const f32x16 (&x)[D / 32], float factor, F dst,
+                                               unsigned char* lds, int lane, int chunks) {
+    const int row = lane & 31, half = lane >> 5;
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);  // (a wave's LDS operations execute in program order)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<uint2*>(lds + row * D * 2 + (((4 * db + g) ^ swz<D>(row)) << 4) + 8 * half) =
+            uint2{T::pack(x[db][4 * g] * factor, x[db][4 * g + 1] * factor),
+                  T::pack(x[db][4 * g + 2] * factor, x[db][4 * g + 3] * factor)};
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = j * kRows + lane / kCh;
+      const int c = (lane % kCh) ^ swz<D>(r);
+      uint16_t* to = dst(r);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(lds + j * 1024 + lane * 16);
+      if (to && c < chunks) *reinterpret_cast<u32x4*>(to + 8 * c) = v;
+    }
+  }
+};
+
+// A stage's loads: kKeys rows of K, then of V, straight into LDS.  The offsets of a whole tile are
+// kept per lane; the sequence's last tile forms its own.
+template <int D, int NW>
+struct KvLoad {
+  using L = TileLoad<D, kKeys, NW>;
+  L at;
+  const uint16_t *k, *v;  // the kv head's first rows
+  int ok[L::kLoads], ov[L::kLoads];
+  __device__ __forceinline__ KvLoad(const AttnArgs& a, const AttnTile& S, int kvh, int wave, int lane)
+      : at(wave, lane, a.dim / 8),
+        k(a.k + S.k0 * a.k_row + kvh * a.k_head),
+        v(a.v + S.k0 * a.v_row + kvh * a.v_head) {
+#pragma unroll
+    for (int j = 0; j < L::kLoads; ++j) {
+      ok[j] = at.row[j] * (int)a.k_row * 2 + at.chunk[j];
+      ov[j] = at.row[j] * (int)a.v_row * 2 + at.chunk[j];
+    }
+  }
+  __device__ __forceinline__ void issue(const AttnArgs& a, const AttnTile& S, uint32_t st, int wave,
+                                        int kt) const {
+    const int first = kt * kKeys;
+    const int last = S.lk - 1 - first;  // last valid row of the tile (>= 0)
+    const rsrc_t rk = rsrc_of(k + (int64_t)first * a.k_row);
+    const rsrc_t rv = rsrc_of(v + (int64_t)first * a.v_row);
+    const uint32_t to = st + wave * L::kLoads * 1024;  // LDS address
+    constexpr int kTile = kKeys * D * 2;
+    if (last >= kKeys - 1) {
+#pragma unroll
+      for (int j = 0; j < L::kLoads; ++j)
+        load_lds16(rk, to + j * 1024, ok[j]);
+#pragma unroll
+      for (int j = 0; j < L::kLoads; ++j)
+        load_lds16(rv, to + kTile + j * 1024, ov[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < L::kLoads; ++j) {
+        const int r = at.row[j] < last ? at.row[j] : last;
+        load_lds16(rk, to + j * 1024, r * (int)a.k_row * 2 + at.chunk[j]);
+        load_lds16(rv, to + kTile + j * 1024, r * (int)a.v_row * 2 + at.chunk[j]);
+      }
+    }
+  }
+};
+
 // A probability from the logarithm (base 2) of it.  An fp32 lse of enormous scores is off by more than
 // a power of two; the clamp (an output modifier, free) keeps such rows finite.
 __device__ __forceinline__ float prob(float x) {
   return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f);
 }
+
+// Scheduling groups: the next n LDS reads / products of the region go here.
+#define sched_ds(n) __builtin_amdgcn_sched_group_barrier(0x100, n, 0)
+#define sched_mfma(n) __builtin_amdgcn_sched_group_barrier(0x008, n, 0)
+#define sched_valu(n) __builtin_amdgcn_sched_group_barrier(0x002, n, 0)
 
 // ---- forward --------------------------------------------------------------------------------
 
@@ -116,16 +247,14 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTile];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % a.kv_heads;
-  const int64_t w = blockIdx.x / a.kv_heads;
-  const int split = (int)(w % a.splits);
-  const int64_t tile = a.tiles - 1 - w / a.splits;  // late tiles see the most keys: first
-  const int sq = find_seq(a.q_off, a.n_seq, a.ts, tile);
-  const Seq S = seq_of(a, sq);
-  const int64_t tok0 = (tile - (S.q0 / a.ts + sq)) * a.ts;
-  if (tok0 < 0 || tok0 >= S.lq) return;
-  const int t0 = (int)tok0;
-  const int n_tok = S.lq - t0 < a.ts ? S.lq - t0 : a.ts;
+  const int kvh = blockIdx.x % (uint32_t)a.kv_heads;
+  const uint32_t w = blockIdx.x / (uint32_t)a.kv_heads;
+  const int split = a.splits > 1 ? w % (uint32_t)a.splits : 0;
+  // late tiles see the most keys: first
+  const uint32_t tile = (uint32_t)a.tiles - 1 - (a.splits > 1 ? w / (uint32_t)a.splits : w);
+  const AttnTile S = a.q_plan ? uniform_tile(a.q_plan + tile) : find_q_tile(a, tile, a.ts);
+  if (S.n == 0) return;
+  const int t0 = S.first, n_tok = S.n;
 
   // this lane's slot
   const int slot = wave * 32 + col;
@@ -146,8 +275,36 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   const int kt0 = k_first + (int)((int64_t)n_kt * split / a.splits);
   const int kt1 = k_first + (int)((int64_t)n_kt * (split + 1) / a.splits);
 
+  // the wave's slots: row r's token within the tile and head, the last slot's past it
+  auto slot_tok = [&](int r) {
+    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
+    return (int)(((uint32_t)s * a.g_inv) >> 16);
+  };
+  auto slot_head = [&](int r, int t) {
+    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
+    return kvh * a.G + s - t * a.G;
+  };
+  const KvLoad<D, NW> ld(a, S, kvh, wave, lane);
+  auto issue = [&](int buf, int kt) { ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt); };
+  // q through the second stage, which the loop fills only after its first barrier
+  static_assert(NW * WaveRows<D>::kBytes <= 2 * kTile, "the wave's rows fit a stage");
+  unsigned char* own = smem + 2 * kTile + wave * WaveRows<D>::kBytes;
+  WaveRows<D>::load(
+      [&](int r) {
+        const int t = slot_tok(r);
+        return a.q + (S.q0 + t0 + t) * a.q_row + slot_head(r, t) * a.q_head;
+      },
+      LDS_ADDRESS(smem) + 2 * kTile + wave * WaveRows<D>::kBytes, lane, a.dim / 8);
+  if (kt0 < kt1) {
+    issue(0, kt0);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * ld.at.kLoads));
+  } else {
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  }
+  const TileReads<D> rd(lane);
   u32x4 q[kS];
-  load_cols<D>(a.q + (S.q0 + tok) * a.q_row + head * a.q_head, a.dim, half, q);
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  WaveRows<D>::cols(rd, own, a.dim, half, q);
 
   f32x16 o[kDb];
 #pragma unroll
@@ -156,36 +313,11 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
     for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
   float m = kNoMax, l = 0.f;
 
-  const TileReads<D> rd(lane);
-  const TileLoad<D, kKeys, NW> ld(wave, lane, a.dim / 8);
-  const uint16_t* kb = a.k + S.k0 * a.k_row + kvh * a.k_head;
-  const uint16_t* vb = a.v + S.k0 * a.v_row + kvh * a.v_head;
-  auto issue = [&](int buf, int kt) {
-    const int first = kt * kKeys;
-    const int last = S.lk - 1 - first;  // last valid row of the tile (>= 0)
-    const __amdgpu_buffer_rsrc_t rk = tile_rsrc(kb + (int64_t)first * a.k_row);
-    const __amdgpu_buffer_rsrc_t rv = tile_rsrc(vb + (int64_t)first * a.v_row);
-    unsigned char* st = smem + buf * 2 * kTile;
-#pragma unroll
-    for (int j = 0; j < ld.kLoads; ++j) {
-      const int r = ld.row[j] < last ? ld.row[j] : last;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(st + (wave * ld.kLoads + j) * 1024),
-                                               16, r * (int)a.k_row * 2 + ld.chunk[j], 0, 0, 0);
-    }
-#pragma unroll
-    for (int j = 0; j < ld.kLoads; ++j) {
-      const int r = ld.row[j] < last ? ld.row[j] : last;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rv, (lds_void_t*)(st + kTile + (wave * ld.kLoads + j) * 1024), 16,
-          r * (int)a.v_row * 2 + ld.chunk[j], 0, 0, 0);
-    }
-  };
-
-  if (kt0 < kt1) issue(0, kt0);
 #pragma unroll 1
   for (int kt = kt0; kt < kt1; ++kt) {
     const int buf = (kt - kt0) & 1;
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     sync_lds();  // the tile has landed, and nobody reads the other stage any more
     if (kt + 1 < kt1) issue(buf ^ 1, kt + 1);
     const int first = kt * kKeys;
@@ -194,12 +326,20 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
     const unsigned char* vs = ks + kTile;
     f32x16 x[2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int r = 0; r < 16; ++r) x[0][r] = x[1][r] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[b][r] = 0.f;
+    for (int s = 0; s < kS; ++s)
 #pragma unroll
-      for (int s = 0; s < kS; ++s) x[b] = T::mfma(rd.row_frag(ks, b, s), q[s], x[b]);
+      for (int b = 0; b < 2; ++b) x[b] = T::mfma(rd.row_frag(ks, b, s), q[s], x[b]);
+    // the operands' reads run two k-steps ahead of the products
+    sched_ds(4);
+#pragma unroll
+    for (int s = 0; s < kS - 2; ++s) {
+      sched_mfma(2);
+      sched_ds(2);
     }
+    sched_mfma(4);
+    __builtin_amdgcn_sched_barrier(0);
     if (first + kKeys > wfirst.hi || first < wlast.lo) {  // some key is not every slot's
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -244,11 +384,11 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
     }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-  if (!live) return;
   l = half_sum(l);
   const int64_t row = (S.q0 + tok) * a.heads + head;
   if (a.splits > 1) {
     // unnormalised sums, their reference maximum and total: attn_join_kernel
+    if (!live) return;
     const int64_t at = ((int64_t)split * a.n_q * a.heads + row);
     float* dst = a.part_o + at * a.dim;
 #pragma unroll
@@ -266,19 +406,18 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
     }
     return;
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  uint16_t* dst = a.out + row * a.dim;
-#pragma unroll
-  for (int db = 0; db < kDb; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d = 32 * db + 8 * g + 4 * half;
-      if (d < a.dim)
-        *reinterpret_cast<uint2*>(dst + d) =
-            uint2{T::pack(o[db][4 * g] * inv, o[db][4 * g + 1] * inv),
-                  T::pack(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv)};
-    }
-  if (a.lse && half == 0) a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
+  if (a.lse && live && half == 0) a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  sync_lds();  // nobody reads the stages any more
+  WaveRows<D>::template store<T>(
+      o, l > 0.f ? 1.f / l : 0.f,
+      [&](int r) -> uint16_t* {
+        const int t = slot_tok(r);
+        return wave * 32 + r < n_slot
+                   ? a.out + ((S.q0 + t0 + t) * a.heads + slot_head(r, t)) * a.dim
+                   : nullptr;
+      },
+      own, lane, a.dim / 8);
 }
 
 // out = the splits' sums joined under their common maximum.  A wave per (token, head), lane d.
@@ -318,14 +457,11 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTile];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % a.kv_heads;
-  const int64_t tile = a.tiles - 1 - blockIdx.x / a.kv_heads;
-  const int sq = find_seq(a.q_off, a.n_seq, a.ts, tile);
-  const Seq S = seq_of(a, sq);
-  const int64_t tok0 = (tile - (S.q0 / a.ts + sq)) * a.ts;
-  if (tok0 < 0 || tok0 >= S.lq) return;
-  const int t0 = (int)tok0;
-  const int n_tok = S.lq - t0 < a.ts ? S.lq - t0 : a.ts;
+  const int kvh = blockIdx.x % (uint32_t)a.kv_heads;
+  const uint32_t tile = (uint32_t)a.tiles - 1 - blockIdx.x / (uint32_t)a.kv_heads;
+  const AttnTile S = a.q_plan ? uniform_tile(a.q_plan + tile) : find_q_tile(a, tile, a.ts);
+  if (S.n == 0) return;
+  const int t0 = S.first, n_tok = S.n;
   const int slot = wave * 32 + col;
   const int n_slot = n_tok * a.G;
   const bool live = slot < n_slot;
@@ -340,13 +476,54 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   const int kt0 = tfirst.lo / kKeys, kt1 = (tlast.hi + kKeys - 1) / kKeys;
 
   const int64_t row = (S.q0 + tok) * a.heads + head;
+  auto slot_tok = [&](int r) {
+    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
+    return (int)(((uint32_t)s * a.g_inv) >> 16);
+  };
+  auto slot_head = [&](int r, int t) {
+    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
+    return kvh * a.G + s - t * a.G;
+  };
+  auto dense_row = [&](int r) {
+    const int t = slot_tok(r);
+    return ((S.q0 + t0 + t) * a.heads + slot_head(r, t)) * a.dim;
+  };
+  const KvLoad<D, NW> ld(a, S, kvh, wave, lane);
+  auto issue = [&](int buf, int kt) { ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt); };
+  // q through the second stage, dout through the first, then out through the second
+  constexpr int kOwn = WaveRows<D>::kBytes;
+  static_assert(NW * kOwn <= 2 * kTile, "the wave's rows fit a stage");
+  const TileReads<D> rd(lane);
+  unsigned char* own = smem + 2 * kTile + wave * kOwn;
+  const uint32_t own_at = LDS_ADDRESS(smem) + 2 * kTile + wave * kOwn;
+  WaveRows<D>::load(
+      [&](int r) {
+        const int t = slot_tok(r);
+        return a.q + (S.q0 + t0 + t) * a.q_row + slot_head(r, t) * a.q_head;
+      },
+      own_at, lane, a.dim / 8);
+  WaveRows<D>::load([&](int r) { return a.dout + dense_row(r); }, LDS_ADDRESS(smem) + wave * kOwn, lane,
+                    a.dim / 8);
+  const float lse2 = a.lse[row] * kLog2e;
   u32x4 q[kS], g[kS];
-  load_cols<D>(a.q + (S.q0 + tok) * a.q_row + head * a.q_head, a.dim, half, q);
-  load_cols<D>(a.dout + row * a.dim, a.dim, half, g);
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  WaveRows<D>::cols(rd, own, a.dim, half, q);
+  WaveRows<D>::cols(rd, smem + wave * kOwn, a.dim, half, g);
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  sync_lds();
+  WaveRows<D>::load([&](int r) { return (const uint16_t*)a.out + dense_row(r); }, own_at, lane, a.dim / 8);
+  if (kt0 < kt1) {
+    issue(0, kt0);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * ld.at.kLoads));
+  } else {
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  }
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
   float delta = 0.f;
   {
     u32x4 o[kS];
-    load_cols<D>(a.out + row * a.dim, a.dim, half, o);
+    WaveRows<D>::cols(rd, own, a.dim, half, o);
 #pragma unroll
     for (int s = 0; s < kS; ++s)
 #pragma unroll
@@ -355,7 +532,6 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
     delta = half_sum(delta);
   }
   if (live && half == 0) a.delta[row] = delta;
-  const float lse2 = a.lse[row] * kLog2e;
 
   f32x16 dq[kDb];
 #pragma unroll
@@ -363,31 +539,11 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
 
-  const TileReads<D> rd(lane);
-  const TileLoad<D, kKeys, NW> ld(wave, lane, a.dim / 8);
-  const uint16_t* kb = a.k + S.k0 * a.k_row + kvh * a.k_head;
-  const uint16_t* vb = a.v + S.k0 * a.v_row + kvh * a.v_head;
-  auto issue = [&](int buf, int kt) {
-    const int first = kt * kKeys;
-    const int last = S.lk - 1 - first;
-    const __amdgpu_buffer_rsrc_t rk = tile_rsrc(kb + (int64_t)first * a.k_row);
-    const __amdgpu_buffer_rsrc_t rv = tile_rsrc(vb + (int64_t)first * a.v_row);
-    unsigned char* st = smem + buf * 2 * kTile;
-#pragma unroll
-    for (int j = 0; j < ld.kLoads; ++j) {
-      const int r = ld.row[j] < last ? ld.row[j] : last;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(st + (wave * ld.kLoads + j) * 1024),
-                                               16, r * (int)a.k_row * 2 + ld.chunk[j], 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rv, (lds_void_t*)(st + kTile + (wave * ld.kLoads + j) * 1024), 16,
-          r * (int)a.v_row * 2 + ld.chunk[j], 0, 0, 0);
-    }
-  };
-  if (kt0 < kt1) issue(0, kt0);
 #pragma unroll 1
   for (int kt = kt0; kt < kt1; ++kt) {
     const int buf = (kt - kt0) & 1;
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     sync_lds();
     if (kt + 1 < kt1) issue(buf ^ 1, kt + 1);
     const int first = kt * kKeys;
@@ -426,18 +582,13 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
     }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-  if (!live || !a.dq) return;
-  uint16_t* dst = a.dq + row * a.dim;
-#pragma unroll
-  for (int db = 0; db < kDb; ++db)
-#pragma unroll
-    for (int gq = 0; gq < 4; ++gq) {
-      const int d = 32 * db + 8 * gq + 4 * half;
-      if (d < a.dim)
-        *reinterpret_cast<uint2*>(dst + d) =
-            uint2{T::pack(dq[db][4 * gq] * a.scale, dq[db][4 * gq + 1] * a.scale),
-                  T::pack(dq[db][4 * gq + 2] * a.scale, dq[db][4 * gq + 3] * a.scale)};
-    }
+  if (!a.dq) return;
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  sync_lds();  // nobody reads the stages any more
+  WaveRows<D>::template store<T>(
+      dq, a.scale,
+      [&](int r) -> uint16_t* { return wave * 32 + r < n_slot ? a.dq + dense_row(r) : nullptr; }, own,
+      lane, a.dim / 8);
 }
 
 // dk and dv of a tile of NW * 32 keys of one kv head, over all the slots that see them, kSlots
@@ -453,17 +604,13 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * kStage];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % a.kv_heads;
-  const int64_t tile = blockIdx.x / a.kv_heads;  // early keys are seen by the most tokens: first
-  const int sq = find_seq(a.k_off, a.n_seq, NW * 32, tile);
-  Seq S = seq_of(a, sq);
-  const int64_t key0 = (tile - (S.k0 / (NW * 32) + sq)) * (NW * 32);
-  // gradient rows exist for the whole of the sequence's room, zero past its key count
-  const int64_t room_end = a.k_off[sq + 1] < a.n_k ? a.k_off[sq + 1] : a.n_k;
-  const int64_t room = room_end - S.k0;
-  if (key0 < 0 || key0 >= room) return;
-  const int key = (int)key0 + wave * 32 + col;
-  const bool live = key < room, seen = key < S.lk;
+  const int kvh = blockIdx.x % (uint32_t)a.kv_heads;
+  const uint32_t tile = blockIdx.x / (uint32_t)a.kv_heads;  // early keys are seen by the most tokens: first
+  const AttnTile S = a.k_plan ? uniform_tile(a.k_plan + tile) : find_k_tile(a, tile, NW * 32);
+  if (S.n == 0) return;
+  const int key0 = S.first;
+  const int key = key0 + wave * 32 + col;
+  const bool seen = key < S.lk;  // (the gradient rows past the key count get zeros)
   const int ck = seen ? key : S.lk - 1;
 
   // tokens that see a key of the tile / of the wave: causal i >= key - (lk - lq), and with a
@@ -478,14 +625,14 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
     const int64_t t = (int64_t)k - shift + a.window;
     return t < 0 ? 0 : (t < S.lq ? (int)t : S.lq);
   };
-  const int kend = (int)key0 + NW * 32 - 1 < S.lk - 1 ? (int)key0 + NW * 32 - 1 : S.lk - 1;
+  const int kend = key0 + NW * 32 - 1 < S.lk - 1 ? key0 + NW * 32 - 1 : S.lk - 1;
   const int ts = a.ts;
   int st0 = 0, st1 = 0;  // stages of ts tokens
-  if ((int)key0 < S.lk) {
-    st0 = first_tok((int)key0) / ts;
+  if (key0 < S.lk) {
+    st0 = first_tok(key0) / ts;
     st1 = (end_tok(kend) + ts - 1) / ts;
   }
-  const int wk0 = (int)key0 + wave * 32;
+  const int wk0 = key0 + wave * 32;
   const bool wave_live = wk0 < S.lk;
   const int wk1 = wk0 + 31 < S.lk - 1 ? wk0 + 31 : S.lk - 1;
   const int my_first = first_tok(key), my_end = seen ? end_tok(key) : 0;
@@ -523,24 +670,21 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
   auto issue = [&](int buf, int st) {
     const int t = st * ts;
     const int last = S.lq - 1 - t;  // last valid token of the stage
-    const __amdgpu_buffer_rsrc_t rq = tile_rsrc(qb + (int64_t)t * a.q_row);
-    const __amdgpu_buffer_rsrc_t rg = tile_rsrc(gb + (int64_t)t * d_row);
-    unsigned char* base = smem + buf * kStage;
+    const rsrc_t rq = rsrc_of(qb + (int64_t)t * a.q_row);
+    const rsrc_t rg = rsrc_of(gb + (int64_t)t * d_row);
+    const uint32_t base = LDS_ADDRESS(smem) + buf * kStage;
 #pragma unroll
     for (int j = 0; j < ld.kLoads; ++j) {
       const int tk = tok_of[j] < last ? tok_of[j] : last;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rq, (lds_void_t*)(base + (wave * ld.kLoads + j) * 1024), 16,
-          (tk * (int)a.q_row + head_of[j] * (int)a.q_head) * 2 + ld.chunk[j], 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rg, (lds_void_t*)(base + kTile + (wave * ld.kLoads + j) * 1024), 16,
-          (tk * a.heads + head_of[j]) * a.dim * 2 + ld.chunk[j], 0, 0, 0);
+      load_lds16(rq, base + (wave * ld.kLoads + j) * 1024,
+                 (tk * (int)a.q_row + head_of[j] * (int)a.q_head) * 2 + ld.chunk[j]);
+      load_lds16(rg, base + kTile + (wave * ld.kLoads + j) * 1024,
+                 (tk * a.heads + head_of[j]) * a.dim * 2 + ld.chunk[j]);
     }
     if (wave < 2) {  // statistics: wave 0 lse, wave 1 delta, a slot per lane
       const int tk = l_tok < last ? l_tok : last;
       const float* src = (wave == 0 ? a.lse : a.delta) + (S.q0 + t + tk) * a.heads + kvh * a.G + l_head;
-      __builtin_amdgcn_global_load_lds((glb_void_t*)src,
-                                       (lds_void_t*)(base + 2 * kTile + wave * kSlots * 4), 4, 0, 0);
+      load_lds4(src, base + 2 * kTile + wave * kSlots * 4);
     }
   };
   if (st0 < st1) issue(0, st0);
@@ -604,22 +748,19 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
     }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-  if (!live) return;
-  const int64_t row = ((S.k0 + key) * a.kv_heads + kvh) * a.dim;
-#pragma unroll
-  for (int db = 0; db < kDb; ++db)
-#pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4) {
-      const int d = 32 * db + 8 * g4 + 4 * half;
-      if (d >= a.dim) continue;
-      const float f = seen ? a.scale : 0.f;
-      *reinterpret_cast<uint2*>(a.dk + row + d) =
-          uint2{T::pack(dk[db][4 * g4] * f, dk[db][4 * g4 + 1] * f),
-                T::pack(dk[db][4 * g4 + 2] * f, dk[db][4 * g4 + 3] * f)};
-      *reinterpret_cast<uint2*>(a.dv + row + d) =
-          uint2{T::pack(dv[db][4 * g4], dv[db][4 * g4 + 1]),
-                T::pack(dv[db][4 * g4 + 2], dv[db][4 * g4 + 3])};
-    }
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  sync_lds();  // nobody reads the stages any more
+  unsigned char* own = smem + wave * WaveRows<D>::kBytes;
+  static_assert(NW * WaveRows<D>::kBytes <= 2 * kStage, "the wave's rows fit");
+  const int left = S.n - wave * 32;  // rows of the wave
+  auto to = [&](uint16_t* base) {
+    return [=](int r) -> uint16_t* {
+      return r < left ? base + ((S.k0 + key0 + wave * 32 + r) * a.kv_heads + kvh) * a.dim : nullptr;
+    };
+  };
+  // (keys that the sequence does not count have no sums)
+  WaveRows<D>::template store<T>(dk, seen ? a.scale : 0.f, to(a.dk), own, lane, a.dim / 8);
+  WaveRows<D>::template store<T>(dv, 1.f, to(a.dv), own, lane, a.dim / 8);
 }
 
 // (The bodies are device functions: the host pass knows no buffer resources.)
@@ -637,13 +778,31 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_dkv_kernel(AttnArgs a) {
 }
 
 constexpr int kFwdWaves = 4, kBwdWaves = 4;
+constexpr int kKeyTile = 32 * kBwdWaves;
+
+// Writes the tiles of query rows (numbers below q_tiles), then those of key rows, a wave each.
+__global__ __launch_bounds__(256) void plan_kernel(AttnArgs a, uint32_t q_tiles, uint32_t k_tiles, int ts) {
+  const uint32_t i = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (i >= q_tiles + k_tiles) return;
+  const AttnTile t = i < q_tiles ? find_q_tile(a, i, ts) : find_k_tile(a, i - q_tiles, kKeyTile);
+  if ((threadIdx.x & 63) == 0) *(i < q_tiles ? a.q_plan + i : a.k_plan + (i - q_tiles)) = t;
+}
+
+hipError_t run_plan(const AttnArgs& a, int64_t q_tiles, int64_t k_tiles, int ts, hipStream_t s) {
+  if (q_tiles + k_tiles == 0) return hipSuccess;
+  hipLaunchKernelGGL(plan_kernel, dim3((unsigned)((q_tiles + k_tiles + 3) / 4)), dim3(256), 0, s, a,
+                     (uint32_t)q_tiles, (uint32_t)k_tiles, ts);
+  return hipGetLastError();
+}
 
 template <class T, int D>
 hipError_t run_fwd(AttnArgs a, hipStream_t s) {
   const int64_t grid = a.tiles * a.kv_heads * a.splits;
+  hipError_t e = run_plan(a, a.q_plan ? a.tiles : 0, 0, a.ts, s);
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL((attn_fwd_kernel<T, D, kFwdWaves>), dim3((unsigned)grid), dim3(64 * kFwdWaves),
                      0, s, a);
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e == hipSuccess && a.splits > 1) {
     const int64_t rows = a.n_q * a.heads;
     hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
@@ -654,19 +813,21 @@ hipError_t run_fwd(AttnArgs a, hipStream_t s) {
 
 template <class T, int D>
 hipError_t run_bwd(AttnArgs a, hipStream_t s) {
-  hipError_t e = hipSuccess;
-  if (a.n_q > 0) {
-    a.ts = 32 * kBwdWaves / a.G;
-    a.tiles = a.n_q / a.ts + a.n_seq;
-    hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves>), dim3((unsigned)(a.tiles * a.kv_heads)),
+  const int ts = 32 * kBwdWaves / a.G;
+  const int64_t q_tiles = a.n_q > 0 ? a.n_q / ts + a.n_seq : 0;
+  const int64_t k_tiles = a.dk && a.n_k > 0 ? a.n_k / kKeyTile + a.n_seq : 0;
+  hipError_t e = run_plan(a, a.q_plan ? q_tiles : 0, a.k_plan ? k_tiles : 0, ts, s);
+  if (e == hipSuccess && q_tiles > 0) {
+    a.ts = ts;
+    a.tiles = q_tiles;
+    hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves>), dim3((unsigned)(q_tiles * a.kv_heads)),
                        dim3(64 * kBwdWaves), 0, s, a);
     e = hipGetLastError();
-    if (e != hipSuccess) return e;
   }
-  if (a.dk && a.n_k > 0) {
+  if (e == hipSuccess && k_tiles > 0) {
     a.ts = kSlots / a.G;
-    a.tiles = a.n_k / (32 * kBwdWaves) + a.n_seq;
-    hipLaunchKernelGGL((attn_dkv_kernel<T, D, kBwdWaves>), dim3((unsigned)(a.tiles * a.kv_heads)),
+    a.tiles = k_tiles;
+    hipLaunchKernelGGL((attn_dkv_kernel<T, D, kBwdWaves>), dim3((unsigned)(k_tiles * a.kv_heads)),
                        dim3(64 * kBwdWaves), 0, s, a);
     e = hipGetLastError();
   }
@@ -689,6 +850,21 @@ int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
   const int64_t most = mean / 256 < 1 ? 1 : mean / 256;
   if (s > most) s = most;
   return (int)(s > 64 ? 64 : s);
+}
+
+// Calls of at least four rounds of workgroups plan their tiles.
+constexpr int64_t kPlanFrom = 2048;
+
+int64_t attn_plan_tiles(int64_t n_q, int n_seq, int heads, int kv_heads) {
+  if (n_q < 1) return 0;
+  const int64_t tiles = n_q / (32 * kFwdWaves / (heads / kv_heads)) + n_seq;
+  return tiles * kv_heads >= kPlanFrom ? tiles : 0;
+}
+
+int64_t attn_plan_key_tiles(int64_t n_k, int n_seq, int kv_heads) {
+  if (n_k < 1) return 0;
+  const int64_t tiles = n_k / kKeyTile + n_seq;
+  return tiles * kv_heads >= kPlanFrom ? tiles : 0;
 }
 
 hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream) {

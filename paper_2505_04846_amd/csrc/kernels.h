@@ -247,6 +247,11 @@ hipError_t launch_retrieval_metrics(const int64_t* idx, int nq, int64_t ld, int 
 
 // Attention over packed sequences (attention.hip, which states the definition).  Strides in
 // elements.  The launchers fill ts and tiles.
+struct AttnTile {      // a tile of query rows, or of key rows, and its sequence
+  int64_t q0, k0;      // the sequence's first query and key rows
+  int32_t lq, lk;      // its query rows and keys
+  int32_t first, n;    // the tile's first row within the sequence, and its rows (0: no tile)
+};
 struct AttnArgs {
   const uint16_t *q, *k, *v;
   int64_t q_row, q_head, k_row, k_head, v_row, v_head;
@@ -267,9 +272,13 @@ struct AttnArgs {
   float* delta;               // [n_q, heads] scratch
   int ts;           // tokens of a tile or stage
   int64_t tiles;    // per kv head
+  AttnTile *q_plan, *k_plan;  // the tiles of query and key rows, where the call plans (may be null)
 };
 constexpr int kMaxGroup = 32;  // query heads of one kv head
 int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
+// Tiles of the forward's and the gradients' plans (0: the call does not plan).
+int64_t attn_plan_tiles(int64_t n_q, int n_seq, int heads, int kv_heads);
+int64_t attn_plan_key_tiles(int64_t n_k, int n_seq, int kv_heads);
 hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream);
 hipError_t launch_attn_bwd(AttnArgs a, hipStream_t stream);
 

@@ -7,13 +7,13 @@
 namespace hpr {
 
 // LDS tiles of `rows` rows of D 16-bit values: the 16-byte chunk c of row r is stored at position
-// c ^ swz(r) of its row.  Eight consecutive rows take eight different values of the low three
-// bits (row_frag reads one chunk of 32 rows) and four consecutive rows four different values of
-// bits 1 and 2 (tr_frag reads 32 bytes of four rows), so that both read all banks evenly.
+// c ^ swz(r) of its row.  LDS serves 256 bytes (64 banks) a cycle.  row_frag reads one chunk of 16
+// consecutive rows a cycle: swz, with the row's own offset at D = 64, spreads them over all 16
+// positions.  tr_frag reads 64 bytes of four consecutive rows a cycle: the swizzle's upper bits, with
+// that offset, send the four rows to the four quarters of the banks.
 template <int D>
 __device__ __forceinline__ int swz(int r) {
-  const int x = ((r & 3) << 1) | ((r >> 2) & 1);
-  return D >= 128 ? x | (((r >> 3) & 1) << 3) : x;
+  return D >= 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
 // Offsets of a lane's reads from an LDS tile.
@@ -46,7 +46,7 @@ struct TileReads {
     const unsigned char* p = tile + (32 * blk + 16 * s) * D * 2 + tr0;
     const int c = trc ^ (db << 6);
     const v2u a = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + c)));
-    const int c1 = D >= 128 ? c ^ 128 : c;  // rows 8 further: bit 3 of swz
+    const int c1 = c ^ 32;  // rows 8 further: bit 1 of swz
     const v2u b = __builtin_bit_cast(
         v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 8 * D * 2 + c1)));
     return u32x4{a[0], a[1], b[0], b[1]};
@@ -57,6 +57,38 @@ __device__ __forceinline__ void sync_lds() {
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
   __builtin_amdgcn_s_barrier();
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+
+// Loads from global memory straight into LDS, 16 (or 4) bytes per lane at lds + 16 (4) lane, of kernels
+// that read LDS by columns: the compiler takes ds_read_b64_tr_b16 to depend on every such load that it
+// knows of and waits for the next stage's in the middle of this one's products (2,100 cycles a tile of
+// the forward instead of 1,600).  Written here, the loads are known to the program alone: it waits
+// for them (s_waitcnt vmcnt) before the barrier that hands the stage over.  They have no output
+// register, and the compiler's own counts of outstanding loads only become stricter.
+typedef u32x4 rsrc_t;  // a raw buffer of 2^31 - 1 bytes from base
+__device__ __forceinline__ rsrc_t rsrc_of(const void* base) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  return rsrc_t{(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+}
+// The LDS address of a __shared__ array (of the array itself: a generic pointer would need a check).
+#define LDS_ADDRESS(array) ((uint32_t)(uintptr_t)(lds_void_t*)(array))
+__device__ __forceinline__ void load_lds16(rsrc_t r, uint32_t lds, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(r)
+               : "memory");
+}
+__device__ __forceinline__ void load_lds16(const void* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src)
+               : "memory");
+}
+__device__ __forceinline__ void load_lds4(const void* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src)
+               : "memory");
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const void* base) {
@@ -84,14 +116,15 @@ struct TileLoad {
   }
 };
 
-// The last s in [0, n) with off[s] / ts + s <= tile (0 if none).  The whole wave searches.
-__device__ __forceinline__ int find_seq(const int64_t* off, int n, int ts, int64_t tile) {
+// The last s in [0, n) with off[s] / ts + s <= tile (0 if none).  The whole wave searches.  (Rows are
+// below 2^31; offsets that are not give some s.)
+__device__ __forceinline__ int find_seq(const int64_t* off, int n, int ts, uint32_t tile) {
   const int lane = threadIdx.x & 63;
   int lo = 0;
   while (n > 1) {
     const int step = (n + 63) / 64;
     const int i = lane * step;
-    const bool ok = i < n && off[lo + i] / ts + lo + i <= tile;
+    const bool ok = i < n && (uint32_t)off[lo + i] / (uint32_t)ts + (uint32_t)(lo + i) <= tile;
     const unsigned long long b = __ballot(ok);
     int c = __popcll(b);
     c = c < 1 ? 1 : c;
