@@ -156,6 +156,15 @@ struct WaveRows {
       if (16 * s + 8 * half >= dim) f[s] = u32x4{0u, 0u, 0u, 0u};
     }
   }
+  // the rows' chunks past dim become zero
+  static __device__ __forceinline__ void clear(unsigned char* lds, int lane, int chunks) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = j * kRows + lane / kCh;
+      if (((lane % kCh) ^ swz<D>(r)) >= chunks)
+        *reinterpret_cast<u32x4*>(lds + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
   // x, times the lane's factor, as 16-bit rows: dst(r) is row r's address, or null
   template <class T, class F>
   static __device__ __forceinline__ void store(const f32x16 (&x)[D / 32], float factor, F dst,
@@ -341,12 +350,13 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
     sched_mfma(4);
     __builtin_amdgcn_sched_barrier(0);
     if (first + kKeys > wfirst.hi || first < wlast.lo) {  // some key is not every slot's
+      const int lo = mine.lo - first - 4 * half, hi = mine.hi - first - 4 * half;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int key = first + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
-          if (key >= mine.hi || key < mine.lo) x[b][r] = -__builtin_inff();
+          const int key = 32 * b + 8 * (r >> 2) + (r & 3);
+          if (key >= hi || key < lo) x[b][r] = -__builtin_inff();
         }
     }
     float top = x[0][0];
@@ -563,14 +573,17 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
       }
       u32x4 ds[2];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float p = prob(__builtin_fmaf(x[r], a.c, -lse2));
-        if (partial) {
-          const int key = first + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
-          if (key >= mine.hi || key < mine.lo) p = 0.f;
+      for (int r = 0; r < 16; ++r) x[r] = prob(__builtin_fmaf(x[r], a.c, -lse2));
+      if (partial) {
+        const int lo = mine.lo - first - 32 * b - 4 * half, hi = mine.hi - first - 32 * b - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = 8 * (r >> 2) + (r & 3);
+          if (key >= hi || key < lo) x[r] = 0.f;
         }
-        x[r] = p * (dp[r] - delta);
       }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] *= dp[r] - delta;
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -593,15 +606,17 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
 
 // dk and dv of a tile of NW * 32 keys of one kv head, over all the slots that see them, kSlots
 // (whole tokens of G slots) at a time.  A wave owns 32 keys; the sum over the group's heads is
-// the sum over slots.
-constexpr int kSlots = 64;
+// the sum over slots.  The wave's K stays in registers, its V in LDS: with the 128 registers of both
+// sums at D = 128, that is what leaves room for two waves per SIMD.
+constexpr int kSlots = 32;
 
 template <class T, int D, int NW>
 __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
   constexpr int kS = D / 16, kDb = D / 32;
   constexpr int kTile = kSlots * D * 2;
-  constexpr int kStage = 2 * kTile + 2 * kSlots * 4;  // q, dout, lse, delta
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * kStage];
+  constexpr int kStage = 2 * kTile + 2 * 64 * 4;  // q, dout, lse, delta (a lane each, 32 used)
+  constexpr int kOwn = WaveRows<D>::kBytes;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * kStage + NW * kOwn];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % (uint32_t)a.kv_heads;
@@ -611,7 +626,6 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
   const int key0 = S.first;
   const int key = key0 + wave * 32 + col;
   const bool seen = key < S.lk;  // (the gradient rows past the key count get zeros)
-  const int ck = seen ? key : S.lk - 1;
 
   // tokens that see a key of the tile / of the wave: causal i >= key - (lk - lq), and with a
   // window i < key - (lk - lq) + window
@@ -639,34 +653,24 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
   const int w_first = first_tok(wk0), w_end = end_tok(wk1);            // any of the wave's keys
   const int w_first_all = first_tok(wk1), w_end_all = end_tok(wk0);    // all of them
 
-  u32x4 k[kS], v[kS];
-#pragma unroll
-  for (int s = 0; s < kS; ++s) k[s] = v[s] = u32x4{0u, 0u, 0u, 0u};
-  if (wave_live) {
-    load_cols<D>(a.k + (S.k0 + ck) * a.k_row + kvh * a.k_head, a.dim, half, k);
-    load_cols<D>(a.v + (S.k0 + ck) * a.v_row + kvh * a.v_head, a.dim, half, v);
-  }
-  f32x16 dk[kDb], dv[kDb];
-#pragma unroll
-  for (int db = 0; db < kDb; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dk[db][r] = 0.f, dv[db][r] = 0.f;
-
   const TileReads<D> rd(lane);
   const TileLoad<D, kSlots, NW> ld(wave, lane, a.dim / 8);
   const int used = ts * a.G;  // slots of a stage
-  int tok_of[ld.kLoads], head_of[ld.kLoads];
+  int tok_of[ld.kLoads], q_at[ld.kLoads], g_at[ld.kLoads];
 #pragma unroll
   for (int j = 0; j < ld.kLoads; ++j) {
     const int r = ld.row[j] < used ? ld.row[j] : used - 1;
-    tok_of[j] = r / a.G;
-    head_of[j] = r % a.G;
+    const int head = r % (uint32_t)a.G;
+    tok_of[j] = r / (uint32_t)a.G;
+    q_at[j] = head * (int)a.q_head * 2 + ld.chunk[j];
+    g_at[j] = head * a.dim * 2 + ld.chunk[j];
   }
   const int lr = lane < used ? lane : used - 1;
-  const int l_tok = lr / a.G, l_head = lr % a.G;
+  const int l_tok = lr / (uint32_t)a.G, l_head = lr % (uint32_t)a.G;
   const int64_t d_row = (int64_t)a.heads * a.dim;
   const uint16_t* qb = a.q + S.q0 * a.q_row + kvh * a.G * a.q_head;
   const uint16_t* gb = a.dout + S.q0 * d_row + kvh * a.G * a.dim;
+  const float* stat = (wave == 0 ? a.lse : a.delta) + S.q0 * a.heads + kvh * a.G + l_head;
   auto issue = [&](int buf, int st) {
     const int t = st * ts;
     const int last = S.lq - 1 - t;  // last valid token of the stage
@@ -676,17 +680,43 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
 #pragma unroll
     for (int j = 0; j < ld.kLoads; ++j) {
       const int tk = tok_of[j] < last ? tok_of[j] : last;
-      load_lds16(rq, base + (wave * ld.kLoads + j) * 1024,
-                 (tk * (int)a.q_row + head_of[j] * (int)a.q_head) * 2 + ld.chunk[j]);
-      load_lds16(rg, base + kTile + (wave * ld.kLoads + j) * 1024,
-                 (tk * a.heads + head_of[j]) * a.dim * 2 + ld.chunk[j]);
+      load_lds16(rq, base + (wave * ld.kLoads + j) * 1024, tk * (int)a.q_row * 2 + q_at[j]);
+      load_lds16(rg, base + kTile + (wave * ld.kLoads + j) * 1024, tk * a.heads * a.dim * 2 + g_at[j]);
     }
-    if (wave < 2) {  // statistics: wave 0 lse, wave 1 delta, a slot per lane
-      const int tk = l_tok < last ? l_tok : last;
-      const float* src = (wave == 0 ? a.lse : a.delta) + (S.q0 + t + tk) * a.heads + kvh * a.G + l_head;
-      load_lds4(src, base + 2 * kTile + wave * kSlots * 4);
-    }
+    if (wave < 2)  // statistics: wave 0 lse, wave 1 delta, a slot per lane
+      load_lds4(stat + (int64_t)(t + (l_tok < last ? l_tok : last)) * a.heads,
+                base + 2 * kTile + wave * 64 * 4);
   };
+
+  // k, then v, through the wave's own rows of LDS, where v stays
+  unsigned char* own = smem + 2 * kStage + wave * kOwn;
+  const uint32_t own_at = LDS_ADDRESS(smem) + 2 * kStage + wave * kOwn;
+  u32x4 k[kS];
+#pragma unroll
+  for (int s = 0; s < kS; ++s) k[s] = u32x4{0u, 0u, 0u, 0u};
+  if (wave_live) {
+    auto row_of = [&](int r) { return S.k0 + (wk0 + r < S.lk ? wk0 + r : S.lk - 1); };
+    WaveRows<D>::load([&](int r) { return a.k + row_of(r) * a.k_row + kvh * a.k_head; }, own_at, lane,
+                      a.dim / 8);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    WaveRows<D>::cols(rd, own, a.dim, half, k);
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    WaveRows<D>::load([&](int r) { return a.v + row_of(r) * a.v_row + kvh * a.v_head; }, own_at, lane,
+                      a.dim / 8);
+    if (a.dim < D) {
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      WaveRows<D>::clear(own, lane, a.dim / 8);
+    }
+  }
+  f32x16 dk[kDb], dv[kDb];
+#pragma unroll
+  for (int db = 0; db < kDb; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[db][r] = 0.f, dv[db][r] = 0.f;
+
   if (st0 < st1) issue(0, st0);
 #pragma unroll 1
   for (int st = st0; st < st1; ++st) {
@@ -699,59 +729,58 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
     const unsigned char* qs = smem + buf * kStage;
     const unsigned char* gs = qs + kTile;
     const float* lse_s = reinterpret_cast<const float*>(qs + 2 * kTile);
-    const float* del_s = lse_s + kSlots;
+    const float* del_s = lse_s + 64;
     // every slot of the stage holds a token that sees every key of the wave
     const bool partial = used < kSlots || t + ts > S.lq || t < w_first_all || t + ts > w_end_all ||
                          wk0 + 31 >= S.lk;
+    f32x16 x, dp;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f32x16 x, dp;
+    for (int r = 0; r < 16; ++r) x[r] = 0.f, dp[r] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = 0.f, dp[r] = 0.f;
-#pragma unroll
-      for (int s = 0; s < kS; ++s) {
-        x = T::mfma(rd.row_frag(qs, b, s), k[s], x);
-        dp = T::mfma(rd.row_frag(gs, b, s), v[s], dp);
-      }
-      u32x4 p16[2], ds[2];
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + 32 * b + 8 * q4 + 4 * half);
-        const f32x4 dl = *reinterpret_cast<const f32x4*>(del_s + 32 * b + 8 * q4 + 4 * half);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * q4 + e;
-          float p = prob(__builtin_fmaf(x[r], a.c, -ls[e] * kLog2e));
-          if (partial) {
-            const int slot = 32 * b + 8 * q4 + 4 * half + e;
-            const int tk = t + (int)(((uint32_t)slot * a.g_inv) >> 16);
-            if (slot >= used || tk < my_first || tk >= my_end) p = 0.f;
-          }
-          x[r] = p;
-          dp[r] = p * (dp[r] - dl[e]);
-        }
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p16[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
-          ds[s][e] = T::pack(dp[8 * s + 2 * e], dp[8 * s + 2 * e + 1]);
-        }
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int db = 0; db < kDb; ++db) {
-          dv[db] = T::mfma(rd.tr_frag(gs, b, s, db), p16[s], dv[db]);
-          dk[db] = T::mfma(rd.tr_frag(qs, b, s, db), ds[s], dk[db]);
-        }
+    for (int s = 0; s < kS; ++s) {
+      x = T::mfma(rd.row_frag(qs, 0, s), k[s], x);
+      dp = T::mfma(rd.row_frag(gs, 0, s), rd.row_frag(own, 0, s), dp);
     }
+    u32x4 p16[2], ds[2];
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + 8 * q4 + 4 * half);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[4 * q4 + e] = prob(__builtin_fmaf(x[4 * q4 + e], a.c, -ls[e] * kLog2e));
+    }
+    if (partial) {  // the lane's key is seen from slots [lo, hi) of the stage
+      const int lo = (my_first - t) * a.G - 4 * half;
+      int hi = (my_end - t) * a.G;
+      hi = (hi < used ? hi : used) - 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int slot = 8 * (r >> 2) + (r & 3);
+        if (slot < lo || slot >= hi) x[r] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x4 dl = *reinterpret_cast<const f32x4*>(del_s + 8 * q4 + 4 * half);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[4 * q4 + e] = x[4 * q4 + e] * (dp[4 * q4 + e] - dl[e]);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p16[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
+        ds[s][e] = T::pack(dp[8 * s + 2 * e], dp[8 * s + 2 * e + 1]);
+      }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < kDb; ++db) {
+        dv[db] = T::mfma(rd.tr_frag(gs, 0, s, db), p16[s], dv[db]);
+        dk[db] = T::mfma(rd.tr_frag(qs, 0, s, db), ds[s], dk[db]);
+      }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-  sync_lds();  // nobody reads the stages any more
-  unsigned char* own = smem + wave * WaveRows<D>::kBytes;
-  static_assert(NW * WaveRows<D>::kBytes <= 2 * kStage, "the wave's rows fit");
   const int left = S.n - wave * 32;  // rows of the wave
   auto to = [&](uint16_t* base) {
     return [=](int r) -> uint16_t* {
@@ -773,7 +802,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(AttnArgs a) {
   attn_dq<T, D, NW>(a);
 }
 template <class T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void attn_dkv_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void attn_dkv_kernel(AttnArgs a) {
   attn_dkv<T, D, NW>(a);
 }
 
