@@ -41,7 +41,7 @@ constexpr float kNoMax = -1e30f;
 // relative rounding does not depend on it), and most tiles skip the rescaling of the output.
 constexpr float kRaise = 8.f;
 
-constexpr int kKeys = 64;  // keys per tile of the forward and dq kernels
+constexpr int kKeys = 64;  // keys per tile of the dq kernel
 
 // max / sum over the two half-waves, in both of them
 __device__ __forceinline__ float half_max(float v) {
@@ -137,14 +137,14 @@ template <int D>
 struct WaveRows {
   static constexpr int kCh = D / 8, kRows = 64 / kCh, kLoads = 32 / kRows;
   static constexpr int kBytes = 32 * D * 2;
-  // src(r): the address of row r of the 32
+  // at(r): the byte offset of row r of the 32 from the buffer's base
   template <class F>
-  static __device__ __forceinline__ void load(F src, uint32_t lds, int lane, int chunks) {
+  static __device__ __forceinline__ void load(rsrc_t from, F at, uint32_t lds, int lane, int chunks) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const int r = j * kRows + lane / kCh;
       const int c = (lane % kCh) ^ swz<D>(r);
-      load_lds16(src(r) + 8 * (c < chunks ? c : chunks - 1), lds + j * 1024);
+      load_lds16(from, lds + j * 1024, at(r) + 16 * (c < chunks ? c : chunks - 1));
     }
   }
   // the loaded rows as right operands, zero past dim
@@ -165,10 +165,10 @@ struct WaveRows {
         *reinterpret_cast<u32x4*>(lds + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
     }
   }
-  // x, times the lane's factor, as 16-bit rows: dst(r) is row r's address, or null
+  // x, times the lane's factor, as 16-bit rows: row r goes to byte offset at(r) from base if r < n
   template <class T, class F>
-  static __device__ __forceinline__ void store(const f32x16 (&x)[D / 32], float factor, F dst,
-                                               unsigned char* lds, int lane, int chunks) {
+  static __device__ __forceinline__ void store(const f32x16 (&x)[D / 32], float factor, uint16_t* base,
+                                               F at, int n, unsigned char* lds, int lane, int chunks) {
     const int row = lane & 31, half = lane >> 5;
     __atomic_signal_fence(__ATOMIC_SEQ_CST);  // (a wave's LDS operations execute in program order)
 #pragma unroll
@@ -179,22 +179,40 @@ struct WaveRows {
             uint2{T::pack(x[db][4 * g] * factor, x[db][4 * g + 1] * factor),
                   T::pack(x[db][4 * g + 2] * factor, x[db][4 * g + 3] * factor)};
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    const int last = n - 1 < 31 ? n - 1 : 31;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const int r = j * kRows + lane / kCh;
       const int c = (lane % kCh) ^ swz<D>(r);
-      uint16_t* to = dst(r);
       const u32x4 v = *reinterpret_cast<const u32x4*>(lds + j * 1024 + lane * 16);
-      if (to && c < chunks) *reinterpret_cast<u32x4*>(to + 8 * c) = v;
+      if (r <= last && c < chunks)
+        *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + (uint32_t)(at(r) + 16 * c)) = v;
     }
   }
 };
 
-// A stage's loads: kKeys rows of K, then of V, straight into LDS.  The offsets of a whole tile are
+// The slots of a wave, as byte offsets from their tile's first token: row r of the 32 is slot
+// first + r (the last slot past it), token slot / G of the tile, head slot % G of the group.
+struct SlotRows {
+  uint32_t first, last, g_inv, step, head;  // step: a token's bytes less G heads', head: a head's
+  __device__ __forceinline__ SlotRows(const AttnArgs& a, int wave, int n_slot, int64_t row, int64_t head_)
+      : first(wave * 32),
+        last(n_slot - 1),
+        g_inv(a.g_inv),
+        step((uint32_t)(row - a.G * head_) * 2u),
+        head((uint32_t)head_ * 2u) {}
+  // (token * row + (slot - token * G) * head, in 32-bit arithmetic that wraps and comes back)
+  __device__ __forceinline__ uint32_t operator()(int r) const {
+    const uint32_t s = first + r < last ? first + r : last;
+    return ((s * g_inv) >> 16) * step + s * head;
+  }
+};
+
+// A stage's loads: KEYS rows of K, then of V, straight into LDS.  The offsets of a whole tile are
 // kept per lane; the sequence's last tile forms its own.
-template <int D, int NW>
+template <int D, int NW, int KEYS>
 struct KvLoad {
-  using L = TileLoad<D, kKeys, NW>;
+  using L = TileLoad<D, KEYS, NW>;
   L at;
   const uint16_t *k, *v;  // the kv head's first rows
   int ok[L::kLoads], ov[L::kLoads];
@@ -210,13 +228,13 @@ struct KvLoad {
   }
   __device__ __forceinline__ void issue(const AttnArgs& a, const AttnTile& S, uint32_t st, int wave,
                                         int kt) const {
-    const int first = kt * kKeys;
+    const int first = kt * KEYS;
     const int last = S.lk - 1 - first;  // last valid row of the tile (>= 0)
     const rsrc_t rk = rsrc_of(k + (int64_t)first * a.k_row);
     const rsrc_t rv = rsrc_of(v + (int64_t)first * a.v_row);
     const uint32_t to = st + wave * L::kLoads * 1024;  // LDS address
-    constexpr int kTile = kKeys * D * 2;
-    if (last >= kKeys - 1) {
+    constexpr int kTile = KEYS * D * 2;
+    if (last >= KEYS - 1) {
 #pragma unroll
       for (int j = 0; j < L::kLoads; ++j)
         load_lds16(rk, to + j * 1024, ok[j]);
@@ -247,13 +265,14 @@ __device__ __forceinline__ float prob(float x) {
 
 // ---- forward --------------------------------------------------------------------------------
 
-// One tile of NW * 32 slots of one kv head against a split of its visible keys, kKeys at a time
-// through two LDS stages.
-template <class T, int D, int NW>
+// One tile of NW * 32 slots of one kv head against a split of its visible keys, KEYS at a time
+// through NST LDS stages.
+template <class T, int D, int NW, int KEYS, int NST>
 __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   constexpr int kS = D / 16, kDb = D / 32;
-  constexpr int kTile = kKeys * D * 2;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTile];
+  constexpr int kB = KEYS / 32;
+  constexpr int kTile = KEYS * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NST * 2 * kTile];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % (uint32_t)a.kv_heads;
@@ -279,31 +298,19 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   const Span tfirst = span_of(a, S, t0), tlast = span_of(a, S, t0 + n_tok - 1);
 
   // key tiles of this split
-  const int k_first = tfirst.lo / kKeys, k_end = (tlast.hi + kKeys - 1) / kKeys;
+  const int k_first = tfirst.lo / KEYS, k_end = (tlast.hi + KEYS - 1) / KEYS;
   const int n_kt = k_end > k_first ? k_end - k_first : 0;
   const int kt0 = k_first + (int)((int64_t)n_kt * split / a.splits);
   const int kt1 = k_first + (int)((int64_t)n_kt * (split + 1) / a.splits);
 
-  // the wave's slots: row r's token within the tile and head, the last slot's past it
-  auto slot_tok = [&](int r) {
-    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
-    return (int)(((uint32_t)s * a.g_inv) >> 16);
-  };
-  auto slot_head = [&](int r, int t) {
-    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
-    return kvh * a.G + s - t * a.G;
-  };
-  const KvLoad<D, NW> ld(a, S, kvh, wave, lane);
+  const KvLoad<D, NW, KEYS> ld(a, S, kvh, wave, lane);
   auto issue = [&](int buf, int kt) { ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt); };
-  // q through the second stage, which the loop fills only after its first barrier
-  static_assert(NW * WaveRows<D>::kBytes <= 2 * kTile, "the wave's rows fit a stage");
+  // q through the later stages, which the loop fills only after its first barrier
+  static_assert(NW * WaveRows<D>::kBytes <= (NST - 1) * 2 * kTile, "the waves' rows fit there");
   unsigned char* own = smem + 2 * kTile + wave * WaveRows<D>::kBytes;
-  WaveRows<D>::load(
-      [&](int r) {
-        const int t = slot_tok(r);
-        return a.q + (S.q0 + t0 + t) * a.q_row + slot_head(r, t) * a.q_head;
-      },
-      LDS_ADDRESS(smem) + 2 * kTile + wave * WaveRows<D>::kBytes, lane, a.dim / 8);
+  WaveRows<D>::load(rsrc_of(a.q + (S.q0 + t0) * a.q_row + kvh * a.G * a.q_head),
+                    SlotRows(a, wave, n_slot, a.q_row, a.q_head),
+                    LDS_ADDRESS(smem) + 2 * kTile + wave * WaveRows<D>::kBytes, lane, a.dim / 8);
   if (kt0 < kt1) {
     issue(0, kt0);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * ld.at.kLoads));
@@ -323,36 +330,45 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   float m = kNoMax, l = 0.f;
 
 #pragma unroll 1
-  for (int kt = kt0; kt < kt1; ++kt) {
-    const int buf = (kt - kt0) & 1;
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  for (int kt = kt0, buf = 0; kt < kt1; ++kt, buf = buf + 1 < NST ? buf + 1 : 0) {
+    if (NST == 2 || kt == kt0 || kt + 1 == kt1)
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    else  // the next tile may be on its way
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * ld.at.kLoads));
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-    sync_lds();  // the tile has landed, and nobody reads the other stage any more
-    if (kt + 1 < kt1) issue(buf ^ 1, kt + 1);
-    const int first = kt * kKeys;
-    if (!wave_live || first >= wlast.hi || first + kKeys <= wfirst.lo) continue;
+    sync_lds();  // the tile has landed, and nobody reads the stage before it any more
+    if (NST == 2) {
+      if (kt + 1 < kt1) issue(buf ^ 1, kt + 1);
+    } else {
+      if (kt == kt0 && kt + 1 < kt1) issue(1, kt + 1);
+      if (kt + 2 < kt1) issue(buf == 0 ? 2 : buf - 1, kt + 2);
+    }
+    const int first = kt * KEYS;
+    if (!wave_live || first >= wlast.hi || first + KEYS <= wfirst.lo) continue;
     const unsigned char* ks = smem + buf * 2 * kTile;
     const unsigned char* vs = ks + kTile;
-    f32x16 x[2];
+    f32x16 x[kB];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[0][r] = x[1][r] = 0.f;
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = 0.f;
 #pragma unroll
     for (int s = 0; s < kS; ++s)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) x[b] = T::mfma(rd.row_frag(ks, b, s), q[s], x[b]);
+      for (int b = 0; b < kB; ++b) x[b] = T::mfma(rd.row_frag(ks, b, s), q[s], x[b]);
     // the operands' reads run two k-steps ahead of the products
-    sched_ds(4);
+    sched_ds(2 * kB);
 #pragma unroll
     for (int s = 0; s < kS - 2; ++s) {
-      sched_mfma(2);
-      sched_ds(2);
+      sched_mfma(kB);
+      sched_ds(kB);
     }
-    sched_mfma(4);
+    sched_mfma(2 * kB);
     __builtin_amdgcn_sched_barrier(0);
-    if (first + kKeys > wfirst.hi || first < wlast.lo) {  // some key is not every slot's
+    if (first + KEYS > wfirst.hi || first < wlast.lo) {  // some key is not every slot's
       const int lo = mine.lo - first - 4 * half, hi = mine.hi - first - 4 * half;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < kB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = 32 * b + 8 * (r >> 2) + (r & 3);
@@ -361,7 +377,7 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
     }
     float top = x[0][0];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][r]);
     top = half_max(top) * a.c;
@@ -376,7 +392,7 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
         for (int r = 0; r < 16; ++r) o[db][r] *= f;
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kB; ++b) {
       u32x4 p[2];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -419,15 +435,10 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   if (a.lse && live && half == 0) a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   sync_lds();  // nobody reads the stages any more
-  WaveRows<D>::template store<T>(
-      o, l > 0.f ? 1.f / l : 0.f,
-      [&](int r) -> uint16_t* {
-        const int t = slot_tok(r);
-        return wave * 32 + r < n_slot
-                   ? a.out + ((S.q0 + t0 + t) * a.heads + slot_head(r, t)) * a.dim
-                   : nullptr;
-      },
-      own, lane, a.dim / 8);
+  WaveRows<D>::template store<T>(o, l > 0.f ? 1.f / l : 0.f,
+                                 a.out + ((S.q0 + t0) * a.heads + kvh * a.G) * a.dim,
+                                 SlotRows(a, wave, n_slot, (int64_t)a.heads * a.dim, a.dim),
+                                 n_slot - wave * 32, own, lane, a.dim / 8);
 }
 
 // out = the splits' sums joined under their common maximum.  A wave per (token, head), lane d.
@@ -486,19 +497,9 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   const int kt0 = tfirst.lo / kKeys, kt1 = (tlast.hi + kKeys - 1) / kKeys;
 
   const int64_t row = (S.q0 + tok) * a.heads + head;
-  auto slot_tok = [&](int r) {
-    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
-    return (int)(((uint32_t)s * a.g_inv) >> 16);
-  };
-  auto slot_head = [&](int r, int t) {
-    const int s = wave * 32 + r < n_slot ? wave * 32 + r : n_slot - 1;
-    return kvh * a.G + s - t * a.G;
-  };
-  auto dense_row = [&](int r) {
-    const int t = slot_tok(r);
-    return ((S.q0 + t0 + t) * a.heads + slot_head(r, t)) * a.dim;
-  };
-  const KvLoad<D, NW> ld(a, S, kvh, wave, lane);
+  const SlotRows dense(a, wave, n_slot, (int64_t)a.heads * a.dim, a.dim);
+  const int64_t dense0 = ((S.q0 + t0) * a.heads + kvh * a.G) * a.dim;
+  const KvLoad<D, NW, kKeys> ld(a, S, kvh, wave, lane);
   auto issue = [&](int buf, int kt) { ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt); };
   // q through the second stage, dout through the first, then out through the second
   constexpr int kOwn = WaveRows<D>::kBytes;
@@ -506,14 +507,9 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   const TileReads<D> rd(lane);
   unsigned char* own = smem + 2 * kTile + wave * kOwn;
   const uint32_t own_at = LDS_ADDRESS(smem) + 2 * kTile + wave * kOwn;
-  WaveRows<D>::load(
-      [&](int r) {
-        const int t = slot_tok(r);
-        return a.q + (S.q0 + t0 + t) * a.q_row + slot_head(r, t) * a.q_head;
-      },
-      own_at, lane, a.dim / 8);
-  WaveRows<D>::load([&](int r) { return a.dout + dense_row(r); }, LDS_ADDRESS(smem) + wave * kOwn, lane,
-                    a.dim / 8);
+  WaveRows<D>::load(rsrc_of(a.q + (S.q0 + t0) * a.q_row + kvh * a.G * a.q_head),
+                    SlotRows(a, wave, n_slot, a.q_row, a.q_head), own_at, lane, a.dim / 8);
+  WaveRows<D>::load(rsrc_of(a.dout + dense0), dense, LDS_ADDRESS(smem) + wave * kOwn, lane, a.dim / 8);
   const float lse2 = a.lse[row] * kLog2e;
   u32x4 q[kS], g[kS];
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
@@ -522,7 +518,7 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   WaveRows<D>::cols(rd, smem + wave * kOwn, a.dim, half, g);
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   sync_lds();
-  WaveRows<D>::load([&](int r) { return (const uint16_t*)a.out + dense_row(r); }, own_at, lane, a.dim / 8);
+  WaveRows<D>::load(rsrc_of(a.out + dense0), dense, own_at, lane, a.dim / 8);
   if (kt0 < kt1) {
     issue(0, kt0);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * ld.at.kLoads));
@@ -598,10 +594,8 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   if (!a.dq) return;
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   sync_lds();  // nobody reads the stages any more
-  WaveRows<D>::template store<T>(
-      dq, a.scale,
-      [&](int r) -> uint16_t* { return wave * 32 + r < n_slot ? a.dq + dense_row(r) : nullptr; }, own,
-      lane, a.dim / 8);
+  WaveRows<D>::template store<T>(dq, a.scale, a.dq + dense0, dense, n_slot - wave * 32, own, lane,
+                                 a.dim / 8);
 }
 
 // dk and dv of a tile of NW * 32 keys of one kv head, over all the slots that see them, kSlots
@@ -695,16 +689,18 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
 #pragma unroll
   for (int s = 0; s < kS; ++s) k[s] = u32x4{0u, 0u, 0u, 0u};
   if (wave_live) {
-    auto row_of = [&](int r) { return S.k0 + (wk0 + r < S.lk ? wk0 + r : S.lk - 1); };
-    WaveRows<D>::load([&](int r) { return a.k + row_of(r) * a.k_row + kvh * a.k_head; }, own_at, lane,
-                      a.dim / 8);
+    const int last = S.lk - 1 - wk0;  // the rows past it repeat it
+    WaveRows<D>::load(rsrc_of(a.k + (S.k0 + wk0) * a.k_row + kvh * a.k_head),
+                      [&](int r) { return (uint32_t)(r < last ? r : last) * (uint32_t)a.k_row * 2u; },
+                      own_at, lane, a.dim / 8);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     WaveRows<D>::cols(rd, own, a.dim, half, k);
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    WaveRows<D>::load([&](int r) { return a.v + row_of(r) * a.v_row + kvh * a.v_head; }, own_at, lane,
-                      a.dim / 8);
+    WaveRows<D>::load(rsrc_of(a.v + (S.k0 + wk0) * a.v_row + kvh * a.v_head),
+                      [&](int r) { return (uint32_t)(r < last ? r : last) * (uint32_t)a.v_row * 2u; },
+                      own_at, lane, a.dim / 8);
     if (a.dim < D) {
       __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
       __atomic_signal_fence(__ATOMIC_SEQ_CST);
@@ -781,21 +777,18 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
       }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-  const int left = S.n - wave * 32;  // rows of the wave
-  auto to = [&](uint16_t* base) {
-    return [=](int r) -> uint16_t* {
-      return r < left ? base + ((S.k0 + key0 + wave * 32 + r) * a.kv_heads + kvh) * a.dim : nullptr;
-    };
-  };
   // (keys that the sequence does not count have no sums)
-  WaveRows<D>::template store<T>(dk, seen ? a.scale : 0.f, to(a.dk), own, lane, a.dim / 8);
-  WaveRows<D>::template store<T>(dv, 1.f, to(a.dv), own, lane, a.dim / 8);
+  const int64_t first = ((S.k0 + wk0) * a.kv_heads + kvh) * a.dim;
+  auto at = [&](int r) { return (uint32_t)r * (uint32_t)(a.kv_heads * a.dim) * 2u; };
+  WaveRows<D>::template store<T>(dk, seen ? a.scale : 0.f, a.dk + first, at, S.n - wave * 32, own, lane,
+                                 a.dim / 8);
+  WaveRows<D>::template store<T>(dv, 1.f, a.dv + first, at, S.n - wave * 32, own, lane, a.dim / 8);
 }
 
 // (The bodies are device functions: the host pass knows no buffer resources.)
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_kernel(AttnArgs a) {
-  attn_fwd<T, D, NW>(a);
+  attn_fwd<T, D, NW, 64, 2>(a);
 }
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(AttnArgs a) {
