@@ -334,9 +334,9 @@ hpr_status check_attention(const hpr_attention* d, const uint16_t* q, const uint
                 d->dim);
   if (d->heads / d->kv_heads > kMaxGroup)
     return fail(HPR_ERR_UNSUPPORTED_SHAPE, "more than %d heads per kv head", kMaxGroup);
-  // (the grids hold up to a tile per 4 rows and kv head, and 64 splits of those below one round)
+  // (the grids hold up to a tile per row and kv head, and 64 splits of those below one round)
   if (d->n_q >= (int64_t(1) << 31) || d->n_k >= (int64_t(1) << 31) || d->kv_heads > 1024 ||
-      (d->n_q / 4 + d->n_k / 128 + d->n_seq) * d->kv_heads >= (int64_t(1) << 31))
+      (d->n_q + d->n_k / 128 + d->n_seq) * d->kv_heads >= (int64_t(1) << 31))
     return fail(HPR_ERR_UNSUPPORTED_SHAPE, "too many rows or heads");
   const int64_t strides[6] = {d->q_row, d->q_head, d->k_row, d->k_head, d->v_row, d->v_head};
   for (int64_t x : strides)
@@ -601,7 +601,7 @@ size_t packed_attention_workspace_size(const hpr_attention* d) {
       d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
     return 0;
   const int64_t splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
-  const size_t plan = align_up((size_t)attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads) *
+  const size_t plan = align_up((size_t)attn_plan_tiles(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads) *
                                sizeof(AttnTile));
   if (splits <= 1) return plan;
   const size_t rows = (size_t)splits * d->n_q * d->heads;
@@ -613,7 +613,7 @@ size_t packed_attention_bwd_workspace_size(const hpr_attention* d) {
       d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
     return 0;
   return align_up((size_t)d->n_q * d->heads * sizeof(float)) +
-         align_up((size_t)attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads) * sizeof(AttnTile)) +
+         align_up((size_t)attn_plan_q_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads) * sizeof(AttnTile)) +
          align_up((size_t)attn_plan_key_tiles(d->n_k, d->n_seq, d->kv_heads) * sizeof(AttnTile));
 }
 
@@ -635,7 +635,7 @@ hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const
   a.lse = lse;
   a.splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
   Carver c(ws);
-  const int64_t plan = attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads);
+  const int64_t plan = attn_plan_tiles(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
   if (plan > 0) a.q_plan = c.take<AttnTile>((size_t)plan * sizeof(AttnTile));
   if (a.splits > 1) {
     const size_t rows = (size_t)a.splits * d->n_q * d->heads;
@@ -673,7 +673,7 @@ hpr_status packed_attention_bwd(const hpr_attention* d, const uint16_t* dout, co
   a.dv = dv;
   Carver c(ws);
   a.delta = c.take<float>((size_t)d->n_q * d->heads * sizeof(float));
-  const int64_t plan = attn_plan_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads);
+  const int64_t plan = attn_plan_q_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads);
   if (plan > 0) a.q_plan = c.take<AttnTile>((size_t)plan * sizeof(AttnTile));
   const int64_t k_plan = attn_plan_key_tiles(d->n_k, d->n_seq, d->kv_heads);
   if (k_plan > 0) a.k_plan = c.take<AttnTile>((size_t)k_plan * sizeof(AttnTile));

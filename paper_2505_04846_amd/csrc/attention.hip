@@ -275,8 +275,18 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NST * 2 * kTile];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % (uint32_t)a.kv_heads;
-  const uint32_t w = blockIdx.x / (uint32_t)a.kv_heads;
+  // Workgroups are dealt to the XCDs in turn.  With several waves a workgroup, heads go round first:
+  // the tiles of a head meet in one L2.  Single waves read every key once: there the heads of a run
+  // of keys go to one XCD, one after another, so that it reads whole rows.
+  uint32_t kvh, w;
+  if constexpr (NW > 1) {
+    kvh = blockIdx.x % (uint32_t)a.kv_heads;
+    w = blockIdx.x / (uint32_t)a.kv_heads;
+  } else {
+    kvh = (blockIdx.x >> 3) % (uint32_t)a.kv_heads;
+    w = (blockIdx.x >> 3) / (uint32_t)a.kv_heads * 8 + (blockIdx.x & 7);
+    if (w >= (uint32_t)(a.tiles * a.splits)) return;
+  }
   const int split = a.splits > 1 ? w % (uint32_t)a.splits : 0;
   // late tiles see the most keys: first
   const uint32_t tile = (uint32_t)a.tiles - 1 - (a.splits > 1 ? w / (uint32_t)a.splits : w);
@@ -441,29 +451,33 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
                                  n_slot - wave * 32, own, lane, a.dim / 8);
 }
 
-// out = the splits' sums joined under their common maximum.  A wave per (token, head), lane d.
+// out = the splits' sums joined under their common maximum.  A wave per (token, head): lane s holds
+// split s's statistics, then lane i values 2 i and 2 i + 1.
+constexpr int kMaxSplits = 64;
+
 template <class T>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int64_t rows = a.n_q * a.heads;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= rows) return;
-  float m = kNoMax;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + row)]);
-  float l = 0.f, o0 = 0.f, o1 = 0.f;
-  const int d = 2 * lane;
+  float2 ml = {kNoMax, 0.f};
+  if (lane < a.splits) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (lane * rows + row));
+  const float m = wave_max(ml.x);
+  const float f = __builtin_amdgcn_exp2f(ml.x - m);
+  const float l = wave_sum(f * ml.y);
+  const int d = 2 * lane < a.dim ? 2 * lane : 0;
+  const float* src = a.part_o + row * a.dim + d;
+  float o0 = 0.f, o1 = 0.f;
+#pragma unroll 4
   for (int s = 0; s < a.splits; ++s) {
-    const int64_t at = s * rows + row;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - m);
-    l += f * a.part_ml[2 * at + 1];
-    if (d < a.dim) {
-      const float2 v = *reinterpret_cast<const float2*>(a.part_o + at * a.dim + d);
-      o0 += f * v.x;
-      o1 += f * v.y;
-    }
+    const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+    const float2 v = *reinterpret_cast<const float2*>(src + s * rows * a.dim);
+    o0 += fs * v.x;
+    o1 += fs * v.y;
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  if (d < a.dim)
+  if (2 * lane < a.dim)
     *reinterpret_cast<uint32_t*>(a.out + row * a.dim + d) = T::pack(o0 * inv, o1 * inv);
   if (a.lse && lane == 0) a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
 }
@@ -786,9 +800,9 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
 }
 
 // (The bodies are device functions: the host pass knows no buffer resources.)
-template <class T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_fwd_kernel(AttnArgs a) {
-  attn_fwd<T, D, NW, 64, 2>(a);
+template <class T, int D, int NW, int KEYS, int NST, int OCC>
+__global__ __launch_bounds__(64 * NW, OCC) void attn_fwd_kernel(AttnArgs a) {
+  attn_fwd<T, D, NW, KEYS, NST>(a);
 }
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(AttnArgs a) {
@@ -799,7 +813,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dkv_kernel(AttnArgs a) {
   attn_dkv<T, D, NW>(a);
 }
 
-constexpr int kFwdWaves = 4, kBwdWaves = 4;
+// The forward's kernels:
+//   kFew    a wave, 32 slots, on its own, 32 keys a stage: calls of at most 32 slots a sequence (a
+//           token of each of many answers).  No wave idles over slots that are not there and none
+//           waits for another; five fit a CU, which keeps the keys' stream going.
+//   kShort  4 waves, 128 slots, 32 keys a stage at three workgroups per CU
+//   kLong   4 waves, 128 slots, 64 keys a stage at two workgroups per CU
+enum FwdShape { kFew, kShort, kLong };
+constexpr int64_t kLongFrom = 2048;  // mean keys per sequence from which kLong was faster
+FwdShape attn_shape(int64_t n_q, int64_t n_k, int n_seq, int G) {
+  if (n_q * G <= 32 * (int64_t)n_seq) return kFew;
+  return n_k < kLongFrom * n_seq ? kShort : kLong;
+}
+int fwd_slots(int64_t n_q, int64_t n_k, int n_seq, int G) {
+  return attn_shape(n_q, n_k, n_seq, G) == kFew ? 32 : 128;
+}
+constexpr int kBwdWaves = 4;
 constexpr int kKeyTile = 32 * kBwdWaves;
 
 // Writes the tiles of query rows (numbers below q_tiles), then those of key rows, a wave each.
@@ -817,13 +846,14 @@ hipError_t run_plan(const AttnArgs& a, int64_t q_tiles, int64_t k_tiles, int ts,
   return hipGetLastError();
 }
 
-template <class T, int D>
-hipError_t run_fwd(AttnArgs a, hipStream_t s) {
-  const int64_t grid = a.tiles * a.kv_heads * a.splits;
+template <class T, int D, int NW, int KEYS, int NST, int OCC>
+hipError_t run_fwd_as(const AttnArgs& a, hipStream_t s) {
+  const int64_t each = a.tiles * a.splits;
+  const int64_t grid = (NW > 1 ? each : (each + 7) / 8 * 8) * a.kv_heads;
   hipError_t e = run_plan(a, a.q_plan ? a.tiles : 0, 0, a.ts, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attn_fwd_kernel<T, D, kFwdWaves>), dim3((unsigned)grid), dim3(64 * kFwdWaves),
-                     0, s, a);
+  hipLaunchKernelGGL((attn_fwd_kernel<T, D, NW, KEYS, NST, OCC>), dim3((unsigned)grid), dim3(64 * NW), 0,
+                     s, a);
   e = hipGetLastError();
   if (e == hipSuccess && a.splits > 1) {
     const int64_t rows = a.n_q * a.heads;
@@ -831,6 +861,15 @@ hipError_t run_fwd(AttnArgs a, hipStream_t s) {
     e = hipGetLastError();
   }
   return e;
+}
+
+template <class T, int D>
+hipError_t run_fwd(const AttnArgs& a, hipStream_t s) {
+  switch (attn_shape(a.n_q, a.n_k, a.n_seq, a.G)) {
+    case kFew: return run_fwd_as<T, D, 1, 32, 2, 2>(a, s);
+    case kShort: return run_fwd_as<T, D, 4, D >= 128 ? 32 : 64, D >= 128 ? 3 : 2, 3>(a, s);
+    default: return run_fwd_as<T, D, 4, 64, 2, 2>(a, s);
+  }
 }
 
 template <class T, int D>
@@ -858,28 +897,37 @@ hipError_t run_bwd(AttnArgs a, hipStream_t s) {
 
 }  // namespace
 
-// Splits of the key axis: enough workgroups for four rounds of the chip's two per CU where the
-// tiles alone are fewer than one, and no fewer than 256 keys of the mean sequence each.
+// Splits of the key axis, where the tiles alone do not fill the chip: kFew up to 4,096 waves, others
+// up to eight workgroups per CU; no fewer than 256 keys of the mean sequence each.
 int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
-  constexpr int n_cu = 256;
+  constexpr int kCus = 256;
+  if (n_q < 1) return 1;
   const int G = heads / kv_heads;
-  const int64_t ts = 32 * kFwdWaves / G;
+  const bool few = attn_shape(n_q, n_k, n_seq, G) == kFew;
+  const int64_t ts = fwd_slots(n_q, n_k, n_seq, G) / G;
   // tiles that hold tokens, at most one a sequence more than the mean length takes
   const int64_t wgs = (n_q / ts + (n_q < n_seq ? n_q : n_seq)) * kv_heads;
-  if (wgs >= 2 * n_cu || n_q == 0) return 1;
-  const int64_t mean = n_k / n_seq;
-  int64_t s = (8 * (int64_t)n_cu + wgs - 1) / wgs;
-  const int64_t most = mean / 256 < 1 ? 1 : mean / 256;
+  const int64_t full = few ? 16 * kCus : 8 * kCus;
+  if (wgs >= (few ? full : full / 4)) return 1;
+  int64_t s = (full + wgs - 1) / wgs;
+  const int64_t most = n_k / n_seq / 256 < 1 ? 1 : n_k / n_seq / 256;
   if (s > most) s = most;
-  return (int)(s > 64 ? 64 : s);
+  return (int)(s > kMaxSplits ? kMaxSplits : s);
 }
 
 // Calls of at least four rounds of workgroups plan their tiles.
 constexpr int64_t kPlanFrom = 2048;
 
-int64_t attn_plan_tiles(int64_t n_q, int n_seq, int heads, int kv_heads) {
+int64_t attn_plan_tiles(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
   if (n_q < 1) return 0;
-  const int64_t tiles = n_q / (32 * kFwdWaves / (heads / kv_heads)) + n_seq;
+  const int G = heads / kv_heads;
+  const int64_t tiles = n_q / (fwd_slots(n_q, n_k, n_seq, G) / G) + n_seq;
+  return tiles * kv_heads >= kPlanFrom ? tiles : 0;
+}
+
+int64_t attn_plan_q_tiles(int64_t n_q, int n_seq, int heads, int kv_heads) {
+  if (n_q < 1) return 0;
+  const int64_t tiles = n_q / (32 * kBwdWaves / (heads / kv_heads)) + n_seq;
   return tiles * kv_heads >= kPlanFrom ? tiles : 0;
 }
 
@@ -891,7 +939,7 @@ int64_t attn_plan_key_tiles(int64_t n_k, int n_seq, int kv_heads) {
 
 hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream) {
   if (a.n_q == 0) return hipSuccess;
-  a.ts = 32 * kFwdWaves / a.G;
+  a.ts = fwd_slots(a.n_q, a.n_k, a.n_seq, a.G) / a.G;
   a.tiles = a.n_q / a.ts + a.n_seq;
   if (a.f16) return a.dim <= 64 ? run_fwd<HalfF16, 64>(a, stream) : run_fwd<HalfF16, 128>(a, stream);
   return a.dim <= 64 ? run_fwd<HalfBf16, 64>(a, stream) : run_fwd<HalfBf16, 128>(a, stream);

@@ -277,7 +277,8 @@ struct AttnArgs {
 constexpr int kMaxGroup = 32;  // query heads of one kv head
 int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
 // Tiles of the forward's and the gradients' plans (0: the call does not plan).
-int64_t attn_plan_tiles(int64_t n_q, int n_seq, int heads, int kv_heads);
+int64_t attn_plan_tiles(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
+int64_t attn_plan_q_tiles(int64_t n_q, int n_seq, int heads, int kv_heads);
 int64_t attn_plan_key_tiles(int64_t n_k, int n_seq, int kv_heads);
 hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream);
 hipError_t launch_attn_bwd(AttnArgs a, hipStream_t stream);
