@@ -36,97 +36,162 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int s) {
   return ad >= 0 && ad < a.n_ad ? ad : -1;
 }
 
+// ---- a wave's own product ----------------------------------------------------------------------
+
+// acc[b] = rows [32 b, 32 b + 32) of P times 32 rows of X, over stages [kk0, kk1) of 64 values, by one wave:
+// its two LDS stages are its own, so waves that split k run without a barrier.  Whole 128-byte lines go
+// straight to LDS (operands read from memory by lanes touch twice as many lines a load: a token's
+// projection took 22 us that way).
+template <class T, int NB>
+struct WaveProduct {
+  static constexpr int kStage = (1 + NB) * 4096;
+  static constexpr int kBytes = 2 * kStage;
+  static constexpr int kLoads = 4 * (1 + NB);
+  // x, p: first rows; x_last, p_last: their last valid row, which the rows past it repeat
+  static __device__ __forceinline__ void run(const uint16_t* x, int x_last, const uint16_t* p, int p_last,
+                                             int k, int kk0, int kk1, unsigned char* lds, int lane,
+                                             f32x16 (&acc)[NB]) {
+    const __amdgpu_buffer_rsrc_t rx = tile_rsrc(x), rp = tile_rsrc(p);
+    const TileReads<64> rd(lane);
+    int off[kLoads], chunk[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = 8 * (j < 4 ? j : j - 4) + (lane >> 3);
+      const int last = j < 4 ? x_last : p_last;
+      chunk[j] = ((lane & 7) ^ swz<64>(r)) * 8;
+      off[j] = (r < last ? r : last) * k * 2 + chunk[j] * 2;
+    }
+    const int whole = k / 64;
+    auto issue = [&](int buf, int kk) {
+      unsigned char* st = lds + buf * kStage;
+      if (kk < whole) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(j < 4 ? rx : rp, (lds_void_t*)(st + j * 1024), 16,
+                                                   off[j], kk * 128, 0, 0);
+      } else {  // the end of k: chunks past it read zeros
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          const char* src = (const char*)(j < 4 ? x : p) + off[j] + kk * 128;
+          const void* from = kk * 64 + chunk[j] < k ? (const void*)src : (const void*)kZero16;
+          __builtin_amdgcn_global_load_lds((glb_void_t*)from, (lds_void_t*)(st + j * 1024), 16, 0, 0);
+        }
+      }
+    };
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+    if (kk0 < kk1) issue(0, kk0);
+#pragma unroll 1
+    for (int kk = kk0; kk < kk1; ++kk) {
+      const int buf = (kk - kk0) & 1;
+      if (kk + 1 < kk1) {
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // the other stage's reads are done
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        issue(buf ^ 1, kk + 1);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
+      } else {
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+      }
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      const unsigned char* st = lds + buf * kStage;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const u32x4 fx = rd.row_frag(st, 0, s);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = T::mfma(rd.row_frag(st + 4096, b, s), fx, acc[b]);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  }
+};
+
 // ---- h ----------------------------------------------------------------------------------------
 
-// h of 32 rows of one request.  The waves split k, each summing its part of the whole [rank, 32]
+// h of 32 rows of one request.  W waves split k, each summing its part of the whole [rank, 32]
 // block (rank on the rows of the product, so that a lane holds 4 consecutive values of its row's
 // h), and join in LDS.  h is rounded to 16 bits once, with its scale: the operand of the product
 // with B.  Its relative rounding reaches only the adapter's part of y.
-constexpr int kShrinkRows = 32, kShrinkWaves = 4;
+constexpr int kShrinkRows = 32;
 
-template <class T, int NB>
-__global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a, uint16_t* h) {
-  __shared__ float part[kShrinkWaves][NB * 16][64];
+template <class T, int NB, int W>
+__device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h) {
+  using P = WaveProduct<T, NB>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // W * P::kBytes
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int s = find_seq(a.off, a.n_req, kShrinkRows, blockIdx.x);
   const Rows R = rows_of(a, s);
-  const int64_t first = R.r0 + ((int64_t)blockIdx.x - (R.r0 / kShrinkRows + s)) * kShrinkRows;
+  const int64_t first =
+      R.r0 + ((int64_t)blockIdx.x - ((uint32_t)R.r0 / kShrinkRows + (uint32_t)s)) * kShrinkRows;
   const int ad = adapter_of(a, s);
   if (first < R.r0 || first >= R.r1 || ad < 0) return;
-  const int64_t t = first + col;
-  const bool live = t < R.r1;
-  const uint16_t* xr = a.x + (live ? t : R.r1 - 1) * (int64_t)a.k;
-  const uint16_t* ar = a.a + (int64_t)ad * a.r * a.k;
-  const uint16_t* arow[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int j = 32 * b + col;
-    arow[b] = ar + (int64_t)(j < a.r ? j : a.r - 1) * a.k;
-  }
+  const int last = R.r1 - first < kShrinkRows ? (int)(R.r1 - first) - 1 : kShrinkRows - 1;
+  const int nk = (a.k + 63) / 64;
   f32x16 acc[NB];
+  unsigned char* own = smem + wave * P::kBytes;
+  P::run(a.x + first * a.k, last, a.a + (int64_t)ad * a.r * a.k, a.r - 1, a.k, nk * wave / W,
+         nk * (wave + 1) / W, own, lane, acc);
+  float* part = reinterpret_cast<float*>(own);  // [NB * 16][64]
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
-  const int steps = (a.k + 15) / 16;
-  const int s0 = steps * wave / kShrinkWaves, s1 = steps * (wave + 1) / kShrinkWaves;
-#pragma unroll 1
-  for (int st = s0; st < s1; ++st) {
-    const int d = 16 * st + 8 * half;
-    const bool in = d < a.k;
-    u32x4 xv = load16(xr + (in ? d : 0));
-    if (!in) xv = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      u32x4 av = load16(arow[b] + (in ? d : 0));
-      if (!in) av = u32x4{0u, 0u, 0u, 0u};
-      acc[b] = T::mfma(av, xv, acc[b]);
-    }
-  }
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) part[wave][16 * b + r][lane] = acc[b][r];
+    for (int r = 0; r < 16; ++r) part[(16 * b + r) * 64 + lane] = acc[b][r];
   __syncthreads();
   const int rp = (a.r + 15) / 16 * 16;
   const float sc = a.scale[ad];
   // register groups of four: group g of NB * 4 holds ranks 32 (g / 4) + 8 (g % 4) + 4 half + 0..3
-  for (int g = wave; g < NB * 4; g += kShrinkWaves) {
+  for (int g = wave; g < NB * 4; g += W) {
     const int j = 32 * (g >> 2) + 8 * (g & 3) + 4 * half;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] = 0.f;
 #pragma unroll
-      for (int w = 0; w < kShrinkWaves; ++w) v[e] += part[w][4 * g + e][lane];
+      for (int w = 0; w < W; ++w)
+        v[e] += reinterpret_cast<const float*>(smem + w * P::kBytes)[(4 * g + e) * 64 + lane];
       v[e] = j + e < a.r ? v[e] * sc : 0.f;
     }
-    if (live && j < rp)
-      *reinterpret_cast<uint2*>(h + t * rp + j) = uint2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+    if (col <= last && j < rp)
+      *reinterpret_cast<uint2*>(h + (first + col) * rp + j) =
+          uint2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
   }
+}
+
+// (The bodies are device functions: the host pass knows no buffer resources.)
+template <class T, int NB, int W>
+__global__ __launch_bounds__(64 * W) void shrink_kernel(AdapterArgs a, uint16_t* h) {
+  shrink_tile<T, NB, W>(a, h);
 }
 
 // ---- y ----------------------------------------------------------------------------------------
 
-// Tile of BT rows of x by BM rows of W (columns of y), WT x WM waves, k in stages of 64 through
-// two LDS stages.  W's rows are the rows of the product, so a lane holds 4 consecutive values of a
-// row of y.  The adapters' part needs no LDS: for every run of rows of one request in the tile,
-// h's rows (zero outside the run) and B's rows are read as operands.
-template <class T, int BT, int BM, int WT, int WM>
+// Tile of BT rows of x by BM rows of W (columns of y), WT x WM waves, k in stages of 64 through NST LDS
+// stages.  W's rows are the rows of the product, so a lane holds 4 consecutive values of a row of y.
+//
+// The adapters' part comes first, while the first stage is on its way, and needs no LDS: for every run of
+// rows of one request in the wave's rows, h's rows and B's rows are read as operands, and the product
+// goes to the rows of the run alone (a B that is not finite is not another request's).
+template <class T, int BT, int BM, int WT, int WM, int NST>
 __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t* __restrict__ h,
                                             uint16_t* __restrict__ y, int n_m) {
   constexpr int kW = WT * WM;
   constexpr int kTb = BT / 32 / WT, kMb = BM / 32 / WM;  // blocks per wave
   constexpr int kXBytes = BT * 128, kWBytes = BM * 128, kStage = kXBytes + kWBytes;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // 2 stages
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // NST stages
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wt = wave % WT, wm = wave / WT;
-  const int64_t lin = xcd_linear(blockIdx.x, gridDim.x);
-  const int64_t tt = lin / n_m;
-  const int tm = (int)(lin - tt * n_m);
-  const int64_t t0 = tt * BT;
+  // An XCD walks a contiguous run of tiles, four row tiles abreast: the tiles that it holds at a time
+  // (32 of the widest) read 4 row tiles and 8 column tiles, not 1 or 2 and all the columns.
+  const uint32_t lin = (uint32_t)xcd_linear(blockIdx.x, gridDim.x);
+  const uint32_t n_t = (uint32_t)((a.n + BT - 1) / BT);
+  const uint32_t g0 = lin / (4u * n_m) * 4u, in_g = lin - g0 * n_m;
+  const uint32_t abreast = n_t - g0 < 4u ? n_t - g0 : 4u;
+  const int tm = (int)(in_g / abreast);
+  const int64_t t0 = (int64_t)(g0 + in_g % abreast) * BT;
   const int m0 = tm * BM;
   const int64_t left_t = a.n - t0;
   const int last_t = left_t < BT ? (int)left_t - 1 : BT - 1;
@@ -135,6 +200,7 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
   const TileReads<64> rd(lane);
   const TileLoad<64, BT, kW> lx(wave, lane, 8);
   const TileLoad<64, BM, kW> lw(wave, lane, 8);
+  constexpr int kLoads = lx.kLoads + lw.kLoads;
   const uint16_t* xb = a.x + t0 * a.k;
   const uint16_t* wb = a.w + (int64_t)m0 * a.k;
   const __amdgpu_buffer_rsrc_t rx = tile_rsrc(xb), rw = tile_rsrc(wb);
@@ -146,6 +212,8 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
   for (int j = 0; j < lw.kLoads; ++j)
     ow[j] = (lw.row[j] < last_m ? lw.row[j] : last_m) * a.k * 2 + lw.chunk[j];
   const int nk = (a.k + 63) / 64, nk_full = a.k / 64;
+  // Stage kk into ring buffer buf.  Chunks past the end of k read zeros, so past the last stage too
+  // (the ring keeps its number of loads in flight).
   auto issue = [&](int buf, int kk) {
     unsigned char* st = smem + buf * kStage;
     if (kk < nk_full) {
@@ -157,7 +225,7 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
       for (int j = 0; j < lw.kLoads; ++j)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
             rw, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, ow[j], kk * 128, 0, 0);
-    } else if (kk < nk) {  // the end of k: chunks past it read zeros
+    } else {
 #pragma unroll
       for (int j = 0; j < lx.kLoads; ++j) {
         const bool in = kk * 64 + lx.chunk[j] / 2 < a.k;
@@ -174,6 +242,8 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
       }
     }
   };
+#pragma unroll
+  for (int s = 0; s < NST - 1; ++s) issue(s, s);
 
   f32x16 acc[kMb][kTb];
 #pragma unroll
@@ -183,116 +253,218 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  issue(0, 0);
-#pragma unroll 1
-  for (int kk = 0; kk < nk; ++kk) {
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-    sync_lds();
-    issue((kk + 1) & 1, kk + 1);
-    const unsigned char* xs = smem + (kk & 1) * kStage;
-    const unsigned char* ws = xs + kXBytes;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      u32x4 fx[kTb], fw[kMb];
-#pragma unroll
-      for (int j = 0; j < kTb; ++j) fx[j] = rd.row_frag(xs, wt * kTb + j, s);
-#pragma unroll
-      for (int i = 0; i < kMb; ++i) fw[i] = rd.row_frag(ws, wm * kMb + i, s);
-#pragma unroll
-      for (int i = 0; i < kMb; ++i)
-#pragma unroll
-        for (int j = 0; j < kTb; ++j) acc[i][j] = T::mfma(fw[i], fx[j], acc[i][j]);
-    }
-  }
-  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-
   // the adapters' part
   if (h && a.n_req > 0) {
     const int rp = (a.r + 15) / 16 * 16;
     const bool whole = a.r % 8 == 0;
-    const int64_t wt0 = t0 + wt * kTb * 32;
-    const int64_t wt1 = wt0 + kTb * 32 < a.n ? wt0 + kTb * 32 : a.n;
-    int s = find_row(a.off, a.n_req, wt0);
-#pragma unroll 1
-    for (; s < a.n_req; ++s) {
-      const Rows R = rows_of(a, s);
-      if (R.r0 >= wt1) break;
-      const int ad = adapter_of(a, s);
-      if (R.r1 <= wt0 || R.r1 <= R.r0 || ad < 0) continue;
-      const uint16_t* br = a.b + (int64_t)ad * a.m * a.r;
-      auto b_frag = [&](int i, int d) {  // values [d, d + 8) of the lane's row of B, zero past r
-        const int m = m0 + (wm * kMb + i) * 32 + col;
-        const uint16_t* p = br + (int64_t)(m < a.m ? m : a.m - 1) * a.r;
-        u32x4 f = {0u, 0u, 0u, 0u};
-        if (whole) {
-          if (d < a.r) f = load16(p + d);
-        } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (d + e < a.r) f[e >> 1] |= (uint32_t)p[d + e] << (16 * (e & 1));
-        }
-        return f;
-      };
-      auto h_frag = [&](int64_t t, int d) {
-        u32x4 f = {0u, 0u, 0u, 0u};
-        if (t >= R.r0 && t < R.r1) f = load16(h + t * rp + d);
-        return f;
-      };
-      if (R.r0 <= wt0 && R.r1 >= wt1) {  // the run covers the wave's rows
+    for (int j = 0; j < kTb; ++j) {
+      const int64_t r0 = t0 + (wt * kTb + j) * 32, r1 = r0 + 32 < a.n ? r0 + 32 : a.n;
+      const int64_t t = r0 + col;
+#pragma unroll 1
+      for (int s = find_row(a.off, a.n_req, r0); s < a.n_req; ++s) {
+        const Rows R = rows_of(a, s);
+        if (R.r0 >= r1) break;
+        const int ad = adapter_of(a, s);
+        if (R.r1 <= r0 || R.r1 <= R.r0 || ad < 0) continue;
+        const uint16_t* br = a.b + (int64_t)ad * a.m * a.r;
+        const bool in = t >= R.r0 && t < R.r1;
+        f32x16 v[kMb];
+#pragma unroll
+        for (int i = 0; i < kMb; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) v[i][r] = 0.f;
 #pragma unroll 1
         for (int d = 8 * half; d < rp; d += 16) {
-          u32x4 fh[kTb], fb[kMb];
-#pragma unroll
-          for (int j = 0; j < kTb; ++j) fh[j] = h_frag(wt0 + 32 * j + col, d);
-#pragma unroll
-          for (int i = 0; i < kMb; ++i) fb[i] = b_frag(i, d);
-#pragma unroll
-          for (int i = 0; i < kMb; ++i)
-#pragma unroll
-            for (int j = 0; j < kTb; ++j) acc[i][j] = T::mfma(fb[i], fh[j], acc[i][j]);
-        }
-      } else {
-        // rows outside the run keep their sums: a B that is not finite is none of theirs
-#pragma unroll
-        for (int j = 0; j < kTb; ++j) {
-          const int64_t t = wt0 + 32 * j + col;
-          if (R.r0 >= wt0 + 32 * j + 32 || R.r1 <= wt0 + 32 * j) continue;
-          const bool in = t >= R.r0 && t < R.r1;
+          u32x4 fh = {0u, 0u, 0u, 0u};
+          if (in) fh = load16(h + t * rp + d);
 #pragma unroll
           for (int i = 0; i < kMb; ++i) {
-            f32x16 v = acc[i][j];
-#pragma unroll 1
-            for (int d = 8 * half; d < rp; d += 16) v = T::mfma(b_frag(i, d), h_frag(t, d), v);
+            const int m = m0 + (wm * kMb + i) * 32 + col;
+            const uint16_t* p = br + (int64_t)(m < a.m ? m : a.m - 1) * a.r;
+            u32x4 fb = {0u, 0u, 0u, 0u};
+            if (whole) {
+              if (d < a.r) fb = load16(p + d);
+            } else {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = in ? v[r] : acc[i][j][r];
+              for (int e = 0; e < 8; ++e)
+                if (d + e < a.r) fb[e >> 1] |= (uint32_t)p[d + e] << (16 * (e & 1));
+            }
+            v[i] = T::mfma(fb, fh, v[i]);
           }
         }
+#pragma unroll
+        for (int i = 0; i < kMb; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = in ? v[i][r] : acc[i][j][r];
       }
     }
   }
 
+  struct Frags {
+    u32x4 x[kTb], w[kMb];
+  };
+  auto read_frags = [&](int buf, int s, Frags& f) {
+    const unsigned char* xs = smem + buf * kStage;
 #pragma unroll
-  for (int j = 0; j < kTb; ++j) {
-    const int64_t t = t0 + (wt * kTb + j) * 32 + col;
-    if (t >= a.n) continue;
+    for (int j = 0; j < kTb; ++j) f.x[j] = rd.row_frag(xs, wt * kTb + j, s);
+#pragma unroll
+    for (int i = 0; i < kMb; ++i) f.w[i] = rd.row_frag(xs + kXBytes, wm * kMb + i, s);
+  };
+  auto mfma = [&](const Frags& f) {
 #pragma unroll
     for (int i = 0; i < kMb; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int m = m0 + (wm * kMb + i) * 32 + 8 * g + 4 * half;
-        if (m < a.m)
-          *reinterpret_cast<uint2*>(y + t * a.m + m) =
-              uint2{T::pack(acc[i][j][4 * g], acc[i][j][4 * g + 1]),
-                    T::pack(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3])};
+      for (int j = 0; j < kTb; ++j) acc[i][j] = T::mfma(f.w[i], f.x[j], acc[i][j]);
+  };
+  // The stages of the ring: NST - 1 are in flight when one is computed on.  One barrier per stage,
+  // before its last k-step, whose products run while the next stage's first operands are read.
+  Frags f0, f1;
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+  sync_lds();
+  read_frags(0, 0, f0);
+#pragma unroll 1
+  for (int kk = 0, buf = 0; kk < nk; ++kk) {
+    const int nxt = buf + 1 < NST ? buf + 1 : 0, free_ = buf > 0 ? buf - 1 : NST - 1;
+    issue(free_, kk + NST - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    read_frags(buf, 1, f1);
+    mfma(f0);
+    read_frags(buf, 2, f0);
+    mfma(f1);
+    read_frags(buf, 3, f1);
+    mfma(f0);
+    // each k-step's products alternate with the reads of the next one's operands
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+#pragma unroll
+      for (int t = 0; t < kMb * kTb; ++t) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (t < kTb + kMb) __builtin_amdgcn_sched_group_barrier(0x100, kMb * kTb >= kTb + kMb ? 1 : kTb + kMb, 0);
       }
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    sync_lds();
+    read_frags(nxt, 0, f0);  // (past the last stage: zeros, or rows that are read by nobody)
+    __builtin_amdgcn_sched_barrier(0);
+    mfma(f1);
+    buf = nxt;
+  }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // no load may still target LDS when it is reused or ends
+
+  // y through LDS, so that memory sees whole rows: a wave's 32 kTb rows of 32 kMb values, one 32-row
+  // block at a time
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  sync_lds();
+  constexpr int kRow = 64 * kMb;                                // bytes of a wave's row
+  static_assert(kW * 32 * kRow <= NST * kStage, "the waves' blocks fit the ring");
+  unsigned char* own = smem + wave * 32 * kRow;
+  constexpr int kCh = kRow / 16, kPer = 64 / kCh;               // chunks of a row, rows of a wave store
+  const int mw = m0 + wm * kMb * 32;
+#pragma unroll
+  for (int j = 0; j < kTb; ++j) {
+    const int64_t r0 = t0 + (wt * kTb + j) * 32;
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);  // (a wave's LDS operations execute in program order)
+#pragma unroll
+    for (int i = 0; i < kMb; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<uint2*>(own + col * kRow + (((4 * i + g) ^ (col % kCh)) << 4) + 8 * half) =
+            uint2{T::pack(acc[i][j][4 * g], acc[i][j][4 * g + 1]),
+                  T::pack(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3])};
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    uint16_t* dst = y + r0 * a.m + mw;
+#pragma unroll
+    for (int k = 0; k < 32 / kPer; ++k) {
+      const int r = k * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
+      if (r0 + r < a.n && mw + 8 * c < a.m) *reinterpret_cast<u32x4*>(dst + (int64_t)r * a.m + 8 * c) = v;
+    }
   }
 }
 
-// (The body is a device function: the host pass knows no buffer resources.)
-template <class T, int BT, int BM, int WT, int WM, int MINB>
+template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
 __global__ __launch_bounds__(64 * WT * WM, MINB) void expand_kernel(AdapterArgs a, const uint16_t* h,
                                                                     uint16_t* y, int n_m) {
-  expand_tile<T, BT, BM, WT, WM>(a, h, y, n_m);
+  expand_tile<T, BT, BM, WT, WM, NST>(a, h, y, n_m);
+}
+
+// Few rows: 32 rows of x by 32 rows of W per workgroup.  The waves split k and join in LDS; then a thread
+// adds the adapter's part of its two values, each from its row's own h and B.
+constexpr int kFewWaves = 8;
+
+template <class T>
+__device__ __forceinline__ void expand_few(const AdapterArgs& a, const uint16_t* h, uint16_t* y, int n_m) {
+  using P = WaveProduct<T, 1>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // kFewWaves * P::kBytes
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m0 = (int)(blockIdx.x % (uint32_t)n_m) * 32;
+  const int64_t t0 = (int64_t)(blockIdx.x / (uint32_t)n_m) * 32;
+  const int nk = (a.k + 63) / 64;
+  f32x16 acc[1];
+  unsigned char* own = smem + wave * P::kBytes;
+  P::run(a.x + t0 * a.k, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31, a.w + (int64_t)m0 * a.k,
+         a.m - m0 < 32 ? a.m - m0 - 1 : 31, a.k, nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own,
+         lane, acc);
+  float* part = reinterpret_cast<float*>(own);  // [16][64]
+#pragma unroll
+  for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][r];
+  __syncthreads();
+  // thread: row t0 + i / 16 of the tile, columns m0 + 2 (i % 16) and the next: entries e, e + 1 of
+  // lane (row, half) with column = 8 (e / 4) + 4 half + e % 4
+  const int row = threadIdx.x >> 4, m = 2 * (threadIdx.x & 15);
+  const int e = 4 * (m >> 3) + (m & 3), at = row + 32 * ((m >> 2) & 1);
+  float v0 = 0.f, v1 = 0.f;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    const float* from = reinterpret_cast<const float*>(smem + w * P::kBytes);
+    v0 += from[e * 64 + at];
+    v1 += from[(e + 1) * 64 + at];
+  }
+  const int64_t t = t0 + row;
+  if (t >= a.n || m0 + m >= a.m) return;
+  if (a.n_req > 0) {
+    // the row's request (the last that starts at or before it)
+    int lo = 0, n = a.n_req;
+    while (n > 1) {
+      const int step = n / 2;
+      if (a.off[lo + step] <= t) lo += step, n -= step;
+      else n = step;
+    }
+    const int ad = adapter_of(a, lo);
+    if (ad >= 0 && a.off[lo] <= t && t < a.off[lo + 1]) {
+      const int rp = (a.r + 15) / 16 * 16;
+      const uint16_t* hr = h + t * rp;
+      const uint16_t* b0 = a.b + ((int64_t)ad * a.m + m0 + m) * a.r;
+      float s0f = 0.f, s1f = 0.f;
+      if (a.r % 8 == 0) {
+        for (int d = 0; d < a.r; d += 8) {
+          const u32x4 hv = load16(hr + d), u = load16(b0 + d), w = load16(b0 + a.r + d);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            s0f += T::lo(hv[q]) * T::lo(u[q]) + T::hi(hv[q]) * T::hi(u[q]);
+            s1f += T::lo(hv[q]) * T::lo(w[q]) + T::hi(hv[q]) * T::hi(w[q]);
+          }
+        }
+      } else {
+        for (int d = 0; d < a.r; ++d) {
+          s0f += T::lo(hr[d]) * T::lo(b0[d]);
+          s1f += T::lo(hr[d]) * T::lo(b0[a.r + d]);
+        }
+      }
+      v0 += s0f;
+      v1 += s1f;
+    }
+  }
+  *reinterpret_cast<uint32_t*>(y + t * a.m + m0 + m) = T::pack(v0, v1);
+}
+
+template <class T>
+__global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(AdapterArgs a, const uint16_t* h,
+                                                                    uint16_t* y, int n_m) {
+  expand_few<T>(a, h, y, n_m);
 }
 
 // ---- transposed weights -----------------------------------------------------------------------
@@ -433,40 +605,64 @@ __global__ __launch_bounds__(256) void outer_join_kernel(AdapterArgs a, int cols
     out[((int64_t)ad * a.r + j) * cols + c] = v;
 }
 
-template <class T>
-hipError_t shrink(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
-  const int64_t grid = a.n / kShrinkRows + a.n_req;
-  const int nb = (a.r + 31) / 32;
-  if (nb == 1)
-    hipLaunchKernelGGL((shrink_kernel<T, 1>), dim3((unsigned)grid), dim3(64 * kShrinkWaves), 0, s, a, h);
-  else if (nb == 2)
-    hipLaunchKernelGGL((shrink_kernel<T, 2>), dim3((unsigned)grid), dim3(64 * kShrinkWaves), 0, s, a, h);
-  else
-    hipLaunchKernelGGL((shrink_kernel<T, 4>), dim3((unsigned)grid), dim3(64 * kShrinkWaves), 0, s, a, h);
+// The dynamic LDS of a kernel beyond the default limit.
+hipError_t allow_lds(const void* fn, int lds) {
+  return lds > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) : hipSuccess;
+}
+
+template <class T, int NB, int W>
+hipError_t shrink_as(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
+  constexpr int lds = W * WaveProduct<T, NB>::kBytes;
+  const hipError_t e = allow_lds((const void*)shrink_kernel<T, NB, W>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((shrink_kernel<T, NB, W>), dim3((unsigned)(a.n / kShrinkRows + a.n_req)), dim3(64 * W),
+                     lds, s, a, h);
   return hipGetLastError();
 }
 
-template <class T, int BT, int BM, int WT, int WM, int MINB>
+// Waves per workgroup: as many as two workgroups per CU allow, or eight where one round of workgroups
+// does not fill the chip.
+template <class T>
+hipError_t shrink(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
+  if (a.r <= 32) {
+    if (a.n / kShrinkRows + a.n_req <= 256) return shrink_as<T, 1, 8>(a, h, s);
+    return shrink_as<T, 1, 4>(a, h, s);
+  }
+  if (a.r <= 64) return shrink_as<T, 2, 3>(a, h, s);
+  return shrink_as<T, 4, 2>(a, h, s);
+}
+
+template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
 hipError_t expand_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipStream_t s) {
   const int n_m = (a.m + BM - 1) / BM;
   const int64_t grid = (a.n + BT - 1) / BT * n_m;
-  constexpr int lds = 2 * (BT + BM) * 128;
-  if (lds > 65536) {  // beyond the default dynamic LDS limit
-    const void* fn = (const void*)expand_kernel<T, BT, BM, WT, WM, MINB>;
-    const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL((expand_kernel<T, BT, BM, WT, WM, MINB>), dim3((unsigned)grid),
+  constexpr int lds = NST * (BT + BM) * 128;
+  const hipError_t e = allow_lds((const void*)expand_kernel<T, BT, BM, WT, WM, NST, MINB>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((expand_kernel<T, BT, BM, WT, WM, NST, MINB>), dim3((unsigned)grid),
                      dim3(64 * WT * WM), lds, s, a, h, y, n_m);
   return hipGetLastError();
 }
 
+// Rows up to which the whole call is one pass over W, and the fewest tiles of the two large sizes.
+constexpr int kFewRows = 64;
+constexpr int kWideFrom = 192, kMidFrom = 256;
+
 template <class T>
 hipError_t expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipStream_t s) {
-  const int64_t tiles = ((a.n + 255) / 256) * ((a.m + 255) / 256);
-  if (tiles >= 128) return expand_as<T, 256, 256, 4, 2, 1>(a, h, y, s);
-  if (a.n > 64) return expand_as<T, 128, 128, 2, 2, 2>(a, h, y, s);
-  return expand_as<T, 32, 64, 1, 2, 2>(a, h, y, s);
+  auto tiles = [&](int b) { return (a.n + b - 1) / b * ((a.m + b - 1) / b); };
+  if (a.n <= kFewRows) {
+    const int n_m = (a.m + 31) / 32;
+    constexpr int lds = kFewWaves * WaveProduct<T, 1>::kBytes;
+    const hipError_t e = allow_lds((const void*)expand_few_kernel<T>, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((expand_few_kernel<T>), dim3((unsigned)((a.n + 31) / 32 * n_m)),
+                       dim3(64 * kFewWaves), lds, s, a, h, y, n_m);
+    return hipGetLastError();
+  }
+  if (tiles(256) >= kWideFrom) return expand_as<T, 256, 256, 4, 2, 2, 1>(a, h, y, s);
+  if (tiles(128) >= kMidFrom) return expand_as<T, 128, 128, 2, 2, 2, 2>(a, h, y, s);
+  return expand_as<T, 64, 64, 2, 2, 4, 2>(a, h, y, s);
 }
 
 template <class T>
