@@ -704,10 +704,11 @@ hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uin
 size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_t r, int32_t n_ad,
                                          int32_t n_req) {
   if (n < 0 || k < 1 || m < 1 || r < 1 || n_ad < 0 || n_req < 0) return 0;
-  const size_t rp = (size_t)adapter_rank_pad(r), most = (size_t)(k > m ? k : m);
+  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req);
   return align_up((size_t)m * k * 2) + align_up((size_t)n_ad * r * k * 2) +
          align_up((size_t)n_ad * r * m * 2) + align_up((size_t)n * rp * 2) +
-         align_up((size_t)adapter_outer_parts(n, n_req) * rp * most * sizeof(float));
+         align_up(slots * rp * k * sizeof(float)) + align_up(slots * rp * m * sizeof(float)) +
+         align_up(2 * slots * sizeof(int32_t));
 }
 
 hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, int32_t k,
@@ -725,13 +726,15 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   if (!ws || ws_bytes < need)
     return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const size_t rp = (size_t)adapter_rank_pad(r), most = (size_t)(k > m ? k : m);
+  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req);
   Carver c(ws);
   uint16_t* wt = c.take<uint16_t>((size_t)m * k * 2);
   uint16_t* at = c.take<uint16_t>((size_t)n_ad * r * k * 2);
   uint16_t* bt = c.take<uint16_t>((size_t)n_ad * r * m * 2);
   uint16_t* g = c.take<uint16_t>((size_t)n * rp * 2);
-  float* part = c.take<float>((size_t)adapter_outer_parts(n, n_req) * rp * most * sizeof(float));
+  float* part_a = c.take<float>(slots * rp * k * sizeof(float));
+  float* part_b = c.take<float>(slots * rp * m * sizeof(float));
+  int32_t* slot_adapter = c.take<int32_t>(2 * slots * sizeof(int32_t));
   // g and dx: the forward's kernels on (dy, W^T, B^T, A^T)
   const AdapterArgs f = {x, w, a, b, scale, req_off, adapter, n, k, m, r, n_ad, n_req,
                          dtype == HPR_F16};
@@ -745,23 +748,21 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   hipError_t e = hipSuccess;
   if (n > 0 && (dx || da)) {
     e = timed("adapter_transpose", s, [&] {
-      hipError_t x1 = launch_transpose(b, bt, n_ad, m, r, s);
-      if (x1 == hipSuccess && dx) x1 = launch_transpose(a, at, n_ad, r, k, s);
-      if (x1 == hipSuccess && dx) x1 = launch_transpose(w, wt, 1, m, k, s);
-      return x1;
+      const TransposeArgs q = {{{w, wt, dx ? 1 : 0, m, k, 0},
+                                {a, at, dx ? n_ad : 0, r, k, 0},
+                                {b, bt, n_ad, m, r, 0}}};
+      return launch_transpose(q, s);
     });
     if (e == hipSuccess) e = timed("adapter_shrink", s, [&] { return launch_adapter_shrink(t, g, s); });
     if (e == hipSuccess && dx)
       e = timed("adapter_expand", s, [&] { return launch_adapter_expand(t, g, dx, s); });
     if (e != hipSuccess) return hip_fail(e, "adapter gradient launch");
   }
-  if (da)
+  if (da || db)
     e = timed("adapter_outer", s, [&] {
-      return launch_adapter_outer(f, g, x, k, false, part, da, s);
-    });
-  if (e == hipSuccess && db)
-    e = timed("adapter_outer", s, [&] {
-      return launch_adapter_outer(f, h, dy, m, true, part, db, s);
+      const OuterArgs o = {{{g, x, k, 0, part_a, da, 0, 0}, {h, dy, m, 1, part_b, db, 0, 0}},
+                           slot_adapter, 0};
+      return launch_adapter_outer(f, o, s);
     });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "adapter gradient launch");
 }

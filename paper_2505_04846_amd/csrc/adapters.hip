@@ -187,11 +187,11 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
   // An XCD walks a contiguous run of tiles, four row tiles abreast: the tiles that it holds at a time
   // (32 of the widest) read 4 row tiles and 8 column tiles, not 1 or 2 and all the columns.
   const uint32_t lin = (uint32_t)xcd_linear(blockIdx.x, gridDim.x);
-  const uint32_t n_t = (uint32_t)((a.n + BT - 1) / BT);
+  const uint32_t n_t = (uint32_t)((a.n - a.row0 + BT - 1) / BT);
   const uint32_t g0 = lin / (4u * n_m) * 4u, in_g = lin - g0 * n_m;
   const uint32_t abreast = n_t - g0 < 4u ? n_t - g0 : 4u;
   const int tm = (int)(in_g / abreast);
-  const int64_t t0 = (int64_t)(g0 + in_g % abreast) * BT;
+  const int64_t t0 = a.row0 + (int64_t)(g0 + in_g % abreast) * BT;
   const int m0 = tm * BM;
   const int64_t left_t = a.n - t0;
   const int last_t = left_t < BT ? (int)left_t - 1 : BT - 1;
@@ -469,44 +469,79 @@ __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(AdapterArgs 
 
 // ---- transposed weights -----------------------------------------------------------------------
 
-__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* in, uint16_t* out, int rows,
-                                                        int cols) {
-  __shared__ uint16_t tile[64][66];
-  const int64_t base = (int64_t)blockIdx.z * rows * cols;
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+// Up to three batches of matrices in one launch, a 64 x 64 tile per workgroup: whole 16-byte pieces of
+// rows in and out where both sizes are multiples of 8, values otherwise.
+__global__ __launch_bounds__(256) void transpose_kernel(TransposeArgs a) {
+  __shared__ __attribute__((aligned(16))) uint16_t tile[64][72];
+  int w = 0;
+  uint32_t b = blockIdx.x;
+  while (w < 2 && b >= a.job[w].blocks) b -= a.job[w++].blocks;
+  const TransposeJob& q = a.job[w];
+  const int rows = q.rows, cols = q.cols;
+  const uint32_t n_c = (uint32_t)(cols + 63) / 64u, n_r = (uint32_t)(rows + 63) / 64u;
+  const int64_t base = (int64_t)(b / (n_c * n_r)) * rows * cols;
+  const uint32_t in_m = b % (n_c * n_r);
+  const int r0 = (int)(in_m / n_c) * 64, c0 = (int)(in_m % n_c) * 64;
+  const uint16_t* in = q.in + base;
+  uint16_t* out = q.out + base;
+  if (rows % 8 == 0 && cols % 8 == 0) {
+    const int x = 8 * (threadIdx.x & 7), y = threadIdx.x >> 3;
+#pragma unroll
+    for (int i = y; i < 64; i += 32)
+      if (r0 + i < rows && c0 + x < cols)
+        *reinterpret_cast<u32x4*>(&tile[i][x]) = load16(in + (int64_t)(r0 + i) * cols + c0 + x);
+    __syncthreads();
+    // thread: 8 rows of one column; a wave's 64 columns of the same rows read LDS without conflicts
+    const int c = threadIdx.x & 63;
+#pragma unroll
+    for (int k = threadIdx.x >> 6; k < 8; k += 4) {
+      if (c0 + c >= cols || r0 + 8 * k >= rows) continue;
+      u32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[e] = (uint32_t)tile[8 * k + 2 * e][c] | (uint32_t)tile[8 * k + 2 * e + 1][c] << 16;
+      *reinterpret_cast<u32x4*>(out + (int64_t)(c0 + c) * rows + r0 + 8 * k) = v;
+    }
+    return;
+  }
   const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
   for (int i = y; i < 64; i += 4)
-    if (r0 + i < rows && c0 + x < cols) tile[i][x] = in[base + (int64_t)(r0 + i) * cols + c0 + x];
+    if (r0 + i < rows && c0 + x < cols) tile[i][x] = in[(int64_t)(r0 + i) * cols + c0 + x];
   __syncthreads();
   for (int i = y; i < 64; i += 4)
-    if (c0 + i < cols && r0 + x < rows) out[base + (int64_t)(c0 + i) * rows + r0 + x] = tile[x][i];
+    if (c0 + i < cols && r0 + x < rows) out[(int64_t)(c0 + i) * rows + r0 + x] = tile[x][i];
 }
 
 // ---- dA, dB -----------------------------------------------------------------------------------
 
 // Partial sums over up to kOuterRows rows of one request: part[slot][j][c] = sum_t L[t,j] M[t,c],
-// 64 ranks and 256 columns per workgroup, 64 columns per wave; rows in tiles of 64, both operands
-// read by columns.
+// 64 ranks and 256 columns per workgroup, 64 columns per wave; rows in tiles of 64 through two LDS
+// stages, both operands read by columns.  dA and dB go in one launch.
 constexpr int kOuterRows = 512, kOuterWaves = 4;
 
 template <class T>
-__global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs a,
-                                                                    const uint16_t* L,
-                                                                    const uint16_t* M, int cols,
-                                                                    int n_cb, float* part) {
+__global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs a, OuterArgs o) {
   constexpr int kTile = 64 * 128;  // 64 rows of 64 values
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[(1 + kOuterWaves) * kTile];
+  constexpr int kStage = (1 + kOuterWaves) * kTile;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // 2 stages
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rp = (a.r + 15) / 16 * 16;
-  const int n_jb = (rp + 63) / 64;
-  const int cb = blockIdx.x % n_cb;
-  const int jb = (int)(blockIdx.x / n_cb) % n_jb;
-  const int64_t slot = blockIdx.x / n_cb / n_jb;
+  const uint32_t n_jb = (uint32_t)(rp + 63) / 64u;
+  const int which = blockIdx.x >= o.job[0].blocks;
+  const OuterJob& q = o.job[which];
+  const uint32_t b0 = blockIdx.x - (which ? o.job[0].blocks : 0u);
+  const int cols = q.cols;
+  const uint32_t n_cb = (uint32_t)(cols + 64 * kOuterWaves - 1) / (64u * kOuterWaves);
+  const int cb = (int)(b0 % n_cb), jb = (int)(b0 / n_cb % n_jb);
+  const uint32_t slot = b0 / n_cb / n_jb;
   const int s = find_seq(a.off, a.n_req, kOuterRows, slot);
   const Rows R = rows_of(a, s);
-  const int64_t first = R.r0 + (slot - (R.r0 / kOuterRows + s)) * kOuterRows;
-  if (first < R.r0 || first >= R.r1 || adapter_of(a, s) < 0) return;
+  const int64_t first =
+      R.r0 + ((int64_t)slot - ((uint32_t)R.r0 / kOuterRows + (uint32_t)s)) * kOuterRows;
+  const int ad = first >= R.r0 && first < R.r1 ? adapter_of(a, s) : -1;
+  if (cb == 0 && jb == 0 && threadIdx.x == 0) o.slot_adapter[which * o.slots + slot] = ad;
+  if (ad < 0) return;
   const int64_t end = R.r1 < first + kOuterRows ? R.r1 : first + kOuterRows;
 
   const int c0 = cb * 64 * kOuterWaves + wave * 64;
@@ -520,34 +555,38 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   const TileReads<64> rd(lane);
   const int lr = lane >> 3;  // row of a wave load, 8 rows of 8 chunks
-#pragma unroll 1
-  for (int64_t t = first; t < end; t += 64) {
-    sync_lds();
-    // rows past the end are zero in both tiles; columns past the last repeat it, and their sums are
-    // not stored
+  // rows past the end are zero in both tiles; columns past the last repeat it, and their sums are
+  // not stored
+  auto issue = [&](int buf, int64_t t) {
+    const uint32_t st = LDS_ADDRESS(smem) + buf * kStage;
+    const int n = end - t < 64 ? (int)(end - t) : 64;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int r = 8 * j + lr;
-      const int c = (lane & 7) ^ swz<64>(r);
-      const bool in = t + r < end;
-      int cc = c0 + 8 * c;
+      int cc = c0 + 8 * ((lane & 7) ^ swz<64>(r));
       if (cc >= cols) cc = cols - 8;
-      const void* p = in ? (const void*)(M + (t + r) * cols + cc) : (const void*)kZero16;
-      load_lds16(p, LDS_ADDRESS(smem) + (1 + wave) * kTile + j * 1024);
+      load_lds16(r < n ? (const void*)(q.m + (t + r) * cols + cc) : (const void*)kZero16,
+                 st + (1 + wave) * kTile + j * 1024);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int r = 8 * (2 * wave + j) + lr;
-      const int c = (lane & 7) ^ swz<64>(r);
-      const bool in = t + r < end;
-      int cc = j0 + 8 * c;
+      int cc = j0 + 8 * ((lane & 7) ^ swz<64>(r));
       if (cc >= rp) cc = rp - 8;
-      const void* p = in ? (const void*)(L + (t + r) * rp + cc) : (const void*)kZero16;
-      load_lds16(p, LDS_ADDRESS(smem) + (2 * wave + j) * 1024);
+      load_lds16(r < n ? (const void*)(q.l + (t + r) * rp + cc) : (const void*)kZero16,
+                 st + (2 * wave + j) * 1024);
     }
+  };
+  issue(0, first);
+  int buf = 0;
+#pragma unroll 1
+  for (int64_t t = first; t < end; t += 64, buf ^= 1) {
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-    sync_lds();
-    const unsigned char* ms = smem + (1 + wave) * kTile;
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    sync_lds();  // the stage has landed, and nobody reads the other any more
+    if (t + 64 < end) issue(buf ^ 1, t + 64);
+    const unsigned char* ls = smem + buf * kStage;
+    const unsigned char* ms = ls + (1 + wave) * kTile;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -556,7 +595,7 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           fm[i] = rd.tr_frag(ms, b, st, i);
-          fl[i] = rd.tr_frag(smem, b, st, i);
+          fl[i] = rd.tr_frag(ls, b, st, i);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -567,8 +606,8 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int jj = j0 + 32 * j + col;
-    if (jj >= rp) continue;
-    float* dst = part + (slot * rp + jj) * (int64_t)cols;
+    if (jj >= a.r) continue;
+    float* dst = q.part + ((int64_t)slot * rp + jj) * cols;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -581,28 +620,49 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
   }
 }
 
-// out[ad] = the sum of its requests' parts, in their order.  A thread per (j, c).
+// out[ad] = the sum of its slots' parts, in their order.  A thread per rank and 4 columns; a wave
+// looks for the adapter's slots 64 at a time and loads 8 of them together.
 template <class T>
-__global__ __launch_bounds__(256) void outer_join_kernel(AdapterArgs a, int cols, int transposed,
-                                                         const float* part, uint16_t* out) {
-  const int ad = blockIdx.y;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int j = (int)(i / cols), c = (int)(i - (int64_t)j * cols);
-  if (j >= a.r) return;
-  const int rp = (a.r + 15) / 16 * 16;
-  float sum = 0.f;
-  for (int s = 0; s < a.n_req; ++s) {
-    if (adapter_of(a, s) != ad) continue;
-    const Rows R = rows_of(a, s);
-    const int64_t slot0 = R.r0 / kOuterRows + s;
-    const int64_t n = (R.r1 - R.r0 + kOuterRows - 1) / kOuterRows;
-    for (int64_t k = 0; k < n; ++k) sum += part[((slot0 + k) * rp + j) * (int64_t)cols + c];
+__global__ __launch_bounds__(256) void outer_join_kernel(AdapterArgs a, OuterArgs o) {
+  const int which = blockIdx.x >= o.job[0].join_blocks;
+  const OuterJob& q = o.job[which];
+  const uint32_t b = blockIdx.x - (which ? o.job[0].join_blocks : 0u);
+  const int ad = blockIdx.y, cols = q.cols;
+  const uint32_t i = b * 256 + threadIdx.x;
+  const uint32_t per = (uint32_t)cols / 4u;
+  const int j = (int)(i / per), c = 4 * (int)(i % per);
+  const bool live = j < a.r;
+  const int rp = (a.r + 15) / 16 * 16, lane = threadIdx.x & 63;
+  const float* src = q.part + (int64_t)(live ? j : 0) * cols + c;
+  const int32_t* slots = o.slot_adapter + which * o.slots;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (uint32_t base = 0; base < o.slots; base += 64) {
+    unsigned long long mine = __ballot(base + lane < o.slots && slots[base + lane] == ad);
+    while (mine) {
+      f32x4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (mine) {
+          const uint32_t s = base + __builtin_ctzll(mine);
+          v[k] = *reinterpret_cast<const f32x4*>(src + (int64_t)s * rp * cols);
+          mine &= mine - 1;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum += v[k];
+    }
   }
-  const uint16_t v = (uint16_t)T::pack(sum, 0.f);
-  if (transposed)
-    out[((int64_t)ad * cols + c) * a.r + j] = v;
-  else
-    out[((int64_t)ad * a.r + j) * cols + c] = v;
+  if (!live) return;
+  uint16_t* out = q.out;
+  if (q.transposed) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      out[((int64_t)ad * cols + c + e) * a.r + j] = (uint16_t)T::pack(sum[e], 0.f);
+  } else {
+    *reinterpret_cast<uint2*>(out + ((int64_t)ad * a.r + j) * cols + c) =
+        uint2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
+  }
 }
 
 // The dynamic LDS of a kernel beyond the default limit.
@@ -635,7 +695,7 @@ hipError_t shrink(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
 template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
 hipError_t expand_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipStream_t s) {
   const int n_m = (a.m + BM - 1) / BM;
-  const int64_t grid = (a.n + BT - 1) / BT * n_m;
+  const int64_t grid = (a.n - a.row0 + BT - 1) / BT * n_m;
   constexpr int lds = NST * (BT + BM) * 128;
   const hipError_t e = allow_lds((const void*)expand_kernel<T, BT, BM, WT, WM, NST, MINB>, lds);
   if (e != hipSuccess) return e;
@@ -647,10 +707,13 @@ hipError_t expand_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipSt
 // Rows up to which the whole call is one pass over W, and the fewest tiles of the two large sizes.
 constexpr int kFewRows = 64;
 constexpr int kWideFrom = 192, kMidFrom = 256;
+// Tiles of a last round of the large size that are left to the next size: at 4096 -> 4096, 13,057 rows
+// are 3.2 rounds of 256 tiles, which took as long as four.
+constexpr int kLastRound = 160;
 
 template <class T>
-hipError_t expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipStream_t s) {
-  auto tiles = [&](int b) { return (a.n + b - 1) / b * ((a.m + b - 1) / b); };
+hipError_t expand(AdapterArgs a, const uint16_t* h, uint16_t* y, hipStream_t s) {
+  auto tiles = [&](int b) { return (a.n - a.row0 + b - 1) / b * ((a.m + b - 1) / b); };
   if (a.n <= kFewRows) {
     const int n_m = (a.m + 31) / 32;
     constexpr int lds = kFewWaves * WaveProduct<T, 1>::kBytes;
@@ -660,31 +723,49 @@ hipError_t expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipStrea
                        dim3(64 * kFewWaves), lds, s, a, h, y, n_m);
     return hipGetLastError();
   }
-  if (tiles(256) >= kWideFrom) return expand_as<T, 256, 256, 4, 2, 2, 1>(a, h, y, s);
-  if (tiles(128) >= kMidFrom) return expand_as<T, 128, 128, 2, 2, 2, 2>(a, h, y, s);
+  if (tiles(256) >= kWideFrom) {
+    const int64_t n_m = (a.m + 255) / 256, rest = tiles(256) % 256;
+    const int64_t rows = (tiles(256) - rest) / n_m * 256;  // of the whole rounds
+    AdapterArgs w = a;
+    if (rest > 0 && rest <= kLastRound && rows > 0) w.n = rows;
+    const hipError_t e = expand_as<T, 256, 256, 4, 2, 2, 1>(w, h, y, s);
+    if (e != hipSuccess || w.n == a.n) return e;
+    a.row0 = rows;
+  }
+  if (tiles(128) >= kMidFrom || a.row0 > 0) return expand_as<T, 128, 128, 4, 2, 4, 1>(a, h, y, s);
   return expand_as<T, 64, 64, 2, 2, 4, 2>(a, h, y, s);
 }
 
 template <class T>
-hipError_t outer(const AdapterArgs& a, const uint16_t* L, const uint16_t* M, int cols, bool transposed,
-                 float* part, uint16_t* out, hipStream_t s) {
-  const int rp = adapter_rank_pad(a.r);
-  const int n_cb = (cols + 64 * kOuterWaves - 1) / (64 * kOuterWaves), n_jb = (rp + 63) / 64;
-  const int64_t grid = adapter_outer_parts(a.n, a.n_req) * n_cb * n_jb;
-  if (grid > 0)
-    hipLaunchKernelGGL((outer_kernel<T>), dim3((unsigned)grid), dim3(64 * kOuterWaves), 0, s, a, L, M,
-                       cols, n_cb, part);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t each = ((int64_t)a.r * cols + 255) / 256;
-  hipLaunchKernelGGL((outer_join_kernel<T>), dim3((unsigned)each, (unsigned)a.n_ad), dim3(256), 0, s, a,
-                     cols, transposed ? 1 : 0, part, out);
+hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
+  const int rp = adapter_rank_pad(a.r), n_jb = (rp + 63) / 64;
+  o.slots = (uint32_t)adapter_outer_slots(a.n, a.n_req);
+  uint32_t blocks = 0, join_blocks = 0;
+  for (OuterJob& q : o.job) {
+    q.blocks = q.join_blocks = 0;
+    if (!q.out) continue;
+    q.blocks = o.slots * (uint32_t)((q.cols + 64 * kOuterWaves - 1) / (64 * kOuterWaves)) * n_jb;
+    q.join_blocks = (uint32_t)(((int64_t)a.r * (q.cols / 4) + 255) / 256);
+    blocks += q.blocks;
+    join_blocks += q.join_blocks;
+  }
+  if (join_blocks == 0) return hipSuccess;
+  hipError_t e = hipSuccess;
+  if (blocks > 0) {
+    constexpr int lds = 2 * (1 + kOuterWaves) * 64 * 128;
+    e = allow_lds((const void*)outer_kernel<T>, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((outer_kernel<T>), dim3(blocks), dim3(64 * kOuterWaves), lds, s, a, o);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((outer_join_kernel<T>), dim3(join_blocks, (unsigned)a.n_ad), dim3(256), 0, s, a, o);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t adapter_outer_parts(int64_t n, int n_req) { return n / kOuterRows + n_req; }
+int64_t adapter_outer_slots(int64_t n, int n_req) { return n_req == 0 ? 0 : n / kOuterRows + n_req; }
 
 hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t stream) {
   if (a.n == 0 || a.n_req == 0) return hipSuccess;
@@ -697,20 +778,20 @@ hipError_t launch_adapter_expand(const AdapterArgs& a, const uint16_t* h, uint16
   return a.f16 ? expand<HalfF16>(a, h, y, stream) : expand<HalfBf16>(a, h, y, stream);
 }
 
-hipError_t launch_transpose(const uint16_t* in, uint16_t* out, int64_t count, int rows, int cols,
-                            hipStream_t stream) {
-  if (count == 0) return hipSuccess;
-  hipLaunchKernelGGL(transpose_kernel,
-                     dim3((unsigned)((cols + 63) / 64), (unsigned)((rows + 63) / 64), (unsigned)count),
-                     dim3(256), 0, stream, in, out, rows, cols);
+hipError_t launch_transpose(TransposeArgs a, hipStream_t stream) {
+  int64_t blocks = 0;
+  for (TransposeJob& q : a.job) {
+    q.blocks = (uint32_t)(q.count * ((q.rows + 63) / 64) * ((q.cols + 63) / 64));
+    blocks += q.blocks;
+  }
+  if (blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
-hipError_t launch_adapter_outer(const AdapterArgs& a, const uint16_t* L, const uint16_t* M, int cols,
-                                bool transposed, float* part, uint16_t* out, hipStream_t stream) {
+hipError_t launch_adapter_outer(const AdapterArgs& a, const OuterArgs& o, hipStream_t stream) {
   if (a.n_ad == 0) return hipSuccess;
-  return a.f16 ? outer<HalfF16>(a, L, M, cols, transposed, part, out, stream)
-               : outer<HalfBf16>(a, L, M, cols, transposed, part, out, stream);
+  return a.f16 ? outer<HalfF16>(a, o, stream) : outer<HalfBf16>(a, o, stream);
 }
 
 }  // namespace hpr

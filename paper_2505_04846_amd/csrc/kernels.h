@@ -307,6 +307,7 @@ struct AdapterArgs {
   int64_t n;
   int k, m, r, n_ad, n_req;
   bool f16;
+  int64_t row0 = 0;               // first row of launch_adapter_expand's y
 };
 constexpr int kMaxRank = 128;
 inline int adapter_rank_pad(int r) { return (r + 15) / 16 * 16; }
@@ -315,15 +316,38 @@ hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t 
 // y[n, m] = x W^T + h B_a^T
 hipError_t launch_adapter_expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y,
                                  hipStream_t stream);
-// out[i] = in[i]^T for count matrices [rows, cols]
-hipError_t launch_transpose(const uint16_t* in, uint16_t* out, int64_t count, int rows, int cols,
-                            hipStream_t stream);
-// Sums over the rows of each adapter's requests, L[n, rank_pad] and M[n, cols]:
-//   out[a][j][c] = sum L[t, j] M[t, c], j < r (transposed: out[a][c][j])
-// through parts of adapter_outer_parts(n, n_req) * rank_pad * cols floats.
-int64_t adapter_outer_parts(int64_t n, int n_req);
-hipError_t launch_adapter_outer(const AdapterArgs& a, const uint16_t* L, const uint16_t* M, int cols,
-                                bool transposed, float* part, uint16_t* out, hipStream_t stream);
+// out[i] = in[i]^T of `count` matrices [rows, cols], three batches in one launch (the launcher fills
+// `blocks`; count 0: none).
+struct TransposeJob {
+  const uint16_t* in;
+  uint16_t* out;
+  int64_t count;
+  int rows, cols;
+  uint32_t blocks;
+};
+struct TransposeArgs {
+  TransposeJob job[3];
+};
+hipError_t launch_transpose(TransposeArgs a, hipStream_t stream);
+// Sums over the rows of each adapter's requests, l[n, rank_pad] and m[n, cols], up to two at a time:
+//   out[a][j][c] = sum l[t, j] m[t, c], j < r (transposed: out[a][c][j]; out null: none)
+// through parts of adapter_outer_slots(n, n_req) * rank_pad * cols floats and slot_adapter, 2 *
+// adapter_outer_slots(n, n_req) words.  The launcher fills slots, blocks and join_blocks.
+struct OuterJob {
+  const uint16_t *l, *m;
+  int cols;
+  int transposed;
+  float* part;
+  uint16_t* out;
+  uint32_t blocks, join_blocks;
+};
+struct OuterArgs {
+  OuterJob job[2];
+  int32_t* slot_adapter;
+  uint32_t slots;
+};
+int64_t adapter_outer_slots(int64_t n, int n_req);
+hipError_t launch_adapter_outer(const AdapterArgs& a, const OuterArgs& o, hipStream_t stream);
 
 // Calibration (calibration.hip): a pure-MFMA kernel of mfma_calibration_waves(n_cu) waves, each
 // running `iters` iterations of four v_mfma_f32_32x32x16_bf16 (sink: at least one float per
