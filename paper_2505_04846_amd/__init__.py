@@ -468,8 +468,14 @@ class _AttentionDesc(ctypes.Structure):
 
 
 def _need_heads(t, name, dtype, device):
-    """[rows, heads, dim] with contiguous values and 16-byte aligned rows and heads (views of a
-    projection's output are fine)."""
+    """Row and head strides of t [rows, heads, dim], with contiguous values and 16-byte aligned rows
+    and heads (views of a projection's output are fine).  A dimension of one row or head is never
+    stepped over: its stride counts as 0."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 3 and t.is_cuda
+            and t.device == device):
+        row, head, one = t.stride()
+        if one == 1 and not (row | head) & 7 and not t.data_ptr() & 15 and dtype in _HALF_TYPES:
+            return row, head
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype or dtype not in _HALF_TYPES:
@@ -480,21 +486,20 @@ def _need_heads(t, name, dtype, device):
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.numel() and (t.stride(2) != 1 or any(x % 8 for x in _strides(t)) or t.data_ptr() % 16):
+    row = t.stride(0) if t.shape[0] > 1 else 0
+    head = t.stride(1) if t.shape[1] > 1 else 0
+    if t.numel() and ((t.stride(2) != 1 and t.shape[2] > 1) or row % 8 or head % 8
+                      or t.data_ptr() % 16):
         raise ValueError(f"{name} must have contiguous values, and rows and heads aligned to 16 bytes")
-
-
-def _strides(t):
-    # (a dimension of one row or head may carry any stride; it is never stepped over)
-    return (t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+    return (row, head) if t.numel() else (0, 0)
 
 
 def _attention_desc(q, k, v, q_off, k_off, k_len, causal, window, scale):
     dtype = getattr(q, "dtype", None)
     dev = getattr(q, "device", None)
-    _need_heads(q, "q", dtype, dev)
-    _need_heads(k, "k", dtype, dev)
-    _need_heads(v, "v", dtype, dev)
+    q_row, q_head = _need_heads(q, "q", dtype, dev)
+    k_row, k_head = _need_heads(k, "k", dtype, dev)
+    v_row, v_head = _need_heads(v, "v", dtype, dev)
     if k.shape != v.shape:
         raise ValueError(f"k and v differ in shape: {tuple(k.shape)}, {tuple(v.shape)}")
     n_q, heads, dim = q.shape
@@ -518,8 +523,8 @@ def _attention_desc(q, k, v, q_off, k_off, k_len, causal, window, scale):
         if k_len.numel() != n_seq:
             raise ValueError("k_len must hold one length per sequence")
     scale = dim ** -0.5 if scale is None and dim else scale
-    d = _AttentionDesc(n_q, n_k, *_strides(q), *_strides(k), *_strides(v), n_seq, heads, kv_heads, dim,
-                       _HALF_TYPES[dtype], bool(causal), int(window), float(scale or 0.0))
+    d = _AttentionDesc(n_q, n_k, q_row, q_head, k_row, k_head, v_row, v_head, n_seq, heads, kv_heads,
+                       dim, _HALF_TYPES[dtype], bool(causal), int(window), float(scale or 0.0))
     return dev, d, k_off
 
 
@@ -700,13 +705,13 @@ def rotary_apply(q, k, pos, cos, sin, inverse=False):
     """
     dtype = getattr(q, "dtype", None)
     dev = getattr(q, "device", None)
-    _need_heads(q, "q", dtype, dev)
+    q_row, q_head = _need_heads(q, "q", dtype, dev)
     n, heads, dim = q.shape
-    kv_heads = 0
+    k_row = k_head = kv_heads = 0
     if k is not None:
-        _need_heads(k, "k", dtype, dev)
-        kv_heads = k.shape[1]
-        if k.shape[0] != n or k.shape[2] != dim:
+        k_row, k_head = _need_heads(k, "k", dtype, dev)
+        rows, kv_heads, k_dim = k.shape
+        if rows != n or k_dim != dim:
             raise ValueError(f"k must be [{n}, kv_heads, {dim}], got {tuple(k.shape)}")
     _need(pos, "pos", torch.int32, 1, dev)
     if pos.numel() != n:
@@ -717,10 +722,10 @@ def rotary_apply(q, k, pos, cos, sin, inverse=False):
         raise ValueError("cos and sin differ in shape")
     q_out = torch.empty((n, heads, dim), dtype=dtype, device=dev)
     k_out = torch.empty((n, kv_heads, dim), dtype=dtype, device=dev) if k is not None else None
-    _launch(lib().rotary_apply, dev, _ptr(q), *_strides(q), heads, _ptr(k),
-            *(_strides(k) if k is not None else (0, 0)), kv_heads, n, dim, 2 * cos.shape[1], _ptr(pos),
-            _ptr(cos), _ptr(sin), cos.shape[0], bool(inverse), _HALF_TYPES[dtype], _ptr(q_out),
-            _ptr(k_out))
+    n_pos, half = cos.shape
+    _launch(lib().rotary_apply, dev, q.data_ptr(), q_row, q_head, heads, _ptr(k), k_row, k_head, kv_heads,
+            n, dim, 2 * half, pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), n_pos, bool(inverse),
+            _HALF_TYPES[dtype], q_out.data_ptr(), _ptr(k_out))
     return q_out, k_out
 
 

@@ -795,7 +795,7 @@ hpr_status rotary_apply(const uint16_t* q, int64_t q_row, int64_t q_head, int32_
     return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
   const RotaryArgs a = {{q, k}, {q_out, k_out}, {q_row, k_row}, {q_head, k_head}, {q_heads, k_heads},
                         pos, cos_table, sin_table, n, n_pos, dim, rot, inverse != 0,
-                        dtype == HPR_F16};
+                        dtype == HPR_F16, 0};
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = timed("rotary", s, [&] { return launch_rotary(a, s); });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "rotary launch");

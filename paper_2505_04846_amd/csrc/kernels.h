@@ -295,8 +295,9 @@ struct RotaryArgs {
   int64_t n, n_pos;
   int dim, rot;
   bool inverse, f16;
+  int64_t first;  // the launcher's
 };
-hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
 
 // Shared projection with low-rank adapters (adapters.hip).
 struct AdapterArgs {
