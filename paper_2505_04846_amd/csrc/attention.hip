@@ -661,7 +661,7 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
   const int w_first = first_tok(wk0), w_end = end_tok(wk1);            // any of the wave's keys
   const int w_first_all = first_tok(wk1), w_end_all = end_tok(wk0);    // all of them
 
-  const TileReads<D> rd(lane);
+  const TileReads<D> rd0(lane);
   const TileLoad<D, kSlots, NW> ld(wave, lane, a.dim / 8);
   const int used = ts * a.G;  // slots of a stage
   int tok_of[ld.kLoads], q_at[ld.kLoads], g_at[ld.kLoads];
@@ -709,7 +709,7 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
                       own_at, lane, a.dim / 8);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    WaveRows<D>::cols(rd, own, a.dim, half, k);
+    WaveRows<D>::cols(rd0, own, a.dim, half, k);
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     WaveRows<D>::load(rsrc_of(a.v + (S.k0 + wk0) * a.v_row + kvh * a.v_head),
@@ -743,6 +743,7 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
     // every slot of the stage holds a token that sees every key of the wave
     const bool partial = used < kSlots || t + ts > S.lq || t < w_first_all || t + ts > w_end_all ||
                          wk0 + 31 >= S.lk;
+    const TileReads<D> rd = rd0.fresh();
     f32x16 x, dp;
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = 0.f, dp[r] = 0.f;
@@ -751,6 +752,15 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
       x = T::mfma(rd.row_frag(qs, 0, s), k[s], x);
       dp = T::mfma(rd.row_frag(gs, 0, s), rd.row_frag(own, 0, s), dp);
     }
+    // the operands' reads run ahead of the products
+    sched_ds(6);
+#pragma unroll
+    for (int s = 0; s < kS - 2; ++s) {
+      sched_mfma(2);
+      sched_ds(3);
+    }
+    sched_mfma(4);
+    __builtin_amdgcn_sched_barrier(0);
     u32x4 p16[2], ds[2];
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {
@@ -789,6 +799,14 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
         dv[db] = T::mfma(rd.tr_frag(gs, 0, s, db), p16[s], dv[db]);
         dk[db] = T::mfma(rd.tr_frag(qs, 0, s, db), ds[s], dk[db]);
       }
+    sched_ds(8);
+#pragma unroll
+    for (int i = 0; i < 2 * kDb - 2; ++i) {
+      sched_mfma(2);
+      sched_ds(4);
+    }
+    sched_mfma(4);
+    __builtin_amdgcn_sched_barrier(0);
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
   // (keys that the sequence does not count have no sums)
@@ -809,7 +827,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(AttnArgs a) {
   attn_dq<T, D, NW>(a);
 }
 template <class T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_dkv_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * NW, D >= 128 ? 2 : 3) void attn_dkv_kernel(AttnArgs a) {
   attn_dkv<T, D, NW>(a);
 }
 

@@ -23,7 +23,7 @@ struct TileReads {
   int chunk0;            // 16 * (half ^ swz)
   int tr0;               // row of tr_frag, byte offset
   int trc;               // its chunk for d block 0, as byte offset, and the byte in the chunk
-  __device__ __forceinline__ TileReads(int lane) {
+  __device__ __forceinline__ explicit TileReads(int lane) {
     const int r = lane & 31, half = lane >> 5;
     row0 = r * D * 2;
     chunk0 = (half ^ swz<D>(r)) << 4;
@@ -31,6 +31,13 @@ struct TileReads {
     const int tr = 4 * half + e;
     tr0 = tr * D * 2;
     trc = (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ swz<D>(tr)) << 4) | ((i & 1) << 3);
+  }
+  // A copy whose addresses are formed where they are used.  Loop-invariant, a tile's 16 addresses would be
+  // kept in registers, which kernels at their limit need to read operands ahead of the products.
+  __device__ __forceinline__ TileReads fresh() const {
+    TileReads r = *this;
+    asm volatile("" : "+v"(r.chunk0), "+v"(r.trc));
+    return r;
   }
   // Rows [32 blk, 32 blk + 32), values [16 s, 16 s + 16): the left operand of a product over d.
   __device__ __forceinline__ u32x4 row_frag(const unsigned char* tile, int blk, int s) const {
