@@ -704,7 +704,7 @@ hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uin
 size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_t r, int32_t n_ad,
                                          int32_t n_req) {
   if (n < 0 || k < 1 || m < 1 || r < 1 || n_ad < 0 || n_req < 0) return 0;
-  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req);
+  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, k, m);
   return align_up((size_t)m * k * 2) + align_up((size_t)n_ad * r * k * 2) +
          align_up((size_t)n_ad * r * m * 2) + align_up((size_t)n * rp * 2) +
          align_up(slots * rp * k * sizeof(float)) + align_up(slots * rp * m * sizeof(float)) +
@@ -726,7 +726,7 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   if (!ws || ws_bytes < need)
     return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req);
+  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, k, m);
   Carver c(ws);
   uint16_t* wt = c.take<uint16_t>((size_t)m * k * 2);
   uint16_t* at = c.take<uint16_t>((size_t)n_ad * r * k * 2);
@@ -761,7 +761,7 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   if (da || db)
     e = timed("adapter_outer", s, [&] {
       const OuterArgs o = {{{g, x, k, 0, part_a, da, 0, 0}, {h, dy, m, 1, part_b, db, 0, 0}},
-                           slot_adapter, 0};
+                           slot_adapter, 0, 0};
       return launch_adapter_outer(f, o, s);
     });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "adapter gradient launch");

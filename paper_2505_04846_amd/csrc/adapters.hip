@@ -38,26 +38,27 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int s) {
 
 // ---- a wave's own product ----------------------------------------------------------------------
 
-// acc[b] = rows [32 b, 32 b + 32) of P times 32 rows of X, over stages [kk0, kk1) of 64 values, by one wave:
+// acc[b][c] = rows [32 b, 32 b + 32) of P times rows [32 c, + 32) of X, over stages [kk0, kk1) of 64 values,
+// by one wave:
 // its two LDS stages are its own, so waves that split k run without a barrier.  Whole 128-byte lines go
 // straight to LDS (operands read from memory by lanes touch twice as many lines a load: a token's
 // projection took 22 us that way).
-template <class T, int NB>
+template <class T, int NB, int XB>
 struct WaveProduct {
-  static constexpr int kStage = (1 + NB) * 4096;
+  static constexpr int kStage = (XB + NB) * 4096;
   static constexpr int kBytes = 2 * kStage;
-  static constexpr int kLoads = 4 * (1 + NB);
+  static constexpr int kX = 4 * XB, kLoads = 4 * (XB + NB);
   // x, p: first rows; x_last, p_last: their last valid row, which the rows past it repeat
   static __device__ __forceinline__ void run(const uint16_t* x, int x_last, const uint16_t* p, int p_last,
                                              int k, int kk0, int kk1, unsigned char* lds, int lane,
-                                             f32x16 (&acc)[NB]) {
+                                             f32x16 (&acc)[NB][XB]) {
     const __amdgpu_buffer_rsrc_t rx = tile_rsrc(x), rp = tile_rsrc(p);
     const TileReads<64> rd(lane);
     int off[kLoads], chunk[kLoads];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int r = 8 * (j < 4 ? j : j - 4) + (lane >> 3);
-      const int last = j < 4 ? x_last : p_last;
+      const int r = 8 * (j < kX ? j : j - kX) + (lane >> 3);
+      const int last = j < kX ? x_last : p_last;
       chunk[j] = ((lane & 7) ^ swz<64>(r)) * 8;
       off[j] = (r < last ? r : last) * k * 2 + chunk[j] * 2;
     }
@@ -67,12 +68,12 @@ struct WaveProduct {
       if (kk < whole) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(j < 4 ? rx : rp, (lds_void_t*)(st + j * 1024), 16,
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kX ? rx : rp, (lds_void_t*)(st + j * 1024), 16,
                                                    off[j], kk * 128, 0, 0);
       } else {  // the end of k: chunks past it read zeros
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-          const char* src = (const char*)(j < 4 ? x : p) + off[j] + kk * 128;
+          const char* src = (const char*)(j < kX ? x : p) + off[j] + kk * 128;
           const void* from = kk * 64 + chunk[j] < k ? (const void*)src : (const void*)kZero16;
           __builtin_amdgcn_global_load_lds((glb_void_t*)from, (lds_void_t*)(st + j * 1024), 16, 0, 0);
         }
@@ -81,7 +82,9 @@ struct WaveProduct {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+      for (int c = 0; c < XB; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
     if (kk0 < kk1) issue(0, kk0);
 #pragma unroll 1
     for (int kk = kk0; kk < kk1; ++kk) {
@@ -98,9 +101,15 @@ struct WaveProduct {
       const unsigned char* st = lds + buf * kStage;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const u32x4 fx = rd.row_frag(st, 0, s);
+        u32x4 fx[XB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = T::mfma(rd.row_frag(st + 4096, b, s), fx, acc[b]);
+        for (int c = 0; c < XB; ++c) fx[c] = rd.row_frag(st, c, s);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const u32x4 fp = rd.row_frag(st + XB * 4096, b, s);
+#pragma unroll
+          for (int c = 0; c < XB; ++c) acc[b][c] = T::mfma(fp, fx[c], acc[b][c]);
+        }
       }
     }
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
@@ -110,60 +119,62 @@ struct WaveProduct {
 
 // ---- h ----------------------------------------------------------------------------------------
 
-// h of 32 rows of one request.  W waves split k, each summing its part of the whole [rank, 32]
+// h of 32 XB rows of one request.  W waves split k, each summing its part of the whole [rank, 32 XB]
 // block (rank on the rows of the product, so that a lane holds 4 consecutive values of its row's
 // h), and join in LDS.  h is rounded to 16 bits once, with its scale: the operand of the product
 // with B.  Its relative rounding reaches only the adapter's part of y.
-constexpr int kShrinkRows = 32;
-
-template <class T, int NB, int W>
+template <class T, int NB, int XB, int W>
 __device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h) {
-  using P = WaveProduct<T, NB>;
+  using P = WaveProduct<T, NB, XB>;
+  constexpr int kRows = 32 * XB;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // W * P::kBytes
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int s = find_seq(a.off, a.n_req, kShrinkRows, blockIdx.x);
+  const int s = find_seq(a.off, a.n_req, kRows, blockIdx.x);
   const Rows R = rows_of(a, s);
-  const int64_t first =
-      R.r0 + ((int64_t)blockIdx.x - ((uint32_t)R.r0 / kShrinkRows + (uint32_t)s)) * kShrinkRows;
+  const int64_t first = R.r0 + ((int64_t)blockIdx.x - ((uint32_t)R.r0 / kRows + (uint32_t)s)) * kRows;
   const int ad = adapter_of(a, s);
   if (first < R.r0 || first >= R.r1 || ad < 0) return;
-  const int last = R.r1 - first < kShrinkRows ? (int)(R.r1 - first) - 1 : kShrinkRows - 1;
+  const int last = R.r1 - first < kRows ? (int)(R.r1 - first) - 1 : kRows - 1;
   const int nk = (a.k + 63) / 64;
-  f32x16 acc[NB];
+  f32x16 acc[NB][XB];
   unsigned char* own = smem + wave * P::kBytes;
   P::run(a.x + first * a.k, last, a.a + (int64_t)ad * a.r * a.k, a.r - 1, a.k, nk * wave / W,
          nk * (wave + 1) / W, own, lane, acc);
-  float* part = reinterpret_cast<float*>(own);  // [NB * 16][64]
+  float* part = reinterpret_cast<float*>(own);  // [NB * XB * 16][64]
+  static_assert(NB * XB * 4096 <= P::kBytes, "the wave's sums fit its stages");
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) part[(16 * b + r) * 64 + lane] = acc[b][r];
+    for (int c = 0; c < XB; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) part[(16 * (b * XB + c) + r) * 64 + lane] = acc[b][c][r];
   __syncthreads();
   const int rp = (a.r + 15) / 16 * 16;
   const float sc = a.scale[ad];
-  // register groups of four: group g of NB * 4 holds ranks 32 (g / 4) + 8 (g % 4) + 4 half + 0..3
-  for (int g = wave; g < NB * 4; g += W) {
-    const int j = 32 * (g >> 2) + 8 * (g & 3) + 4 * half;
+  // register groups of four: group g of block (b, c) holds ranks 32 b + 8 g + 4 half + 0..3 of row
+  // 32 c + col
+  for (int i = wave; i < NB * XB * 4; i += W) {
+    const int bc = i >> 2, j = 32 * (bc / XB) + 8 * (i & 3) + 4 * half, t = 32 * (bc % XB) + col;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w)
-        v[e] += reinterpret_cast<const float*>(smem + w * P::kBytes)[(4 * g + e) * 64 + lane];
+        v[e] += reinterpret_cast<const float*>(smem + w * P::kBytes)[(4 * i + e) * 64 + lane];
       v[e] = j + e < a.r ? v[e] * sc : 0.f;
     }
-    if (col <= last && j < rp)
-      *reinterpret_cast<uint2*>(h + (first + col) * rp + j) =
+    if (t <= last && j < rp)
+      *reinterpret_cast<uint2*>(h + (first + t) * rp + j) =
           uint2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
   }
 }
 
 // (The bodies are device functions: the host pass knows no buffer resources.)
-template <class T, int NB, int W>
+template <class T, int NB, int XB, int W>
 __global__ __launch_bounds__(64 * W) void shrink_kernel(AdapterArgs a, uint16_t* h) {
-  shrink_tile<T, NB, W>(a, h);
+  shrink_tile<T, NB, XB, W>(a, h);
 }
 
 // ---- y ----------------------------------------------------------------------------------------
@@ -396,21 +407,21 @@ constexpr int kFewWaves = 8;
 
 template <class T>
 __device__ __forceinline__ void expand_few(const AdapterArgs& a, const uint16_t* h, uint16_t* y, int n_m) {
-  using P = WaveProduct<T, 1>;
+  using P = WaveProduct<T, 1, 1>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // kFewWaves * P::kBytes
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m0 = (int)(blockIdx.x % (uint32_t)n_m) * 32;
   const int64_t t0 = (int64_t)(blockIdx.x / (uint32_t)n_m) * 32;
   const int nk = (a.k + 63) / 64;
-  f32x16 acc[1];
+  f32x16 acc[1][1];
   unsigned char* own = smem + wave * P::kBytes;
   P::run(a.x + t0 * a.k, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31, a.w + (int64_t)m0 * a.k,
          a.m - m0 < 32 ? a.m - m0 - 1 : 31, a.k, nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own,
          lane, acc);
   float* part = reinterpret_cast<float*>(own);  // [16][64]
 #pragma unroll
-  for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][r];
+  for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];
   __syncthreads();
   // thread: row t0 + i / 16 of the tile, columns m0 + 2 (i % 16) and the next: entries e, e + 1 of
   // lane (row, half) with column = 8 (e / 4) + 4 half + e % 4
@@ -514,10 +525,10 @@ __global__ __launch_bounds__(256) void transpose_kernel(TransposeArgs a) {
 
 // ---- dA, dB -----------------------------------------------------------------------------------
 
-// Partial sums over up to kOuterRows rows of one request: part[slot][j][c] = sum_t L[t,j] M[t,c],
+// Partial sums over up to o.rows rows of one request: part[slot][j][c] = sum_t L[t,j] M[t,c],
 // 64 ranks and 256 columns per workgroup, 64 columns per wave; rows in tiles of 64 through two LDS
 // stages, both operands read by columns.  dA and dB go in one launch.
-constexpr int kOuterRows = 512, kOuterWaves = 4;
+constexpr int kOuterWaves = 4;
 
 template <class T>
 __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs a, OuterArgs o) {
@@ -535,14 +546,14 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
   const uint32_t n_cb = (uint32_t)(cols + 64 * kOuterWaves - 1) / (64u * kOuterWaves);
   const int cb = (int)(b0 % n_cb), jb = (int)(b0 / n_cb % n_jb);
   const uint32_t slot = b0 / n_cb / n_jb;
-  const int s = find_seq(a.off, a.n_req, kOuterRows, slot);
+  const int s = find_seq(a.off, a.n_req, o.rows, slot);
   const Rows R = rows_of(a, s);
   const int64_t first =
-      R.r0 + ((int64_t)slot - ((uint32_t)R.r0 / kOuterRows + (uint32_t)s)) * kOuterRows;
+      R.r0 + ((int64_t)slot - ((uint32_t)R.r0 / (uint32_t)o.rows + (uint32_t)s)) * o.rows;
   const int ad = first >= R.r0 && first < R.r1 ? adapter_of(a, s) : -1;
   if (cb == 0 && jb == 0 && threadIdx.x == 0) o.slot_adapter[which * o.slots + slot] = ad;
   if (ad < 0) return;
-  const int64_t end = R.r1 < first + kOuterRows ? R.r1 : first + kOuterRows;
+  const int64_t end = R.r1 < first + o.rows ? R.r1 : first + o.rows;
 
   const int c0 = cb * 64 * kOuterWaves + wave * 64;
   const int j0 = jb * 64;
@@ -670,26 +681,25 @@ hipError_t allow_lds(const void* fn, int lds) {
   return lds > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) : hipSuccess;
 }
 
-template <class T, int NB, int W>
+template <class T, int NB, int XB, int W>
 hipError_t shrink_as(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
-  constexpr int lds = W * WaveProduct<T, NB>::kBytes;
-  const hipError_t e = allow_lds((const void*)shrink_kernel<T, NB, W>, lds);
+  constexpr int lds = W * WaveProduct<T, NB, XB>::kBytes;
+  const hipError_t e = allow_lds((const void*)shrink_kernel<T, NB, XB, W>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((shrink_kernel<T, NB, W>), dim3((unsigned)(a.n / kShrinkRows + a.n_req)), dim3(64 * W),
-                     lds, s, a, h);
+  hipLaunchKernelGGL((shrink_kernel<T, NB, XB, W>), dim3((unsigned)(a.n / (32 * XB) + a.n_req)),
+                     dim3(64 * W), lds, s, a, h);
   return hipGetLastError();
 }
 
 // Waves per workgroup: as many as two workgroups per CU allow, or eight where one round of workgroups
-// does not fill the chip.
+// does not fill the chip.  Ranks above 32 read as much of A as of x per 32 rows and more: there 64 rows
+// share it, where they fill the chip.
 template <class T>
 hipError_t shrink(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
-  if (a.r <= 32) {
-    if (a.n / kShrinkRows + a.n_req <= 256) return shrink_as<T, 1, 8>(a, h, s);
-    return shrink_as<T, 1, 4>(a, h, s);
-  }
-  if (a.r <= 64) return shrink_as<T, 2, 3>(a, h, s);
-  return shrink_as<T, 4, 2>(a, h, s);
+  const int64_t tiles = a.n / 32 + a.n_req;
+  if (a.r <= 32) return tiles <= 256 ? shrink_as<T, 1, 1, 8>(a, h, s) : shrink_as<T, 1, 1, 4>(a, h, s);
+  if (a.r <= 64) return tiles <= 256 ? shrink_as<T, 2, 1, 6>(a, h, s) : shrink_as<T, 2, 2, 4>(a, h, s);
+  return shrink_as<T, 4, 1, 2>(a, h, s);
 }
 
 template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
@@ -716,7 +726,7 @@ hipError_t expand(AdapterArgs a, const uint16_t* h, uint16_t* y, hipStream_t s) 
   auto tiles = [&](int b) { return (a.n - a.row0 + b - 1) / b * ((a.m + b - 1) / b); };
   if (a.n <= kFewRows) {
     const int n_m = (a.m + 31) / 32;
-    constexpr int lds = kFewWaves * WaveProduct<T, 1>::kBytes;
+    constexpr int lds = kFewWaves * WaveProduct<T, 1, 1>::kBytes;
     const hipError_t e = allow_lds((const void*)expand_few_kernel<T>, lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((expand_few_kernel<T>), dim3((unsigned)((a.n + 31) / 32 * n_m)),
@@ -739,7 +749,8 @@ hipError_t expand(AdapterArgs a, const uint16_t* h, uint16_t* y, hipStream_t s) 
 template <class T>
 hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
   const int rp = adapter_rank_pad(a.r), n_jb = (rp + 63) / 64;
-  o.slots = (uint32_t)adapter_outer_slots(a.n, a.n_req);
+  o.rows = adapter_outer_rows(a.n, a.k, a.m);
+  o.slots = (uint32_t)adapter_outer_slots(a.n, a.n_req, a.k, a.m);
   uint32_t blocks = 0, join_blocks = 0;
   for (OuterJob& q : o.job) {
     q.blocks = q.join_blocks = 0;
@@ -765,7 +776,13 @@ hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
 
 }  // namespace
 
-int64_t adapter_outer_slots(int64_t n, int n_req) { return n_req == 0 ? 0 : n / kOuterRows + n_req; }
+// 1,024 rows a slot where that leaves most of a round of workgroups (two per CU), 512 otherwise: more
+// rows, fewer partial sums to write and join (13,057 rows of 4096 on both sides: 66 us of 512 rows).
+int adapter_outer_rows(int64_t n, int k, int m) { return (n / 1024) * ((k + m) / 256) >= 384 ? 1024 : 512; }
+
+int64_t adapter_outer_slots(int64_t n, int n_req, int k, int m) {
+  return n_req == 0 ? 0 : n / adapter_outer_rows(n, k, m) + n_req;
+}
 
 hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t stream) {
   if (a.n == 0 || a.n_req == 0) return hipSuccess;

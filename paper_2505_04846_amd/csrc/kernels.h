@@ -332,8 +332,8 @@ struct TransposeArgs {
 hipError_t launch_transpose(TransposeArgs a, hipStream_t stream);
 // Sums over the rows of each adapter's requests, l[n, rank_pad] and m[n, cols], up to two at a time:
 //   out[a][j][c] = sum l[t, j] m[t, c], j < r (transposed: out[a][c][j]; out null: none)
-// through parts of adapter_outer_slots(n, n_req) * rank_pad * cols floats and slot_adapter, 2 *
-// adapter_outer_slots(n, n_req) words.  The launcher fills slots, blocks and join_blocks.
+// through parts of slots * rank_pad * cols floats and slot_adapter, 2 * slots words, slots =
+// adapter_outer_slots.  The launcher fills rows, slots, blocks and join_blocks.
 struct OuterJob {
   const uint16_t *l, *m;
   int cols;
@@ -346,8 +346,10 @@ struct OuterArgs {
   OuterJob job[2];
   int32_t* slot_adapter;
   uint32_t slots;
+  int rows;
 };
-int64_t adapter_outer_slots(int64_t n, int n_req);
+int adapter_outer_rows(int64_t n, int k, int m);  // rows of a slot
+int64_t adapter_outer_slots(int64_t n, int n_req, int k, int m);
 hipError_t launch_adapter_outer(const AdapterArgs& a, const OuterArgs& o, hipStream_t stream);
 
 // Calibration (calibration.hip): a pure-MFMA kernel of mfma_calibration_waves(n_cu) waves, each

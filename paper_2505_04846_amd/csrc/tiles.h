@@ -85,6 +85,13 @@ __device__ __forceinline__ void load_lds16(rsrc_t r, uint32_t lds, uint32_t offs
                : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(r)
                : "memory");
 }
+// The same without a place in the caches, for what is read once.
+__device__ __forceinline__ void load_lds16_stream(rsrc_t r, uint32_t lds, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(r)
+               : "memory");
+}
 __device__ __forceinline__ void load_lds16(const void* src, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
