@@ -936,6 +936,9 @@ int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
   int64_t s = (full + wgs - 1) / wgs;
   const int64_t most = n_k / n_seq / 256 < 1 ? 1 : n_k / n_seq / 256;
   if (s > most) s = most;
+  // (the grid also has the tiles of empty sequences: no more than 2^22 workgroups for the splits' sake)
+  const int64_t grid = (n_q / ts + n_seq) * kv_heads;
+  if (s * grid > (int64_t(1) << 22)) s = (int64_t(1) << 22) / grid < 1 ? 1 : (int64_t(1) << 22) / grid;
   return (int)(s > kMaxSplits ? kMaxSplits : s);
 }
 
