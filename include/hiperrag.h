@@ -347,8 +347,8 @@ hpr_status hpr_scale_grads_bf16(const float* dq, int64_t n_q, uint16_t* dq_out, 
  *   out [n_q, heads, dim] dense; lse fp32 [n_q, heads] or NULL
  *   ws     workspace of packed_attention_workspace_size(d) bytes (may be 0)
  * Preconditions, like those above not checked on the device: both offsets start at 0, never fall
- * and end at n_q and n_k; every row that some query sees is finite.  Key rows past k_len[s] are not
- * read.
+ * and end at n_q and n_k; q, dout and every key row that some query sees are finite.  Key rows that no
+ * query sees (past k_len[s], or left behind by every window) may hold anything.
  * ------------------------------------------------------------------------------------------- */
 #define HPR_BF16 0
 #define HPR_F16 1

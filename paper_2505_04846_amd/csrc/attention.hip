@@ -119,18 +119,6 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, const AttnTile& s, in
   return r;
 }
 
-// The right operand's registers of one 32-row column block straight from memory: values
-// [16 s, 16 s + 16) of the lane's row, zero past dim.
-template <int D>
-__device__ __forceinline__ void load_cols(const uint16_t* row, int dim, int half, u32x4 (&f)[D / 16]) {
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    const int d = 16 * s + 8 * half;
-    f[s] = u32x4{0u, 0u, 0u, 0u};
-    if (d < dim) f[s] = load16(row + d);
-  }
-}
-
 // A wave's own 32 rows through its own 32 * D * 2 bytes of LDS, so that memory sees whole rows (by
 // lanes a row's pieces of 16 or 32 bytes would be requests of their own).
 template <int D>
@@ -209,7 +197,8 @@ struct SlotRows {
 };
 
 // A stage's loads: KEYS rows of K, then of V, straight into LDS.  The offsets of a whole tile are
-// kept per lane; the sequence's last tile forms its own.
+// kept per lane; the sequence's last tile forms its own, and so does the one where a window begins:
+// keys that no query sees may hold anything, and their probability of 0 would keep a NaN or an infinity.
 template <int D, int NW, int KEYS, bool STREAM = false>
 struct KvLoad {
   using L = TileLoad<D, KEYS, NW>;
@@ -233,14 +222,15 @@ struct KvLoad {
       load_lds16(r, lds, offset);
   }
   __device__ __forceinline__ void issue(const AttnArgs& a, const AttnTile& S, uint32_t st, int wave,
-                                        int kt) const {
+                                        int kt, int lo) const {
     const int first = kt * KEYS;
     const int last = S.lk - 1 - first;  // last valid row of the tile (>= 0)
+    const int low = lo - first;         // its first row that a query sees (<= last)
     const rsrc_t rk = rsrc_of(k + (int64_t)first * a.k_row);
     const rsrc_t rv = rsrc_of(v + (int64_t)first * a.v_row);
     const uint32_t to = st + wave * L::kLoads * 1024;  // LDS address
     constexpr int kTile = KEYS * D * 2;
-    if (last >= KEYS - 1) {
+    if (last >= KEYS - 1 && low <= 0) {
 #pragma unroll
       for (int j = 0; j < L::kLoads; ++j) load(rk, to + j * 1024, ok[j]);
 #pragma unroll
@@ -248,7 +238,7 @@ struct KvLoad {
     } else {
 #pragma unroll
       for (int j = 0; j < L::kLoads; ++j) {
-        const int r = at.row[j] < last ? at.row[j] : last;
+        const int up = at.row[j] > low ? at.row[j] : low, r = up < last ? up : last;
         load(rk, to + j * 1024, r * (int)a.k_row * 2 + at.chunk[j]);
         load(rv, to + kTile + j * 1024, r * (int)a.v_row * 2 + at.chunk[j]);
       }
@@ -265,7 +255,6 @@ __device__ __forceinline__ float prob(float x) {
 // Scheduling groups: the next n LDS reads / products of the region go here.
 #define sched_ds(n) __builtin_amdgcn_sched_group_barrier(0x100, n, 0)
 #define sched_mfma(n) __builtin_amdgcn_sched_group_barrier(0x008, n, 0)
-#define sched_valu(n) __builtin_amdgcn_sched_group_barrier(0x002, n, 0)
 
 // ---- forward --------------------------------------------------------------------------------
 
@@ -318,7 +307,9 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   const int kt1 = k_first + (int)((int64_t)n_kt * (split + 1) / a.splits);
 
   const KvLoad<D, NW, KEYS, NW == 1> ld(a, S, kvh, wave, lane);
-  auto issue = [&](int buf, int kt) { ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt); };
+  auto issue = [&](int buf, int kt) {
+    ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt, tfirst.lo);
+  };
   // q through the later stages, which the loop fills only after its first barrier
   static_assert(NW * WaveRows<D>::kBytes <= (NST - 1) * 2 * kTile, "the waves' rows fit there");
   unsigned char* own = smem + 2 * kTile + wave * WaveRows<D>::kBytes;
@@ -518,7 +509,9 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   const SlotRows dense(a, wave, n_slot, (int64_t)a.heads * a.dim, a.dim);
   const int64_t dense0 = ((S.q0 + t0) * a.heads + kvh * a.G) * a.dim;
   const KvLoad<D, NW, kKeys> ld(a, S, kvh, wave, lane);
-  auto issue = [&](int buf, int kt) { ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt); };
+  auto issue = [&](int buf, int kt) {
+    ld.issue(a, S, LDS_ADDRESS(smem) + buf * 2 * kTile, wave, kt, tfirst.lo);
+  };
   // q through the second stage, dout through the first, then out through the second
   constexpr int kOwn = WaveRows<D>::kBytes;
   static_assert(NW * kOwn <= 2 * kTile, "the wave's rows fit a stage");
@@ -780,7 +773,7 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int slot = 8 * (r >> 2) + (r & 3);
-        if (slot < lo || slot >= hi) x[r] = 0.f;
+        if (slot < lo || slot >= hi) x[r] = dp[r] = 0.f;  // (dp of a key that no query sees may be NaN)
       }
     }
 #pragma unroll

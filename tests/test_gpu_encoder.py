@@ -221,6 +221,38 @@ def test_attention_sequences_do_not_touch():
             assert torch.equal(b[name][s], cb[name][s])
 
 
+@pytest.mark.parametrize("ty", ["bf16", "f16"])
+@pytest.mark.parametrize("q_lens,k_lens,H,Hk,D,window", [
+    ([1] * 5, [2, 500, 333, 1, 77], 12, 12, 64, 50),     # a token each: few rows
+    ([40, 3], [300, 64], 4, 2, 72, 20),
+    ([130, 257], [401, 300], 8, 2, 128, 33),
+    ([9], [2600], 4, 2, 128, 700),                       # the keys split over workgroups
+    ([70], [5000], 2, 1, 64, 100),
+])
+def test_attention_keys_that_no_query_sees(ty, q_lens, k_lens, H, Hk, D, window):
+    """Rows that every query's window has left behind may hold anything."""
+    case = (q_lens, k_lens, None, H, Hk, D, ty, True, window)
+    q, k, v, q_off, k_off, _, how, dout = attention_case(case, seed=54)
+
+    def run():
+        r = hpr.packed_attention_fwd(q, k, v, q_off, **how)
+        b = hpr.packed_attention_bwd(dout, q, k, v, r["out"], r["lse"], q_off, **how)
+        return [r["out"], r["lse"], b["dq"], b["dk"], b["dv"]]
+
+    clean, gone, start = run(), [], 0
+    for lq, lk in zip(q_lens, k_lens):
+        gone += range(start, start + max(lk - lq - window + 1, 0))
+        start += lk
+    assert gone
+    k[gone], v[gone] = math.inf, math.nan
+    for x, y in zip(run(), clean):
+        assert torch.equal(x, y)
+    k[gone], v[gone] = math.nan, -math.inf
+    for x, y in zip(run(), clean):
+        assert torch.equal(x, y)
+    assert not clean[3][gone].any() and not clean[4][gone].any()
+
+
 def test_attention_bits_repeat_and_streams():
     case = ([300, 1, 77, 500], None, None, 8, 2, 128, "bf16", True, 0)
     q, k, v, q_off, _, _, how, dout = attention_case(case, seed=53)
