@@ -600,7 +600,7 @@ size_t packed_attention_workspace_size(const hpr_attention* d) {
   if (!d || d->n_q < 1 || d->n_seq < 1 || d->heads < 1 || d->kv_heads < 1 || d->dim < 1 ||
       d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
     return 0;
-  const int64_t splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
+  const int64_t splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads, d->dim);
   const size_t plan = align_up((size_t)attn_plan_tiles(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads) *
                                sizeof(AttnTile));
   if (splits <= 1) return plan;
@@ -633,7 +633,7 @@ hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const
     return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
   a.out = out;
   a.lse = lse;
-  a.splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
+  a.splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads, d->dim);
   Carver c(ws);
   const int64_t plan = attn_plan_tiles(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads);
   if (plan > 0) a.q_plan = c.take<AttnTile>((size_t)plan * sizeof(AttnTile));

@@ -449,6 +449,7 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
 // out = the splits' sums joined under their common maximum.  A wave per (token, head): lane s holds
 // split s's statistics, then lane i values 2 i and 2 i + 1.
 constexpr int kMaxSplits = 64;
+static_assert(kMaxSplits <= 64 && kMaxSplits % 4 == 0, "a lane per split, four splits a step");
 
 template <class T>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
@@ -459,17 +460,24 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   float2 ml = {kNoMax, 0.f};
   if (lane < a.splits) ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (lane * rows + row));
   const float m = wave_max(ml.x);
-  const float f = __builtin_amdgcn_exp2f(ml.x - m);
+  const float f = lane < a.splits ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
   const float l = wave_sum(f * ml.y);
   const int d = 2 * lane < a.dim ? 2 * lane : 0;
   const float* src = a.part_o + row * a.dim + d;
   float o0 = 0.f, o1 = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < a.splits; ++s) {
-    const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
-    const float2 v = *reinterpret_cast<const float2*>(src + s * rows * a.dim);
-    o0 += fs * v.x;
-    o1 += fs * v.y;
+  for (int s0 = 0; s0 < a.splits; s0 += 4) {  // four loads together, the last split again past the end
+    float2 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = s0 + i < a.splits ? s0 + i : a.splits - 1;
+      v[i] = *reinterpret_cast<const float2*>(src + s * rows * a.dim);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + i));
+      o0 += fs * v[i].x;
+      o1 += fs * v[i].y;
+    }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   if (2 * lane < a.dim)
@@ -914,25 +922,45 @@ hipError_t run_bwd(AttnArgs a, hipStream_t s) {
 
 }  // namespace
 
-// Splits of the key axis, where the tiles alone do not fill the chip: kFew up to 4,096 waves, others
-// up to eight workgroups per CU; no fewer than 256 keys of the mean sequence each.
-int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
+// Splits of the key axis, where the tiles alone do not fill the chip: none of fewer than 128 keys of the
+// mean sequence.
+//   kFew: up to four waves per CU, from 512 keys.  A token of each of 8 (32; 64) sequences of 4,096 keys, 8
+//     kv heads of 128: 103 us unsplit (120; 188), 29 so (91; 174), eight per CU 29 (93; 176); of 16 sequences
+//     of 700 keys 21.9 and 15.1, of 500 keys 17.3 and 17.2.
+//   Others: a split's sums go out and come back as fp32, so the split of the least estimated time, from what
+//     workgroups take on their own (18 ns a key, 14 at 64 values a head), half as long again when most CUs
+//     hold two, the join's launch (4 us) and 4 TB/s for its sums.  32 heads of 128, 8 kv heads: 128 rows of 2
+//     sequences of 4,096 keys 77 -> 37 us, of 8 sequences 107 -> 86, 512 rows of one 75 -> 49; left whole: a
+//     sequence of 512 rows 21 us (two splits 23), 4 sequences of 512 with 12 heads of 64 11 us (24).
+int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim) {
   constexpr int kCus = 256;
   if (n_q < 1) return 1;
   const int G = heads / kv_heads;
   const bool few = attn_shape(n_q, n_k, n_seq, G) == kFew;
-  const int64_t ts = fwd_slots(n_q, n_k, n_seq, G) / G;
-  // tiles that hold tokens, at most one a sequence more than the mean length takes
-  const int64_t wgs = (n_q / ts + (n_q < n_seq ? n_q : n_seq)) * kv_heads;
-  const int64_t full = few ? 16 * kCus : 8 * kCus;
-  if (wgs >= (few ? full : full / 4)) return 1;
-  int64_t s = (full + wgs - 1) / wgs;
-  const int64_t most = n_k / n_seq / 256 < 1 ? 1 : n_k / n_seq / 256;
-  if (s > most) s = most;
+  const int64_t ts = fwd_slots(n_q, n_k, n_seq, G) / G, mean = n_k / n_seq;
+  // workgroups that hold tokens, if the sequences are of one length
+  const int64_t live = n_q < n_seq ? n_q : n_seq;
+  const int64_t wgs = live * ((n_q / live + ts - 1) / ts) * kv_heads;
+  const int64_t full = few ? 4 * kCus : 2 * kCus;
+  if (wgs >= full) return 1;
+  int64_t most = mean / 128 < kMaxSplits ? mean / 128 : kMaxSplits;
   // (the grid also has the tiles of empty sequences: no more than 2^22 workgroups for the splits' sake)
   const int64_t grid = (n_q / ts + n_seq) * kv_heads;
-  if (s * grid > (int64_t(1) << 22)) s = (int64_t(1) << 22) / grid < 1 ? 1 : (int64_t(1) << 22) / grid;
-  return (int)(s > kMaxSplits ? kMaxSplits : s);
+  if (most > (int64_t(1) << 22) / grid) most = (int64_t(1) << 22) / grid;
+  if (few) {
+    const int64_t s = (full + wgs - 1) / wgs;
+    return mean < 512 || most < 1 ? 1 : (int)(s < most ? s : most);
+  }
+  const double sums = (double)n_q * heads * dim * 8 / 4e6;  // us a split, out and back
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= most; ++s) {
+    const int64_t w = wgs * s;
+    const double share = w <= 3 * kCus / 4 ? 1. : w <= 2 * kCus ? 1.5 : 1.6 * w / (2 * kCus);
+    const double us = (double)mean / s * (dim > 64 ? 0.018 : 0.014) * share + (s > 1 ? 4. + s * sums : 0.);
+    if (us < least) least = us, best = s;
+  }
+  return best;
 }
 
 // Calls of at least four rounds of workgroups plan their tiles.

@@ -275,7 +275,7 @@ struct AttnArgs {
   AttnTile *q_plan, *k_plan;  // the tiles of query and key rows, where the call plans (may be null)
 };
 constexpr int kMaxGroup = 32;  // query heads of one kv head
-int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
+int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim);
 // Tiles of the forward's and the gradients' plans (0: the call does not plan).
 int64_t attn_plan_tiles(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
 int64_t attn_plan_q_tiles(int64_t n_q, int n_seq, int heads, int kv_heads);
