@@ -714,17 +714,22 @@ hipError_t expand_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipSt
   return hipGetLastError();
 }
 
-// Rows up to which the whole call is one pass over W, and the fewest tiles of the two large sizes.
-constexpr int kFewRows = 64;
-constexpr int kWideFrom = 192, kMidFrom = 256;
-// Tiles of a last round of the large size that are left to the next size: at 4096 -> 4096, 13,057 rows
-// are 3.2 rounds of 256 tiles, which took as long as four.
-constexpr int kLastRound = 160;
+// The tile of y, by the number of tiles that the call has (the projections alone, us):
+//   32 x 32    up to 384 of them: 4096 -> 4096, 64 rows (256 tiles) 19 (64 x 64: 31), 96 rows (384) 29 (32),
+//              256 rows (2,048) 49 (30); 4096 -> 16384, 8 rows (512) 38 (34), 33 rows (1,024) 67 (35)
+//   64 x 64    otherwise, until
+//   128 x 128  there are 160 of these: 4096 -> 4096, 512 rows (128 tiles) 39 (64 x 64: 36), 768 rows (192)
+//              42 (55), 1,024 rows (256) 47 (62)
+//   256 x 256  there are 144 of these: 4096 -> 4096, 2,048 rows (128 tiles) 87 (128 x 128: 83), 2,560 rows
+//              (160) 93 (111), 4,096 rows (256) 121 (157)
+// and a last round (of 256, one a CU) of up to 112 of the largest is left to the next size: 512 tiles and 64
+// more 274 (305 without that), 96 more 303 (307), 128 more 312 (308), 160 more 341 (315).
+constexpr int kFewTo = 384, kMidFrom = 160, kWideFrom = 144, kLastRound = 112;
 
 template <class T>
 hipError_t expand(AdapterArgs a, const uint16_t* h, uint16_t* y, hipStream_t s) {
   auto tiles = [&](int b) { return (a.n - a.row0 + b - 1) / b * ((a.m + b - 1) / b); };
-  if (a.n <= kFewRows) {
+  if (tiles(32) <= kFewTo) {
     const int n_m = (a.m + 31) / 32;
     constexpr int lds = kFewWaves * WaveProduct<T, 1, 1>::kBytes;
     const hipError_t e = allow_lds((const void*)expand_few_kernel<T>, lds);

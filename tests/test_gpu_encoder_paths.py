@@ -65,6 +65,8 @@ def test_planned_attention_graph_replays():
 ADAPTER_SIZES = {
     # the large tile with its last round left to the middle one, the end of k inside a stage
     "large": ([1000, 3, 0, 1500, 1697], [1, 0, 0, 2, 1], 72, 4096, 16, 3, "bf16"),
+    # one round of the large tile, ragged on both sides
+    "large_ragged": ([2400, 77], [1, 0], 136, 4008, 8, 2, "f16"),
     "middle": ([700, 900, 500], [0, 1, -1], 136, 2048, 8, 2, "f16"),
     # 64 rows a workgroup for h at ranks above 32
     "rank_64_many_rows": ([5000, 4000], [1, 0], 72, 64, 64, 2, "bf16"),
