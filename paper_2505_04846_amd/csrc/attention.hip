@@ -924,9 +924,11 @@ hipError_t run_bwd(AttnArgs a, hipStream_t s) {
 
 // Splits of the key axis, where the tiles alone do not fill the chip: none of fewer than 128 keys of the
 // mean sequence.
-//   kFew: up to four waves per CU, from 512 keys.  A token of each of 8 (32; 64) sequences of 4,096 keys, 8
-//     kv heads of 128: 103 us unsplit (120; 188), 29 so (91; 174), eight per CU 29 (93; 176); of 16 sequences
-//     of 700 keys 21.9 and 15.1, of 500 keys 17.3 and 17.2.
+//   kFew, from 512 keys: four waves per CU, or up to sixteen of no fewer than 512 keys, which evens out
+//     sequences of different lengths.  A token each, 8 kv heads of 128, us (equal sequences of 4,096 keys;
+//     uneven ones of 64 to 8,192): 8 sequences in 16 splits 29; 42, in 32 33; 50.  32 in 4 splits 91; 102, in
+//     8 92; 89, in 16 101; 93.  64 in 2 splits 178; 220, in 8 181; 191, in 16 195; 195.  16 of 700 keys 22
+//     whole, 15 in 5.
 //   Others: a split's sums go out and come back as fp32, so the split of the least estimated time, from what
 //     workgroups take on their own (18 ns a key, 14 at 64 values a head), half as long again when most CUs
 //     hold two, the join's launch (4 us) and 4 TB/s for its sums.  32 heads of 128, 8 kv heads: 128 rows of 2
@@ -941,15 +943,16 @@ int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, in
   // workgroups that hold tokens, if the sequences are of one length
   const int64_t live = n_q < n_seq ? n_q : n_seq;
   const int64_t wgs = live * ((n_q / live + ts - 1) / ts) * kv_heads;
-  const int64_t full = few ? 4 * kCus : 2 * kCus;
-  if (wgs >= full) return 1;
+  if (wgs >= (few ? 16 : 2) * kCus) return 1;
   int64_t most = mean / 128 < kMaxSplits ? mean / 128 : kMaxSplits;
   // (the grid also has the tiles of empty sequences: no more than 2^22 workgroups for the splits' sake)
   const int64_t grid = (n_q / ts + n_seq) * kv_heads;
   if (most > (int64_t(1) << 22) / grid) most = (int64_t(1) << 22) / grid;
   if (few) {
-    const int64_t s = (full + wgs - 1) / wgs;
-    return mean < 512 || most < 1 ? 1 : (int)(s < most ? s : most);
+    if (mean < 512 || most < 1) return 1;
+    const int64_t four = (4 * kCus + wgs - 1) / wgs, all = (16 * kCus + wgs - 1) / wgs, wide = mean / 512;
+    const int64_t s = all < wide ? all : wide;
+    return (int)((s > four ? s : four) < most ? (s > four ? s : four) : most);
   }
   const double sums = (double)n_q * heads * dim * 8 / 4e6;  // us a split, out and back
   int best = 1;
