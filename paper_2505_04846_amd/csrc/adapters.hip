@@ -39,15 +39,16 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int s) {
 // ---- a wave's own product ----------------------------------------------------------------------
 
 // acc[b][c] = rows [32 b, 32 b + 32) of P times rows [32 c, + 32) of X, over stages [kk0, kk1) of 64 values,
-// by one wave:
-// its two LDS stages are its own, so waves that split k run without a barrier.  Whole 128-byte lines go
-// straight to LDS (operands read from memory by lanes touch twice as many lines a load: a token's
-// projection took 22 us that way).
-template <class T, int NB, int XB>
+// by one wave: its NST LDS stages are its own, so waves that split k run without a barrier.  Whole 128-byte
+// lines go straight to LDS (operands read from memory by lanes touch twice as many lines a load: a token's
+// projection took 22 us that way).  Of P, ROWS rows are loaded; the results of the rest of its last 32 are
+// not to be used (their operands are what LDS holds past the stage, of this wave's or another's).
+template <class T, int NB, int XB, int NST = 2, int ROWS = 32 * NB>
 struct WaveProduct {
-  static constexpr int kStage = (XB + NB) * 4096;
-  static constexpr int kBytes = 2 * kStage;
-  static constexpr int kX = 4 * XB, kLoads = 4 * (XB + NB);
+  static constexpr int kStage = XB * 4096 + ROWS * 128;
+  static constexpr int kBytes = NST * kStage;
+  static constexpr int kPast = (32 * NB - ROWS) * 128;  // LDS read past the stages
+  static constexpr int kX = 4 * XB, kLoads = 4 * XB + ROWS / 8;
   // x, p: first rows; x_last, p_last: their last valid row, which the rows past it repeat
   static __device__ __forceinline__ void run(const uint16_t* x, int x_last, const uint16_t* p, int p_last,
                                              int k, int kk0, int kk1, unsigned char* lds, int lane,
@@ -85,14 +86,18 @@ struct WaveProduct {
       for (int c = 0; c < XB; ++c)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
+    static_assert(NST == 2 || NST == 3, "the waits below");
+    static_assert(NST == 2 || NST == 3, "the waits below");
     if (kk0 < kk1) issue(0, kk0);
+    if (NST == 3 && kk0 + 1 < kk1) issue(1, kk0 + 1);
 #pragma unroll 1
-    for (int kk = kk0; kk < kk1; ++kk) {
-      const int buf = (kk - kk0) & 1;
-      if (kk + 1 < kk1) {
-        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // the other stage's reads are done
+    for (int kk = kk0, buf = 0; kk < kk1; ++kk, buf = buf + 1 < NST ? buf + 1 : 0) {
+      if (kk + NST - 1 < kk1) {
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // that stage's reads are done
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
-        issue(buf ^ 1, kk + 1);
+        issue(buf > 0 ? buf - 1 : NST - 1, kk + NST - 1);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 1) * kLoads));
+      } else if (NST == 3 && kk + 1 < kk1) {
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
       } else {
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
@@ -119,7 +124,7 @@ struct WaveProduct {
 
 // ---- h ----------------------------------------------------------------------------------------
 
-// h of 32 XB rows of one request.  W waves split k, each summing its part of the whole [rank, 32 XB]
+// h of 32 XB rows of one request, 32 NB ranks.  W waves split k, each summing its part of the [32 NB, 32 XB]
 // block (rank on the rows of the product, so that a lane holds 4 consecutive values of its row's
 // h), and join in LDS.  h is rounded to 16 bits once, with its scale: the operand of the product
 // with B.  Its relative rounding reaches only the adapter's part of y.
@@ -137,10 +142,11 @@ __device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h) {
   if (first < R.r0 || first >= R.r1 || ad < 0) return;
   const int last = R.r1 - first < kRows ? (int)(R.r1 - first) - 1 : kRows - 1;
   const int nk = (a.k + 63) / 64;
+  const int j0 = blockIdx.y * 32 * NB, left = a.r - j0;  // ranks
   f32x16 acc[NB][XB];
   unsigned char* own = smem + wave * P::kBytes;
-  P::run(a.x + first * a.k, last, a.a + (int64_t)ad * a.r * a.k, a.r - 1, a.k, nk * wave / W,
-         nk * (wave + 1) / W, own, lane, acc);
+  P::run(a.x + first * a.k, last, a.a + ((int64_t)ad * a.r + j0) * a.k,
+         left < 32 * NB ? left - 1 : 32 * NB - 1, a.k, nk * wave / W, nk * (wave + 1) / W, own, lane, acc);
   float* part = reinterpret_cast<float*>(own);  // [NB * XB * 16][64]
   static_assert(NB * XB * 4096 <= P::kBytes, "the wave's sums fit its stages");
 #pragma unroll
@@ -152,10 +158,10 @@ __device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h) {
   __syncthreads();
   const int rp = (a.r + 15) / 16 * 16;
   const float sc = a.scale[ad];
-  // register groups of four: group g of block (b, c) holds ranks 32 b + 8 g + 4 half + 0..3 of row
+  // register groups of four: group g of block (b, c) holds ranks j0 + 32 b + 8 g + 4 half + 0..3 of row
   // 32 c + col
   for (int i = wave; i < NB * XB * 4; i += W) {
-    const int bc = i >> 2, j = 32 * (bc / XB) + 8 * (i & 3) + 4 * half, t = 32 * (bc % XB) + col;
+    const int bc = i >> 2, j = j0 + 32 * (bc / XB) + 8 * (i & 3) + 4 * half, t = 32 * (bc % XB) + col;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -401,31 +407,36 @@ __global__ __launch_bounds__(64 * WT * WM, MINB) void expand_kernel(AdapterArgs 
   expand_tile<T, BT, BM, WT, WM, NST>(a, h, y, n_m);
 }
 
-// Few rows: 32 rows of x by 32 rows of W per workgroup.  The waves split k and join in LDS; then a thread
-// adds the adapter's part of its two values, each from its row's own h and B.
+// Few rows: 32 rows of x by BM = 32 or 16 rows of W per workgroup.  The waves split k and join in LDS; then
+// a thread adds the adapter's part of its two values, each from its row's own h and B.
 constexpr int kFewWaves = 8;
+template <class T, int BM>
+using FewProduct = WaveProduct<T, 1, 1, BM == 32 ? 2 : 3, BM>;
+template <class T, int BM>
+constexpr int kFewLds = kFewWaves * FewProduct<T, BM>::kBytes + FewProduct<T, BM>::kPast;
 
-template <class T>
+template <class T, int BM>
 __device__ __forceinline__ void expand_few(const AdapterArgs& a, const uint16_t* h, uint16_t* y, int n_m) {
-  using P = WaveProduct<T, 1, 1>;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // kFewWaves * P::kBytes
+  using P = FewProduct<T, BM>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // kFewLds
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m0 = (int)(blockIdx.x % (uint32_t)n_m) * 32;
+  const int m0 = (int)(blockIdx.x % (uint32_t)n_m) * BM;
   const int64_t t0 = (int64_t)(blockIdx.x / (uint32_t)n_m) * 32;
   const int nk = (a.k + 63) / 64;
   f32x16 acc[1][1];
   unsigned char* own = smem + wave * P::kBytes;
   P::run(a.x + t0 * a.k, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31, a.w + (int64_t)m0 * a.k,
-         a.m - m0 < 32 ? a.m - m0 - 1 : 31, a.k, nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own,
+         a.m - m0 < BM ? a.m - m0 - 1 : BM - 1, a.k, nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own,
          lane, acc);
   float* part = reinterpret_cast<float*>(own);  // [16][64]
 #pragma unroll
   for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];
   __syncthreads();
-  // thread: row t0 + i / 16 of the tile, columns m0 + 2 (i % 16) and the next: entries e, e + 1 of
+  // thread: two columns of a row: entries e, e + 1 of
   // lane (row, half) with column = 8 (e / 4) + 4 half + e % 4
-  const int row = threadIdx.x >> 4, m = 2 * (threadIdx.x & 15);
+  if (threadIdx.x >= 16 * BM) return;
+  const int row = threadIdx.x / (BM / 2), m = 2 * (threadIdx.x % (BM / 2));
   const int e = 4 * (m >> 3) + (m & 3), at = row + 32 * ((m >> 2) & 1);
   float v0 = 0.f, v1 = 0.f;
 #pragma unroll
@@ -472,10 +483,10 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const uint16_t*
   *reinterpret_cast<uint32_t*>(y + t * a.m + m0 + m) = T::pack(v0, v1);
 }
 
-template <class T>
+template <class T, int BM>
 __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(AdapterArgs a, const uint16_t* h,
                                                                     uint16_t* y, int n_m) {
-  expand_few<T>(a, h, y, n_m);
+  expand_few<T, BM>(a, h, y, n_m);
 }
 
 // ---- transposed weights -----------------------------------------------------------------------
@@ -686,18 +697,24 @@ hipError_t shrink_as(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
   constexpr int lds = W * WaveProduct<T, NB, XB>::kBytes;
   const hipError_t e = allow_lds((const void*)shrink_kernel<T, NB, XB, W>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((shrink_kernel<T, NB, XB, W>), dim3((unsigned)(a.n / (32 * XB) + a.n_req)),
+  hipLaunchKernelGGL((shrink_kernel<T, NB, XB, W>),
+                     dim3((unsigned)(a.n / (32 * XB) + a.n_req), (unsigned)(a.r + 32 * NB - 1) / (32 * NB)),
                      dim3(64 * W), lds, s, a, h);
   return hipGetLastError();
 }
 
-// Waves per workgroup: as many as two workgroups per CU allow, or eight where one round of workgroups
-// does not fill the chip.  Ranks above 32 read as much of A as of x per 32 rows and more: there 64 rows
-// share it, where they fill the chip.
+// By the number of tiles of 32 rows (k 4096, us of a call with a small W):
+//   8 waves on 32 ranks each while all of these workgroups run at a time: rank 128, 32 rows 19 (2 waves on
+//     all the ranks: 37), 2,048 rows 38 (50); rank 64, 32 rows 17 (6 waves on 64 ranks: 18), 1,024 rows
+//     27 (30), 4,096 rows 40 (36); rank 16, 8,192 rows 42 (4 waves: 45), 10,000 rows 66 (64)
+//   then as many waves as two workgroups per CU allow on all the ranks.  Ranks above 32 read as much of A
+//     as of x per 32 rows and more: there 64 rows share it, where they fill the chip: 10,000 rows of
+//     rank 64 68 (75).
 template <class T>
 hipError_t shrink(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
   const int64_t tiles = a.n / 32 + a.n_req;
-  if (a.r <= 32) return tiles <= 256 ? shrink_as<T, 1, 1, 8>(a, h, s) : shrink_as<T, 1, 1, 4>(a, h, s);
+  if (tiles * ((a.r + 31) / 32) <= (a.r <= 64 ? 256 : 512)) return shrink_as<T, 1, 1, 8>(a, h, s);
+  if (a.r <= 32) return shrink_as<T, 1, 1, 4>(a, h, s);
   if (a.r <= 64) return tiles <= 256 ? shrink_as<T, 2, 1, 6>(a, h, s) : shrink_as<T, 2, 2, 4>(a, h, s);
   return shrink_as<T, 4, 1, 2>(a, h, s);
 }
@@ -714,7 +731,20 @@ hipError_t expand_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipSt
   return hipGetLastError();
 }
 
+template <class T, int BM>
+hipError_t few_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipStream_t s) {
+  const int n_m = (a.m + BM - 1) / BM;
+  constexpr int lds = kFewLds<T, BM>;
+  const hipError_t e = allow_lds((const void*)expand_few_kernel<T, BM>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((expand_few_kernel<T, BM>), dim3((unsigned)((a.n + 31) / 32 * n_m)),
+                     dim3(64 * kFewWaves), lds, s, a, h, y, n_m);
+  return hipGetLastError();
+}
+
 // The tile of y, by the number of tiles that the call has (the projections alone, us):
+//   32 x 16    up to 128 tiles of 32 x 32, which leave CUs idle: 4096 -> 4096, 1 row 14.9 (32 x 32: 15.5), 32
+//              rows 16.9 (19.1), 64 rows (256 tiles) 25 (19); 14336 -> 4096, 32 rows 39 (43)
 //   32 x 32    up to 384 of them: 4096 -> 4096, 64 rows (256 tiles) 19 (64 x 64: 31), 96 rows (384) 29 (32),
 //              256 rows (2,048) 49 (30); 4096 -> 16384, 8 rows (512) 38 (34), 33 rows (1,024) 67 (35)
 //   64 x 64    otherwise, until
@@ -724,20 +754,12 @@ hipError_t expand_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipSt
 //              (160) 93 (111), 4,096 rows (256) 121 (157)
 // and a last round (of 256, one a CU) of up to 112 of the largest is left to the next size: 512 tiles and 64
 // more 274 (305 without that), 96 more 303 (307), 128 more 312 (308), 160 more 341 (315).
-constexpr int kFewTo = 384, kMidFrom = 160, kWideFrom = 144, kLastRound = 112;
+constexpr int kHalfTo = 128, kFewTo = 384, kMidFrom = 160, kWideFrom = 144, kLastRound = 112;
 
 template <class T>
 hipError_t expand(AdapterArgs a, const uint16_t* h, uint16_t* y, hipStream_t s) {
   auto tiles = [&](int b) { return (a.n - a.row0 + b - 1) / b * ((a.m + b - 1) / b); };
-  if (tiles(32) <= kFewTo) {
-    const int n_m = (a.m + 31) / 32;
-    constexpr int lds = kFewWaves * WaveProduct<T, 1, 1>::kBytes;
-    const hipError_t e = allow_lds((const void*)expand_few_kernel<T>, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((expand_few_kernel<T>), dim3((unsigned)((a.n + 31) / 32 * n_m)),
-                       dim3(64 * kFewWaves), lds, s, a, h, y, n_m);
-    return hipGetLastError();
-  }
+  if (tiles(32) <= kFewTo) return tiles(32) <= kHalfTo ? few_as<T, 16>(a, h, y, s) : few_as<T, 32>(a, h, y, s);
   if (tiles(256) >= kWideFrom) {
     const int64_t n_m = (a.m + 255) / 256, rest = tiles(256) % 256;
     const int64_t rows = (tiles(256) - rest) / n_m * 256;  // of the whole rounds
@@ -782,8 +804,10 @@ hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
 }  // namespace
 
 // 1,024 rows a slot where that leaves most of a round of workgroups (two per CU), 512 otherwise: more
-// rows, fewer partial sums to write and join (13,057 rows of 4096 on both sides: 66 us of 512 rows).
-int adapter_outer_rows(int64_t n, int k, int m) { return (n / 1024) * ((k + m) / 256) >= 384 ? 1024 : 512; }
+// rows, fewer partial sums to write and join.  All of the gradients, rank 16, 1,024 (512) rows a slot:
+// 4096 -> 4096, 13,057 rows (384 workgroups) 444 us (452), 8,192 rows (256) 288 (287); 1024 -> 1024, 40,000
+// rows (312) 151 (156), 13,057 rows (96) 67 (63).
+int adapter_outer_rows(int64_t n, int k, int m) { return (n / 1024) * ((k + m) / 256) >= 300 ? 1024 : 512; }
 
 int64_t adapter_outer_slots(int64_t n, int n_req, int k, int m) {
   return n_req == 0 ? 0 : n / adapter_outer_rows(n, k, m) + n_req;
