@@ -87,7 +87,6 @@ struct WaveProduct {
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
     static_assert(NST == 2 || NST == 3, "the waits below");
-    static_assert(NST == 2 || NST == 3, "the waits below");
     if (kk0 < kk1) issue(0, kk0);
     if (NST == 3 && kk0 + 1 < kk1) issue(1, kk0 + 1);
 #pragma unroll 1
@@ -259,8 +258,12 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
       }
     }
   };
+  // A wave of one block reads a whole stage's operands ahead of its products, and so hands the stage back
+  // when the next is begun (4096 -> 14336, 146 rows: 51 -> 46 us of the call); the others keep the stage
+  // that they compute on.
+  constexpr bool kAhead = kMb * kTb == 1;
 #pragma unroll
-  for (int s = 0; s < NST - 1; ++s) issue(s, s);
+  for (int s = 0; s < (kAhead ? NST : NST - 1); ++s) issue(s, s);
 
   f32x16 acc[kMb][kTb];
 #pragma unroll
@@ -270,51 +273,59 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  // the adapters' part
+  // the adapters' part: a lane looks at one request of the wave's rows, 64 at a time
   if (h && a.n_req > 0) {
     const int rp = (a.r + 15) / 16 * 16;
     const bool whole = a.r % 8 == 0;
-#pragma unroll
-    for (int j = 0; j < kTb; ++j) {
-      const int64_t r0 = t0 + (wt * kTb + j) * 32, r1 = r0 + 32 < a.n ? r0 + 32 : a.n;
-      const int64_t t = r0 + col;
+    const int64_t w0 = t0 + wt * kTb * 32;
 #pragma unroll 1
-      for (int s = find_row(a.off, a.n_req, r0); s < a.n_req; ++s) {
-        const Rows R = rows_of(a, s);
-        if (R.r0 >= r1) break;
-        const int ad = adapter_of(a, s);
-        if (R.r1 <= r0 || R.r1 <= R.r0 || ad < 0) continue;
-        const uint16_t* br = a.b + (int64_t)ad * a.m * a.r;
-        const bool in = t >= R.r0 && t < R.r1;
-        f32x16 v[kMb];
+    for (int base = find_row(a.off, a.n_req, w0); base < a.n_req; base += 64) {
+      const int s = base + lane < a.n_req ? base + lane : a.n_req - 1;
+      const Rows R = rows_of(a, s);
+      const int ad = adapter_of(a, s);
+      auto in_wave = [&](int64_t r) { return (int)(r < w0 ? 0 : (r - w0 < 32 * kTb ? r - w0 : 32 * kTb)); };
+      const int lo = in_wave(R.r0), hi = in_wave(R.r1);
+      const unsigned long long runs = __ballot(base + lane < a.n_req && lo < hi && ad >= 0);
 #pragma unroll
-        for (int i = 0; i < kMb; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) v[i][r] = 0.f;
+      for (int j = 0; j < kTb; ++j) {
+        const int row = 32 * j + col;
 #pragma unroll 1
-        for (int d = 8 * half; d < rp; d += 16) {
-          u32x4 fh = {0u, 0u, 0u, 0u};
-          if (in) fh = load16(h + t * rp + d);
+        for (unsigned long long left = runs & __ballot(lo < 32 * j + 32 && hi > 32 * j); left; left &= left - 1) {
+          const int i = __builtin_ctzll(left);
+          const int r_lo = __builtin_amdgcn_readlane(lo, i), r_hi = __builtin_amdgcn_readlane(hi, i);
+          const uint16_t* br = a.b + (int64_t)__builtin_amdgcn_readlane(ad, i) * a.m * a.r;
+          const bool in = row >= r_lo && row < r_hi;
+          f32x16 v[kMb];
 #pragma unroll
-          for (int i = 0; i < kMb; ++i) {
-            const int m = m0 + (wm * kMb + i) * 32 + col;
-            const uint16_t* p = br + (int64_t)(m < a.m ? m : a.m - 1) * a.r;
-            u32x4 fb = {0u, 0u, 0u, 0u};
-            if (whole) {
-              if (d < a.r) fb = load16(p + d);
-            } else {
+          for (int i = 0; i < kMb; ++i)
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (d + e < a.r) fb[e >> 1] |= (uint32_t)p[d + e] << (16 * (e & 1));
+            for (int r = 0; r < 16; ++r) v[i][r] = 0.f;
+#pragma unroll 1
+          for (int d = 8 * half; d < rp; d += 16) {
+            u32x4 fh = {0u, 0u, 0u, 0u};
+            if (in) fh = load16(h + (w0 + row) * rp + d);
+#pragma unroll
+            for (int i = 0; i < kMb; ++i) {
+              const int m = m0 + (wm * kMb + i) * 32 + col;
+              const uint16_t* p = br + (int64_t)(m < a.m ? m : a.m - 1) * a.r;
+              u32x4 fb = {0u, 0u, 0u, 0u};
+              if (whole) {
+                if (d < a.r) fb = load16(p + d);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (d + e < a.r) fb[e >> 1] |= (uint32_t)p[d + e] << (16 * (e & 1));
+              }
+              v[i] = T::mfma(fb, fh, v[i]);
             }
-            v[i] = T::mfma(fb, fh, v[i]);
           }
+#pragma unroll
+          for (int i = 0; i < kMb; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = in ? v[i][r] : acc[i][j][r];
         }
-#pragma unroll
-        for (int i = 0; i < kMb; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] = in ? v[i][r] : acc[i][j][r];
       }
+      if (__any(R.r0 >= w0 + 32 * kTb)) break;
     }
   }
 
@@ -334,39 +345,66 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
 #pragma unroll
       for (int j = 0; j < kTb; ++j) acc[i][j] = T::mfma(f.w[i], f.x[j], acc[i][j]);
   };
-  // The stages of the ring: NST - 1 are in flight when one is computed on.  One barrier per stage,
-  // before its last k-step, whose products run while the next stage's first operands are read.
-  Frags f0, f1;
-  __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
-  sync_lds();
-  read_frags(0, 0, f0);
-#pragma unroll 1
-  for (int kk = 0, buf = 0; kk < nk; ++kk) {
-    const int nxt = buf + 1 < NST ? buf + 1 : 0, free_ = buf > 0 ? buf - 1 : NST - 1;
-    issue(free_, kk + NST - 1);
-    __builtin_amdgcn_sched_barrier(0);
-    read_frags(buf, 1, f1);
-    mfma(f0);
-    read_frags(buf, 2, f0);
-    mfma(f1);
-    read_frags(buf, 3, f1);
-    mfma(f0);
-    // each k-step's products alternate with the reads of the next one's operands
+  if constexpr (kAhead) {
+    Frags f[2][4];
+    auto stage = [&](int buf, int kk, Frags (&now)[4], Frags (&then)[4]) {
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      sync_lds();  // the next stage has landed, and nobody reads this one any more
+      issue(buf, kk + NST);
+      const int nxt = buf + 1 < NST ? buf + 1 : 0;
 #pragma unroll
-    for (int u = 0; u < 3; ++u) {
+      for (int s = 0; s < 4; ++s) read_frags(nxt, s, then[s]);  // (past the last stage: zeros, not used)
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < kMb * kTb; ++t) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if (t < kTb + kMb) __builtin_amdgcn_sched_group_barrier(0x100, kMb * kTb >= kTb + kMb ? 1 : kTb + kMb, 0);
-      }
-    }
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
-    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      for (int s = 0; s < 4; ++s) mfma(now[s]);
+      return nxt;
+    };
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 1) * kLoads));
     sync_lds();
-    read_frags(nxt, 0, f0);  // (past the last stage: zeros, or rows that are read by nobody)
-    __builtin_amdgcn_sched_barrier(0);
-    mfma(f1);
-    buf = nxt;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) read_frags(0, s, f[0][s]);
+    int buf = 0;
+#pragma unroll 1
+    for (int kk = 0; kk < nk; kk += 2) {
+      buf = stage(buf, kk, f[0], f[1]);
+      if (kk + 1 < nk) buf = stage(buf, kk + 1, f[1], f[0]);
+    }
+  } else {
+    // The stages of the ring: NST - 1 are in flight when one is computed on.  One barrier per stage,
+    // before its last k-step, whose products run while the next stage's first operands are read.
+    Frags f0, f1;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+    sync_lds();
+    read_frags(0, 0, f0);
+#pragma unroll 1
+    for (int kk = 0, buf = 0; kk < nk; ++kk) {
+      const int nxt = buf + 1 < NST ? buf + 1 : 0, free_ = buf > 0 ? buf - 1 : NST - 1;
+      issue(free_, kk + NST - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      read_frags(buf, 1, f1);
+      mfma(f0);
+      read_frags(buf, 2, f0);
+      mfma(f1);
+      read_frags(buf, 3, f1);
+      mfma(f0);
+      // each k-step's products alternate with the reads of the next one's operands
+#pragma unroll
+      for (int u = 0; u < 3; ++u) {
+#pragma unroll
+        for (int t = 0; t < kMb * kTb; ++t) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          if (t < kTb + kMb) __builtin_amdgcn_sched_group_barrier(0x100, kMb * kTb >= kTb + kMb ? 1 : kTb + kMb, 0);
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      sync_lds();
+      read_frags(nxt, 0, f0);  // (past the last stage: zeros, or rows that are read by nobody)
+      __builtin_amdgcn_sched_barrier(0);
+      mfma(f1);
+      buf = nxt;
+    }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // no load may still target LDS when it is reused or ends
 
@@ -407,13 +445,50 @@ __global__ __launch_bounds__(64 * WT * WM, MINB) void expand_kernel(AdapterArgs 
   expand_tile<T, BT, BM, WT, WM, NST>(a, h, y, n_m);
 }
 
-// Few rows: 32 rows of x by BM = 32 or 16 rows of W per workgroup.  The waves split k and join in LDS; then
-// a thread adds the adapter's part of its two values, each from its row's own h and B.
+// Few rows: 32 rows of x by BM = 32 or 16 rows of W per workgroup.  Eight waves split k; meanwhile the
+// threads of BM / 4 others form the adapter's part of two values of y each, from their row's own h and B,
+// and add the eight sums to it in the end.
 constexpr int kFewWaves = 8;
 template <class T, int BM>
 using FewProduct = WaveProduct<T, 1, 1, BM == 32 ? 2 : 3, BM>;
 template <class T, int BM>
 constexpr int kFewLds = kFewWaves * FewProduct<T, BM>::kBytes + FewProduct<T, BM>::kPast;
+template <int BM>
+constexpr int kFewThreads = 64 * (kFewWaves + BM / 4);
+
+// Two values of B h of row t, columns m and m + 1.
+template <class T>
+__device__ __forceinline__ float2 adapter_part(const AdapterArgs& a, const uint16_t* h, int64_t t, int m) {
+  float2 v = {0.f, 0.f};
+  if (a.n_req == 0 || t >= a.n || m >= a.m) return v;
+  // the row's request (the last that starts at or before it)
+  int lo = 0, n = a.n_req;
+  while (n > 1) {
+    const int step = n / 2;
+    if (a.off[lo + step] <= t) lo += step, n -= step;
+    else n = step;
+  }
+  const int ad = adapter_of(a, lo);
+  if (ad < 0 || a.off[lo] > t || t >= a.off[lo + 1]) return v;
+  const uint16_t* hr = h + t * ((a.r + 15) / 16 * 16);
+  const uint16_t* b0 = a.b + ((int64_t)ad * a.m + m) * a.r;
+  if (a.r % 8 == 0) {
+    for (int d = 0; d < a.r; d += 8) {
+      const u32x4 hv = load16(hr + d), u = load16(b0 + d), w = load16(b0 + a.r + d);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v.x += T::lo(hv[q]) * T::lo(u[q]) + T::hi(hv[q]) * T::hi(u[q]);
+        v.y += T::lo(hv[q]) * T::lo(w[q]) + T::hi(hv[q]) * T::hi(w[q]);
+      }
+    }
+  } else {
+    for (int d = 0; d < a.r; ++d) {
+      v.x += T::lo(hr[d]) * T::lo(b0[d]);
+      v.y += T::lo(hr[d]) * T::lo(b0[a.r + d]);
+    }
+  }
+  return v;
+}
 
 template <class T, int BM>
 __device__ __forceinline__ void expand_few(const AdapterArgs& a, const uint16_t* h, uint16_t* y, int n_m) {
@@ -423,69 +498,38 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const uint16_t*
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m0 = (int)(blockIdx.x % (uint32_t)n_m) * BM;
   const int64_t t0 = (int64_t)(blockIdx.x / (uint32_t)n_m) * 32;
-  const int nk = (a.k + 63) / 64;
-  f32x16 acc[1][1];
-  unsigned char* own = smem + wave * P::kBytes;
-  P::run(a.x + t0 * a.k, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31, a.w + (int64_t)m0 * a.k,
-         a.m - m0 < BM ? a.m - m0 - 1 : BM - 1, a.k, nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own,
-         lane, acc);
-  float* part = reinterpret_cast<float*>(own);  // [16][64]
+  if (wave < kFewWaves) {
+    const int nk = (a.k + 63) / 64;
+    f32x16 acc[1][1];
+    unsigned char* own = smem + wave * P::kBytes;
+    P::run(a.x + t0 * a.k, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31, a.w + (int64_t)m0 * a.k,
+           a.m - m0 < BM ? a.m - m0 - 1 : BM - 1, a.k, nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own,
+           lane, acc);
+    float* part = reinterpret_cast<float*>(own);  // [16][64]
 #pragma unroll
-  for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];
-  __syncthreads();
-  // thread: two columns of a row: entries e, e + 1 of
-  // lane (row, half) with column = 8 (e / 4) + 4 half + e % 4
-  if (threadIdx.x >= 16 * BM) return;
-  const int row = threadIdx.x / (BM / 2), m = 2 * (threadIdx.x % (BM / 2));
-  const int e = 4 * (m >> 3) + (m & 3), at = row + 32 * ((m >> 2) & 1);
-  float v0 = 0.f, v1 = 0.f;
-#pragma unroll
-  for (int w = 0; w < kFewWaves; ++w) {
-    const float* from = reinterpret_cast<const float*>(smem + w * P::kBytes);
-    v0 += from[e * 64 + at];
-    v1 += from[(e + 1) * 64 + at];
+    for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];
+    __syncthreads();
+    return;
   }
+  // thread: two columns of a row: entries e, e + 1 of lane (row, half) with column = 8 (e / 4) + 4 half + e % 4
+  const int i = threadIdx.x - 64 * kFewWaves, row = i / (BM / 2), m = 2 * (i % (BM / 2));
   const int64_t t = t0 + row;
-  if (t >= a.n || m0 + m >= a.m) return;
-  if (a.n_req > 0) {
-    // the row's request (the last that starts at or before it)
-    int lo = 0, n = a.n_req;
-    while (n > 1) {
-      const int step = n / 2;
-      if (a.off[lo + step] <= t) lo += step, n -= step;
-      else n = step;
-    }
-    const int ad = adapter_of(a, lo);
-    if (ad >= 0 && a.off[lo] <= t && t < a.off[lo + 1]) {
-      const int rp = (a.r + 15) / 16 * 16;
-      const uint16_t* hr = h + t * rp;
-      const uint16_t* b0 = a.b + ((int64_t)ad * a.m + m0 + m) * a.r;
-      float s0f = 0.f, s1f = 0.f;
-      if (a.r % 8 == 0) {
-        for (int d = 0; d < a.r; d += 8) {
-          const u32x4 hv = load16(hr + d), u = load16(b0 + d), w = load16(b0 + a.r + d);
+  float2 v = adapter_part<T>(a, h, t, m0 + m);
+  __syncthreads();
+  const int e = 4 * (m >> 3) + (m & 3), at = row + 32 * ((m >> 2) & 1);
+  float2 w = {0.f, 0.f};
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            s0f += T::lo(hv[q]) * T::lo(u[q]) + T::hi(hv[q]) * T::hi(u[q]);
-            s1f += T::lo(hv[q]) * T::lo(w[q]) + T::hi(hv[q]) * T::hi(w[q]);
-          }
-        }
-      } else {
-        for (int d = 0; d < a.r; ++d) {
-          s0f += T::lo(hr[d]) * T::lo(b0[d]);
-          s1f += T::lo(hr[d]) * T::lo(b0[a.r + d]);
-        }
-      }
-      v0 += s0f;
-      v1 += s1f;
-    }
+  for (int k = 0; k < kFewWaves; ++k) {
+    const float* from = reinterpret_cast<const float*>(smem + k * P::kBytes);
+    w.x += from[e * 64 + at];
+    w.y += from[(e + 1) * 64 + at];
   }
-  *reinterpret_cast<uint32_t*>(y + t * a.m + m0 + m) = T::pack(v0, v1);
+  if (t < a.n && m0 + m < a.m) *reinterpret_cast<uint32_t*>(y + t * a.m + m0 + m) = T::pack(w.x + v.x, w.y + v.y);
 }
 
 template <class T, int BM>
-__global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(AdapterArgs a, const uint16_t* h,
-                                                                    uint16_t* y, int n_m) {
+__global__ __launch_bounds__(kFewThreads<BM>) void expand_few_kernel(AdapterArgs a, const uint16_t* h,
+                                                                     uint16_t* y, int n_m) {
   expand_few<T, BM>(a, h, y, n_m);
 }
 
@@ -738,7 +782,7 @@ hipError_t few_as(const AdapterArgs& a, const uint16_t* h, uint16_t* y, hipStrea
   const hipError_t e = allow_lds((const void*)expand_few_kernel<T, BM>, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((expand_few_kernel<T, BM>), dim3((unsigned)((a.n + 31) / 32 * n_m)),
-                     dim3(64 * kFewWaves), lds, s, a, h, y, n_m);
+                     dim3(kFewThreads<BM>), lds, s, a, h, y, n_m);
   return hipGetLastError();
 }
 
