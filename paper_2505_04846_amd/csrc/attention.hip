@@ -497,7 +497,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // ---- gradients --------------------------------------------------------------------------------
 
 // dq of a tile of slots, over all their visible keys; also delta (fp32), which the dk/dv kernel reads.
-// ds is rounded to 16 bits as the operand of the product with k, dq once.  Two kernels, this and the
+// ds is rounded to 16 bits as the operand of the product with k, dq once.  FINE, bf16 calls of short sequences:
+// what that rounding leaves of ds is a second operand, and delta is handed on with the sum of ds, which is
+// delta's own error (that of out's rounding).  On the documents below dq is off by 1.9e-3 and dk by 2.35e-3
+// (root mean squares against 64 bits; an exact result rounded to bf16: 1.7e-3), 2.5e-3 both without, and the
+// kernel takes 430 us instead of 385.  Where the products bound the time that costs more (sequences of 1,024
+// tokens 686 us, 554 without; 8,192: 3,620 and 2,810): from 512 keys on, not done.  Two kernels, this and the
 // dk/dv kernel, each with the sums of its own rows in registers: fused, one of the sums would go out
 // through atomics, whose order changes results, or as fp32 parts.
 //
@@ -505,7 +510,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // bound by HBM (1.7 GB, 255 us) and by a workgroup's start (three dependent loads: q and dout, out, keys; two
 // workgroups per CU); the matrix cores are busy 24 % of the cycles.  One sequence of 8,192 tokens: both kernels
 // at 1.09 PFLOP/s of the visible pairs.
-template <class T, int D, int NW>
+template <class T, int D, int NW, bool FINE>
 __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   constexpr int kS = D / 16, kDb = D / 32;
   constexpr int kTile = kKeys * D * 2;
@@ -573,8 +578,9 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
         delta += T::lo(g[s][e]) * T::lo(o[s][e]) + T::hi(g[s][e]) * T::hi(o[s][e]);
     delta = half_sum(delta);
   }
-  if (live && half == 0) a.delta[row] = delta;
+  if (!FINE && live && half == 0) a.delta[row] = delta;
 
+  float rest = 0.f;  // the sum of ds
   f32x16 dq[kDb];
 #pragma unroll
   for (int db = 0; db < kDb; ++db)
@@ -603,7 +609,7 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
         x = T::mfma(rd.row_frag(ks, b, s), q[s], x);
         dp = T::mfma(rd.row_frag(vs, b, s), g[s], dp);
       }
-      u32x4 ds[2];
+      u32x4 ds[2], low[2];
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = prob(__builtin_fmaf(x[r], a.c, -lse2));
       if (partial) {
@@ -615,18 +621,33 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
         }
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] *= dp[r] - delta;
+      for (int r = 0; r < 16; ++r) {
+        x[r] *= dp[r] - delta;
+        if (FINE) rest += x[r];
+      }
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ds[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
+        for (int e = 0; e < 4; ++e) {
+          ds[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
+          if (FINE)
+            low[s][e] = T::pack(x[8 * s + 2 * e] - T::lo(ds[s][e]), x[8 * s + 2 * e + 1] - T::hi(ds[s][e]));
+        }
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int db = 0; db < kDb; ++db) dq[db] = T::mfma(rd.tr_frag(ks, b, s, db), ds[s], dq[db]);
+        for (int db = 0; db < kDb; ++db) {
+          const u32x4 f = rd.tr_frag(ks, b, s, db);
+          dq[db] = T::mfma(f, ds[s], dq[db]);
+          if (FINE) dq[db] = T::mfma(f, low[s], dq[db]);
+        }
     }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  if (FINE) {
+    rest = half_sum(rest);
+    if (live && half == 0) a.delta[row] = delta + rest;
+  }
   if (!a.dq) return;
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   sync_lds();  // nobody reads the stages any more
@@ -846,9 +867,9 @@ template <class T, int D, int NW, int KEYS, int NST, int OCC>
 __global__ __launch_bounds__(64 * NW, OCC) void attn_fwd_kernel(AttnArgs a) {
   attn_fwd<T, D, NW, KEYS, NST>(a);
 }
-template <class T, int D, int NW>
+template <class T, int D, int NW, bool FINE>
 __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(AttnArgs a) {
-  attn_dq<T, D, NW>(a);
+  attn_dq<T, D, NW, FINE>(a);
 }
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, D >= 128 ? 2 : 3) void attn_dkv_kernel(AttnArgs a) {
@@ -876,6 +897,7 @@ int fwd_slots(int64_t n_q, int64_t n_k, int n_seq, int G) {
   return attn_shape(n_q, n_k, n_seq, G) == kFew ? 32 : 128;
 }
 constexpr int kBwdWaves = 4;
+constexpr int64_t kFineTo = 512;  // mean keys per sequence: see attn_dq
 constexpr int kKeyTile = 32 * kBwdWaves;
 
 // Writes the tiles of query rows (numbers below q_tiles), then those of key rows, a wave each: 4 to 5 us,
@@ -929,8 +951,11 @@ hipError_t run_bwd(AttnArgs a, hipStream_t s) {
   if (e == hipSuccess && q_tiles > 0) {
     a.ts = ts;
     a.tiles = q_tiles;
-    hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves>), dim3((unsigned)(q_tiles * a.kv_heads)),
-                       dim3(64 * kBwdWaves), 0, s, a);
+    const dim3 grid((unsigned)(q_tiles * a.kv_heads)), block(64 * kBwdWaves);
+    if (T::kCoarse && a.n_k < kFineTo * a.n_seq)
+      hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves, T::kCoarse>), grid, block, 0, s, a);
+    else
+      hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves, false>), grid, block, 0, s, a);
     e = hipGetLastError();
   }
   if (e == hipSuccess && k_tiles > 0) {
