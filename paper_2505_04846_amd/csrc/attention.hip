@@ -102,6 +102,11 @@ __device__ __forceinline__ AttnTile uniform_tile(const AttnTile* p) {
   return r;
 }
 
+// Token of a tile's slot (a slot of at most 128).
+__device__ __forceinline__ int token_of(const AttnArgs& a, int slot) {
+  return (int)((uint32_t)slot * a.g_inv >> 16);
+}
+
 // Keys [lo, hi) visible from token i (of lq, with lk keys).
 struct Span {
   int lo, hi;
@@ -139,9 +144,11 @@ struct WaveRows {
   static __device__ __forceinline__ void cols(const TileReads<D>& rd, const unsigned char* lds, int dim,
                                               int half, u32x4 (&f)[D / 16]) {
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      f[s] = rd.row_frag(lds, 0, s);
-      if (16 * s + 8 * half >= dim) f[s] = u32x4{0u, 0u, 0u, 0u};
+    for (int s = 0; s < D / 16; ++s) f[s] = rd.row_frag(lds, 0, s);
+    if (dim < D) {
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s)
+        if (16 * s + 8 * half >= dim) f[s] = u32x4{0u, 0u, 0u, 0u};
     }
   }
   // the rows' chunks past dim become zero
@@ -301,18 +308,21 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   const bool live = slot < n_slot;
   const bool wave_live = wave * 32 < n_slot;
   const int cs = live ? slot : n_slot - 1;
-  const int tok = t0 + cs / a.G, head = kvh * a.G + cs % a.G;
+  const int tok = t0 + token_of(a, cs), head = kvh * a.G + cs - token_of(a, cs) * a.G;
   const Span mine = span_of(a, S, tok);
   const int last_slot = wave * 32 + 31 < n_slot ? wave * 32 + 31 : n_slot - 1;
-  const Span wfirst = span_of(a, S, t0 + (wave_live ? wave * 32 : 0) / a.G);
-  const Span wlast = span_of(a, S, t0 + last_slot / a.G);
+  const Span wfirst = span_of(a, S, t0 + token_of(a, wave_live ? wave * 32 : 0));
+  const Span wlast = span_of(a, S, t0 + token_of(a, last_slot));
   const Span tfirst = span_of(a, S, t0), tlast = span_of(a, S, t0 + n_tok - 1);
 
   // key tiles of this split
   const int k_first = tfirst.lo / KEYS, k_end = (tlast.hi + KEYS - 1) / KEYS;
   const int n_kt = k_end > k_first ? k_end - k_first : 0;
-  const int kt0 = k_first + (int)((int64_t)n_kt * split / a.splits);
-  const int kt1 = k_first + (int)((int64_t)n_kt * (split + 1) / a.splits);
+  int kt0 = k_first, kt1 = k_first + n_kt;
+  if (a.splits > 1) {  // (below 2^26 tiles, times 64)
+    kt0 = k_first + (int)((uint32_t)n_kt * (uint32_t)split / (uint32_t)a.splits);
+    kt1 = k_first + (int)((uint32_t)n_kt * (uint32_t)(split + 1) / (uint32_t)a.splits);
+  }
 
   const KvLoad<D, NW, KEYS, NW == 1> ld(a, S, kvh, wave, lane);
   auto issue = [&](int buf, int kt) {
@@ -378,15 +388,21 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
     }
     sched_mfma(2 * kB);
     __builtin_amdgcn_sched_barrier(0);
-    if (first + KEYS > wfirst.hi || first < wlast.lo) {  // some key is not every slot's
-      const int lo = mine.lo - first - 4 * half, hi = mine.hi - first - 4 * half;
+    if (first + KEYS > wfirst.hi) {  // some key is past some slot's last
+      const int hi = mine.hi - first - 4 * half;
 #pragma unroll
       for (int b = 0; b < kB; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = 32 * b + 8 * (r >> 2) + (r & 3);
-          if (key >= hi || key < lo) x[b][r] = -__builtin_inff();
-        }
+        for (int r = 0; r < 16; ++r)
+          if (32 * b + 8 * (r >> 2) + (r & 3) >= hi) x[b][r] = -__builtin_inff();
+    }
+    if (first < wlast.lo) {  // or before some slot's first
+      const int lo = mine.lo - first - 4 * half;
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * b + 8 * (r >> 2) + (r & 3) < lo) x[b][r] = -__builtin_inff();
     }
     float top = x[0][0];
 #pragma unroll
@@ -527,11 +543,11 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   const bool live = slot < n_slot;
   const bool wave_live = wave * 32 < n_slot;
   const int cs = live ? slot : n_slot - 1;
-  const int tok = t0 + cs / a.G, head = kvh * a.G + cs % a.G;
+  const int tok = t0 + token_of(a, cs), head = kvh * a.G + cs - token_of(a, cs) * a.G;
   const Span mine = span_of(a, S, tok);
   const int last_slot = wave * 32 + 31 < n_slot ? wave * 32 + 31 : n_slot - 1;
-  const Span wfirst = span_of(a, S, t0 + (wave_live ? wave * 32 : 0) / a.G);
-  const Span wlast = span_of(a, S, t0 + last_slot / a.G);
+  const Span wfirst = span_of(a, S, t0 + token_of(a, wave_live ? wave * 32 : 0));
+  const Span wlast = span_of(a, S, t0 + token_of(a, last_slot));
   const Span tfirst = span_of(a, S, t0), tlast = span_of(a, S, t0 + n_tok - 1);
   const int kt0 = tfirst.lo / kKeys, kt1 = (tlast.hi + kKeys - 1) / kKeys;
 
@@ -545,7 +561,7 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   // q through the second stage, dout through the first, then out through the second
   constexpr int kOwn = WaveRows<D>::kBytes;
   static_assert(NW * kOwn <= 2 * kTile, "the wave's rows fit a stage");
-  const TileReads<D> rd(lane);
+  const TileReads<D> rd0(lane);
   unsigned char* own = smem + 2 * kTile + wave * kOwn;
   const uint32_t own_at = LDS_ADDRESS(smem) + 2 * kTile + wave * kOwn;
   WaveRows<D>::load(rsrc_of(a.q + (S.q0 + t0) * a.q_row + kvh * a.G * a.q_head),
@@ -555,8 +571,8 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   u32x4 q[kS], g[kS];
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
-  WaveRows<D>::cols(rd, own, a.dim, half, q);
-  WaveRows<D>::cols(rd, smem + wave * kOwn, a.dim, half, g);
+  WaveRows<D>::cols(rd0, own, a.dim, half, q);
+  WaveRows<D>::cols(rd0, smem + wave * kOwn, a.dim, half, g);
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   sync_lds();
   WaveRows<D>::load(rsrc_of(a.out + dense0), dense, own_at, lane, a.dim / 8);
@@ -570,7 +586,7 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   float delta = 0.f;
   {
     u32x4 o[kS];
-    WaveRows<D>::cols(rd, own, a.dim, half, o);
+    WaveRows<D>::cols(rd0, own, a.dim, half, o);
 #pragma unroll
     for (int s = 0; s < kS; ++s)
 #pragma unroll
@@ -598,7 +614,9 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
     if (!wave_live || first >= wlast.hi || first + kKeys <= wfirst.lo) continue;
     const unsigned char* ks = smem + buf * 2 * kTile;
     const unsigned char* vs = ks + kTile;
-    const bool partial = first + kKeys > wfirst.hi || first < wlast.lo;
+    // some key is past some slot's last, or before some slot's first
+    const bool past = first + kKeys > wfirst.hi, before = first < wlast.lo;
+    const TileReads<D> rd = FINE ? rd0.fresh() : rd0;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       f32x16 x, dp;
@@ -612,13 +630,17 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
       u32x4 ds[2], low[2];
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = prob(__builtin_fmaf(x[r], a.c, -lse2));
-      if (partial) {
-        const int lo = mine.lo - first - 32 * b - 4 * half, hi = mine.hi - first - 32 * b - 4 * half;
+      if (past) {
+        const int hi = mine.hi - first - 32 * b - 4 * half;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = 8 * (r >> 2) + (r & 3);
-          if (key >= hi || key < lo) x[r] = 0.f;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r >> 2) + (r & 3) >= hi) x[r] = 0.f;
+      }
+      if (before) {
+        const int lo = mine.lo - first - 32 * b - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r >> 2) + (r & 3) < lo) x[r] = 0.f;
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -713,13 +735,13 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
 #pragma unroll
   for (int j = 0; j < ld.kLoads; ++j) {
     const int r = ld.row[j] < used ? ld.row[j] : used - 1;
-    const int head = r % (uint32_t)a.G;
-    tok_of[j] = r / (uint32_t)a.G;
+    tok_of[j] = token_of(a, r);
+    const int head = r - tok_of[j] * a.G;
     q_at[j] = head * (int)a.q_head * 2 + ld.chunk[j];
     g_at[j] = head * a.dim * 2 + ld.chunk[j];
   }
   const int lr = lane < used ? lane : used - 1;
-  const int l_tok = lr / (uint32_t)a.G, l_head = lr % (uint32_t)a.G;
+  const int l_tok = token_of(a, lr), l_head = lr - l_tok * a.G;
   const int64_t d_row = (int64_t)a.heads * a.dim;
   const uint16_t* qb = a.q + S.q0 * a.q_row + kvh * a.G * a.q_head;
   const uint16_t* gb = a.dout + S.q0 * d_row + kvh * a.G * a.dim;
@@ -785,9 +807,9 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
     const unsigned char* gs = qs + kTile;
     const float* lse_s = reinterpret_cast<const float*>(qs + 2 * kTile);
     const float* del_s = lse_s + 64;
-    // every slot of the stage holds a token that sees every key of the wave
-    const bool partial = used < kSlots || t + ts > S.lq || t < w_first_all || t + ts > w_end_all ||
-                         wk0 + 31 >= S.lk;
+    // some slot's token comes before those that see some key of the wave, or after them (or is none)
+    const bool before = t < w_first_all;
+    const bool past = used < kSlots || t + ts > S.lq || t + ts > w_end_all || wk0 + 31 >= S.lk;
     const TileReads<D> rd = rd0.fresh();
     f32x16 x, dp;
 #pragma unroll
@@ -814,15 +836,19 @@ __device__ __forceinline__ void attn_dkv(const AttnArgs& a) {
       for (int e = 0; e < 4; ++e)
         x[4 * q4 + e] = prob(__builtin_fmaf(x[4 * q4 + e], a.c, -ls[e] * kLog2e));
     }
-    if (partial) {  // the lane's key is seen from slots [lo, hi) of the stage
+    // the lane's key is seen from slots [lo, hi) of the stage (dp of a key that no query sees may be NaN)
+    if (before) {
       const int lo = (my_first - t) * a.G - 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (8 * (r >> 2) + (r & 3) < lo) x[r] = dp[r] = 0.f;
+    }
+    if (past) {
       int hi = (my_end - t) * a.G;
       hi = (hi < used ? hi : used) - 4 * half;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int slot = 8 * (r >> 2) + (r & 3);
-        if (slot < lo || slot >= hi) x[r] = dp[r] = 0.f;  // (dp of a key that no query sees may be NaN)
-      }
+      for (int r = 0; r < 16; ++r)
+        if (8 * (r >> 2) + (r & 3) >= hi) x[r] = dp[r] = 0.f;
     }
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {

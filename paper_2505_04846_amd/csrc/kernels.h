@@ -261,7 +261,7 @@ struct AttnArgs {
   int window;       // 0: none
   bool causal, f16;
   float scale, c;   // c = scale * log2(e)
-  uint32_t g_inv;   // 65536 / G + 1: (slot * g_inv) >> 16 = slot / G for slot < 64
+  uint32_t g_inv;   // 65536 / G + 1: (slot * g_inv) >> 16 = slot / G for slot <= 128
   uint16_t* out;    // [n_q, heads, dim] (the gradients read it)
   float* lse;       // [n_q, heads], may be null in the forward
   int splits;       // of the key axis; above 1 the parts go through
