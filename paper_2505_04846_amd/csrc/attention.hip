@@ -614,11 +614,13 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
     if (!wave_live || first >= wlast.hi || first + kKeys <= wfirst.lo) continue;
     const unsigned char* ks = smem + buf * 2 * kTile;
     const unsigned char* vs = ks + kTile;
-    // some key is past some slot's last, or before some slot's first
-    const bool past = first + kKeys > wfirst.hi, before = first < wlast.lo;
     const TileReads<D> rd = FINE ? rd0.fresh() : rd0;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+      const int at = first + 32 * b;
+      if (at >= wlast.hi || at + 32 <= wfirst.lo) continue;
+      // some key is past some slot's last, or before some slot's first
+      const bool past = at + 32 > wfirst.hi, before = at < wlast.lo;
       f32x16 x, dp;
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = 0.f, dp[r] = 0.f;
@@ -631,13 +633,13 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = prob(__builtin_fmaf(x[r], a.c, -lse2));
       if (past) {
-        const int hi = mine.hi - first - 32 * b - 4 * half;
+        const int hi = mine.hi - at - 4 * half;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (8 * (r >> 2) + (r & 3) >= hi) x[r] = 0.f;
       }
       if (before) {
-        const int lo = mine.lo - first - 32 * b - 4 * half;
+        const int lo = mine.lo - at - 4 * half;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (8 * (r >> 2) + (r & 3) < lo) x[r] = 0.f;
