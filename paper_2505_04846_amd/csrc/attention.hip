@@ -517,12 +517,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // what that rounding leaves of ds is a second operand, and delta is handed on with the sum of ds, which is
 // delta's own error (that of out's rounding).  On the documents below dq is off by 1.9e-3 and dk by 2.35e-3
 // (root mean squares against 64 bits; an exact result rounded to bf16: 1.7e-3), 2.5e-3 both without, and the
-// kernel takes 430 us instead of 385.  Where the products bound the time that costs more (sequences of 1,024
-// tokens 686 us, 554 without; 8,192: 3,620 and 2,810): from 512 keys on, not done.  Two kernels, this and the
+// kernel takes 400 us instead of 370.  Where the products bound the time that costs more (sequences of 1,024
+// tokens 668 us, 572 without; 8,192: 3,720 and 2,900): from 512 keys on, not done.  Two kernels, this and the
 // dk/dv kernel, each with the sums of its own rows in registers: fused, one of the sums would go out
 // through atomics, whose order changes results, or as fp32 parts.
 //
-// Measured, 192 documents of 64 to 448 tokens and 24 questions, 32 heads of 128 on 8 kv heads, causal: 380 us,
+// Measured, 192 documents of 64 to 448 tokens and 24 questions, 32 heads of 128 on 8 kv heads, causal: 400 us,
 // bound by HBM (1.7 GB, 255 us) and by a workgroup's start (three dependent loads: q and dout, out, keys; two
 // workgroups per CU); the matrix cores are busy 24 % of the cycles.  One sequence of 8,192 tokens: both kernels
 // at 1.09 PFLOP/s of the visible pairs.
