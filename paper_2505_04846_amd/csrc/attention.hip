@@ -513,20 +513,18 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // ---- gradients --------------------------------------------------------------------------------
 
 // dq of a tile of slots, over all their visible keys; also delta (fp32), which the dk/dv kernel reads.
-// ds is rounded to 16 bits as the operand of the product with k, dq once.  FINE, bf16 calls of short sequences:
-// what that rounding leaves of ds is a second operand, and delta is handed on with the sum of ds, which is
-// delta's own error (that of out's rounding).  On the documents below dq is off by 1.9e-3 and dk by 2.35e-3
-// (root mean squares against 64 bits; an exact result rounded to bf16: 1.7e-3), 2.5e-3 both without, and the
-// kernel takes 400 us instead of 370.  Where the products bound the time that costs more (sequences of 1,024
-// tokens 668 us, 572 without; 8,192: 3,720 and 2,900): from 512 keys on, not done.  Two kernels, this and the
-// dk/dv kernel, each with the sums of its own rows in registers: fused, one of the sums would go out
+// ds is rounded to 16 bits as the operand of the product with k, dq once.  Where all the keys that a wave's
+// rows see lie in one stage, delta is summed from p and dp before ds is formed: of few keys, p (dp - delta)
+// cancels, and the rounding of out would be seen in it (a row's first key alone: ds is 0).  On the documents below dq and dk were off by 2.5e-3 without
+// that and are by 2.4e-3 (an exact result rounded to bf16: 1.7e-3), in the same time.  Two kernels, this and
+// the dk/dv kernel, each with the sums of its own rows in registers: fused, one of the sums would go out
 // through atomics, whose order changes results, or as fp32 parts.
 //
-// Measured, 192 documents of 64 to 448 tokens and 24 questions, 32 heads of 128 on 8 kv heads, causal: 400 us,
+// Measured, 192 documents of 64 to 448 tokens and 24 questions, 32 heads of 128 on 8 kv heads, causal: 370 us,
 // bound by HBM (1.7 GB, 255 us) and by a workgroup's start (three dependent loads: q and dout, out, keys; two
 // workgroups per CU); the matrix cores are busy 24 % of the cycles.  One sequence of 8,192 tokens: both kernels
 // at 1.09 PFLOP/s of the visible pairs.
-template <class T, int D, int NW, bool FINE>
+template <class T, int D, int NW>
 __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   constexpr int kS = D / 16, kDb = D / 32;
   constexpr int kTile = kKeys * D * 2;
@@ -561,7 +559,7 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   // q through the second stage, dout through the first, then out through the second
   constexpr int kOwn = WaveRows<D>::kBytes;
   static_assert(NW * kOwn <= 2 * kTile, "the wave's rows fit a stage");
-  const TileReads<D> rd0(lane);
+  const TileReads<D> rd(lane);
   unsigned char* own = smem + 2 * kTile + wave * kOwn;
   const uint32_t own_at = LDS_ADDRESS(smem) + 2 * kTile + wave * kOwn;
   WaveRows<D>::load(rsrc_of(a.q + (S.q0 + t0) * a.q_row + kvh * a.G * a.q_head),
@@ -571,8 +569,8 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   u32x4 q[kS], g[kS];
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
-  WaveRows<D>::cols(rd0, own, a.dim, half, q);
-  WaveRows<D>::cols(rd0, smem + wave * kOwn, a.dim, half, g);
+  WaveRows<D>::cols(rd, own, a.dim, half, q);
+  WaveRows<D>::cols(rd, smem + wave * kOwn, a.dim, half, g);
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   sync_lds();
   WaveRows<D>::load(rsrc_of(a.out + dense0), dense, own_at, lane, a.dim / 8);
@@ -586,7 +584,7 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
   float delta = 0.f;
   {
     u32x4 o[kS];
-    WaveRows<D>::cols(rd0, own, a.dim, half, o);
+    WaveRows<D>::cols(rd, own, a.dim, half, o);
 #pragma unroll
     for (int s = 0; s < kS; ++s)
 #pragma unroll
@@ -594,9 +592,7 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
         delta += T::lo(g[s][e]) * T::lo(o[s][e]) + T::hi(g[s][e]) * T::hi(o[s][e]);
     delta = half_sum(delta);
   }
-  if (!FINE && live && half == 0) a.delta[row] = delta;
 
-  float rest = 0.f;  // the sum of ds
   f32x16 dq[kDb];
 #pragma unroll
   for (int db = 0; db < kDb; ++db)
@@ -614,14 +610,8 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
     if (!wave_live || first >= wlast.hi || first + kKeys <= wfirst.lo) continue;
     const unsigned char* ks = smem + buf * 2 * kTile;
     const unsigned char* vs = ks + kTile;
-    const TileReads<D> rd = FINE ? rd0.fresh() : rd0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int at = first + 32 * b;
-      if (at >= wlast.hi || at + 32 <= wfirst.lo) continue;
-      // some key is past some slot's last, or before some slot's first
-      const bool past = at + 32 > wfirst.hi, before = at < wlast.lo;
-      f32x16 x, dp;
+    // p and dp of 32 keys from `at`, the second or first half of the stage
+    auto scores = [&](int b, int at, f32x16& x, f32x16& dp) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = 0.f, dp[r] = 0.f;
 #pragma unroll
@@ -629,49 +619,54 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
         x = T::mfma(rd.row_frag(ks, b, s), q[s], x);
         dp = T::mfma(rd.row_frag(vs, b, s), g[s], dp);
       }
-      u32x4 ds[2], low[2];
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = prob(__builtin_fmaf(x[r], a.c, -lse2));
-      if (past) {
+      if (at + 32 > wfirst.hi) {  // some key is past some slot's last
         const int hi = mine.hi - at - 4 * half;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (8 * (r >> 2) + (r & 3) >= hi) x[r] = 0.f;
       }
-      if (before) {
+      if (at < wlast.lo) {  // or before some slot's first
         const int lo = mine.lo - at - 4 * half;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (8 * (r >> 2) + (r & 3) < lo) x[r] = 0.f;
       }
+    };
+    if (first <= wfirst.lo && wlast.hi <= first + kKeys) {
+      delta = 0.f;
+#pragma unroll 1
+      for (int b = 0; b < 2; ++b) {
+        if (first + 32 * b >= wlast.hi) break;
+        f32x16 x, dp;
+        scores(b, first + 32 * b, x, dp);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[r] *= dp[r] - delta;
-        if (FINE) rest += x[r];
+        for (int r = 0; r < 16; ++r) delta += x[r] * dp[r];
       }
+      delta = half_sum(delta);
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int at = first + 32 * b;
+      if (at >= wlast.hi || at + 32 <= wfirst.lo) continue;
+      f32x16 x, dp;
+      scores(b, at, x, dp);
+      u32x4 ds[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] *= dp[r] - delta;
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          ds[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
-          if (FINE)
-            low[s][e] = T::pack(x[8 * s + 2 * e] - T::lo(ds[s][e]), x[8 * s + 2 * e + 1] - T::hi(ds[s][e]));
-        }
+        for (int e = 0; e < 4; ++e) ds[s][e] = T::pack(x[8 * s + 2 * e], x[8 * s + 2 * e + 1]);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int db = 0; db < kDb; ++db) {
-          const u32x4 f = rd.tr_frag(ks, b, s, db);
-          dq[db] = T::mfma(f, ds[s], dq[db]);
-          if (FINE) dq[db] = T::mfma(f, low[s], dq[db]);
-        }
+        for (int db = 0; db < kDb; ++db) dq[db] = T::mfma(rd.tr_frag(ks, b, s, db), ds[s], dq[db]);
     }
   }
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-  if (FINE) {
-    rest = half_sum(rest);
-    if (live && half == 0) a.delta[row] = delta + rest;
-  }
+  if (live && half == 0) a.delta[row] = delta;
   if (!a.dq) return;
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   sync_lds();  // nobody reads the stages any more
@@ -895,9 +890,9 @@ template <class T, int D, int NW, int KEYS, int NST, int OCC>
 __global__ __launch_bounds__(64 * NW, OCC) void attn_fwd_kernel(AttnArgs a) {
   attn_fwd<T, D, NW, KEYS, NST>(a);
 }
-template <class T, int D, int NW, bool FINE>
+template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(AttnArgs a) {
-  attn_dq<T, D, NW, FINE>(a);
+  attn_dq<T, D, NW>(a);
 }
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, D >= 128 ? 2 : 3) void attn_dkv_kernel(AttnArgs a) {
@@ -925,7 +920,6 @@ int fwd_slots(int64_t n_q, int64_t n_k, int n_seq, int G) {
   return attn_shape(n_q, n_k, n_seq, G) == kFew ? 32 : 128;
 }
 constexpr int kBwdWaves = 4;
-constexpr int64_t kFineTo = 512;  // mean keys per sequence: see attn_dq
 constexpr int kKeyTile = 32 * kBwdWaves;
 
 // Writes the tiles of query rows (numbers below q_tiles), then those of key rows, a wave each: 4 to 5 us,
@@ -979,11 +973,8 @@ hipError_t run_bwd(AttnArgs a, hipStream_t s) {
   if (e == hipSuccess && q_tiles > 0) {
     a.ts = ts;
     a.tiles = q_tiles;
-    const dim3 grid((unsigned)(q_tiles * a.kv_heads)), block(64 * kBwdWaves);
-    if (T::kCoarse && a.n_k < kFineTo * a.n_seq)
-      hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves, T::kCoarse>), grid, block, 0, s, a);
-    else
-      hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((attn_dq_kernel<T, D, kBwdWaves>), dim3((unsigned)(q_tiles * a.kv_heads)),
+                       dim3(64 * kBwdWaves), 0, s, a);
     e = hipGetLastError();
   }
   if (e == hipSuccess && k_tiles > 0) {

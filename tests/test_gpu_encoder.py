@@ -253,6 +253,25 @@ def test_attention_keys_that_no_query_sees(ty, q_lens, k_lens, H, Hk, D, window)
     assert not clean[3][gone].any() and not clean[4][gone].any()
 
 
+@pytest.mark.parametrize("ty", ["bf16", "f16"])
+@pytest.mark.parametrize("H,Hk,D", [(8, 2, 128), (12, 12, 64), (4, 1, 40)])
+def test_attention_gradient_of_one_visible_key(ty, H, Hk, D):
+    """The first row of a causal sequence sees one key with probability 1: its dq is 0, up to fp32 sums,
+    whatever the rounding of out."""
+    case = ([1, 2, 17, 200, 64], None, None, H, Hk, D, ty, True, 0)
+    q, k, v, q_off, _, _, how, dout = attention_case(case, seed=55)
+    r = hpr.packed_attention_fwd(q, k, v, q_off, **how)
+    b = hpr.packed_attention_bwd(dout, q, k, v, r["out"], r["lse"], q_off, **how)
+    first = q_off[:-1].tolist()
+    # |ds| <= (error of p and of two sums of D products) * sum |g v|, a hundred roundings of fp32 and more
+    most = ((D + 100) * 2.0 ** -24 * np.abs(f64(dout)[first]).max() * np.abs(f64(v)[first]).max() * D
+            * D ** -0.5 * np.abs(f64(k)[first]).max())
+    assert np.abs(f64(b["dq"])[first]).max() <= most
+    # ... and a sequence of one token gives no dk
+    assert np.abs(f64(b["dk"])[first[0]]).max() <= most * (H // Hk) * max(
+        1.0, np.abs(f64(q)[first]).max() / np.abs(f64(k)[first]).max())
+
+
 def test_attention_bits_repeat_and_streams():
     case = ([300, 1, 77, 500], None, None, 8, 2, 128, "bf16", True, 0)
     q, k, v, q_off, _, _, how, dout = attention_case(case, seed=53)
