@@ -515,10 +515,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // dq of a tile of slots, over all their visible keys; also delta (fp32), which the dk/dv kernel reads.
 // ds is rounded to 16 bits as the operand of the product with k, dq once.  Where all the keys that a wave's
 // rows see lie in one stage, delta is summed from p and dp before ds is formed: of few keys, p (dp - delta)
-// cancels, and the rounding of out would be seen in it (a row's first key alone: ds is 0).  On the documents below dq and dk were off by 2.5e-3 without
-// that and are by 2.4e-3 (an exact result rounded to bf16: 1.7e-3), in the same time.  Two kernels, this and
-// the dk/dv kernel, each with the sums of its own rows in registers: fused, one of the sums would go out
-// through atomics, whose order changes results, or as fp32 parts.
+// cancels, and the rounding of out would be seen in it (a row's first key alone: ds is 0).  On the documents
+// below dq and dk were off by 2.5e-3 without that and are by 2.4e-3 (an exact result rounded to bf16: 1.7e-3),
+// in the same time.  Two kernels, this and the dk/dv kernel, each with the sums of its own rows in
+// registers: fused, one of the sums would go out through atomics, whose order changes results, or as fp32
+// parts.
 //
 // Measured, 192 documents of 64 to 448 tokens and 24 questions, 32 heads of 128 on 8 kv heads, causal: 370 us,
 // bound by HBM (1.7 GB, 255 us) and by a workgroup's start (three dependent loads: q and dout, out, keys; two
