@@ -68,6 +68,13 @@ ADAPTER_SIZES = {
     # one round of the large tile, ragged on both sides
     "large_ragged": ([2400, 77], [1, 0], 136, 4008, 8, 2, "f16"),
     "middle": ([700, 900, 500], [0, 1, -1], 136, 2048, 8, 2, "f16"),
+    # more requests than one look covers inside a tile's rows, most of them empty
+    "empty_requests": ([3] + [0] * 100 + [20] + [0] * 70 + [25], [i % 3 - 1 for i in range(173)], 72, 8192,
+                       16, 2, "bf16"),
+    "empty_requests_few": ([3] + [0] * 100 + [20] + [0] * 70 + [25], [i % 3 - 1 for i in range(173)], 136,
+                           200, 20, 2, "f16"),
+    # ranks over workgroups, past one block of 32
+    "rank_128_few_rows": ([40, 3, 0, 90], [1, 0, 1, -1], 520, 264, 128, 2, "bf16"),
     # 64 rows a workgroup for h at ranks above 32
     "rank_64_many_rows": ([5000, 4000], [1, 0], 72, 64, 64, 2, "bf16"),
     "rank_40_many_rows": ([8300, 33], [0, 0], 64, 72, 40, 1, "f16"),
