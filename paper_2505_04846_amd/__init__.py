@@ -579,6 +579,33 @@ def packed_attention_bwd(dout, q, k, v, out, lse, q_off, k_off=None, k_len=None,
     return {"dq": dq, "dk": dk, "dv": dv}
 
 
+class _FirstOrder(torch.autograd.Function):
+    """Gradients as they are, as functions of the tensors after them that has no derivative."""
+
+    @staticmethod
+    def forward(ctx, name, count, *tensors):
+        ctx.name = name
+        return tuple(t.detach() for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(f"{ctx.name} has no second derivatives")
+
+
+def _first_order(name, grads, *of):
+    """grads (some None) of a backward pass that autograd does not see into.  While it records one
+    (create_graph), they are tied to the tensors `of` that they depend on: a second derivative raises
+    instead of leaving their terms out."""
+    if not torch.is_grad_enabled():
+        return grads
+    of = [t for t in of if t.requires_grad]
+    some = [g for g in grads if g is not None]
+    if not of or not some:
+        return grads
+    tied = iter(_FirstOrder.apply(name, len(some), *some, *of))
+    return [g if g is None else next(tied) for g in grads]
+
+
 class _PackedAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, q_off, k_off, k_len, causal, window, scale):
@@ -596,12 +623,14 @@ class _PackedAttention(torch.autograd.Function):
         need = ctx.needs_input_grad
         g = packed_attention_bwd(grad_out.contiguous(), q, k, v, out, lse, q_off, k_off, k_len,
                                  *ctx.how, need_dq=need[0], need_dkv=need[1] or need[2])
-        return (g["dq"], g["dk"] if need[1] else None, g["dv"] if need[2] else None,
-                None, None, None, None, None, None)
+        dq, dk, dv = _first_order("packed_attention", [g["dq"], g["dk"] if need[1] else None,
+                                                       g["dv"] if need[2] else None],
+                                  grad_out, q, k, v)
+        return dq, dk, dv, None, None, None, None, None, None
 
 
 def packed_attention(q, k, v, q_off, k_off=None, k_len=None, causal=True, window=0, scale=None):
-    """packed_attention_fwd's out, differentiable (gradients reach q, k and v)."""
+    """packed_attention_fwd's out, differentiable once (gradients reach q, k and v)."""
     return _PackedAttention.apply(q, k, v, q_off, k_off, k_len, causal, window, scale)
 
 
@@ -684,13 +713,16 @@ class _AdapterLinear(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad_y):
         need = ctx.needs_input_grad
-        g = adapter_linear_bwd(grad_y.contiguous(), *ctx.saved_tensors, need_dx=need[0],
-                               need_da=need[2], need_db=need[3])
-        return g["dx"], None, g["da"], g["db"], None, None, None
+        saved = ctx.saved_tensors
+        g = adapter_linear_bwd(grad_y.contiguous(), *saved, need_dx=need[0], need_da=need[2],
+                               need_db=need[3])
+        x, _, A, B = saved[:4]
+        dx, da, db = _first_order("adapter_linear", [g["dx"], g["da"], g["db"]], grad_y, x, A, B)
+        return dx, None, da, db, None, None, None
 
 
 def adapter_linear(x, W, A, B, scale, off, adapter):
-    """adapter_linear_fwd's y, differentiable (gradients reach x, A and B; W and scale are frozen)."""
+    """adapter_linear_fwd's y, differentiable once (gradients reach x, A and B; W and scale are frozen)."""
     for t, name in ((W, "W"), (scale, "scale")):
         if isinstance(t, torch.Tensor) and t.requires_grad:
             raise ValueError(f"{name} is frozen: it must not require a gradient")

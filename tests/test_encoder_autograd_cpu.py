@@ -1,0 +1,96 @@
+"""CPU-only: what the encoder operators' autograd functions do around their kernels, which plain torch
+stands in for."""
+
+import pytest
+import torch
+
+import paper_2505_04846_amd as hpr
+
+
+def _attention(q, k, v):
+    x = torch.matmul(q.transpose(0, 1), k.permute(1, 2, 0)) * q.shape[2] ** -0.5
+    return torch.matmul(x.softmax(-1), v.transpose(0, 1)).transpose(0, 1)
+
+
+def _adapters(x, W, A, B):
+    return x @ W.T + (x @ A[0].T) @ B[0].T
+
+
+def _grads(fn, inputs, g):
+    with torch.enable_grad():
+        t = [z.detach().requires_grad_() for z in inputs]
+        return torch.autograd.grad(fn(*t), t, g)
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    """One sequence, all keys visible; one request."""
+
+    def attention_fwd(q, k, v, *args, need_lse=True, **how):
+        return {"out": _attention(q, k, v), "lse": torch.zeros(q.shape[:2])}
+
+    def attention_bwd(dout, q, k, v, *args, **how):
+        return dict(zip(("dq", "dk", "dv"), _grads(_attention, (q, k, v), dout)))
+
+    def adapters_fwd(x, W, A, B, *args):
+        return {"y": _adapters(x, W, A, B), "h": x}
+
+    def adapters_bwd(dy, x, W, A, B, *args, need_dx=True, need_da=True, need_db=True):
+        dx, _, da, db = _grads(_adapters, (x, W, A, B), dy)
+        return {"dx": dx if need_dx else None, "da": da if need_da else None,
+                "db": db if need_db else None}
+
+    for name, fn in (("packed_attention_fwd", attention_fwd), ("packed_attention_bwd", attention_bwd),
+                     ("adapter_linear_fwd", adapters_fwd), ("adapter_linear_bwd", adapters_bwd)):
+        monkeypatch.setattr(hpr, name, fn)
+
+
+def _attention_inputs():
+    g = torch.Generator().manual_seed(1)
+    return [torch.randn(5, 2, 8, generator=g, dtype=torch.float64) for _ in range(3)]
+
+
+def _adapter_inputs():
+    g = torch.Generator().manual_seed(2)
+    return [torch.randn(*s, generator=g, dtype=torch.float64)
+            for s in ((5, 8), (6, 8), (1, 3, 8), (1, 6, 3))]
+
+
+def _calls():
+    q, k, v = _attention_inputs()
+    x, W, A, B = _adapter_inputs()
+    none = torch.zeros(1)
+    return {
+        "packed_attention": (lambda *t: hpr.packed_attention(*t, None), [q, k, v], _attention),
+        "adapter_linear": (lambda x, A, B: hpr.adapter_linear(x, W, A, B, none, none, none),
+                           [x, A, B], lambda x, A, B: _adapters(x, W, A, B)),
+    }
+
+
+@pytest.mark.parametrize("name", ["packed_attention", "adapter_linear"])
+def test_second_derivatives_raise(plain, name):
+    fn, inputs, formula = _calls()[name]
+    t = [z.clone().requires_grad_() for z in inputs]
+    # the gradient itself is there under create_graph, and says that it depends on the inputs
+    y = fn(*t)
+    first = torch.autograd.grad(y.sum(), t, create_graph=True)
+    for got, want in zip(first, _grads(formula, inputs, torch.ones_like(y))):
+        assert torch.allclose(got, want) and got.requires_grad
+    with pytest.raises(RuntimeError, match=f"{name} has no second derivatives"):
+        (y.sum() + sum((g ** 2).sum() for g in first)).backward()
+    # ... so does one with respect to a single input, through a gradient of y that depends on others
+    last = inputs[-1].clone().requires_grad_()
+    up = torch.ones_like(y).requires_grad_()
+    g, = torch.autograd.grad(fn(*inputs[:-1], last), last, up, create_graph=True)
+    with pytest.raises(RuntimeError, match="no second derivatives"):
+        g.sum().backward()
+
+
+@pytest.mark.parametrize("name", ["packed_attention", "adapter_linear"])
+def test_first_derivatives_under_create_graph(plain, name):
+    """A backward pass that is recorded and never differentiated again is as any other."""
+    fn, inputs, formula = _calls()[name]
+    t = [z.clone().requires_grad_() for z in inputs]
+    fn(*t).sum().backward(create_graph=True)
+    for z, want in zip(t, _grads(formula, inputs, torch.ones_like(fn(*inputs)))):
+        assert torch.allclose(z.grad, want)
