@@ -763,27 +763,28 @@ def rotary_apply(q, k, pos, cos, sin, inverse=False):
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, pos, cos, sin):
+    def forward(ctx, q, k, pos, cos, sin, inverse):
         ctx.save_for_backward(pos, cos, sin)
-        return rotary_apply(q.detach(), k.detach() if k is not None else None, pos, cos, sin)
+        ctx.inverse = inverse
+        return rotary_apply(q.detach(), k.detach() if k is not None else None, pos, cos, sin, inverse)
 
     @staticmethod
     def backward(ctx, gq, gk):
-        pos, cos, sin = ctx.saved_tensors
         need_q, need_k = ctx.needs_input_grad[:2]
         a, b = [g.contiguous() if g is not None and need else None
                 for g, need in ((gq, need_q), (gk, need_k))]
-        if a is None and b is None:
-            return None, None, None, None, None
-        if a is None:
-            return None, rotary_apply(b, None, pos, cos, sin, inverse=True)[0], None, None, None
-        dq, dk = rotary_apply(a, b, pos, cos, sin, inverse=True)
-        return dq, dk, None, None, None
+        back = (*ctx.saved_tensors, not ctx.inverse)
+        # (a rotation too, and differentiable as one)
+        if a is not None:
+            a, b = _Rotary.apply(a, b, *back)
+        elif b is not None:
+            b, _ = _Rotary.apply(b, None, *back)
+        return a, b, None, None, None, None
 
 
 def rotary(q, k, pos, cos, sin):
     """rotary_apply, differentiable (gradients reach q and k, by the rotation back)."""
-    return _Rotary.apply(q, k, pos, cos, sin)
+    return _Rotary.apply(q, k, pos, cos, sin, False)
 
 
 def calibrate(device="cuda:0", mfma_iters=20000, read_bytes=16 << 30, reps=3):

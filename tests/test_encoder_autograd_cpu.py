@@ -16,6 +16,12 @@ def _adapters(x, W, A, B):
     return x @ W.T + (x @ A[0].T) @ B[0].T
 
 
+def _rotate(x, pos, cos, sin, inverse=False):
+    c, s = cos[pos.long()][:, None], (-sin if inverse else sin)[pos.long()][:, None]
+    a, b = x.chunk(2, -1)
+    return torch.cat([a * c - b * s, b * c + a * s], -1)
+
+
 def _grads(fn, inputs, g):
     with torch.enable_grad():
         t = [z.detach().requires_grad_() for z in inputs]
@@ -24,7 +30,7 @@ def _grads(fn, inputs, g):
 
 @pytest.fixture
 def plain(monkeypatch):
-    """One sequence, all keys visible; one request."""
+    """One sequence, all keys visible; one request.  Nothing that these compute is seen by autograd."""
 
     def attention_fwd(q, k, v, *args, need_lse=True, **how):
         return {"out": _attention(q, k, v), "lse": torch.zeros(q.shape[:2])}
@@ -40,8 +46,13 @@ def plain(monkeypatch):
         return {"dx": dx if need_dx else None, "da": da if need_da else None,
                 "db": db if need_db else None}
 
+    def rotary_apply(q, k, pos, cos, sin, inverse=False):
+        return tuple(t if t is None else _rotate(t.detach(), pos, cos, sin, inverse)
+                     for t in (q, k))
+
     for name, fn in (("packed_attention_fwd", attention_fwd), ("packed_attention_bwd", attention_bwd),
-                     ("adapter_linear_fwd", adapters_fwd), ("adapter_linear_bwd", adapters_bwd)):
+                     ("adapter_linear_fwd", adapters_fwd), ("adapter_linear_bwd", adapters_bwd),
+                     ("rotary_apply", rotary_apply)):
         monkeypatch.setattr(hpr, name, fn)
 
 
@@ -94,3 +105,25 @@ def test_first_derivatives_under_create_graph(plain, name):
     fn(*t).sum().backward(create_graph=True)
     for z, want in zip(t, _grads(formula, inputs, torch.ones_like(fn(*inputs)))):
         assert torch.allclose(z.grad, want)
+
+
+@pytest.mark.parametrize("which", ["both", "q", "k", "q alone"])
+def test_rotary_second_derivatives(plain, which):
+    """The gradient is a rotation of the gradient from above, and differentiable as one."""
+    g = torch.Generator().manual_seed(3)
+    q, k = [torch.randn(5, h, 8, generator=g, dtype=torch.float64) for h in (3, 2)]
+    angle = torch.rand(7, 4, generator=g, dtype=torch.float64)
+    cos, sin, pos = angle.cos(), angle.sin(), torch.tensor([6, 0, 3, 3, 1])
+    q.requires_grad_(which != "k")
+    k = k.requires_grad_(which in ("both", "k")) if which != "q alone" else None
+    t = [z for z in (q, k) if z is not None and z.requires_grad]
+
+    def second(fn):
+        """Gradients of a sum that the first gradients enter as squares."""
+        y = [z for z in fn() if z is not None and z.requires_grad]
+        first = torch.autograd.grad(sum((z ** 3).sum() for z in y), t, create_graph=True)
+        return torch.autograd.grad(sum((z ** 2).sum() for z in first), t)
+
+    got = second(lambda: hpr.rotary(q, k, pos, cos, sin))
+    want = second(lambda: [z if z is None else _rotate(z, pos, cos, sin) for z in (q, k)])
+    assert all(torch.allclose(a, b) for a, b in zip(got, want))
