@@ -592,6 +592,13 @@ class _FirstOrder(torch.autograd.Function):
         raise RuntimeError(f"{ctx.name} has no second derivatives")
 
 
+def _frozen(**operands):
+    """Raises where an operand that no gradient reaches asks for one."""
+    for name, t in operands.items():
+        if isinstance(t, torch.Tensor) and t.requires_grad:
+            raise ValueError(f"{name} is frozen: it must not require a gradient")
+
+
 def _first_order(name, grads, *of):
     """grads (some None) of a backward pass that autograd does not see into.  While it records one
     (create_graph), they are tied to the tensors `of` that they depend on: a second derivative raises
@@ -630,7 +637,8 @@ class _PackedAttention(torch.autograd.Function):
 
 
 def packed_attention(q, k, v, q_off, k_off=None, k_len=None, causal=True, window=0, scale=None):
-    """packed_attention_fwd's out, differentiable once (gradients reach q, k and v)."""
+    """packed_attention_fwd's out, differentiable once (gradients reach q, k and v; scale is frozen)."""
+    _frozen(scale=scale)
     return _PackedAttention.apply(q, k, v, q_off, k_off, k_len, causal, window, scale)
 
 
@@ -723,9 +731,7 @@ class _AdapterLinear(torch.autograd.Function):
 
 def adapter_linear(x, W, A, B, scale, off, adapter):
     """adapter_linear_fwd's y, differentiable once (gradients reach x, A and B; W and scale are frozen)."""
-    for t, name in ((W, "W"), (scale, "scale")):
-        if isinstance(t, torch.Tensor) and t.requires_grad:
-            raise ValueError(f"{name} is frozen: it must not require a gradient")
+    _frozen(W=W, scale=scale)
     return _AdapterLinear.apply(x, W, A, B, scale, off, adapter)
 
 
@@ -783,7 +789,9 @@ class _Rotary(torch.autograd.Function):
 
 
 def rotary(q, k, pos, cos, sin):
-    """rotary_apply, differentiable (gradients reach q and k, by the rotation back)."""
+    """rotary_apply, differentiable (gradients reach q and k, by the rotation back; cos and sin are
+    frozen)."""
+    _frozen(cos=cos, sin=sin)
     return _Rotary.apply(q, k, pos, cos, sin, False)
 
 

@@ -127,3 +127,21 @@ def test_rotary_second_derivatives(plain, which):
     got = second(lambda: hpr.rotary(q, k, pos, cos, sin))
     want = second(lambda: [z if z is None else _rotate(z, pos, cos, sin) for z in (q, k)])
     assert all(torch.allclose(a, b) for a, b in zip(got, want))
+
+
+def test_operands_without_a_gradient_refuse_one(plain):
+    q, k, v = _attention_inputs()
+    angle = torch.rand(7, 4)
+    pos = torch.zeros(5, dtype=torch.int32)
+    one = torch.ones(1, requires_grad=True)
+    for cos, sin, name in ((angle.cos().requires_grad_(), angle.sin(), "cos"),
+                           (angle.cos(), angle.sin().requires_grad_(), "sin")):
+        with pytest.raises(ValueError, match=f"{name} is frozen"):
+            hpr.rotary(q, k, pos, cos, sin)
+    with pytest.raises(ValueError, match="scale is frozen"):
+        hpr.packed_attention(q, k, v, None, scale=one)
+    x, W, A, B = _adapter_inputs()
+    with pytest.raises(ValueError, match="W is frozen"):
+        hpr.adapter_linear(x, W.requires_grad_(), A, B, None, None, None)
+    with pytest.raises(ValueError, match="scale is frozen"):
+        hpr.adapter_linear(x, W.detach(), A, B, one, None, None)
