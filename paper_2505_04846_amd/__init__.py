@@ -474,6 +474,11 @@ def _need_heads(t, name, dtype, device):
     if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 3 and t.is_cuda
             and t.device == device):
         row, head, one = t.stride()
+        n, heads, _ = t.shape
+        if n < 2:
+            row = 0
+        if heads < 2:
+            head = 0
         if one == 1 and not (row | head) & 7 and not t.data_ptr() & 15 and dtype in _HALF_TYPES:
             return row, head
     if not isinstance(t, torch.Tensor):
