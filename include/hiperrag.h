@@ -89,8 +89,14 @@ typedef int32_t hpr_status;
  *   dense_ip_topk: dim % 8 == 0, 8 <= dim <= 8192; n < 2^31.
  *   semantic_chunk: dim % 8 == 0, 8 <= dim <= 4096; 1 <= n < 2^31.
  *   packed_attention_*: dim % 8 == 0, 8 <= dim <= 128; heads a multiple of kv_heads, at most 32
- *     heads per kv head; strides of q, k and v multiples of 8 in [0, 2^22); fewer than 2^31 rows.
- *   adapter_linear_*: k % 8 == 0, m % 8 == 0, both <= 65536; 1 <= r <= 128; fewer than 2^31 rows.
+ *     heads per kv head (g); kv_heads <= 1024; strides of q, k and v multiples of 8 in [0, 2^22);
+ *     fewer than 2^31 rows; (n_q / (128 / g) + n_seq) * kv_heads < 2^24, in the backward also
+ *     (n_k / 128 + n_seq) * kv_heads < 2^24; a forward of at most 32 / g query rows a sequence on
+ *     average: (n_q / (32 / g) + n_seq + 7) * kv_heads < 2^26 instead.
+ *   adapter_linear_*: k % 8 == 0, m % 8 == 0, both <= 65536; 1 <= r <= 128; n_ad <= 65535; fewer than
+ *     2^31 rows; n / 32 + n_req < 2^24; (n / 256) * (m / 256) < 2^23, in the backward also with k
+ *     for m, and (k / 64 + m / 64) * n_ad * (r / 64) + (m / 64) * (k / 64) < 2^24 and
+ *     (n / 512 + n_req) * (k / 256 + m / 256) * (r / 64) < 2^24 (quotients rounded up, n / 512 down).
  *   rotary_apply: rot % 16 == 0, 16 <= rot <= dim, dim % 8 == 0, dim <= 1024; strides multiples of
  *     8; fewer than 2^31 rows.
  */

@@ -314,7 +314,7 @@ hpr_status run_loss(const uint16_t* q, int32_t nq, int32_t lq, const uint16_t* d
 // Shared checks of the attention calls; fills what both directions read.
 hpr_status check_attention(const hpr_attention* d, const uint16_t* q, const uint16_t* k,
                            const uint16_t* v, const int64_t* q_off, const int64_t* k_off,
-                           const int64_t* k_len, AttnArgs* out) {
+                           const int64_t* k_len, bool grads, AttnArgs* out) {
   if (!d) return fail(HPR_ERR_INVALID_ARG, "the description must be non-NULL");
   if (d->n_q < 0 || d->n_k < 0 || d->n_seq < 0)
     return fail(HPR_ERR_INVALID_ARG, "n_q, n_k and n_seq must be >= 0");
@@ -334,10 +334,9 @@ hpr_status check_attention(const hpr_attention* d, const uint16_t* q, const uint
                 d->dim);
   if (d->heads / d->kv_heads > kMaxGroup)
     return fail(HPR_ERR_UNSUPPORTED_SHAPE, "more than %d heads per kv head", kMaxGroup);
-  // (the grids hold up to a tile per row and kv head, and 64 splits of those below one round)
   if (d->n_q >= (int64_t(1) << 31) || d->n_k >= (int64_t(1) << 31) || d->kv_heads > 1024 ||
-      (d->n_q + d->n_k / 128 + d->n_seq) * d->kv_heads >= (int64_t(1) << 31))
-    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "too many rows or heads");
+      !attn_fits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads, grads))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "too many rows, sequences or heads");
   const int64_t strides[6] = {d->q_row, d->q_head, d->k_row, d->k_head, d->v_row, d->v_head};
   for (int64_t x : strides)
     if (x < 0 || x % 8 != 0 || x >= (int64_t(1) << 22))
@@ -382,7 +381,7 @@ hpr_status check_attention(const hpr_attention* d, const uint16_t* q, const uint
 hpr_status check_adapters(const uint16_t* x, int64_t n, int32_t k, const uint16_t* w, int32_t m,
                           const uint16_t* a, const uint16_t* b, int32_t r, int32_t n_ad,
                           const float* scale, const int64_t* req_off, const int32_t* adapter,
-                          int32_t n_req, int32_t dtype) {
+                          int32_t n_req, int32_t dtype, bool grads) {
   if (n < 0 || n_ad < 0 || n_req < 0)
     return fail(HPR_ERR_INVALID_ARG, "n, n_ad and n_req must be >= 0");
   if (k < 1 || m < 1 || r < 1)
@@ -393,9 +392,7 @@ hpr_status check_adapters(const uint16_t* x, int64_t n, int32_t k, const uint16_
     return fail(HPR_ERR_UNSUPPORTED_SHAPE,
                 "adapters need k and m multiples of 8 up to 65536 (k=%d, m=%d)", k, m);
   if (r > kMaxRank) return fail(HPR_ERR_UNSUPPORTED_SHAPE, "r=%d exceeds %d", r, kMaxRank);
-  // (the grids hold up to a workgroup per 32 x 64 outputs, 64 x 64 weights, or 512 x 256 x 64)
-  if (n >= (int64_t(1) << 31) || (n / 32 + 1) * (int64_t)((m > k ? m : k) / 64 + 1) >= (int64_t(1) << 31) ||
-      (n / 512 + n_req) * (int64_t)((m > k ? m : k) / 256 + 1) * 2 >= (int64_t(1) << 31) || n_ad > 65535)
+  if (n >= (int64_t(1) << 31) || n_ad > 65535 || !adapters_fit(n, k, m, r, n_ad, n_req, grads))
     return fail(HPR_ERR_UNSUPPORTED_SHAPE, "too many rows, requests or adapters");
   if ((n > 0 && !x) || !w || (n_ad > 0 && (!a || !b || !scale)) || (n_req > 0 && (!req_off || !adapter)))
     return fail(HPR_ERR_INVALID_ARG, "x, w, the adapters, their scales and the requests must be non-NULL");
@@ -622,7 +619,7 @@ hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const
                                 const int64_t* k_len, uint16_t* out, float* lse, void* ws,
                                 size_t ws_bytes, void* stream) {
   AttnArgs a;
-  hpr_status st = check_attention(d, q, k, v, q_off, k_off, k_len, &a);
+  hpr_status st = check_attention(d, q, k, v, q_off, k_off, k_len, false, &a);
   if (st != HPR_OK) return st;
   if (d->n_q == 0) return HPR_OK;
   if (!out) return fail(HPR_ERR_INVALID_ARG, "out must be non-NULL");
@@ -653,7 +650,7 @@ hpr_status packed_attention_bwd(const hpr_attention* d, const uint16_t* dout, co
                                 const int64_t* k_len, uint16_t* dq, uint16_t* dk, uint16_t* dv,
                                 void* ws, size_t ws_bytes, void* stream) {
   AttnArgs a;
-  hpr_status st = check_attention(d, q, k, v, q_off, k_off, k_len, &a);
+  hpr_status st = check_attention(d, q, k, v, q_off, k_off, k_len, true, &a);
   if (st != HPR_OK) return st;
   if (d->n_q > 0 && (!dout || !out || !lse))
     return fail(HPR_ERR_INVALID_ARG, "dout, out and lse must be non-NULL");
@@ -686,7 +683,8 @@ hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uin
                               const uint16_t* a, const uint16_t* b, int32_t r, int32_t n_ad,
                               const float* scale, const int64_t* req_off, const int32_t* adapter,
                               int32_t n_req, int32_t dtype, uint16_t* h, uint16_t* y, void* stream) {
-  hpr_status st = check_adapters(x, n, k, w, m, a, b, r, n_ad, scale, req_off, adapter, n_req, dtype);
+  hpr_status st =
+      check_adapters(x, n, k, w, m, a, b, r, n_ad, scale, req_off, adapter, n_req, dtype, false);
   if (st != HPR_OK) return st;
   if (n == 0) return HPR_OK;
   if (!h || !y) return fail(HPR_ERR_INVALID_ARG, "h and y must be non-NULL");
@@ -717,7 +715,8 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
                               const int32_t* adapter, int32_t n_req, int32_t dtype,
                               const uint16_t* h, uint16_t* dx, uint16_t* da, uint16_t* db, void* ws,
                               size_t ws_bytes, void* stream) {
-  hpr_status st = check_adapters(x, n, k, w, m, a, b, r, n_ad, scale, req_off, adapter, n_req, dtype);
+  hpr_status st =
+      check_adapters(x, n, k, w, m, a, b, r, n_ad, scale, req_off, adapter, n_req, dtype, true);
   if (st != HPR_OK) return st;
   if (n > 0 && (!dy || !h)) return fail(HPR_ERR_INVALID_ARG, "dy and h must be non-NULL");
   if (!aligned16(dy) || !aligned16(h) || !aligned16(dx) || !aligned16(da) || !aligned16(db))

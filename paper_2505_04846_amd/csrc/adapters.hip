@@ -869,6 +869,20 @@ int64_t adapter_outer_slots(int64_t n, int n_req, int k, int m) {
   return n_req == 0 ? 0 : n / adapter_outer_rows(n, k, m) + n_req;
 }
 
+// (The tiles of y are 256 x 256 by 512 threads in every call of this size, those of h 32 rows by 256.)
+bool adapters_fit(int64_t n, int k, int m, int r, int n_ad, int n_req, bool grads) {
+  auto blocks = [](int64_t size, int of) { return (size + of - 1) / of; };
+  const int64_t wide = k > m ? k : m;
+  if (!launch_fits(blocks(n, 256) * blocks(grads ? wide : m, 256), 512)) return false;
+  if (!launch_fits(blocks(n, 32) + n_req, 256)) return false;
+  if (!grads) return true;
+  const int64_t transposes =
+      blocks(m, 64) * blocks(k, 64) + n_ad * blocks(r, 64) * (blocks(k, 64) + blocks(m, 64));
+  const int64_t outer = adapter_outer_slots(n, n_req, k, m) * blocks(adapter_rank_pad(r), 64) *
+                        (blocks(k, 64 * kOuterWaves) + blocks(m, 64 * kOuterWaves));
+  return launch_fits(transposes, 256) && launch_fits(outer, 64 * kOuterWaves);
+}
+
 hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t stream) {
   if (a.n == 0 || a.n_req == 0) return hipSuccess;
   return a.f16 ? shrink<HalfF16>(a, h, stream) : shrink<HalfBf16>(a, h, stream);

@@ -1059,6 +1059,19 @@ int64_t attn_plan_key_tiles(int64_t n_k, int n_seq, int kv_heads) {
   return tiles * kv_heads >= kPlanFrom ? tiles : 0;
 }
 
+// (Split calls are of at most 2^22 workgroups, and the plans' and the join's launches smaller than these.)
+bool attn_fits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, bool grads) {
+  const int G = heads / kv_heads;
+  if (!grads) {
+    if (n_q == 0) return true;
+    const bool few = attn_shape(n_q, n_k, n_seq, G) == kFew;
+    const int64_t tiles = n_q / (fwd_slots(n_q, n_k, n_seq, G) / G) + n_seq;
+    return launch_fits((tiles + (few ? 7 : 0)) * kv_heads, few ? 64 : 256);
+  }
+  const int64_t q_tiles = n_q / (32 * kBwdWaves / G) + n_seq, k_tiles = n_k / kKeyTile + n_seq;
+  return launch_fits((q_tiles > k_tiles ? q_tiles : k_tiles) * kv_heads, 64 * kBwdWaves);
+}
+
 hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream) {
   if (a.n_q == 0) return hipSuccess;
   a.ts = fwd_slots(a.n_q, a.n_k, a.n_seq, a.G) / a.G;

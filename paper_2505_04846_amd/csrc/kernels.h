@@ -245,6 +245,11 @@ hipError_t launch_retrieval_metrics(const int64_t* idx, int nq, int64_t ld, int 
                                     const int64_t* pos, int32_t* ranks, double* out,
                                     hipStream_t stream);
 
+// A launch has fewer than 2^32 threads along each axis.
+inline bool launch_fits(int64_t workgroups, int threads) {
+  return workgroups < (int64_t(1) << 32) / threads;
+}
+
 // Attention over packed sequences (attention.hip, which states the definition).  Strides in
 // elements.  The launchers fill ts and tiles.
 struct AttnTile {      // a tile of query rows, or of key rows, and its sequence
@@ -280,6 +285,8 @@ int attn_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, in
 int64_t attn_plan_tiles(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
 int64_t attn_plan_q_tiles(int64_t n_q, int n_seq, int heads, int kv_heads);
 int64_t attn_plan_key_tiles(int64_t n_k, int n_seq, int kv_heads);
+// Whether every launch of the forward, or of the gradients, is one that can be made (launch_fits).
+bool attn_fits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, bool grads);
 hipError_t launch_attn_fwd(AttnArgs a, hipStream_t stream);
 hipError_t launch_attn_bwd(AttnArgs a, hipStream_t stream);
 
@@ -348,6 +355,8 @@ struct OuterArgs {
   uint32_t slots;
   int rows;
 };
+// Whether every launch of the forward, or of the gradients, is one that can be made (launch_fits).
+bool adapters_fit(int64_t n, int k, int m, int r, int n_ad, int n_req, bool grads);
 int adapter_outer_rows(int64_t n, int k, int m);  // rows of a slot
 int64_t adapter_outer_slots(int64_t n, int n_req, int k, int m);
 hipError_t launch_adapter_outer(const AdapterArgs& a, const OuterArgs& o, hipStream_t stream);
