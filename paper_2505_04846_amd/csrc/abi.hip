@@ -311,6 +311,14 @@ hpr_status run_loss(const uint16_t* q, int32_t nq, int32_t lq, const uint16_t* d
   return HPR_OK;
 }
 
+// Whether the attention calls take these sizes: outside, the size queries' products could overflow.
+bool attention_sizes(const hpr_attention* d) {
+  constexpr int64_t kRows = int64_t(1) << 31;
+  return d && d->n_q >= 0 && d->n_q < kRows && d->n_k >= 0 && d->n_k < kRows && d->n_seq >= 1 &&
+         d->kv_heads >= 1 && d->kv_heads <= 1024 && d->heads >= 1 && d->heads % d->kv_heads == 0 &&
+         d->heads / d->kv_heads <= kMaxGroup && d->dim >= 1 && d->dim <= 128;
+}
+
 // Shared checks of the attention calls; fills what both directions read.
 hpr_status check_attention(const hpr_attention* d, const uint16_t* q, const uint16_t* k,
                            const uint16_t* v, const int64_t* q_off, const int64_t* k_off,
@@ -594,9 +602,7 @@ hpr_status retrieval_metrics(const int64_t* topk_idx, int32_t nq, int32_t ld, in
 }
 
 size_t packed_attention_workspace_size(const hpr_attention* d) {
-  if (!d || d->n_q < 1 || d->n_seq < 1 || d->heads < 1 || d->kv_heads < 1 || d->dim < 1 ||
-      d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
-    return 0;
+  if (!attention_sizes(d) || d->n_q == 0) return 0;
   const int64_t splits = attn_splits(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads, d->dim);
   const size_t plan = align_up((size_t)attn_plan_tiles(d->n_q, d->n_k, d->n_seq, d->heads, d->kv_heads) *
                                sizeof(AttnTile));
@@ -606,9 +612,7 @@ size_t packed_attention_workspace_size(const hpr_attention* d) {
 }
 
 size_t packed_attention_bwd_workspace_size(const hpr_attention* d) {
-  if (!d || d->n_q < 0 || d->n_seq < 0 || d->heads < 1 || d->kv_heads < 1 ||
-      d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup)
-    return 0;
+  if (!attention_sizes(d)) return 0;
   return align_up((size_t)d->n_q * d->heads * sizeof(float)) +
          align_up((size_t)attn_plan_q_tiles(d->n_q, d->n_seq, d->heads, d->kv_heads) * sizeof(AttnTile)) +
          align_up((size_t)attn_plan_key_tiles(d->n_k, d->n_seq, d->kv_heads) * sizeof(AttnTile));
@@ -701,7 +705,9 @@ hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uin
 
 size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_t r, int32_t n_ad,
                                          int32_t n_req) {
-  if (n < 0 || k < 1 || m < 1 || r < 1 || n_ad < 0 || n_req < 0) return 0;
+  if (n < 0 || n >= (int64_t(1) << 31) || k < 1 || k > 65536 || m < 1 || m > 65536 || r < 1 ||
+      r > kMaxRank || n_ad < 0 || n_ad > 65535 || n_req < 0)
+    return 0;
   const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, k, m);
   return align_up((size_t)m * k * 2) + align_up((size_t)n_ad * r * k * 2) +
          align_up((size_t)n_ad * r * m * 2) + align_up((size_t)n * rp * 2) +
