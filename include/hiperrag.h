@@ -382,7 +382,8 @@ hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const
  * ds_ij = p_ij (<dout_i, v_j> - delta_i):
  *     dv_j = sum_i p_ij dout_i;  dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i
  * those of a kv head summed over its query heads.  p and ds are rounded to 16 bits as operands of the
- * second products; all sums are fp32 with a fixed order (no atomics).  Rows that see no key and keys
+ * second products, in fp16 times powers of two that keep them out of the range below 2^-14 (exactly
+ * undone in the fp32 sums); all sums are fp32 with a fixed order (no atomics).  Rows that see no key and keys
  * that no row sees get zeros.
  *
  *   dout [n_q, heads, dim] dense; out and lse as the forward wrote them

@@ -9,6 +9,7 @@ namespace hpr {
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 struct HalfBf16 {
+  static constexpr bool kNarrow = false;  // whether fp32 values may lie outside its exponents
   static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
   }
@@ -22,6 +23,7 @@ struct HalfBf16 {
 };
 
 struct HalfF16 {
+  static constexpr bool kNarrow = true;
   typedef _Float16 h2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(as_f16x8(a), as_f16x8(b), c, 0, 0, 0);

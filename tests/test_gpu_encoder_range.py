@@ -1,0 +1,94 @@
+"""fp16 gradients whose intermediate values lie below fp16's normal range, where the results do not: by
+norm against the fp64 oracle.
+
+The tolerance: every rounding of an operand is by at most u = 2^-11 of it, in no common direction, so
+that a gradient, a sum of many such terms, is off by less than u of its norm from each of the roundings
+(p or ds, the forward's output in delta; g or h), and 4 u hold all of them.  Added is what rounding the
+exact result to fp16 takes, which is more than that where the result itself is small."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_04846_amd as hpr
+from oracle import encoder as E
+from test_gpu_encoder import DEV, f64, gen, off
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -11
+
+
+def near(got, want, what):
+    got = f64(got)
+    assert np.isfinite(got).all(), f"{what}: not finite"
+    size = np.linalg.norm(want)
+    rounded = np.linalg.norm(want.astype(np.float16).astype(np.float64) - want)
+    err = np.linalg.norm(got - want)
+    assert size > 0 and err <= 4 * U * size + rounded, \
+        f"{what}: off by {err / size:.2e} of the norm, rounding alone by {rounded / size:.2e}"
+
+
+def half(t):
+    return t.to(torch.float16).to(DEV)
+
+
+# lengths, heads, kv heads, D, causal, window
+SHAPES = {"both_ways": ([2048], 2, 1, 64, False, 0), "causal": ([900, 1500], 4, 2, 128, True, 0),
+          "window": ([1700], 3, 1, 80, True, 600)}
+# standard deviation of dout; with "rows" it doubles every 100 rows, and that of v, from 2^-8, every 160
+# keys
+DOUT = {"1e-3": (1e-3, False), "1e-4": (1e-4, False), "1e-5": (1e-5, False), "300": (300.0, False),
+        "rows": (1e-5, True)}
+
+
+@pytest.mark.parametrize("large", ["q", "k"])
+@pytest.mark.parametrize("dout", DOUT)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_attention_gradients_of_any_size(shape, dout, large):
+    """Large keys keep dq in the normal range, and large queries dk; the scores are the same."""
+    lens, H, Hk, D, causal, window = SHAPES[shape]
+    std, grows = DOUT[dout]
+    g = gen(600)
+    n = sum(lens)
+    row = torch.arange(n, dtype=torch.float64)[:, None, None]
+    up = 16.0 if large == "q" else 1 / 16
+    q = half(torch.randn(n, H, D, generator=g, dtype=torch.float64) * up)
+    k = half(torch.randn(n, Hk, D, generator=g, dtype=torch.float64) / up)
+    v = half(torch.randn(n, Hk, D, generator=g, dtype=torch.float64)
+             * (2 ** (row / 160 - 8) if grows else 1))
+    do = half(torch.randn(n, H, D, generator=g, dtype=torch.float64)
+              * (std * 2 ** (row / 100) if grows else std))
+    o = off(lens)
+    how = dict(causal=causal, window=window)
+    r = hpr.packed_attention_fwd(q, k, v, o, **how)
+    b = hpr.packed_attention_bwd(do, q, k, v, r["out"], r["lse"], o, **how)
+    host = o.cpu().numpy()
+    want = E.packed_attention(f64(q), f64(k), f64(v), host, host, None, causal, window, D ** -0.5,
+                              dout=f64(do))
+    for name in ("dq", "dk", "dv"):
+        near(b[name], want[name], name)
+
+
+def test_attention_gradients_of_keys_that_get_little_attention():
+    """Keys whose probabilities are below 2^-22 in every row."""
+    n, D = 1024, 64
+    g = gen(601)
+    q, k = [torch.randn(n, 1, D, generator=g, dtype=torch.float64) * 0.5 for _ in range(2)]
+    q[..., 0] = 24.0
+    k[..., 0] = 0.0
+    far = torch.arange(n) % 2 == 1
+    k[far, :, 0] = -3.0
+    q, k = half(q), half(k)
+    v = half(torch.randn(n, 1, D, generator=g, dtype=torch.float64))
+    do = half(torch.randn(n, 1, D, generator=g, dtype=torch.float64) * 4096)
+    o = off([n])
+    r = hpr.packed_attention_fwd(q, k, v, o, causal=False)
+    b = hpr.packed_attention_bwd(do, q, k, v, r["out"], r["lse"], o, causal=False)
+    want = E.packed_attention(f64(q), f64(k), f64(v), [0, n], [0, n], None, False, 0, D ** -0.5,
+                              dout=f64(do))
+    far = far.numpy()
+    for rows in (far, ~far):
+        for name in ("dk", "dv"):
+            near(b[name][torch.from_numpy(rows).to(DEV)], want[name][rows], name)
+    near(b["dq"], want["dq"], "dq")
