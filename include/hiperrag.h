@@ -96,7 +96,8 @@ typedef int32_t hpr_status;
  *   adapter_linear_*: k % 8 == 0, m % 8 == 0, both <= 65536; 1 <= r <= 128; n_ad <= 65535; fewer than
  *     2^31 rows; n / 32 + n_req < 2^24; (n / 256) * (m / 256) < 2^23, in the backward also with k
  *     for m, and (k / 64 + m / 64) * n_ad * (r / 64) + (m / 64) * (k / 64) < 2^24 and
- *     (n / 512 + n_req) * (k / 256 + m / 256) * (r / 64) < 2^24 (quotients rounded up, n / 512 down).
+ *     (n / 512 + s) * (k / 256 + m / 256) * (r / 64) < 2^24 with s the fewer of n_req
+ *     and n_ad + 12288 (quotients rounded up, n / 512 down).
  *   rotary_apply: rot % 16 == 0, 16 <= rot <= dim, dim % 8 == 0, dim <= 1024; strides multiples of
  *     8; fewer than 2^31 rows.
  */
@@ -423,9 +424,10 @@ hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uin
  *
  *     g[t] = scale[i] B[i]^T dy[t]     dx[t] = W^T dy[t] + A[i]^T g[t]
  *     dA[i] = sum_t g[t] x[t]^T        dB[i] = sum_t dy[t] h[t]^T      over the adapter's rows
- * g is rounded once to 16 bits; the sums are fp32, in the order of the rows' blocks (no atomics).
- * Adapters without a row get zeros.  dx, da and db may each be NULL.
- *   ws     workspace of adapter_linear_bwd_workspace_size(...) bytes
+ * g is rounded once to 16 bits; the sums are fp32, in the order of the adapter's rows in fixed blocks
+ * (bits repeat).  Adapters without a row get zeros.  dx, da and db may each be NULL.
+ *   ws     workspace of adapter_linear_bwd_workspace_size(...) bytes: the transposed weights, g, and
+ *          partial sums that follow the rows and, past 12 MB, the fewer of requests and adapters
  * ------------------------------------------------------------------------------------------- */
 size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_t r, int32_t n_ad,
                                          int32_t n_req);

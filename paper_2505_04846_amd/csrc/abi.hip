@@ -708,11 +708,14 @@ size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_
   if (n < 0 || n >= (int64_t(1) << 31) || k < 1 || k > 65536 || m < 1 || m > 65536 || r < 1 ||
       r > kMaxRank || n_ad < 0 || n_ad > 65535 || n_req < 0)
     return 0;
-  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, k, m);
+  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, n_ad, k, m, r);
   return align_up((size_t)m * k * 2) + align_up((size_t)n_ad * r * k * 2) +
          align_up((size_t)n_ad * r * m * 2) + align_up((size_t)n * rp * 2) +
          align_up(slots * rp * k * sizeof(float)) + align_up(slots * rp * m * sizeof(float)) +
-         align_up(2 * slots * sizeof(int32_t));
+         align_up(2 * slots * sizeof(int32_t)) +
+         (adapter_ordered(n, n_req, n_ad, k, m, r)
+              ? align_up((size_t)(n_ad + 1) * sizeof(int64_t)) + align_up((size_t)n * sizeof(int32_t))
+              : 0);
 }
 
 hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, int32_t k,
@@ -731,7 +734,7 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   if (!ws || ws_bytes < need)
     return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, k, m);
+  const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, n_ad, k, m, r);
   Carver c(ws);
   uint16_t* wt = c.take<uint16_t>((size_t)m * k * 2);
   uint16_t* at = c.take<uint16_t>((size_t)n_ad * r * k * 2);
@@ -740,6 +743,11 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   float* part_a = c.take<float>(slots * rp * k * sizeof(float));
   float* part_b = c.take<float>(slots * rp * m * sizeof(float));
   int32_t* slot_adapter = c.take<int32_t>(2 * slots * sizeof(int32_t));
+  AdapterOrder order = {nullptr, nullptr};
+  if (adapter_ordered(n, n_req, n_ad, k, m, r)) {
+    order.off = c.take<int64_t>((size_t)(n_ad + 1) * sizeof(int64_t));
+    order.list = c.take<int32_t>((size_t)n * sizeof(int32_t));
+  }
   // g and dx: the forward's kernels on (dy, W^T, B^T, A^T)
   const AdapterArgs f = {x, w, a, b, scale, req_off, adapter, n, k, m, r, n_ad, n_req,
                          dtype == HPR_F16};
@@ -750,23 +758,27 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   t.b = at;
   t.k = m;
   t.m = k;
+  const bool need_g = n > 0 && (dx || da), need_order = order.list && (da || db);
   hipError_t e = hipSuccess;
-  if (n > 0 && (dx || da)) {
+  if (need_g || need_order)
     e = timed("adapter_transpose", s, [&] {
-      const TransposeArgs q = {{{w, wt, dx ? 1 : 0, m, k, 0},
-                                {a, at, dx ? n_ad : 0, r, k, 0},
-                                {b, bt, n_ad, m, r, 0}}};
-      return launch_transpose(q, s);
+      const TransposeArgs q = {{{w, wt, need_g && dx ? 1 : 0, m, k, 0},
+                                {a, at, need_g && dx ? n_ad : 0, r, k, 0},
+                                {b, bt, need_g ? n_ad : 0, m, r, 0}},
+                               need_order ? order : AdapterOrder{nullptr, nullptr},
+                               0};
+      return launch_adapter_prepare(f, q, s);
     });
-    if (e == hipSuccess) e = timed("adapter_shrink", s, [&] { return launch_adapter_shrink(t, g, s); });
+  if (e == hipSuccess && need_g) {
+    e = timed("adapter_shrink", s, [&] { return launch_adapter_shrink(t, g, s); });
     if (e == hipSuccess && dx)
       e = timed("adapter_expand", s, [&] { return launch_adapter_expand(t, g, dx, s); });
-    if (e != hipSuccess) return hip_fail(e, "adapter gradient launch");
   }
+  if (e != hipSuccess) return hip_fail(e, "adapter gradient launch");
   if (da || db)
     e = timed("adapter_outer", s, [&] {
       const OuterArgs o = {{{g, x, k, 0, part_a, da, 0, 0}, {h, dy, m, 1, part_b, db, 0, 0}},
-                           slot_adapter, 0, 0};
+                           order, slot_adapter, 0, 0};
       return launch_adapter_outer(f, o, s);
     });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "adapter gradient launch");

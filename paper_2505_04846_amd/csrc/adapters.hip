@@ -6,7 +6,7 @@
 // and for g_t = scale_a B_a^T dy_t:
 //   dx_t = W^T dy_t + A_a^T g_t,   dA_a = sum_t g_t x_t^T,   dB_a = sum_t dy_t h_t^T.
 // dx is the same operation on (dy, W^T, B^T, A^T), so the gradients run the forward's two kernels
-// on transposed weights (transpose_kernel), and dA and dB are one kernel, outer_kernel, on (g, x)
+// on transposed weights (prepare_kernel), and dA and dB are one kernel, outer_kernel, on (g, x)
 // and (h, dy).
 #include "common.h"
 #include "half.h"
@@ -23,13 +23,14 @@ __device__ __attribute__((aligned(16))) const uint32_t kZero16[4] = {0u, 0u, 0u,
 struct Rows {
   int64_t r0, r1;
 };
-__device__ __forceinline__ Rows rows_of(const AdapterArgs& a, int s) {
+__device__ __forceinline__ Rows rows_of(const int64_t* off, int64_t n, int s) {
   auto clamp = [](int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); };
   Rows r;
-  r.r0 = clamp(a.off[s], 0, a.n);
-  r.r1 = clamp(a.off[s + 1], r.r0, a.n);
+  r.r0 = clamp(off[s], 0, n);
+  r.r1 = clamp(off[s + 1], r.r0, n);
   return r;
 }
+__device__ __forceinline__ Rows rows_of(const AdapterArgs& a, int s) { return rows_of(a.off, a.n, s); }
 // Adapter of request s, -1 for none (or one out of range).
 __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int s) {
   const int ad = a.adapter[s];
@@ -542,15 +543,120 @@ __global__ __launch_bounds__(kFewThreads<BM>) void expand_few_kernel(AdapterArgs
   expand_few<T, BM>(a, h, y, n_m);
 }
 
+// ---- rows by adapter --------------------------------------------------------------------------
+
+// A workgroup for kOrderAdapters adapters: counts their rows, places every request of theirs behind the
+// earlier ones of its adapter, and writes down its rows.  Four waves take a run of requests each, 64 at a
+// time.  The only atomics add integers, whose sum has no order.  (Whatever the offsets hold, nothing is
+// written past n; what then stays unwritten is clamped where it is read.)
+constexpr int kOrderAdapters = 256;
+constexpr int kOrderLds = 4 * kOrderAdapters + 8;  // words
+
+__device__ __forceinline__ void order_rows(const AdapterArgs& a, const AdapterOrder& to, uint32_t* lds, int a0) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t* sums = lds + 4 * kOrderAdapters;
+  uint32_t* count = lds + wave * kOrderAdapters;  // rows of the wave's requests, then where the next ones go
+#pragma unroll
+  for (int w = 0; w < 4; ++w) lds[w * kOrderAdapters + threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t chunks = (a.n_req + 63) / 64;
+  const int c0 = (int)(chunks * wave / 4), c1 = (int)(chunks * (wave + 1) / 4);
+  struct Request {
+    int first;
+    uint32_t rows;
+    int ad;  // of the workgroup's, -1: another or none
+    bool below;
+  };
+  auto request = [&](int c) {
+    const int s = 64 * c + lane;
+    Request r = {0, 0u, -1, false};
+    if (s >= a.n_req) return r;
+    const Rows R = rows_of(a, s);
+    const int ad = adapter_of(a, s);
+    r.first = (int)R.r0;
+    r.rows = (uint32_t)(R.r1 - R.r0);
+    r.below = ad >= 0 && ad < a0;
+    if (ad >= a0 && ad < a0 + kOrderAdapters) r.ad = ad - a0;
+    return r;
+  };
+  uint32_t below = 0;  // rows of lower adapters
+  for (int c = c0; c < c1; ++c) {
+    const Request r = request(c);
+    if (r.below) below += r.rows;
+    if (r.ad >= 0) atomicAdd(count + r.ad, r.rows);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) below += (uint32_t)__shfl_xor((int)below, d);
+  if (lane == 0) sums[wave] = below;
+  __syncthreads();
+  uint32_t mine[4], total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) total += mine[w] = lds[w * kOrderAdapters + threadIdx.x];
+  uint32_t upto = total;  // with the lower lanes'
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t v = (uint32_t)__shfl_up((int)upto, d);
+    if (lane >= d) upto += v;
+  }
+  if (lane == 63) sums[4 + wave] = upto;
+  __syncthreads();
+  uint32_t start = upto - total;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) start += sums[w] + (w < wave ? sums[4 + w] : 0u);
+  const int ad = a0 + (int)threadIdx.x;
+  auto in_n = [&](uint32_t x) { return (int64_t)x < a.n ? (int64_t)x : a.n; };
+  if (ad < a.n_ad) to.off[ad] = in_n(start);
+  if (ad == a.n_ad - 1) to.off[a.n_ad] = in_n(start + total);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    lds[w * kOrderAdapters + threadIdx.x] = start;
+    start += mine[w];
+  }
+  __syncthreads();
+  for (int c = c0; c < c1; ++c) {
+    const Request r = request(c);
+    const bool in = r.ad >= 0 && r.rows > 0;
+    if (!__any(in)) continue;
+    uint32_t at = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i)  // rows of earlier requests of the 64 with this one's adapter
+      if (__builtin_amdgcn_readlane(r.ad, i) == r.ad && i < lane)
+        at += (uint32_t)__builtin_amdgcn_readlane((int)r.rows, i);
+    if (in) {
+      at += count[r.ad];
+      atomicAdd(count + r.ad, r.rows);
+    }
+    constexpr uint32_t kOwn = 16;  // rows that a lane writes by itself
+    const bool few = in && r.rows <= kOwn;
+    for (uint32_t j = 0; j < kOwn && __any(few && j < r.rows); ++j)
+      if (few && j < r.rows && (int64_t)at + j < a.n) to.list[at + j] = r.first + (int)j;
+    for (unsigned long long left = __ballot(in && !few); left; left &= left - 1) {
+      const int i = __builtin_ctzll(left);
+      const int64_t p = (uint32_t)__builtin_amdgcn_readlane((int)at, i);
+      const int first = __builtin_amdgcn_readlane(r.first, i);
+      int64_t n = (uint32_t)__builtin_amdgcn_readlane((int)r.rows, i);
+      if (n > a.n - p) n = a.n - p;
+      for (int64_t j = lane; j < n; j += 64) to.list[p + j] = first + (int)j;
+    }
+  }
+}
+
 // ---- transposed weights -----------------------------------------------------------------------
 
 // Up to three batches of matrices in one launch, a 64 x 64 tile per workgroup: whole 16-byte pieces of
 // rows in and out where both sizes are multiples of 8, values otherwise.  Bound by memory and its launch: W of
 // 4096 x 4096 and an adapter of rank 64, 17.5 us (69 MB, 3.9 TB/s).
-__global__ __launch_bounds__(256) void transpose_kernel(TransposeArgs a) {
+__global__ __launch_bounds__(256) void prepare_kernel(AdapterArgs g, TransposeArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t tile[64][72];
   int w = 0;
   uint32_t b = blockIdx.x;
+  if (b < a.order_blocks) {
+    static_assert(sizeof(tile) >= 4 * kOrderLds, "the counts fit the tile");
+    order_rows(g, a.order, reinterpret_cast<uint32_t*>(tile), (int)b * kOrderAdapters);
+    return;
+  }
+  b -= a.order_blocks;
   while (w < 2 && b >= a.job[w].blocks) b -= a.job[w++].blocks;
   const TransposeJob& q = a.job[w];
   const int rows = q.rows, cols = q.cols;
@@ -590,13 +696,14 @@ __global__ __launch_bounds__(256) void transpose_kernel(TransposeArgs a) {
 
 // ---- dA, dB -----------------------------------------------------------------------------------
 
-// Partial sums over up to o.rows rows of one request: part[slot][j][c] = sum_t L[t,j] M[t,c],
-// 64 ranks and 256 columns per workgroup, 64 columns per wave; rows in tiles of 64 through two LDS
-// stages, both operands read by columns.  dA and dB go in one launch.  Bound by x and dy: 13,057 rows of
+// Partial sums over up to o.rows rows of one request, or, in calls of many requests, of one adapter by the
+// order of order_rows (LIST), so that the parts do not grow with the requests: part[slot][j][c] = sum_t
+// L[t,j] M[t,c], 64 ranks and 256 columns per workgroup, 64 columns per wave; rows in tiles of 64 through two
+// LDS stages, both operands read by columns.  dA and dB go in one launch.  Bound by x and dy: 13,057 rows of
 // 4096 each, rank 64: 45 us (214 MB and 27 MB of parts, 5.4 TB/s).
 constexpr int kOuterWaves = 4;
 
-template <class T>
+template <class T, bool LIST>
 __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs a, OuterArgs o) {
   constexpr int kTile = 64 * 128;  // 64 rows of 64 values
   constexpr int kStage = (1 + kOuterWaves) * kTile;
@@ -612,11 +719,12 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
   const uint32_t n_cb = (uint32_t)(cols + 64 * kOuterWaves - 1) / (64u * kOuterWaves);
   const int cb = (int)(b0 % n_cb), jb = (int)(b0 / n_cb % n_jb);
   const uint32_t slot = b0 / n_cb / n_jb;
-  const int s = find_seq(a.off, a.n_req, o.rows, slot);
-  const Rows R = rows_of(a, s);
+  const int64_t* off = LIST ? o.order.off : a.off;
+  const int s = find_seq(off, LIST ? a.n_ad : a.n_req, o.rows, slot);
+  const Rows R = rows_of(off, a.n, s);
   const int64_t first =
       R.r0 + ((int64_t)slot - ((uint32_t)R.r0 / (uint32_t)o.rows + (uint32_t)s)) * o.rows;
-  const int ad = first >= R.r0 && first < R.r1 ? adapter_of(a, s) : -1;
+  const int ad = first >= R.r0 && first < R.r1 ? LIST ? s : adapter_of(a, s) : -1;
   if (cb == 0 && jb == 0 && threadIdx.x == 0) o.slot_adapter[which * o.slots + slot] = ad;
   if (ad < 0) return;
   const int64_t end = R.r1 < first + o.rows ? R.r1 : first + o.rows;
@@ -632,9 +740,14 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   const TileReads<64> rd(lane);
   const int lr = lane >> 3;  // row of a wave load, 8 rows of 8 chunks
+  // With a list, a lane holds the row of the tile that is its own number, read a stage ahead.
+  auto rows_at = [&](int64_t t) {
+    const uint32_t r = LIST ? (uint32_t)o.order.list[t + lane < end ? t + lane : end - 1] : 0u;
+    return (int)(r < (uint32_t)a.n ? r : (uint32_t)a.n - 1u);
+  };
   // rows past the end are zero in both tiles; columns past the last repeat it, and their sums are
   // not stored
-  auto issue = [&](int buf, int64_t t) {
+  auto issue = [&](int buf, int64_t t, int listed) {
     const uint32_t st = LDS_ADDRESS(smem) + buf * kStage;
     const int n = end - t < 64 ? (int)(end - t) : 64;
 #pragma unroll
@@ -642,7 +755,8 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
       const int r = 8 * j + lr;
       int cc = c0 + 8 * ((lane & 7) ^ swz<64>(r));
       if (cc >= cols) cc = cols - 8;
-      load_lds16(r < n ? (const void*)(q.m + (t + r) * cols + cc) : (const void*)kZero16,
+      const int64_t row = LIST ? (int64_t)__shfl(listed, r) : t + r;
+      load_lds16(r < n ? (const void*)(q.m + row * cols + cc) : (const void*)kZero16,
                  st + (1 + wave) * kTile + j * 1024);
     }
 #pragma unroll
@@ -650,18 +764,23 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
       const int r = 8 * (2 * wave + j) + lr;
       int cc = j0 + 8 * ((lane & 7) ^ swz<64>(r));
       if (cc >= rp) cc = rp - 8;
-      load_lds16(r < n ? (const void*)(q.l + (t + r) * rp + cc) : (const void*)kZero16,
+      const int64_t row = LIST ? (int64_t)__shfl(listed, r) : t + r;
+      load_lds16(r < n ? (const void*)(q.l + row * rp + cc) : (const void*)kZero16,
                  st + (2 * wave + j) * 1024);
     }
   };
-  issue(0, first);
+  issue(0, first, rows_at(first));
+  int next = rows_at(first + 64);
   int buf = 0;
 #pragma unroll 1
   for (int64_t t = first; t < end; t += 64, buf ^= 1) {
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     sync_lds();  // the stage has landed, and nobody reads the other any more
-    if (t + 64 < end) issue(buf ^ 1, t + 64);
+    if (t + 64 < end) {
+      issue(buf ^ 1, t + 64, next);
+      next = rows_at(t + 128);
+    }
     const unsigned char* ls = smem + buf * kStage;
     const unsigned char* ms = ls + (1 + wave) * kTile;
 #pragma unroll
@@ -833,7 +952,7 @@ template <class T>
 hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
   const int rp = adapter_rank_pad(a.r), n_jb = (rp + 63) / 64;
   o.rows = adapter_outer_rows(a.n, a.k, a.m);
-  o.slots = (uint32_t)adapter_outer_slots(a.n, a.n_req, a.k, a.m);
+  o.slots = (uint32_t)adapter_outer_slots(a.n, a.n_req, a.n_ad, a.k, a.m, a.r);
   uint32_t blocks = 0, join_blocks = 0;
   for (OuterJob& q : o.job) {
     q.blocks = q.join_blocks = 0;
@@ -847,10 +966,13 @@ hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (blocks > 0) {
     constexpr int lds = 2 * (1 + kOuterWaves) * 64 * 128;
-    e = allow_lds((const void*)outer_kernel<T>, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((outer_kernel<T>), dim3(blocks), dim3(64 * kOuterWaves), lds, s, a, o);
-    e = hipGetLastError();
+    auto run = [&](auto kernel) {
+      const hipError_t f = allow_lds((const void*)kernel, lds);
+      if (f != hipSuccess) return f;
+      hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * kOuterWaves), lds, s, a, o);
+      return hipGetLastError();
+    };
+    e = adapter_ordered(a.n, a.n_req, a.n_ad, a.k, a.m, a.r) ? run(outer_kernel<T, true>) : run(outer_kernel<T, false>);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL((outer_join_kernel<T>), dim3(join_blocks, (unsigned)a.n_ad), dim3(256), 0, s, a, o);
@@ -865,8 +987,22 @@ hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
 // rows (312) 151 (156), 13,057 rows (96) 67 (63).
 int adapter_outer_rows(int64_t n, int k, int m) { return (n / 1024) * ((k + m) / 256) >= 300 ? 1024 : 512; }
 
-int64_t adapter_outer_slots(int64_t n, int n_req, int k, int m) {
-  return n_req == 0 ? 0 : n / adapter_outer_rows(n, k, m) + n_req;
+// Slots of one request each where that is not many: the order takes 9 us (the prepare kernel's and the wait
+// for the list in the outer kernel's), which the parts of the slots that it saves outweigh from 12 MB on.  All of
+// the gradients and the forward, us ordered (by request): 768 -> 768, rank 8, 4 adapters, 64 requests (6 MB) 48
+// (47), 256 (25 MB) 56 (66), 1,024 of 2 rows 86 (130); 768 -> 2304, 37 requests of 5 (6 MB) 60 (51); 4096 -> 4096,
+// rank 16, 32 requests of 4 adapters (15 MB) 88 (94), 64 of 16 in 13,063 rows (25 MB) 919 (918), 4,096 of one row,
+// 8 adapters (2.1 GB) 596 (1,980).
+constexpr int64_t kOrderFrom = 12 << 20;  // bytes
+
+bool adapter_ordered(int64_t n, int n_req, int n_ad, int k, int m, int r) {
+  if (n == 0 || n_ad == 0 || n_req <= n_ad) return false;
+  return (int64_t)(n_req - n_ad) * adapter_rank_pad(r) * (k + m) * (int64_t)sizeof(float) >= kOrderFrom;
+}
+
+int64_t adapter_outer_slots(int64_t n, int n_req, int n_ad, int k, int m, int r) {
+  if (n == 0 || n_req == 0 || n_ad == 0) return 0;
+  return n / adapter_outer_rows(n, k, m) + (adapter_ordered(n, n_req, n_ad, k, m, r) ? n_ad : n_req);
 }
 
 // (The tiles of y are 256 x 256 by 512 threads in every call of this size, those of h 32 rows by 256.)
@@ -876,11 +1012,11 @@ bool adapters_fit(int64_t n, int k, int m, int r, int n_ad, int n_req, bool grad
   if (!launch_fits(blocks(n, 256) * blocks(grads ? wide : m, 256), 512)) return false;
   if (!launch_fits(blocks(n, 32) + n_req, 256)) return false;
   if (!grads) return true;
-  const int64_t transposes =
-      blocks(m, 64) * blocks(k, 64) + n_ad * blocks(r, 64) * (blocks(k, 64) + blocks(m, 64));
-  const int64_t outer = adapter_outer_slots(n, n_req, k, m) * blocks(adapter_rank_pad(r), 64) *
+  const int64_t prepare =
+      blocks(n_ad, kOrderAdapters) + blocks(m, 64) * blocks(k, 64) + n_ad * blocks(r, 64) * (blocks(k, 64) + blocks(m, 64));
+  const int64_t outer = adapter_outer_slots(n, n_req, n_ad, k, m, r) * blocks(adapter_rank_pad(r), 64) *
                         (blocks(k, 64 * kOuterWaves) + blocks(m, 64 * kOuterWaves));
-  return launch_fits(transposes, 256) && launch_fits(outer, 64 * kOuterWaves);
+  return launch_fits(prepare, 256) && launch_fits(outer, 64 * kOuterWaves);
 }
 
 hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t stream) {
@@ -894,14 +1030,15 @@ hipError_t launch_adapter_expand(const AdapterArgs& a, const uint16_t* h, uint16
   return a.f16 ? expand<HalfF16>(a, h, y, stream) : expand<HalfBf16>(a, h, y, stream);
 }
 
-hipError_t launch_transpose(TransposeArgs a, hipStream_t stream) {
-  int64_t blocks = 0;
+hipError_t launch_adapter_prepare(const AdapterArgs& g, TransposeArgs a, hipStream_t stream) {
+  a.order_blocks = a.order.list ? (uint32_t)((g.n_ad + kOrderAdapters - 1) / kOrderAdapters) : 0u;
+  int64_t blocks = a.order_blocks;
   for (TransposeJob& q : a.job) {
     q.blocks = (uint32_t)(q.count * ((q.rows + 63) / 64) * ((q.cols + 63) / 64));
     blocks += q.blocks;
   }
   if (blocks == 0) return hipSuccess;
-  hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(prepare_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, g, a);
   return hipGetLastError();
 }
 

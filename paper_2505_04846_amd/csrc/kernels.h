@@ -324,8 +324,14 @@ hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t 
 // y[n, m] = x W^T + h B_a^T
 hipError_t launch_adapter_expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y,
                                  hipStream_t stream);
-// out[i] = in[i]^T of `count` matrices [rows, cols], three batches in one launch (the launcher fills
-// `blocks`; count 0: none).
+// The order of the rows by adapter, for launch_adapter_outer: list[off[i]..off[i+1]] are the rows with adapter
+// i, in their order.  Workspace of n and n_ad + 1 entries; null: none.
+struct AdapterOrder {
+  int64_t* off;
+  int32_t* list;
+};
+// out[i] = in[i]^T of `count` matrices [rows, cols], three batches in one launch, and the order (the launcher
+// fills `blocks` and `order_blocks`; count 0: none).
 struct TransposeJob {
   const uint16_t* in;
   uint16_t* out;
@@ -335,9 +341,11 @@ struct TransposeJob {
 };
 struct TransposeArgs {
   TransposeJob job[3];
+  AdapterOrder order;
+  uint32_t order_blocks;
 };
-hipError_t launch_transpose(TransposeArgs a, hipStream_t stream);
-// Sums over the rows of each adapter's requests, l[n, rank_pad] and m[n, cols], up to two at a time:
+hipError_t launch_adapter_prepare(const AdapterArgs& a, TransposeArgs t, hipStream_t stream);
+// Sums over the rows of each adapter, l[n, rank_pad] and m[n, cols], up to two at a time:
 //   out[a][j][c] = sum l[t, j] m[t, c], j < r (transposed: out[a][c][j]; out null: none)
 // through parts of slots * rank_pad * cols floats and slot_adapter, 2 * slots words, slots =
 // adapter_outer_slots.  The launcher fills rows, slots, blocks and join_blocks.
@@ -351,6 +359,7 @@ struct OuterJob {
 };
 struct OuterArgs {
   OuterJob job[2];
+  AdapterOrder order;  // by launch_adapter_prepare, where adapter_ordered
   int32_t* slot_adapter;
   uint32_t slots;
   int rows;
@@ -358,7 +367,9 @@ struct OuterArgs {
 // Whether every launch of the forward, or of the gradients, is one that can be made (launch_fits).
 bool adapters_fit(int64_t n, int k, int m, int r, int n_ad, int n_req, bool grads);
 int adapter_outer_rows(int64_t n, int k, int m);  // rows of a slot
-int64_t adapter_outer_slots(int64_t n, int n_req, int k, int m);
+// Whether the rows are ordered by adapter first.
+bool adapter_ordered(int64_t n, int n_req, int n_ad, int k, int m, int r);
+int64_t adapter_outer_slots(int64_t n, int n_req, int n_ad, int k, int m, int r);
 hipError_t launch_adapter_outer(const AdapterArgs& a, const OuterArgs& o, hipStream_t stream);
 
 // Calibration (calibration.hip): a pure-MFMA kernel of mfma_calibration_waves(n_cu) waves, each

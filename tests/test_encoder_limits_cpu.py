@@ -29,8 +29,8 @@ def test_attention(call, desc, status):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(n=1 << 26, n_req=(1 << 24) - (1 << 21), k=8, m=8), OUTSIDE),
-    (dict(n=32, n_req=(1 << 23) - 1, k=8, m=8), NO_WORKSPACE),
-    (dict(n=32, n_req=1 << 23, k=8, m=8), OUTSIDE),
+    (dict(n=32, n_req=(1 << 24) - 2, k=8, m=8), NO_WORKSPACE),
+    (dict(n=32, n_req=(1 << 24) - 1, k=8, m=8), OUTSIDE),
     (dict(n=1 << 24, k=1 << 15, m=8), OUTSIDE),
     (dict(n=(1 << 24) - 256, k=1 << 15, m=8), NO_WORKSPACE),
     (dict(n=32, n_ad=1 << 14, k=1 << 16, m=8, r=1), OUTSIDE),
@@ -45,3 +45,15 @@ def test_adapter_gradients(kw, status):
 def test_adapter_forward(kw):
     assert _adapters("fwd", **kw) == OUTSIDE
     assert hpr.lib().hpr_last_error()
+
+
+@pytest.mark.parametrize("n,r,n_ad,n_req", [(13_000, 64, 1, 13_000), (13_057, 64, 1, 216),
+                                            (4_096, 16, 8, 4_096), (100_000, 64, 4, 100_000)])
+def test_adapter_workspace_does_not_grow_with_requests(n, r, n_ad, n_req):
+    """The partial sums follow the rows and the adapters: less than twice what one request per adapter
+    takes, and 4 bytes a row."""
+    size = hpr.lib().adapter_linear_bwd_workspace_size
+    assert size(n, 4096, 4096, r, n_ad, n_req) <= 2 * size(n, 4096, 4096, r, n_ad, n_ad) + 4 * n
+    # ... and with the requests where they are the fewer
+    few = size(n, 4096, 4096, r, 1000, 1)
+    assert size(n, 4096, 4096, r, 1000, 2) - few < 16 * r * 8192
