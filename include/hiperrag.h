@@ -96,7 +96,7 @@ typedef int32_t hpr_status;
  *   adapter_linear_*: k % 8 == 0, m % 8 == 0, both <= 65536; 1 <= r <= 128; n_ad <= 65535; fewer than
  *     2^31 rows; n / 32 + n_req < 2^24; (n / 256) * (m / 256) < 2^23, in the backward also with k
  *     for m, and (k / 64 + m / 64) * n_ad * (r / 64) + (m / 64) * (k / 64) < 2^24 and
- *     (n / 512 + s) * (k / 256 + m / 256) * (r / 64) < 2^24 with s the fewer of n_req
+ *     (n / 512 + s) * (k / 256 + m / 256) * (r / 32) < 2^24 with s the fewer of n_req
  *     and n_ad + 12288 (quotients rounded up, n / 512 down).
  *   rotary_apply: rot % 16 == 0, 16 <= rot <= dim, dim % 8 == 0, dim <= 1024; strides multiples of
  *     8; fewer than 2^31 rows.
@@ -405,8 +405,8 @@ hpr_status packed_attention_bwd(const hpr_attention* d, const uint16_t* dout, co
  * may hold rows of many requests, each with its own adapter.  Row t of request s (req_off[s] <= t <
  * req_off[s+1]) with adapter i = adapter[s] (negative, or not below n_ad: none):
  *     h[t] = scale[i] A[i] x[t]        y[t] = W x[t] + B[i] h[t]
- * Arithmetic: 16-bit products accumulated in fp32 (MFMA), h rounded once to 16 bits, y once.  Sums
- * have a fixed order.  Requests may be empty; rows of no request get W x.
+ * Arithmetic: 16-bit products accumulated in fp32 (MFMA), h rounded once to 16 bits, y once (in fp16 an h
+ * past 65504 is infinite, and one below 2^-14 rounded by up to 2^-25, as y is).  Sums have a fixed order.  Requests may be empty; rows of no request get W x.
  *
  *   x [n, k], W [m, k], A [n_ad, r, k], B [n_ad, m, r]: dtype HPR_BF16 or HPR_F16, dense
  *   scale fp32 [n_ad]; req_off int64 [n_req + 1] (starts at 0, never falls, ends at n); adapter
@@ -424,8 +424,10 @@ hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uin
  *
  *     g[t] = scale[i] B[i]^T dy[t]     dx[t] = W^T dy[t] + A[i]^T g[t]
  *     dA[i] = sum_t g[t] x[t]^T        dB[i] = sum_t dy[t] h[t]^T      over the adapter's rows
- * g is rounded once to 16 bits; the sums are fp32, in the order of the adapter's rows in fixed blocks
- * (bits repeat).  Adapters without a row get zeros.  dx, da and db may each be NULL.
+ * g is rounded once to 16 bits; in fp16 the sums of dA and dB read g and h (formed again from x) in two
+ * numbers, so that they lose nothing below fp16's normal range.  The sums are fp32, in the order of the
+ * adapter's rows in fixed blocks (bits repeat).  Adapters without a row get zeros.  dx, da and db may
+ * each be NULL.
  *   ws     workspace of adapter_linear_bwd_workspace_size(...) bytes: the transposed weights, g, and
  *          partial sums that follow the rows and, past 12 MB, the fewer of requests and adapters
  * ------------------------------------------------------------------------------------------- */

@@ -697,7 +697,10 @@ hpr_status adapter_linear_fwd(const uint16_t* x, int64_t n, int32_t k, const uin
   const AdapterArgs g = {x, w, a, b, scale, req_off, adapter, n, k, m, r, n_ad, n_req,
                          dtype == HPR_F16};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e = timed("adapter_shrink", s, [&] { return launch_adapter_shrink(g, h, s); });
+  hipError_t e = timed("adapter_shrink", s, [&] {
+    const ShrinkJob job = {g, h, nullptr};
+    return launch_adapter_shrink(&job, 1, s);
+  });
   if (e == hipSuccess)
     e = timed("adapter_expand", s, [&] { return launch_adapter_expand(g, h, y, s); });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "adapter launch");
@@ -710,7 +713,7 @@ size_t adapter_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t m, int32_
     return 0;
   const size_t rp = (size_t)adapter_rank_pad(r), slots = (size_t)adapter_outer_slots(n, n_req, n_ad, k, m, r);
   return align_up((size_t)m * k * 2) + align_up((size_t)n_ad * r * k * 2) +
-         align_up((size_t)n_ad * r * m * 2) + align_up((size_t)n * rp * 2) +
+         align_up((size_t)n_ad * r * m * 2) + 4 * align_up((size_t)n * rp * 2) +
          align_up(slots * rp * k * sizeof(float)) + align_up(slots * rp * m * sizeof(float)) +
          align_up(2 * slots * sizeof(int32_t)) +
          (adapter_ordered(n, n_req, n_ad, k, m, r)
@@ -739,7 +742,11 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
   uint16_t* wt = c.take<uint16_t>((size_t)m * k * 2);
   uint16_t* at = c.take<uint16_t>((size_t)n_ad * r * k * 2);
   uint16_t* bt = c.take<uint16_t>((size_t)n_ad * r * m * 2);
-  uint16_t* g = c.take<uint16_t>((size_t)n * rp * 2);
+  // g and, in fp16, what its rounding leaves (ShrinkJob), and both for h: the forward's rounding is not enough
+  uint16_t* rows[4];
+  for (uint16_t*& p : rows) p = c.take<uint16_t>((size_t)n * rp * 2);
+  uint16_t* const g = rows[0];
+  const bool narrow = dtype == HPR_F16;
   float* part_a = c.take<float>(slots * rp * k * sizeof(float));
   float* part_b = c.take<float>(slots * rp * m * sizeof(float));
   int32_t* slot_adapter = c.take<int32_t>(2 * slots * sizeof(int32_t));
@@ -769,15 +776,24 @@ hpr_status adapter_linear_bwd(const uint16_t* dy, const uint16_t* x, int64_t n, 
                                0};
       return launch_adapter_prepare(f, q, s);
     });
-  if (e == hipSuccess && need_g) {
-    e = timed("adapter_shrink", s, [&] { return launch_adapter_shrink(t, g, s); });
+  const bool need_h = n > 0 && narrow && db;
+  if (e == hipSuccess && (need_g || need_h))
+    e = timed("adapter_shrink", s, [&] {
+      ShrinkJob jobs[2];
+      int count = 0;
+      if (need_g) jobs[count++] = {t, g, narrow && da ? rows[1] : nullptr};
+      if (need_h) jobs[count++] = {f, rows[2], rows[3]};
+      return launch_adapter_shrink(jobs, count, s);
+    });
+  if (need_g) {
     if (e == hipSuccess && dx)
       e = timed("adapter_expand", s, [&] { return launch_adapter_expand(t, g, dx, s); });
   }
   if (e != hipSuccess) return hip_fail(e, "adapter gradient launch");
   if (da || db)
     e = timed("adapter_outer", s, [&] {
-      const OuterArgs o = {{{g, x, k, 0, part_a, da, 0, 0}, {h, dy, m, 1, part_b, db, 0, 0}},
+      const OuterArgs o = {{{g, rows[1], x, k, 0, part_a, da, 0, 0},
+                            {narrow ? rows[2] : h, rows[3], dy, m, 1, part_b, db, 0, 0}},
                            order, slot_adapter, 0, 0};
       return launch_adapter_outer(f, o, s);
     });

@@ -130,8 +130,22 @@ struct WaveProduct {
 // with B.  Its relative rounding reaches only the adapter's part of y.  Bound by x: 13,063 rows of 4096
 // of 64 requests, rank 16, 20 us (107 MB, 5.3 TB/s out of the caches); 32 rows of 32 requests 8 us, a
 // wave's eight waits for memory.
+//
+// fp16 has no bits below 2^-24 and few below 2^-14, where g lies while B is near its start at zero and dy is small,
+// and h where A or x is.  The gradients of A and B, in which nothing else covers that loss, read g and h in
+// two numbers (LOW): the value's rounding and, below 1 (above, the rounding alone keeps 11 bits), the rest of it
+// times 2^24, exactly apart.  4096 rows, B and dy of 1e-4: dA was off by 2.7e-2, as rounding g alone makes it.
+// y and dx read the roundings alone: what they lose there, at most 2^-25 a rank, is of the size of what their own
+// rounding loses.  Forward and gradients in fp16, us with it (without): 13,057 rows, 4096 -> 4096, rank 64 1,006
+// (937: h again, x and dy read twice for 64 ranks), 4,000 rows, 768 -> 768, rank 16 60 (54), 764 rows, 768 -> 2304,
+// rank 8 53 (52).
+constexpr float kRest = 0x1p24f;
+__device__ __forceinline__ float rest(float v, float rounded) {
+  return __builtin_fabsf(v) < 1.f ? (v - rounded) * kRest : 0.f;
+}
+
 template <class T, int NB, int XB, int W>
-__device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h) {
+__device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h, uint16_t* low) {
   using P = WaveProduct<T, NB, XB>;
   constexpr int kRows = 32 * XB;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // W * P::kBytes
@@ -173,16 +187,27 @@ __device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h) {
         v[e] += reinterpret_cast<const float*>(smem + w * P::kBytes)[(4 * i + e) * 64 + lane];
       v[e] = j + e < a.r ? v[e] * sc : 0.f;
     }
-    if (t <= last && j < rp)
-      *reinterpret_cast<uint2*>(h + (first + t) * rp + j) =
-          uint2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+    if (t <= last && j < rp) {
+      const uint2 w = {T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+      *reinterpret_cast<uint2*>(h + (first + t) * rp + j) = w;
+      if constexpr (T::kNarrow)
+        if (low)
+          *reinterpret_cast<uint2*>(low + (first + t) * rp + j) =
+              uint2{T::pack(rest(v[0], T::lo(w.x)), rest(v[1], T::hi(w.x))),
+                    T::pack(rest(v[2], T::lo(w.y)), rest(v[3], T::hi(w.y)))};
+    }
   }
 }
 
+struct ShrinkArgs {
+  ShrinkJob job[2];
+};
+
 // (The bodies are device functions: the host pass knows no buffer resources.)
 template <class T, int NB, int XB, int W>
-__global__ __launch_bounds__(64 * W) void shrink_kernel(AdapterArgs a, uint16_t* h) {
-  shrink_tile<T, NB, XB, W>(a, h);
+__global__ __launch_bounds__(64 * W) void shrink_kernel(ShrinkArgs p) {
+  const ShrinkJob& q = p.job[blockIdx.z];
+  shrink_tile<T, NB, XB, W>(q.a, q.h, q.low);
 }
 
 // ---- y ----------------------------------------------------------------------------------------
@@ -703,6 +728,10 @@ __global__ __launch_bounds__(256) void prepare_kernel(AdapterArgs g, TransposeAr
 // 4096 each, rank 64: 45 us (214 MB and 27 MB of parts, 5.4 TB/s).
 constexpr int kOuterWaves = 4;
 
+// ranks of a workgroup: in fp16 the other half of the tile's 64 columns is the rest of L (kRest)
+template <class T>
+constexpr int kOuterRanks = T::kNarrow ? 32 : 64;
+
 template <class T, bool LIST>
 __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs a, OuterArgs o) {
   constexpr int kTile = 64 * 128;  // 64 rows of 64 values
@@ -711,7 +740,7 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rp = (a.r + 15) / 16 * 16;
-  const uint32_t n_jb = (uint32_t)(rp + 63) / 64u;
+  const uint32_t n_jb = (uint32_t)(rp + kOuterRanks<T> - 1) / kOuterRanks<T>;
   const int which = blockIdx.x >= o.job[0].blocks;
   const OuterJob& q = o.job[which];
   const uint32_t b0 = blockIdx.x - (which ? o.job[0].blocks : 0u);
@@ -730,7 +759,7 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
   const int64_t end = R.r1 < first + o.rows ? R.r1 : first + o.rows;
 
   const int c0 = cb * 64 * kOuterWaves + wave * 64;
-  const int j0 = jb * 64;
+  const int j0 = jb * kOuterRanks<T>;
   f32x16 acc[2][2];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -762,10 +791,11 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int r = 8 * (2 * wave + j) + lr;
-      int cc = j0 + 8 * ((lane & 7) ^ swz<64>(r));
+      const int ch = 8 * ((lane & 7) ^ swz<64>(r));
+      int cc = j0 + ch % kOuterRanks<T>;
       if (cc >= rp) cc = rp - 8;
       const int64_t row = LIST ? (int64_t)__shfl(listed, r) : t + r;
-      load_lds16(r < n ? (const void*)(q.l + row * rp + cc) : (const void*)kZero16,
+      load_lds16(r < n ? (const void*)((ch < kOuterRanks<T> ? q.l : q.low) + row * rp + cc) : (const void*)kZero16,
                  st + (2 * wave + j) * 1024);
     }
   };
@@ -799,8 +829,14 @@ __global__ __launch_bounds__(64 * kOuterWaves, 2) void outer_kernel(AdapterArgs 
           for (int j = 0; j < 2; ++j) acc[i][j] = T::mfma(fm[i], fl[j], acc[i][j]);
       }
   }
+  if constexpr (T::kNarrow) {
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][0][r] += acc[i][1][r] * (1.f / kRest);
+  }
+#pragma unroll
+  for (int j = 0; j < kOuterRanks<T> / 32; ++j) {
     const int jj = j0 + 32 * j + col;
     if (jj >= a.r) continue;
     float* dst = q.part + ((int64_t)slot * rp + jj) * cols;
@@ -868,13 +904,15 @@ hipError_t allow_lds(const void* fn, int lds) {
 }
 
 template <class T, int NB, int XB, int W>
-hipError_t shrink_as(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
+hipError_t shrink_as(const ShrinkArgs& p, int count, hipStream_t s) {
+  const AdapterArgs& a = p.job[0].a;
   constexpr int lds = W * WaveProduct<T, NB, XB>::kBytes;
   const hipError_t e = allow_lds((const void*)shrink_kernel<T, NB, XB, W>, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((shrink_kernel<T, NB, XB, W>),
-                     dim3((unsigned)(a.n / (32 * XB) + a.n_req), (unsigned)(a.r + 32 * NB - 1) / (32 * NB)),
-                     dim3(64 * W), lds, s, a, h);
+                     dim3((unsigned)(a.n / (32 * XB) + a.n_req), (unsigned)(a.r + 32 * NB - 1) / (32 * NB),
+                          (unsigned)count),
+                     dim3(64 * W), lds, s, p);
   return hipGetLastError();
 }
 
@@ -886,12 +924,14 @@ hipError_t shrink_as(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
 //     as of x per 32 rows and more: there 64 rows share it, where they fill the chip: 10,000 rows of
 //     rank 64 68 (75).
 template <class T>
-hipError_t shrink(const AdapterArgs& a, uint16_t* h, hipStream_t s) {
+hipError_t shrink(const ShrinkArgs& p, int count, hipStream_t s) {
+  const AdapterArgs& a = p.job[0].a;
   const int64_t tiles = a.n / 32 + a.n_req;
-  if (tiles * ((a.r + 31) / 32) <= (a.r <= 64 ? 256 : 512)) return shrink_as<T, 1, 1, 8>(a, h, s);
-  if (a.r <= 32) return shrink_as<T, 1, 1, 4>(a, h, s);
-  if (a.r <= 64) return tiles <= 256 ? shrink_as<T, 2, 1, 6>(a, h, s) : shrink_as<T, 2, 2, 4>(a, h, s);
-  return shrink_as<T, 4, 1, 2>(a, h, s);
+  if (tiles * ((a.r + 31) / 32) <= (a.r <= 64 ? 256 : 512)) return shrink_as<T, 1, 1, 8>(p, count, s);
+  if (a.r <= 32) return shrink_as<T, 1, 1, 4>(p, count, s);
+  if (a.r <= 64)
+    return tiles <= 256 ? shrink_as<T, 2, 1, 6>(p, count, s) : shrink_as<T, 2, 2, 4>(p, count, s);
+  return shrink_as<T, 4, 1, 2>(p, count, s);
 }
 
 template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
@@ -950,7 +990,7 @@ hipError_t expand(AdapterArgs a, const uint16_t* h, uint16_t* y, hipStream_t s) 
 
 template <class T>
 hipError_t outer(const AdapterArgs& a, OuterArgs o, hipStream_t s) {
-  const int rp = adapter_rank_pad(a.r), n_jb = (rp + 63) / 64;
+  const int rp = adapter_rank_pad(a.r), n_jb = (rp + kOuterRanks<T> - 1) / kOuterRanks<T>;
   o.rows = adapter_outer_rows(a.n, a.k, a.m);
   o.slots = (uint32_t)adapter_outer_slots(a.n, a.n_req, a.n_ad, a.k, a.m, a.r);
   uint32_t blocks = 0, join_blocks = 0;
@@ -1014,14 +1054,16 @@ bool adapters_fit(int64_t n, int k, int m, int r, int n_ad, int n_req, bool grad
   if (!grads) return true;
   const int64_t prepare =
       blocks(n_ad, kOrderAdapters) + blocks(m, 64) * blocks(k, 64) + n_ad * blocks(r, 64) * (blocks(k, 64) + blocks(m, 64));
-  const int64_t outer = adapter_outer_slots(n, n_req, n_ad, k, m, r) * blocks(adapter_rank_pad(r), 64) *
+  const int64_t outer = adapter_outer_slots(n, n_req, n_ad, k, m, r) * blocks(adapter_rank_pad(r), 32) *
                         (blocks(k, 64 * kOuterWaves) + blocks(m, 64 * kOuterWaves));
   return launch_fits(prepare, 256) && launch_fits(outer, 64 * kOuterWaves);
 }
 
-hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t stream) {
+hipError_t launch_adapter_shrink(const ShrinkJob* jobs, int count, hipStream_t stream) {
+  const AdapterArgs& a = jobs[0].a;
   if (a.n == 0 || a.n_req == 0) return hipSuccess;
-  return a.f16 ? shrink<HalfF16>(a, h, stream) : shrink<HalfBf16>(a, h, stream);
+  const ShrinkArgs p = {{jobs[0], jobs[count - 1]}};
+  return a.f16 ? shrink<HalfF16>(p, count, stream) : shrink<HalfBf16>(p, count, stream);
 }
 
 hipError_t launch_adapter_expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y,

@@ -319,8 +319,14 @@ struct AdapterArgs {
 };
 constexpr int kMaxRank = 128;
 inline int adapter_rank_pad(int r) { return (r + 15) / 16 * 16; }
-// h[n, rank_pad] = scale_a x A_a^T (zero past r), rows of requests without an adapter unwritten
-hipError_t launch_adapter_shrink(const AdapterArgs& a, uint16_t* h, hipStream_t stream);
+// h[n, rank_pad] = scale_a x A_a^T (zero past r), rows of requests without an adapter unwritten; low (may be
+// null, fp16 alone): what h leaves of it below 1, times 2^24.  One or two such products of the same requests
+// and ranks in one launch.
+struct ShrinkJob {
+  AdapterArgs a;
+  uint16_t *h, *low;
+};
+hipError_t launch_adapter_shrink(const ShrinkJob* jobs, int count, hipStream_t stream);
 // y[n, m] = x W^T + h B_a^T
 hipError_t launch_adapter_expand(const AdapterArgs& a, const uint16_t* h, uint16_t* y,
                                  hipStream_t stream);
@@ -350,7 +356,7 @@ hipError_t launch_adapter_prepare(const AdapterArgs& a, TransposeArgs t, hipStre
 // through parts of slots * rank_pad * cols floats and slot_adapter, 2 * slots words, slots =
 // adapter_outer_slots.  The launcher fills rows, slots, blocks and join_blocks.
 struct OuterJob {
-  const uint16_t *l, *m;
+  const uint16_t *l, *low, *m;  // low: the rest of l in fp16 (ShrinkJob)
   int cols;
   int transposed;
   float* part;

@@ -92,3 +92,37 @@ def test_attention_gradients_of_keys_that_get_little_attention():
         for name in ("dk", "dv"):
             near(b[name][torch.from_numpy(rows).to(DEV)], want[name][rows], name)
     near(b["dq"], want["dq"], "dq")
+
+
+# rows per request, their adapters, k, m, rank, n_ad
+ADAPTERS = {
+    "one": ([2048], [0], 512, 1024, 16, 1),
+    "rank_70": ([900, 300], [0, 1], 136, 520, 70, 2),
+    "few_rows": ([60, 1, 3], [0, 1, 1], 4096, 768, 8, 2),
+    # rows ordered by adapter (see test_gpu_adapter_order.py)
+    "ordered": ([7] * 130, [i % 2 for i in range(130)], 1024, 1024, 33, 2),
+}
+
+
+# standard deviations of x, A, B and dy: g is about B dy sqrt(m), h about x A sqrt(k)
+@pytest.mark.parametrize("stds", [(1.0, 0.03, 1e-3, 1e-4), (1.0, 0.03, 1e-4, 1e-4), (300.0, 0.03, 1e-4, 1e-5),
+                                  (1e-4, 1e-3, 0.1, 30.0), (1e-3, 1e-4, 0.1, 30.0),
+                                  (3.0, 0.3, 0.3, 3.0)],
+                         ids=["B-3_dy-4", "B-4_dy-4", "B-4_dy-5", "x-4_A-3", "x-3_A-4", "large"])
+@pytest.mark.parametrize("shape", ADAPTERS)
+def test_adapter_gradients_of_any_size(shape, stds):
+    lens, adapter, k, m, r, n_ad = ADAPTERS[shape]
+    g = gen(610)
+    n = sum(lens)
+    x, A, B, dy = [half(torch.randn(*s, generator=g, dtype=torch.float64) * std)
+                   for s, std in zip(((n, k), (n_ad, r, k), (n_ad, m, r), (n, m)), stds)]
+    W = half(torch.randn(m, k, generator=g, dtype=torch.float64) * k ** -0.5)
+    scale = (0.5 + torch.rand(n_ad, generator=g)).to(DEV)
+    args = (x, W, A, B, scale, off(lens), torch.tensor(adapter, dtype=torch.int32, device=DEV))
+    b = hpr.adapter_linear_bwd(dy, *args, hpr.adapter_linear_fwd(*args)["h"])
+    want = E.adapter_linear(*[f64(t) for t in args[:5]], args[5].cpu().numpy(), adapter, f64(dy))
+    for name in ("dx", "da", "db"):
+        near(b[name], want[name], name)
+    for i in range(n_ad):  # each adapter by itself, and each rank of it
+        near(b["da"][i], want["da"][i], f"da[{i}]")
+        near(b["db"][i, :, r - 1], want["db"][i, :, r - 1], f"db[{i}]")
