@@ -298,7 +298,9 @@ hpr_status retrieval_metrics(const int64_t* topk_idx, int32_t nq, int32_t ld, in
 
 /* Workspace sizes in bytes for the calls above (0 is a valid size only when stated).  Those of
  * maxsim_topk, dense_ip_topk and semantic_chunk never fall as nq, n_docs or n grow: one workspace
- * of a program's largest call holds its smaller ones. */
+ * of a program's largest call holds its smaller ones.  Those of packed_attention and adapter_linear_bwd
+ * do fall where a larger call takes another kernel (few query rows split their keys, many do not; slots
+ * of adapter gradients grow longer): ask for every size that a program uses, and take the largest. */
 size_t maxsim_score_workspace_size(int32_t nq, int32_t lq, int64_t n_docs, int64_t n_tok,
                                    int32_t dim);
 size_t maxsim_topk_workspace_size(int32_t nq, int32_t lq, int64_t n_docs, int64_t n_tok,
@@ -354,8 +356,10 @@ hpr_status hpr_scale_grads_bf16(const float* dq, int64_t n_q, uint16_t* dq_out, 
  *   out [n_q, heads, dim] dense; lse fp32 [n_q, heads] or NULL
  *   ws     workspace of packed_attention_workspace_size(d) bytes (may be 0)
  * Preconditions, like those above not checked on the device: both offsets start at 0, never fall
- * and end at n_q and n_k; q, dout and every key row that some query sees are finite.  Key rows that no
- * query sees (past k_len[s], or left behind by every window) may hold anything.
+ * and end at n_q and n_k; q, dout and every key row that some query sees are finite, and no scale <q_i, k_j>
+ * passes 2^30 in magnitude.  Key rows that no query sees (past k_len[s], or left behind by every window) may
+ * hold anything.  What breaks this stays within its sequence, but not every output that it should reach by
+ * the formulas need show it: a caller that scales fp16 losses looks for overflow in out and in dout.
  * ------------------------------------------------------------------------------------------- */
 #define HPR_BF16 0
 #define HPR_F16 1
@@ -379,8 +383,9 @@ hpr_status packed_attention_fwd(const hpr_attention* d, const uint16_t* q, const
 /* ---------------------------------------------------------------------------------------------
  * packed_attention_bwd -- the gradients of packed_attention_fwd.
  *
- * With p the forward's probabilities (recomputed from lse), delta_i = <dout_i, out_i> and
- * ds_ij = p_ij (<dout_i, v_j> - delta_i):
+ * With p the forward's probabilities (recomputed from lse), delta_i = <dout_i, out_i> (summed as
+ * sum_j p_ij <dout_i, v_j>, free of the rounding of out, where all the keys that the 32 rows of a wave see lie
+ * in one block of 64 keys from a multiple of 64 on) and ds_ij = p_ij (<dout_i, v_j> - delta_i):
  *     dv_j = sum_i p_ij dout_i;  dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i
  * those of a kv head summed over its query heads.  p and ds are rounded to 16 bits as operands of the
  * second products, in fp16 times powers of two that keep them out of the range below 2^-14 (exactly

@@ -17,12 +17,14 @@ fallback: if the library is not built, or a call fails, an exception is raised.
     retrieval_metrics(idx, positive, k)           -> dict(p_at_k, mrr_at_k, ranks) on the device
     csr_validate(off, n_tok)                      -> (status name, first bad document or -1)
 
-The encoder's operators over the same packed sequences, in bf16 or fp16:
+The encoder's operators over the same packed sequences, in bf16 or fp16 (attention's q and dout, and the
+keys that some query sees, must be finite: what is not stays within its sequence, but need not show in
+every output, so look for the overflow of a scaled fp16 loss in out and in dout):
 
-    packed_attention(q, k, v, q_off, ...)         -> out like q, with autograd to q, k and v
+    packed_attention(q, k, v, q_off, ...)         -> out like q, with autograd (once) to q, k and v
     packed_attention_fwd(q, k, v, q_off, ...)     -> dict(out, lse)
     packed_attention_bwd(dout, q, k, v, out, lse, q_off, ...) -> dict(dq, dk, dv)
-    adapter_linear(x, W, A, B, scale, off, adapter) -> y [n, m], with autograd to x, A and B
+    adapter_linear(x, W, A, B, scale, off, adapter) -> y [n, m], with autograd (once) to x, A and B
     adapter_linear_fwd(x, W, A, B, scale, off, adapter)       -> dict(y, h)
     adapter_linear_bwd(dy, x, W, A, B, scale, off, adapter, h) -> dict(dx, da, db)
     rotary(q, k, pos, cos, sin)                   -> (q, k) rotated, with autograd to q and k
@@ -540,7 +542,8 @@ def packed_attention_fwd(q, k, v, q_off, k_off=None, k_len=None, causal=True, wi
     q [n_q, heads, dim], k and v [n_k, kv_heads, dim], bf16 or fp16; sequence s has query rows
     q_off[s]..q_off[s+1] and key rows k_off[s]..k_off[s+1] (int64; None: q_off), of which the first
     k_len[s] count (int64 [n_seq]; None: all).  causal aligns the last query with the last key;
-    window > 0 also hides keys more than window - 1 before it.  scale defaults to dim ** -0.5.
+    window > 0 also hides keys more than window - 1 before it.  scale defaults to dim ** -0.5.  A ws that
+    is too small is not used; the size a call needs is not monotone in its sizes.
     """
     dev, d, k_off = _attention_desc(q, k, v, q_off, k_off, k_len, causal, window, scale)
     L = lib()
@@ -696,7 +699,8 @@ def adapter_linear_fwd(x, W, A, B, scale, off, adapter, out=None):
 def adapter_linear_bwd(dy, x, W, A, B, scale, off, adapter, h, need_dx=True, need_da=True, need_db=True,
                        ws=None):
     """Gradients of adapter_linear_fwd's y: dict(dx, da, db), of the inputs' type, None where not
-    needed.  W and scale are frozen."""
+    needed.  W and scale are frozen.  A ws that is too small is not used; the size a call needs is not
+    monotone in its sizes."""
     dev, n, k, m, r, n_ad, n_req, code = _adapter_inputs(x, W, A, B, scale, off, adapter)
     _need(dy, "dy", x.dtype, 2, dev)
     if dy.shape != (n, m):

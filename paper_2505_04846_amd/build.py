@@ -45,9 +45,12 @@ COMMON_FLAGS = [
 ]
 
 
-# Per-file extra flags.  The MaxSim and attention kernels take inputs that are finite by contract (the header
-# states it), so NaN semantics need not be honoured there: without this every fmaxf of the
-# running max is preceded by two NaN-quieting self-maxes, tripling the VALU work per tile.
+# Per-file extra flags.  The MaxSim kernels take inputs that are finite by contract, and the attention kernels q,
+# dout and every key row that some query sees (the header states both), so NaN semantics need not be honoured
+# there: without this every fmaxf of the running max is preceded by two NaN-quieting self-maxes, tripling the VALU
+# work per tile.  Key rows that no query sees may hold NaN.  The attention kernels do not load them, but for the
+# 32 keys of a wave of the dk/dv kernel, whose scores and products are replaced by selects before anything is
+# computed from them: the flag lets the compiler assume about a value that is used, not about one that a select drops.
 FILE_FLAGS = {"maxsim.hip": ["-fno-honor-nans"], "maxsim_argmax.hip": ["-fno-honor-nans"],
               "attention.hip": ["-fno-honor-nans"]}
 

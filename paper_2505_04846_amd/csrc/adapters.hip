@@ -215,10 +215,10 @@ __global__ __launch_bounds__(64 * W) void shrink_kernel(ShrinkArgs p) {
 // Tile of BT rows of x by BM rows of W (columns of y), WT x WM waves, k in stages of 64 through NST LDS
 // stages.  W's rows are the rows of the product, so a lane holds 4 consecutive values of a row of y.
 //
-// Measured: 13,063 rows, 4096 -> 6144 (256 x 256 tiles) 525-570 us, 1.15-1.25 PFLOP/s, where the library's
-// product of 12,960 rows alone takes 588 us; 13,057 rows, 4096 -> 4096 340 us and 40 us for its last round in 128 x 128
-// tiles, 1.15 PFLOP/s (library 343 us).  The matrix cores are busy 63-70 % of the cycles; on random operands
-// the card's power limit then holds the clock at 1.6-1.8 GHz.  764 rows, 768 -> 2304 (64 x 64) 11 us: launch
+// Measured: 13,063 rows, 4096 -> 6144 (256 x 256 tiles) 505-590 us from card to card, 1.11-1.30 PFLOP/s,
+// where the library's product of 12,960 rows alone takes 584-588 us; 13,057 rows, 4096 -> 4096 340-370 us and 40 us
+// for its last round in 128 x 128 tiles, 1.07-1.15 PFLOP/s (library 332-343 us).  The matrix cores are busy 65-70 %
+// of the cycles; on random operands the card's power limit then holds the clock at 1.6-1.8 GHz.  764 rows, 768 -> 2304 (64 x 64) 11 us: launch
 // and the waits for the request, its h and its B, then 12 stages at 0.17 us.
 //
 // The adapters' part comes first, while the first stage is on its way, and needs no LDS: for every run of

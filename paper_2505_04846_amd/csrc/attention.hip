@@ -263,9 +263,9 @@ __device__ __forceinline__ float prob(float x) {
 // where they lie for long rows and for small gradients (2,048 keys, dout of 1e-5: dq was off by 23 %, as
 // rounding ds alone makes it).  So a lane's column of ds is held times a power of two, by which the sums are
 // divided in the end: lowered, and the sums so far with it, where the column would pass 2^15, so that its
-// largest entry is then in [2^9, 2^10).  p, which is at most 1, is held times 2^15.  It costs 3 to 5 %: forward
-// and gradients of 128 documents of up to 512 tokens, 12 heads of 64, 267 us (259 without), of 4 of 4,000 both
-// ways 1,043 (989).
+// largest entry is then in [2^9, 2^10).  p, which is at most 1, is held times 2^15.  The forward
+// and the gradients take 3 to 5 % longer for it: 128 documents of up to 512 tokens, 12 heads of 64, 265 us (253;
+// dq 87 and 82, dk/dv 119 and 109), 4 of 4,000 both ways 1,043 (989).
 constexpr float kDsFrom = 0x1p60f;  // products of three fp16 sums stay finite
 constexpr float kDsMost = 0x1p15f, kPScale = 0x1p15f;
 template <int N>
@@ -296,12 +296,13 @@ __device__ __forceinline__ void keep_range(f32x16& ds, f32x16 (&sum)[N], float& 
 // through NST LDS stages: one pass with the running maximum and sum of the softmax (fp32) in registers.
 // Probabilities are rounded to 16 bits as the operand of the product with v, the output once.
 //
-// Measured, 32 heads of 128 on 8 kv heads, causal: one sequence of 32,768 tokens 7.6-7.9 ms, 1.12-1.15
-// PFLOP/s of the visible pairs, the matrix cores busy 58 % of the cycles at the 1.8 GHz that the card's power
-// limit leaves on random operands (zeros run in 5.9-6.8 ms).  256 sequences of 32 to 384 tokens 0.26 ms,
-// where q, k, v and the output alone take 0.16 ms of HBM: half of the pairs of the tiles computed are masked,
-// and a workgroup lives for a few stages.  A token of each of 64 caches of up to 8,192 keys 185 us and 5 us
-// for the join, 6.1 TB/s of keys and values.
+// Measured, 32 heads of 128 on 8 kv heads, causal: one sequence of 32,768 tokens 7.9-8.3 ms from card to card,
+// 1.06-1.12 PFLOP/s of the visible pairs, the matrix cores busy 59 % of the cycles at the 1.7 GHz that the
+// card's power limit leaves on random operands (zeros run in 5.9-6.8 ms).  256 sequences of 32 to 384 tokens
+// 0.25-0.26 ms, where q, k, v and the output, the whole of its traffic, take 0.16 ms of HBM: a workgroup lives
+// for 4.7 stages on average, so that its start and end are seen (matrix cores busy 23 %, vector instructions 41
+// % of the cycles; 87 % of the pairs that the waves compute are visible).  A token of each of 64 caches of up to
+// 8,192 keys 185-190 us and 5 us for the join, 6.1 TB/s of keys and values.
 template <class T, int D, int NW, int KEYS, int NST>
 __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
   constexpr int kS = D / 16, kDb = D / 32;
@@ -541,15 +542,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 
 // dq of a tile of slots, over all their visible keys; also delta (fp32), which the dk/dv kernel reads.
 // ds is rounded to 16 bits as the operand of the product with k, dq once.  Where all the keys that a wave's
-// rows see lie in one stage, delta is summed from p and dp before ds is formed: of few keys, p (dp - delta)
+// rows see lie in one stage (of 64 keys from a multiple of 64 on), delta is summed from p and dp before ds is formed: of few keys, p (dp - delta)
 // cancels, and the rounding of out would be seen in it (a row's first key alone: ds is 0).  On the documents
 // below dq and dk were off by 2.5e-3 without that and are by 2.4e-3 (an exact result rounded to bf16: 1.7e-3),
 // in the same time.  Two kernels, this and the dk/dv kernel, each with the sums of its own rows in
 // registers: fused, one of the sums would go out through atomics, whose order changes results, or as fp32
 // parts.
 //
-// Measured, 192 documents of 64 to 448 tokens and 24 questions, 32 heads of 128 on 8 kv heads, causal: 370 us,
-// bound by HBM (1.7 GB, 255 us) and by a workgroup's start (three dependent loads: q and dout, out, keys; two
+// Measured, 192 documents of 64 to 448 tokens and 24 questions, 32 heads of 128 on 8 kv heads, causal: 365-390
+// us, bound by HBM (1.4 GB read and 0.4 written, 265 us) and by a workgroup's start (three dependent loads: q and dout, out, keys; two
 // workgroups per CU); the matrix cores are busy 24 % of the cycles.  One sequence of 8,192 tokens: both kernels
 // at 1.09 PFLOP/s of the visible pairs.
 template <class T, int D, int NW>
@@ -714,8 +715,9 @@ __device__ __forceinline__ void attn_dq(const AttnArgs& a) {
 // (whole tokens of G slots) at a time.  A wave owns 32 keys; the sum over the group's heads is
 // the sum over slots.  The wave's K stays in registers, its V in LDS: with the 128 registers of both
 // sums at D = 128, that is what leaves room for two waves per SIMD (one wave, with V in registers: 930 us
-// on the documents of the dq kernel's comment, 405 us so).  Bound there as the dq kernel is (1.2 GB, 27 % busy).
-// With 12 heads of 64, fp16: 86 us (dq) and 110 us.
+// on the documents of the dq kernel's comment, 390-415 us so).  Bound there as the dq kernel is (q and dout are
+// read again for every 128 keys: 1.6 GB read and 0.2 written, 267 us of HBM; matrix cores 28 % busy).  128
+// documents of up to 512 tokens, both ways, 12 heads of 64, fp16: 88 us (dq) and 118 us.
 constexpr int kSlots = 32;
 
 template <class T, int D, int NW>
