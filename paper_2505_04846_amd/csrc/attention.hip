@@ -40,6 +40,11 @@ constexpr float kNoMax = -1e30f;
 // the exponentials then stay below 2^8, harmless in fp32 sums and 16-bit products alike (their
 // relative rounding does not depend on it), and most tiles skip the rescaling of the output.
 constexpr float kRaise = 8.f;
+// fp16 keeps fewer bits below 2^-14 and none below 2^-25, which is where the many keys of a row lie beside one that
+// takes most of the attention: there the reference stays this much below the maximum, and the exponentials of a
+// row reach from 2^15 down.
+template <class T>
+constexpr float kBelow = T::kNarrow ? 7.f : 0.f;
 
 constexpr int kKeys = 64;  // keys per tile of the dq kernel
 
@@ -438,8 +443,8 @@ __device__ __forceinline__ void attn_fwd(const AttnArgs& a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][r]);
     top = half_max(top) * a.c;
-    if (__any(top > m + kRaise)) {
-      const float mn = fmaxf(m, top);
+    if (__any(top > m + (kRaise + kBelow<T>))) {
+      const float mn = fmaxf(m, top - kBelow<T>);
       const float f = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= f;

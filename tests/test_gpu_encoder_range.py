@@ -70,6 +70,24 @@ def test_attention_gradients_of_any_size(shape, dout, large):
         near(b[name], want[name], name)
 
 
+@pytest.mark.parametrize("n_q,n,D", [(1, 8192, 128), (1, 300, 64), (200, 900, 64), (64, 2500, 96)])
+def test_attention_beside_one_key_that_takes_most(n_q, n, D):
+    """Probabilities of about 2^-24.4 beside one of almost 1, whose value is 0."""
+    g = gen(602)
+    q, k = [torch.randn(m, h, D, generator=g, dtype=torch.float64) * 0.1 for m, h in ((n_q, 4), (n, 2))]
+    q[..., 0] = 16.0
+    k[..., 0] = -16.9 * D ** 0.5 / 16.0
+    k[0] = 0.0
+    v = 50.0 + torch.randn(n, 2, D, generator=g, dtype=torch.float64)
+    v[0] = 0.0
+    q, k, v = half(q), half(k), half(v)
+    q_off, k_off = off([n_q]), off([n])
+    r = hpr.packed_attention_fwd(q, k, v, q_off, k_off=k_off, causal=False)
+    want = E.packed_attention(f64(q), f64(k), f64(v), [0, n_q], [0, n], None, False, 0, D ** -0.5)
+    assert 0 < np.abs(want["out"]).max() < 0.1
+    near(r["out"], want["out"], "out")
+
+
 def test_attention_gradients_of_keys_that_get_little_attention():
     """Keys whose probabilities are below 2^-22 in every row."""
     n, D = 1024, 64
