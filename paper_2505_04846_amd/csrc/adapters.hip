@@ -11,13 +11,12 @@
 #include "common.h"
 #include "half.h"
 #include "kernels.h"
+#include "product.h"
 #include "tiles.h"
 
 namespace hpr {
 
 namespace {
-
-__device__ __attribute__((aligned(16))) const uint32_t kZero16[4] = {0u, 0u, 0u, 0u};
 
 // Bounds of request s, inside [0, n) whatever the offsets hold.
 struct Rows {
@@ -36,91 +35,6 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int s) {
   const int ad = a.adapter[s];
   return ad >= 0 && ad < a.n_ad ? ad : -1;
 }
-
-// ---- a wave's own product ----------------------------------------------------------------------
-
-// acc[b][c] = rows [32 b, 32 b + 32) of P times rows [32 c, + 32) of X, over stages [kk0, kk1) of 64 values,
-// by one wave: its NST LDS stages are its own, so waves that split k run without a barrier.  Whole 128-byte
-// lines go straight to LDS (operands read from memory by lanes touch twice as many lines a load: a token's
-// projection took 22 us that way).  Of P, ROWS rows are loaded; the results of the rest of its last 32 are
-// not to be used (their operands are what LDS holds past the stage, of this wave's or another's).
-template <class T, int NB, int XB, int NST = 2, int ROWS = 32 * NB>
-struct WaveProduct {
-  static constexpr int kStage = XB * 4096 + ROWS * 128;
-  static constexpr int kBytes = NST * kStage;
-  static constexpr int kPast = (32 * NB - ROWS) * 128;  // LDS read past the stages
-  static constexpr int kX = 4 * XB, kLoads = 4 * XB + ROWS / 8;
-  // x, p: first rows; x_last, p_last: their last valid row, which the rows past it repeat
-  static __device__ __forceinline__ void run(const uint16_t* x, int x_last, const uint16_t* p, int p_last,
-                                             int k, int kk0, int kk1, unsigned char* lds, int lane,
-                                             f32x16 (&acc)[NB][XB]) {
-    const __amdgpu_buffer_rsrc_t rx = tile_rsrc(x), rp = tile_rsrc(p);
-    const TileReads<64> rd(lane);
-    int off[kLoads], chunk[kLoads];
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int r = 8 * (j < kX ? j : j - kX) + (lane >> 3);
-      const int last = j < kX ? x_last : p_last;
-      chunk[j] = ((lane & 7) ^ swz<64>(r)) * 8;
-      off[j] = (r < last ? r : last) * k * 2 + chunk[j] * 2;
-    }
-    const int whole = k / 64;
-    auto issue = [&](int buf, int kk) {
-      unsigned char* st = lds + buf * kStage;
-      if (kk < whole) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kX ? rx : rp, (lds_void_t*)(st + j * 1024), 16,
-                                                   off[j], kk * 128, 0, 0);
-      } else {  // the end of k: chunks past it read zeros
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-          const char* src = (const char*)(j < kX ? x : p) + off[j] + kk * 128;
-          const void* from = kk * 64 + chunk[j] < k ? (const void*)src : (const void*)kZero16;
-          __builtin_amdgcn_global_load_lds((glb_void_t*)from, (lds_void_t*)(st + j * 1024), 16, 0, 0);
-        }
-      }
-    };
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int c = 0; c < XB; ++c)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
-    static_assert(NST == 2 || NST == 3, "the waits below");
-    if (kk0 < kk1) issue(0, kk0);
-    if (NST == 3 && kk0 + 1 < kk1) issue(1, kk0 + 1);
-#pragma unroll 1
-    for (int kk = kk0, buf = 0; kk < kk1; ++kk, buf = buf + 1 < NST ? buf + 1 : 0) {
-      if (kk + NST - 1 < kk1) {
-        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // that stage's reads are done
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);
-        issue(buf > 0 ? buf - 1 : NST - 1, kk + NST - 1);
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 1) * kLoads));
-      } else if (NST == 3 && kk + 1 < kk1) {
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
-      } else {
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-      }
-      __atomic_signal_fence(__ATOMIC_SEQ_CST);
-      const unsigned char* st = lds + buf * kStage;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        u32x4 fx[XB];
-#pragma unroll
-        for (int c = 0; c < XB; ++c) fx[c] = rd.row_frag(st, c, s);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const u32x4 fp = rd.row_frag(st + XB * 4096, b, s);
-#pragma unroll
-          for (int c = 0; c < XB; ++c) acc[b][c] = T::mfma(fp, fx[c], acc[b][c]);
-        }
-      }
-    }
-    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-  }
-};
 
 // ---- h ----------------------------------------------------------------------------------------
 
@@ -161,8 +75,9 @@ __device__ __forceinline__ void shrink_tile(const AdapterArgs& a, uint16_t* h, u
   const int j0 = blockIdx.y * 32 * NB, left = a.r - j0;  // ranks
   f32x16 acc[NB][XB];
   unsigned char* own = smem + wave * P::kBytes;
-  P::run(a.x + first * a.k, last, a.a + ((int64_t)ad * a.r + j0) * a.k,
-         left < 32 * NB ? left - 1 : 32 * NB - 1, a.k, nk * wave / W, nk * (wave + 1) / W, own, lane, acc);
+  const uint16_t* ranks = a.a + ((int64_t)ad * a.r + j0) * a.k;
+  P::run(a.x + first * a.k, a.k, last, {{ranks, nullptr}, a.k, left < 32 * NB ? left - 1 : 32 * NB - 1}, a.k,
+         nk * wave / W, nk * (wave + 1) / W, own, lane, acc);
   float* part = reinterpret_cast<float*>(own);  // [NB * XB * 16][64]
   static_assert(NB * XB * 4096 <= P::kBytes, "the wave's sums fit its stages");
 #pragma unroll
@@ -227,88 +142,22 @@ __global__ __launch_bounds__(64 * W) void shrink_kernel(ShrinkArgs p) {
 template <class T, int BT, int BM, int WT, int WM, int NST>
 __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t* __restrict__ h,
                                             uint16_t* __restrict__ y, int n_m) {
-  constexpr int kW = WT * WM;
-  constexpr int kTb = BT / 32 / WT, kMb = BM / 32 / WM;  // blocks per wave
-  constexpr int kXBytes = BT * 128, kWBytes = BM * 128, kStage = kXBytes + kWBytes;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // NST stages
+  using P = TileProduct<T, BT, BM, WT, WM, NST>;
+  constexpr int kTb = P::kTb, kMb = P::kMb;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // P::kLds
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wt = wave % WT, wm = wave / WT;
-  // An XCD walks a contiguous run of tiles, four row tiles abreast: the tiles that it holds at a time
-  // (32 of the widest) read 4 row tiles and 8 column tiles, not 1 or 2 and all the columns.
-  const uint32_t lin = (uint32_t)xcd_linear(blockIdx.x, gridDim.x);
-  const uint32_t n_t = (uint32_t)((a.n - a.row0 + BT - 1) / BT);
-  const uint32_t g0 = lin / (4u * n_m) * 4u, in_g = lin - g0 * n_m;
-  const uint32_t abreast = n_t - g0 < 4u ? n_t - g0 : 4u;
-  const int tm = (int)(in_g / abreast);
-  const int64_t t0 = a.row0 + (int64_t)(g0 + in_g % abreast) * BT;
-  const int m0 = tm * BM;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + BT - 1) / BT), n_m);
+  const int64_t t0 = a.row0 + (int64_t)at.t * BT;
+  const int m0 = at.m * BM;
   const int64_t left_t = a.n - t0;
   const int last_t = left_t < BT ? (int)left_t - 1 : BT - 1;
   const int last_m = a.m - m0 < BM ? a.m - m0 - 1 : BM - 1;
 
-  const TileReads<64> rd(lane);
-  const TileLoad<64, BT, kW> lx(wave, lane, 8);
-  const TileLoad<64, BM, kW> lw(wave, lane, 8);
-  constexpr int kLoads = lx.kLoads + lw.kLoads;
-  const uint16_t* xb = a.x + t0 * a.k;
-  const uint16_t* wb = a.w + (int64_t)m0 * a.k;
-  const __amdgpu_buffer_rsrc_t rx = tile_rsrc(xb), rw = tile_rsrc(wb);
-  int ox[lx.kLoads], ow[lw.kLoads];
-#pragma unroll
-  for (int j = 0; j < lx.kLoads; ++j)
-    ox[j] = (lx.row[j] < last_t ? lx.row[j] : last_t) * a.k * 2 + lx.chunk[j];
-#pragma unroll
-  for (int j = 0; j < lw.kLoads; ++j)
-    ow[j] = (lw.row[j] < last_m ? lw.row[j] : last_m) * a.k * 2 + lw.chunk[j];
-  const int nk = (a.k + 63) / 64, nk_full = a.k / 64;
-  // Stage kk into ring buffer buf.  Chunks past the end of k read zeros, so past the last stage too
-  // (the ring keeps its number of loads in flight).
-  auto issue = [&](int buf, int kk) {
-    unsigned char* st = smem + buf * kStage;
-    if (kk < nk_full) {
-#pragma unroll
-      for (int j = 0; j < lx.kLoads; ++j)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rx, (lds_void_t*)(st + (wave * lx.kLoads + j) * 1024), 16, ox[j], kk * 128, 0, 0);
-#pragma unroll
-      for (int j = 0; j < lw.kLoads; ++j)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rw, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, ow[j], kk * 128, 0, 0);
-    } else {
-#pragma unroll
-      for (int j = 0; j < lx.kLoads; ++j) {
-        const bool in = kk * 64 + lx.chunk[j] / 2 < a.k;
-        const void* p = in ? (const void*)((const char*)xb + ox[j] + kk * 128) : (const void*)kZero16;
-        __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)(st + (wave * lx.kLoads + j) * 1024),
-                                         16, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < lw.kLoads; ++j) {
-        const bool in = kk * 64 + lw.chunk[j] / 2 < a.k;
-        const void* p = in ? (const void*)((const char*)wb + ow[j] + kk * 128) : (const void*)kZero16;
-        __builtin_amdgcn_global_load_lds(
-            (glb_void_t*)p, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, 0, 0);
-      }
-    }
-  };
-  // A wave of one block reads a whole stage's operands ahead of its products, and so hands the stage back
-  // when the next is begun (4096 -> 14336, 146 rows: 51 -> 46 us of the call); the others keep the stage
-  // that they compute on.
-  constexpr bool kAhead = kMb * kTb == 1;
-#pragma unroll
-  for (int s = 0; s < (kAhead ? NST : NST - 1); ++s) issue(s, s);
-
-  f32x16 acc[kMb][kTb];
-#pragma unroll
-  for (int i = 0; i < kMb; ++i)
-#pragma unroll
-    for (int j = 0; j < kTb; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
   // the adapters' part: a lane looks at one request of the wave's rows, 64 at a time
-  if (h && a.n_req > 0) {
+  auto adapters = [&](typename P::Acc& acc) {
+    if (!h || a.n_req <= 0) return;
     const int rp = (a.r + 15) / 16 * 16;
     const bool whole = a.r % 8 == 0;
     const int64_t w0 = t0 + wt * kTb * 32;
@@ -361,115 +210,22 @@ __device__ __forceinline__ void expand_tile(const AdapterArgs& a, const uint16_t
       }
       if (__any(R.r0 >= w0 + 32 * kTb)) break;
     }
-  }
+  };
 
-  struct Frags {
-    u32x4 x[kTb], w[kMb];
-  };
-  auto read_frags = [&](int buf, int s, Frags& f) {
-    const unsigned char* xs = smem + buf * kStage;
-#pragma unroll
-    for (int j = 0; j < kTb; ++j) f.x[j] = rd.row_frag(xs, wt * kTb + j, s);
-#pragma unroll
-    for (int i = 0; i < kMb; ++i) f.w[i] = rd.row_frag(xs + kXBytes, wm * kMb + i, s);
-  };
-  auto mfma = [&](const Frags& f) {
-#pragma unroll
-    for (int i = 0; i < kMb; ++i)
-#pragma unroll
-      for (int j = 0; j < kTb; ++j) acc[i][j] = T::mfma(f.w[i], f.x[j], acc[i][j]);
-  };
-  if constexpr (kAhead) {
-    Frags f[2][4];
-    auto stage = [&](int buf, int kk, Frags (&now)[4], Frags (&then)[4]) {
-      __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
-      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-      sync_lds();  // the next stage has landed, and nobody reads this one any more
-      issue(buf, kk + NST);
-      const int nxt = buf + 1 < NST ? buf + 1 : 0;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) read_frags(nxt, s, then[s]);  // (past the last stage: zeros, not used)
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int s = 0; s < 4; ++s) mfma(now[s]);
-      return nxt;
-    };
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 1) * kLoads));
-    sync_lds();
-#pragma unroll
-    for (int s = 0; s < 4; ++s) read_frags(0, s, f[0][s]);
-    int buf = 0;
-#pragma unroll 1
-    for (int kk = 0; kk < nk; kk += 2) {
-      buf = stage(buf, kk, f[0], f[1]);
-      if (kk + 1 < nk) buf = stage(buf, kk + 1, f[1], f[0]);
-    }
-  } else {
-    // The stages of the ring: NST - 1 are in flight when one is computed on.  One barrier per stage,
-    // before its last k-step, whose products run while the next stage's first operands are read.
-    Frags f0, f1;
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
-    sync_lds();
-    read_frags(0, 0, f0);
-#pragma unroll 1
-    for (int kk = 0, buf = 0; kk < nk; ++kk) {
-      const int nxt = buf + 1 < NST ? buf + 1 : 0, free_ = buf > 0 ? buf - 1 : NST - 1;
-      issue(free_, kk + NST - 1);
-      __builtin_amdgcn_sched_barrier(0);
-      read_frags(buf, 1, f1);
-      mfma(f0);
-      read_frags(buf, 2, f0);
-      mfma(f1);
-      read_frags(buf, 3, f1);
-      mfma(f0);
-      // each k-step's products alternate with the reads of the next one's operands
-#pragma unroll
-      for (int u = 0; u < 3; ++u) {
-#pragma unroll
-        for (int t = 0; t < kMb * kTb; ++t) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          if (t < kTb + kMb) __builtin_amdgcn_sched_group_barrier(0x100, kMb * kTb >= kTb + kMb ? 1 : kTb + kMb, 0);
-        }
-      }
-      __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
-      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-      sync_lds();
-      read_frags(nxt, 0, f0);  // (past the last stage: zeros, or rows that are read by nobody)
-      __builtin_amdgcn_sched_barrier(0);
-      mfma(f1);
-      buf = nxt;
-    }
-  }
-  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // no load may still target LDS when it is reused or ends
+  typename P::Acc acc;
+  P::run(a.x + t0 * a.k, a.k, last_t, {{a.w + (int64_t)m0 * a.k, nullptr}, a.k, last_m}, a.k, smem, wave, lane,
+         acc, adapters);
 
   // y through LDS, so that memory sees whole rows: a wave's 32 kTb rows of 32 kMb values, one 32-row
   // block at a time
-  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-  sync_lds();
-  constexpr int kRow = 64 * kMb;                                // bytes of a wave's row
-  static_assert(kW * 32 * kRow <= NST * kStage, "the waves' blocks fit the ring");
-  unsigned char* own = smem + wave * 32 * kRow;
-  constexpr int kCh = kRow / 16, kPer = 64 / kCh;               // chunks of a row, rows of a wave store
+  static_assert(P::kW * 32 * 64 * kMb <= P::kLds, "the waves' blocks fit the ring");
+  unsigned char* own = smem + wave * 32 * 64 * kMb;
   const int mw = m0 + wm * kMb * 32;
 #pragma unroll
   for (int j = 0; j < kTb; ++j) {
     const int64_t r0 = t0 + (wt * kTb + j) * 32;
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);  // (a wave's LDS operations execute in program order)
-#pragma unroll
-    for (int i = 0; i < kMb; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<uint2*>(own + col * kRow + (((4 * i + g) ^ (col % kCh)) << 4) + 8 * half) =
-            uint2{T::pack(acc[i][j][4 * g], acc[i][j][4 * g + 1]),
-                  T::pack(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3])};
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    uint16_t* dst = y + r0 * a.m + mw;
-#pragma unroll
-    for (int k = 0; k < 32 / kPer; ++k) {
-      const int r = k * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh);
-      const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
-      if (r0 + r < a.n && mw + 8 * c < a.m) *reinterpret_cast<u32x4*>(dst + (int64_t)r * a.m + 8 * c) = v;
-    }
+    store_rows<T, kMb>(y + r0 * a.m + mw, a.m, a.n - r0, a.m - mw, own, lane,
+                       [&](int i, int r) { return acc[i][j][r]; });
   }
 }
 
@@ -537,9 +293,9 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const uint16_t*
     const int nk = (a.k + 63) / 64;
     f32x16 acc[1][1];
     unsigned char* own = smem + wave * P::kBytes;
-    P::run(a.x + t0 * a.k, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31, a.w + (int64_t)m0 * a.k,
-           a.m - m0 < BM ? a.m - m0 - 1 : BM - 1, a.k, nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own,
-           lane, acc);
+    P::run(a.x + t0 * a.k, a.k, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31,
+           {{a.w + (int64_t)m0 * a.k, nullptr}, a.k, a.m - m0 < BM ? a.m - m0 - 1 : BM - 1}, a.k,
+           nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own, lane, acc);
     float* part = reinterpret_cast<float*>(own);  // [16][64]
 #pragma unroll
     for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];

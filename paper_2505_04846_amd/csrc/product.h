@@ -1,0 +1,322 @@
+// Products of rows with rows, out[t][m] = <x_t, w_m>, of 16-bit operands on the matrix cores: a workgroup's
+// tile, and a wave's own part.  Shared by the encoder's projections.
+//
+// W's rows are the rows of the matrix product, so that a lane holds values of one row of x: entry e of block
+// (i, j) is row 8 (e / 4) + 4 half + e % 4 of W's block i and row lane & 31 of x's block j.
+#pragma once
+
+#include "common.h"
+#include "half.h"
+#include "tiles.h"
+
+namespace hpr {
+
+__device__ __attribute__((aligned(16))) const uint32_t kZero16[4] = {0u, 0u, 0u, 0u};
+
+// Rows of the right operand.  A paired tile (PAIR) takes its rows from two matrices, the same rows of each:
+// one half of every wave's rows from w[0], the other from w[1].
+struct PanelW {
+  const uint16_t* w[2];  // first rows (w[1] of a paired tile alone)
+  int ld;                // elements from a row to the next
+  int last;              // last valid row, which the rows past it repeat
+};
+
+// ---- a wave's own product ----------------------------------------------------------------------
+
+// acc[b][c] = rows [32 b, 32 b + 32) of P times rows [32 c, + 32) of X, over stages [kk0, kk1) of 64 values,
+// by one wave: its NST LDS stages are its own, so waves that split k run without a barrier.  Whole 128-byte
+// lines go straight to LDS (operands read from memory by lanes touch twice as many lines a load: a token's
+// projection took 22 us that way).  Of P, ROWS rows are loaded; the results of the rest of its last 32 are
+// not to be used (their operands are what LDS holds past the stage, of this wave's or another's).
+template <class T, int NB, int XB, int NST = 2, int ROWS = 32 * NB, bool PAIR = false>
+struct WaveProduct {
+  static constexpr int kStage = XB * 4096 + ROWS * 128;
+  static constexpr int kBytes = NST * kStage;
+  static constexpr int kPast = (32 * NB - ROWS) * 128;  // LDS read past the stages
+  static constexpr int kX = 4 * XB, kLoads = 4 * XB + ROWS / 8;
+  // x: first row; x_last: its last valid row, which the rows past it repeat
+  static __device__ __forceinline__ void run(const uint16_t* x, int x_ld, int x_last, const PanelW& p,
+                                             int k, int kk0, int kk1, unsigned char* lds, int lane,
+                                             f32x16 (&acc)[NB][XB]) {
+    static_assert(!PAIR || ROWS % 16 == 0, "a load's eight rows are of one matrix");
+    const __amdgpu_buffer_rsrc_t rx = tile_rsrc(x), rp = tile_rsrc(p.w[0]), rq = tile_rsrc(p.w[PAIR]);
+    const TileReads<64> rd(lane);
+    int off[kLoads], chunk[kLoads];
+    auto second = [](int j) { return PAIR && j >= kX + ROWS / 16; };  // a load of w[1]
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      int r = 8 * (j < kX ? j : j - kX) + (lane >> 3);
+      chunk[j] = ((lane & 7) ^ swz<64>(r)) * 8;
+      if (second(j)) r -= ROWS / 2;
+      const int last = j < kX ? x_last : p.last;
+      off[j] = (r < last ? r : last) * (j < kX ? x_ld : p.ld) * 2 + chunk[j] * 2;
+    }
+    const int whole = k / 64;
+    auto issue = [&](int buf, int kk) {
+      unsigned char* st = lds + buf * kStage;
+      if (kk < whole) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kX ? rx : (second(j) ? rq : rp),
+                                                   (lds_void_t*)(st + j * 1024), 16, off[j], kk * 128, 0, 0);
+      } else {  // the end of k: chunks past it read zeros
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          const char* src = (const char*)(j < kX ? x : p.w[second(j)]) + off[j] + kk * 128;
+          const void* from = kk * 64 + chunk[j] < k ? (const void*)src : (const void*)kZero16;
+          __builtin_amdgcn_global_load_lds((glb_void_t*)from, (lds_void_t*)(st + j * 1024), 16, 0, 0);
+        }
+      }
+    };
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int c = 0; c < XB; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][c][r] = 0.f;
+    static_assert(NST == 2 || NST == 3, "the waits below");
+    if (kk0 < kk1) issue(0, kk0);
+    if (NST == 3 && kk0 + 1 < kk1) issue(1, kk0 + 1);
+#pragma unroll 1
+    for (int kk = kk0, buf = 0; kk < kk1; ++kk, buf = buf + 1 < NST ? buf + 1 : 0) {
+      if (kk + NST - 1 < kk1) {
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // that stage's reads are done
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        issue(buf > 0 ? buf - 1 : NST - 1, kk + NST - 1);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 1) * kLoads));
+      } else if (NST == 3 && kk + 1 < kk1) {
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
+      } else {
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+      }
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      const unsigned char* st = lds + buf * kStage;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        u32x4 fx[XB];
+#pragma unroll
+        for (int c = 0; c < XB; ++c) fx[c] = rd.row_frag(st, c, s);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const u32x4 fp = rd.row_frag(st + XB * 4096, b, s);
+#pragma unroll
+          for (int c = 0; c < XB; ++c) acc[b][c] = T::mfma(fp, fx[c], acc[b][c]);
+        }
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  }
+};
+
+// ---- a workgroup's product ---------------------------------------------------------------------
+
+// Tile of BT rows of x by BM rows of W, WT x WM waves, k in stages of 64 through NST LDS stages.  Wave
+// (wt, wm) holds the rows [32 kTb wt, + 32 kTb) of x and [32 kMb wm, + 32 kMb) of W; of a paired tile the
+// blocks i < kMb / 2 are columns of w[0], the others the same columns of w[1].
+template <class T, int BT, int BM, int WT, int WM, int NST, bool PAIR = false>
+struct TileProduct {
+  static constexpr int kW = WT * WM;
+  static constexpr int kTb = BT / 32 / WT, kMb = BM / 32 / WM;  // blocks per wave
+  static constexpr int kXBytes = BT * 128, kWBytes = BM * 128, kStage = kXBytes + kWBytes;
+  static constexpr int kLds = NST * kStage;
+  static constexpr int kCols = PAIR ? BM / 2 : BM;         // columns of the output
+  static constexpr int kWaveCols = kCols / WM;
+  static_assert(!PAIR || kMb % 2 == 0, "a wave holds both halves of its columns");
+  typedef f32x16 Acc[kMb][kTb];
+
+  // x: first row of the tile.  `first` is called between the first stages' loads and the products, to add
+  // to acc (zero there).  LDS is free for the caller when this returns.
+  template <class First>
+  static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k,
+                                             unsigned char* smem, int wave, int lane, Acc& acc,
+                                             First&& first) {
+    const int wt = wave % WT, wm = wave / WT;
+    const TileReads<64> rd(lane);
+    const TileLoad<64, BT, kW> lx(wave, lane, 8);
+    const TileLoad<64, BM, kW> lw(wave, lane, 8);
+    constexpr int kLoads = lx.kLoads + lw.kLoads;
+    const __amdgpu_buffer_rsrc_t rx = tile_rsrc(xb), rw0 = tile_rsrc(w.w[0]), rw1 = tile_rsrc(w.w[PAIR]);
+    // the eight rows of a wave load are of one half of a wave's rows
+    auto second = [&](int j) { return PAIR && (wave * lw.kLoads + j) * 8 % (BM / WM) >= kWaveCols; };
+    int ox[lx.kLoads], ow[lw.kLoads];
+#pragma unroll
+    for (int j = 0; j < lx.kLoads; ++j)
+      ox[j] = (lx.row[j] < last_t ? lx.row[j] : last_t) * ldx * 2 + lx.chunk[j];
+#pragma unroll
+    for (int j = 0; j < lw.kLoads; ++j) {
+      const int row = PAIR ? lw.row[j] / (BM / WM) * kWaveCols + lw.row[j] % kWaveCols : lw.row[j];
+      ow[j] = (row < w.last ? row : w.last) * w.ld * 2 + lw.chunk[j];
+    }
+    const int nk = (k + 63) / 64, nk_full = k / 64;
+    // Stage kk into ring buffer buf.  Chunks past the end of k read zeros, so past the last stage too
+    // (the ring keeps its number of loads in flight).
+    auto issue = [&](int buf, int kk) {
+      unsigned char* st = smem + buf * kStage;
+      if (kk < nk_full) {
+#pragma unroll
+        for (int j = 0; j < lx.kLoads; ++j)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(
+              rx, (lds_void_t*)(st + (wave * lx.kLoads + j) * 1024), 16, ox[j], kk * 128, 0, 0);
+#pragma unroll
+        for (int j = 0; j < lw.kLoads; ++j)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(
+              second(j) ? rw1 : rw0, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, ow[j],
+              kk * 128, 0, 0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < lx.kLoads; ++j) {
+          const bool in = kk * 64 + lx.chunk[j] / 2 < k;
+          const void* p = in ? (const void*)((const char*)xb + ox[j] + kk * 128) : (const void*)kZero16;
+          __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)(st + (wave * lx.kLoads + j) * 1024),
+                                           16, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < lw.kLoads; ++j) {
+          const bool in = kk * 64 + lw.chunk[j] / 2 < k;
+          const char* wb = (const char*)w.w[second(j)];
+          const void* p = in ? (const void*)(wb + ow[j] + kk * 128) : (const void*)kZero16;
+          __builtin_amdgcn_global_load_lds(
+              (glb_void_t*)p, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, 0, 0);
+        }
+      }
+    };
+    // A wave of one block reads a whole stage's operands ahead of its products, and so hands the stage back
+    // when the next is begun (4096 -> 14336, 146 rows: 51 -> 46 us of the call); the others keep the stage
+    // that they compute on.
+    constexpr bool kAhead = kMb * kTb == 1;
+#pragma unroll
+    for (int s = 0; s < (kAhead ? NST : NST - 1); ++s) issue(s, s);
+
+#pragma unroll
+    for (int i = 0; i < kMb; ++i)
+#pragma unroll
+      for (int j = 0; j < kTb; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    first(acc);
+
+    struct Frags {
+      u32x4 x[kTb], w[kMb];
+    };
+    auto read_frags = [&](int buf, int s, Frags& f) {
+      const unsigned char* xs = smem + buf * kStage;
+#pragma unroll
+      for (int j = 0; j < kTb; ++j) f.x[j] = rd.row_frag(xs, wt * kTb + j, s);
+#pragma unroll
+      for (int i = 0; i < kMb; ++i) f.w[i] = rd.row_frag(xs + kXBytes, wm * kMb + i, s);
+    };
+    auto mfma = [&](const Frags& f) {
+#pragma unroll
+      for (int i = 0; i < kMb; ++i)
+#pragma unroll
+        for (int j = 0; j < kTb; ++j) acc[i][j] = T::mfma(f.w[i], f.x[j], acc[i][j]);
+    };
+    if constexpr (kAhead) {
+      Frags f[2][4];
+      auto stage = [&](int buf, int kk, Frags (&now)[4], Frags (&then)[4]) {
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+        sync_lds();  // the next stage has landed, and nobody reads this one any more
+        issue(buf, kk + NST);
+        const int nxt = buf + 1 < NST ? buf + 1 : 0;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) read_frags(nxt, s, then[s]);  // (past the last stage: zeros, not used)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) mfma(now[s]);
+        return nxt;
+      };
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 1) * kLoads));
+      sync_lds();
+#pragma unroll
+      for (int s = 0; s < 4; ++s) read_frags(0, s, f[0][s]);
+      int buf = 0;
+#pragma unroll 1
+      for (int kk = 0; kk < nk; kk += 2) {
+        buf = stage(buf, kk, f[0], f[1]);
+        if (kk + 1 < nk) buf = stage(buf, kk + 1, f[1], f[0]);
+      }
+    } else {
+      // The stages of the ring: NST - 1 are in flight when one is computed on.  One barrier per stage,
+      // before its last k-step, whose products run while the next stage's first operands are read.
+      Frags f0, f1;
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+      sync_lds();
+      read_frags(0, 0, f0);
+#pragma unroll 1
+      for (int kk = 0, buf = 0; kk < nk; ++kk) {
+        const int nxt = buf + 1 < NST ? buf + 1 : 0, free_ = buf > 0 ? buf - 1 : NST - 1;
+        issue(free_, kk + NST - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        read_frags(buf, 1, f1);
+        mfma(f0);
+        read_frags(buf, 2, f0);
+        mfma(f1);
+        read_frags(buf, 3, f1);
+        mfma(f0);
+        // each k-step's products alternate with the reads of the next one's operands
+#pragma unroll
+        for (int u = 0; u < 3; ++u) {
+#pragma unroll
+          for (int t = 0; t < kMb * kTb; ++t) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (t < kTb + kMb) __builtin_amdgcn_sched_group_barrier(0x100, kMb * kTb >= kTb + kMb ? 1 : kTb + kMb, 0);
+          }
+        }
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * kLoads));
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+        sync_lds();
+        read_frags(nxt, 0, f0);  // (past the last stage: zeros, or rows that are read by nobody)
+        __builtin_amdgcn_sched_barrier(0);
+        mfma(f1);
+        buf = nxt;
+      }
+    }
+    // no load may still target LDS when it is reused or ends, and nobody may still read it
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    sync_lds();
+  }
+};
+
+// Tile of block b of a grid of n_t row tiles by n_m column tiles.  An XCD walks a contiguous run of tiles,
+// four row tiles abreast: the tiles that it holds at a time (32 of the widest) read 4 row tiles and 8 column
+// tiles, not 1 or 2 and all the columns.
+struct TileAt {
+  uint32_t t;
+  int m;
+};
+__device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint32_t n_t, int n_m) {
+  const uint32_t lin = (uint32_t)xcd_linear(block, blocks);
+  const uint32_t g0 = lin / (4u * n_m) * 4u, in_g = lin - g0 * n_m;
+  const uint32_t abreast = n_t - g0 < 4u ? n_t - g0 : 4u;
+  return {g0 + in_g % abreast, (int)(in_g / abreast)};
+}
+
+// A wave's rows of results to memory in whole rows, through LDS of its own: BLOCKS blocks of 32 columns of
+// each of 32 rows at a time.  dst: the first row's first column; value(i, r): entry r of block i of these
+// rows; rows before `from`, from n_rows on and columns from n_cols on are not written.
+template <class T, int BLOCKS, class Value>
+__device__ __forceinline__ void store_rows(uint16_t* dst, int64_t ld, int64_t n_rows, int n_cols,
+                                           unsigned char* own, int lane, Value&& value, int64_t from = 0) {
+  constexpr int kRow = 64 * BLOCKS;                             // bytes of a row
+  constexpr int kCh = kRow / 16, kPer = 64 / kCh;               // chunks of a row, rows of a wave store
+  const int half = lane >> 5, col = lane & 31;
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);  // (a wave's LDS operations execute in program order)
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<uint2*>(own + col * kRow + (((4 * i + g) ^ (col % kCh)) << 4) + 8 * half) =
+          uint2{T::pack(value(i, 4 * g), value(i, 4 * g + 1)), T::pack(value(i, 4 * g + 2), value(i, 4 * g + 3))};
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+  for (int k = 0; k < 32 / kPer; ++k) {
+    const int r = k * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
+    if (r >= from && r < n_rows && 8 * c < n_cols) *reinterpret_cast<u32x4*>(dst + (int64_t)r * ld + 8 * c) = v;
+  }
+}
+
+}  // namespace hpr
