@@ -464,6 +464,118 @@ hpr_status rotary_apply(const uint16_t* q, int64_t q_row, int64_t q_head, int32_
                         const float* sin_table, int64_t n_pos, int32_t inverse, int32_t dtype,
                         uint16_t* q_out, uint16_t* k_out, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * checkpoint_pack, checkpoint_unpack -- activations kept in 8 bits for a backward pass.
+ *
+ * Fine-tuning keeps every block's rows until the backward pass reads them.  32 values of a row share a
+ * power of two, each is a whole number of at most 127 times it:
+ *     e = max(floor(log2 max |x|) - 6, least)   least: -24 in fp16, -126 in bf16
+ *     code = x / 2^e rounded to nearest, ties to even, and to +-127
+ * (a row's last block has what is left of it).  Values are off by at most 2^(e-1), those past 127.5 2^e by up to
+ * 2^e; code 2^e is a number of dtype, so that reading back rounds nothing and packing it again changes nothing.
+ * A block with a value that is not finite reads back as NaN.
+ *
+ *   x [n, dim] with row stride x_row in elements (unpack: dense); dtype HPR_BF16 or HPR_F16
+ *   codes int8 [n, dim]; exps uint8 [n, ceil(dim / 32)]: e + 127, or 255 for NaN
+ * gated_linear_bwd and residual_norm_bwd read these in place of 16-bit rows.
+ * ------------------------------------------------------------------------------------------- */
+hpr_status checkpoint_pack(const uint16_t* x, int64_t x_row, int64_t n, int32_t dim, int32_t dtype,
+                           int8_t* codes, uint8_t* exps, void* stream);
+hpr_status checkpoint_unpack(const int8_t* codes, const uint8_t* exps, int64_t n, int32_t dim,
+                             int32_t dtype, uint16_t* x, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * gated_linear_fwd -- the gated feed-forward projections, their activation and their product.
+ *
+ *     h[t] = act(w_gate x[t]) * (w_up x[t])
+ * with act HPR_SILU: z / (1 + e^-z), HPR_GELU: z Phi(z), or HPR_GELU_TANH: z (1 + tanh(sqrt(2 / pi)
+ * (z + 0.044715 z^3))) / 2.  Arithmetic: 16-bit products accumulated in fp32 (MFMA), the activation and the
+ * product in fp32, h rounded once.  Sums have a fixed order.  (The projection after it is adapter_linear's.)
+ *
+ *   x [n, k] with row stride x_row in elements, w_gate and w_up [f, k] dense: dtype HPR_BF16 or HPR_F16
+ *   h [n, f]: output
+ * ------------------------------------------------------------------------------------------- */
+#define HPR_SILU 0
+#define HPR_GELU 1
+#define HPR_GELU_TANH 2
+
+hpr_status gated_linear_fwd(const uint16_t* x, int64_t x_row, int64_t n, int32_t k,
+                            const uint16_t* w_gate, const uint16_t* w_up, int32_t f, int32_t act,
+                            int32_t dtype, uint16_t* h, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * gated_linear_bwd -- the gradients of gated_linear_fwd, from x and dh alone.
+ *
+ * With g = w_gate x[t] and u = w_up x[t], formed again, dg = dh u act'(g) and du = dh act(g):
+ *     dx[t] = w_gate^T dg[t] + w_up^T du[t];  dw_gate = sum_t dg[t] x[t]^T;  dw_up = sum_t du[t] x[t]^T
+ * dg and du are rounded once to 16 bits as operands, in fp16 times powers of two that bring every row's (for
+ * dx) or column's (for dw_gate and dw_up) largest |dh| to [1, 2), exactly undone in the fp32 sums (products
+ * of act(g) or u act'(g) past 32752 overflow).  All sums are fp32 with a fixed order.
+ *
+ *   dh [n, f] dense; x [n, k] with row stride x_row or, with x_exps, checkpoint_pack's codes (dense; the
+ *   gradients are those at the values that they stand for); dx [n, k] and dw_gate, dw_up [f, k], dense; dx, or
+ *   dw_gate and dw_up together, may be NULL
+ *   ws     workspace of gated_linear_bwd_workspace_size(...) bytes: transposed operands, and dg and du each way
+ *          that is needed (8 n f bytes for both); packed, need_dx, need_dw: 0 or 1
+ * ------------------------------------------------------------------------------------------- */
+size_t gated_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t f, int32_t packed, int32_t need_dx,
+                                       int32_t need_dw);
+hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_exps, int64_t x_row,
+                            int64_t n, int32_t k, const uint16_t* w_gate, const uint16_t* w_up,
+                            int32_t f, int32_t act, int32_t dtype, uint16_t* dx, uint16_t* dw_gate,
+                            uint16_t* dw_up, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * residual_norm_fwd -- the norm after a block, its gate and residual scale, the residual sum and the norm before
+ * the next block, in one pass over the rows.
+ *
+ * With N(v; w, c) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) w + c (HPR_LAYER_NORM) or
+ * v / sqrt(mean(v^2) + eps) w (HPR_RMS_NORM), over a row's dim values:
+ *     p = N(b; post_weight, post_bias), or b where post_weight is NULL
+ *     r = x + scale gate p,  or x where b is NULL          y = N(r; weight, bias)
+ * In fp32 throughout, r and y rounded once (y from the unrounded r).
+ *
+ *   x and b [n, dim] with row strides in elements; b may be NULL (a norm alone: post_weight, gate and r are NULL
+ *   then); dtype HPR_BF16 or HPR_F16 for every tensor
+ *   weight, bias, post_weight, post_bias [dim]; gate [dim], or [n, dim] dense with gate_rows; NULL: none.  The
+ *   biases belong to their weights and to HPR_LAYER_NORM
+ *   r and y [n, dim] dense, not overlapping the inputs; r may be NULL, and y, where weight is too
+ * Preconditions: the squares of a row's values sum to less than fp32's largest number.
+ * ------------------------------------------------------------------------------------------- */
+#define HPR_RMS_NORM 0
+#define HPR_LAYER_NORM 1
+
+typedef struct {
+  int64_t n, x_row, b_row;          /* rows, strides in elements                                */
+  int32_t dim, dtype, kind;         /* HPR_BF16 or HPR_F16; HPR_RMS_NORM or HPR_LAYER_NORM      */
+  int32_t gate_rows;                /* 0 or 1                                                   */
+  float scale, eps;                 /* finite; positive                                         */
+} hpr_norm;
+
+hpr_status residual_norm_fwd(const hpr_norm* d, const uint16_t* x, const uint16_t* b,
+                             const uint16_t* weight, const uint16_t* bias,
+                             const uint16_t* post_weight, const uint16_t* post_bias,
+                             const uint16_t* gate, uint16_t* r, uint16_t* y, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * residual_norm_bwd -- the gradients of residual_norm_fwd, from x and b alone.
+ *
+ * dr and dy [n, dim] dense, either may be NULL (zero; dy is, where weight is).  x and b are 16-bit rows or, with
+ * x_exps and b_exps, checkpoint_pack's codes (both, dense; the gradients are those at the values that they
+ * stand for).  dx, db [n, dim]; dweight, dbias, dpost_weight, dpost_bias [dim]; dgate [dim] or [n, dim], as gate:
+ * each may be NULL, and is, where what it is the gradient of is (dbias apart, which needs weight alone).
+ * In fp32 throughout, each output rounded once; the sums over rows have a fixed order (no atomics).
+ *   ws     workspace of residual_norm_bwd_workspace_size(d) bytes: partial sums over the rows
+ * ------------------------------------------------------------------------------------------- */
+size_t residual_norm_bwd_workspace_size(const hpr_norm* d);
+hpr_status residual_norm_bwd(const hpr_norm* d, const uint16_t* dr, const uint16_t* dy, const void* x,
+                             const uint8_t* x_exps, const void* b, const uint8_t* b_exps,
+                             const uint16_t* weight, const uint16_t* post_weight,
+                             const uint16_t* post_bias, const uint16_t* gate, uint16_t* dx,
+                             uint16_t* db, uint16_t* dweight, uint16_t* dbias, uint16_t* dpost_weight,
+                             uint16_t* dpost_bias, uint16_t* dgate, void* ws, size_t ws_bytes,
+                             void* stream);
+
 /* Calibration for benchmarks: what the device sustains, to report beside the published peaks.
  *   hpr_mfma_calibration  launches a kernel of 8 waves per CU, each running `iters` iterations
  *                         of four independent v_mfma_f32_32x32x16_bf16 on register operands (no
@@ -488,7 +600,8 @@ hpr_status hpr_read_calibration(const void* buf, int64_t bytes, uint32_t* sink, 
  * "grad_d", "scale_grads", "dense_sample" (the sample's scores, or every score where they are all
  * stored), "dense_scan", "dense_merge", "dense_fallback", "semantic_chunk", "retrieval_metrics",
  * "attn_fwd" and "attn_bwd" (all launches of a call), "adapter_shrink", "adapter_expand",
- * "adapter_transpose", "adapter_outer", "rotary", "mfma_calibration", "read_calibration"), returns the sum of their durations in milliseconds and
+ * "adapter_transpose", "adapter_outer", "rotary", "checkpoint", "gated" (h, or dg and du), "gated_prepare" (the
+ * gradients' transposes, and fp16's maxima), "gated_product" (dx, dw_gate and dw_up), "norm_fwd", "norm_bwd", "mfma_calibration", "read_calibration"), returns the sum of their durations in milliseconds and
  * the launch count (0 and 0 for any other name, such as "pool", which is no launch of its own any
  * more), and forgets them. */
 hpr_status hpr_kernel_timing(int32_t enable);

@@ -29,6 +29,15 @@ every output, so look for the overflow of a scaled fp16 loss in out and in dout)
     adapter_linear_bwd(dy, x, W, A, B, scale, off, adapter, h) -> dict(dx, da, db)
     rotary(q, k, pos, cos, sin)                   -> (q, k) rotated, with autograd to q and k
     rotary_apply(q, k, pos, cos, sin, inverse)    -> (q, k) rotated
+    residual_norm(x, b, weight, ...)              -> (r, y): the norm after a block, gate, residual sum and the
+                                                     norm before the next, with autograd (once) to everything
+    residual_norm_fwd(x, b, weight, ...)          -> dict(r, y)
+    residual_norm_bwd(dr, dy, x, b, weight, ...)  -> dict(dx, db, dweight, dbias, dpost_weight, dpost_bias, dgate)
+    gated_linear(x, w_gate, w_up, act)            -> h = act(x w_gate^T) * (x w_up^T), with autograd (once)
+    gated_linear_fwd(x, w_gate, w_up, act)        -> dict(h)
+    gated_linear_bwd(dh, x, w_gate, w_up, act)    -> dict(dx, dw_gate, dw_up)
+    checkpoint_pack(x)                            -> Checkpoint: rows in 8 bits, which the two backward passes read
+    checkpoint_unpack(c)                          -> the rows that it stands for
 
 Q and D are bf16 CUDA tensors ([nq, lq, dim] and [n_tok, dim]); off is int64 [n_docs + 1];
 pos is int32 [nq]; Q and X of dense_ip_topk are fp16 [nq, dim] and [n, dim].  A valid CSR is a
@@ -39,6 +48,7 @@ synchronisation) and raises HprError on an invalid one.
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -100,6 +110,15 @@ _SIGNATURES = {
                                   _I32, _P, _P, _P, _P, _P, _SZ, _P]),
     "rotary_apply": (_I32, [_P, _I64, _I64, _I32, _P, _I64, _I64, _I32, _I64, _I32, _I32, _P, _P, _P,
                             _I64, _I32, _I32, _P, _P, _P]),
+    "checkpoint_pack": (_I32, [_P, _I64, _I64, _I32, _I32, _P, _P, _P]),
+    "checkpoint_unpack": (_I32, [_P, _P, _I64, _I32, _I32, _P, _P]),
+    "gated_linear_fwd": (_I32, [_P, _I64, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _P]),
+    "gated_linear_bwd_workspace_size": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I32]),
+    "gated_linear_bwd": (_I32, [_P, _P, _P, _I64, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P, _SZ,
+                                _P]),
+    "residual_norm_fwd": (_I32, [_P] * 11),
+    "residual_norm_bwd_workspace_size": (_SZ, [_P]),
+    "residual_norm_bwd": (_I32, [_P] * 19 + [_SZ, _P]),
     "hpr_mfma_calibration": (_I32, [_I64, _I32, _P, ctypes.POINTER(ctypes.c_double), _P]),
     "hpr_read_calibration": (_I32, [_P, _I64, _P, _P]),
     "hpr_csr_validate": (_I32, [_P, _I64, _I64, _P, _P, _P]),
@@ -802,6 +821,341 @@ def rotary(q, k, pos, cos, sin):
     frozen)."""
     _frozen(cos=cos, sin=sin)
     return _Rotary.apply(q, k, pos, cos, sin, False)
+
+
+def _need_rows(t, name, dtype, device):
+    """Row stride of t [rows, values], with contiguous values and 16-byte aligned rows (columns of a wider
+    tensor are fine).  One row is never stepped over: its stride counts as 0."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype or dtype not in _HALF_TYPES:
+        raise TypeError(f"{name} must be bfloat16 or float16, the same for every tensor, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have 2 dimensions, got {t.dim()}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    row = t.stride(0) if t.shape[0] > 1 else 0
+    if t.numel() and ((t.stride(1) != 1 and t.shape[1] > 1) or row % 8 or t.data_ptr() % 16):
+        raise ValueError(f"{name} must have contiguous values, and rows aligned to 16 bytes")
+    return row if t.numel() else 0
+
+
+class Checkpoint(NamedTuple):
+    """Rows in 8 bits (checkpoint_pack): codes int8 [n, dim], exps uint8 [n, ceil(dim / 32)], and the rows' type."""
+
+    codes: torch.Tensor
+    exps: torch.Tensor
+    dtype: torch.dtype
+
+
+def _need_checkpoint(c, name, dtype=None, device=None):
+    if c.dtype not in _HALF_TYPES or (dtype is not None and c.dtype != dtype):
+        raise TypeError(f"{name} must stand for {dtype or 'bfloat16 or float16'}, got {c.dtype}")
+    _need(c.codes, f"{name}.codes", torch.int8, 2, device)
+    _need(c.exps, f"{name}.exps", torch.uint8, 2, c.codes.device)
+    n, dim = c.codes.shape
+    if tuple(c.exps.shape) != (n, (dim + 31) // 32):
+        raise ValueError(f"{name}.exps must be {(n, (dim + 31) // 32)}, got {tuple(c.exps.shape)}")
+
+
+def _rows_or_checkpoint(t, name, dtype, device):
+    """(pointer, exps pointer, row stride, shape) of 16-bit rows or of a checkpoint of them."""
+    if isinstance(t, Checkpoint):
+        _need_checkpoint(t, name, dtype, device)
+        return _ptr(t.codes), _ptr(t.exps), 0, tuple(t.codes.shape)
+    row = _need_rows(t, name, dtype, device)
+    return _ptr(t), None, row, tuple(t.shape)
+
+
+def checkpoint_pack(x):
+    """x [n, dim], bf16 or fp16 (rows may be strided), in 8 bits: for every 32 values of a row a power of two
+    2^e, e = floor(log2 max|x|) - 6, and whole numbers of at most 127 times it.  A block that holds a value that
+    is not finite reads back as NaN."""
+    dtype = getattr(x, "dtype", None)
+    dev = getattr(x, "device", None)
+    row = _need_rows(x, "x", dtype, dev)
+    n, dim = x.shape
+    codes = torch.empty((n, dim), dtype=torch.int8, device=dev)
+    exps = torch.empty((n, (dim + 31) // 32), dtype=torch.uint8, device=dev)
+    _launch(lib().checkpoint_pack, dev, _ptr(x), row, n, dim, _HALF_TYPES[dtype], _ptr(codes), _ptr(exps))
+    return Checkpoint(codes, exps, dtype)
+
+
+def checkpoint_unpack(c, out=None):
+    """The rows [n, dim] that a checkpoint stands for, in its type (exactly)."""
+    if not isinstance(c, Checkpoint):
+        raise TypeError("c must be a Checkpoint")
+    _need_checkpoint(c, "c")
+    dev = c.codes.device
+    n, dim = c.codes.shape
+    if out is None:
+        out = torch.empty((n, dim), dtype=c.dtype, device=dev)
+    else:
+        _need(out, "out", c.dtype, 2, dev)
+        if out.shape != (n, dim):
+            raise ValueError(f"out must be {(n, dim)}")
+    _launch(lib().checkpoint_unpack, dev, _ptr(c.codes), _ptr(c.exps), n, dim, _HALF_TYPES[c.dtype], _ptr(out))
+    return out
+
+
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def _gated_weights(w_gate, w_up, act):
+    dtype = getattr(w_gate, "dtype", None)
+    if dtype not in _HALF_TYPES:
+        raise TypeError(f"w_gate must be a bfloat16 or float16 tensor, got {dtype or type(w_gate).__name__}")
+    _need(w_gate, "w_gate", dtype, 2)
+    dev = w_gate.device
+    _need(w_up, "w_up", dtype, 2, dev)
+    if w_gate.shape != w_up.shape:
+        raise ValueError(f"w_gate and w_up differ in shape: {tuple(w_gate.shape)}, {tuple(w_up.shape)}")
+    if act not in _ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(_ACTIVATIONS)}, got {act!r}")
+    return dev, dtype, *w_gate.shape
+
+
+def gated_linear_fwd(x, w_gate, w_up, act="silu", out=None):
+    """The gated feed-forward projections: dict(h [n, f]), h = act(x w_gate^T) * (x w_up^T).
+
+    x [n, k] (rows may be strided), w_gate and w_up [f, k], bf16 or fp16; act "silu", "gelu" or "gelu_tanh".
+    """
+    dev, dtype, f, k = _gated_weights(w_gate, w_up, act)
+    row = _need_rows(x, "x", dtype, dev)
+    n = x.shape[0]
+    if x.shape[1] != k:
+        raise ValueError(f"x has {x.shape[1]} columns, w_gate {k}")
+    if out is None:
+        out = torch.empty((n, f), dtype=dtype, device=dev)
+    else:
+        _need(out, "out", dtype, 2, dev)
+        if out.shape != (n, f):
+            raise ValueError(f"out must be {(n, f)}")
+    _launch(lib().gated_linear_fwd, dev, _ptr(x), row, n, k, _ptr(w_gate), _ptr(w_up), f, _ACTIVATIONS[act],
+            _HALF_TYPES[dtype], _ptr(out))
+    return {"h": out}
+
+
+def gated_linear_bwd(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=True, ws=None):
+    """Gradients of gated_linear_fwd's h: dict(dx, dw_gate, dw_up), dense and of the inputs' type, None where
+    not needed.  x: the forward's, or a Checkpoint of it (the gradients are those at the values that it stands
+    for).  A ws that is too small is not used."""
+    dev, dtype, f, k = _gated_weights(w_gate, w_up, act)
+    x_ptr, exps, row, shape = _rows_or_checkpoint(x, "x", dtype, dev)
+    n = shape[0]
+    if shape[1] != k:
+        raise ValueError(f"x has {shape[1]} columns, w_gate {k}")
+    _need(dh, "dh", dtype, 2, dev)
+    if dh.shape != (n, f):
+        raise ValueError(f"dh must be {(n, f)}")
+    L = lib()
+    need = L.gated_linear_bwd_workspace_size(n, k, f, exps is not None, bool(need_dx), bool(need_dw))
+    ws = ws if ws is not None and ws.numel() >= need else _workspace(need, dev)
+    dx = torch.empty((n, k), dtype=dtype, device=dev) if need_dx else None
+    dw = [torch.empty((f, k), dtype=dtype, device=dev) if need_dw else None for _ in range(2)]
+    _launch(L.gated_linear_bwd, dev, _ptr(dh), x_ptr, exps, row, n, k, _ptr(w_gate), _ptr(w_up), f,
+            _ACTIVATIONS[act], _HALF_TYPES[dtype], _ptr(dx), _ptr(dw[0]), _ptr(dw[1]), _ptr(ws), ws.numel())
+    return {"dx": dx, "dw_gate": dw[0], "dw_up": dw[1]}
+
+
+def _no_second(name):
+    """A backward pass that reads a checkpoint has not its inputs to tie a second derivative to."""
+    if torch.is_grad_enabled():
+        raise RuntimeError(f"{name} from a checkpoint has no second derivatives (create_graph)")
+
+
+class _GatedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, act, checkpoint):
+        h = gated_linear_fwd(x.detach(), w_gate.detach(), w_up.detach(), act)["h"]
+        ctx.act, ctx.packed = act, None
+        if checkpoint and any(ctx.needs_input_grad[:3]):
+            c = checkpoint_pack(x.detach())
+            ctx.packed = c.dtype
+            ctx.save_for_backward(w_gate, w_up, c.codes, c.exps)
+        else:
+            ctx.save_for_backward(w_gate, w_up, x)
+        return h
+
+    @staticmethod
+    def backward(ctx, grad_h):
+        w_gate, w_up, *x = ctx.saved_tensors
+        if ctx.packed is not None:
+            _no_second("gated_linear")
+        need = ctx.needs_input_grad
+        of = x[0].detach() if ctx.packed is None else Checkpoint(*x, ctx.packed)
+        g = gated_linear_bwd(grad_h.contiguous(), of, w_gate.detach(), w_up.detach(), ctx.act, need_dx=need[0],
+                             need_dw=need[1] or need[2])
+        dx, dg, du = _first_order("gated_linear", [g["dx"], g["dw_gate"] if need[1] else None,
+                                                   g["dw_up"] if need[2] else None],
+                                  grad_h, w_gate, w_up, *([] if ctx.packed else x))
+        return dx, dg, du, None, None
+
+
+def gated_linear(x, w_gate, w_up, act="silu", checkpoint=False):
+    """gated_linear_fwd's h, differentiable once (gradients reach x, w_gate and w_up).  Of the forward it keeps
+    x alone, with checkpoint in 8 bits."""
+    return _GatedLinear.apply(x, w_gate, w_up, act, bool(checkpoint))
+
+
+_NORMS = {"rms": 0, "layer": 1}
+
+
+class _NormDesc(ctypes.Structure):
+    _fields_ = [(n, _I64) for n in ("n", "x_row", "b_row")] + \
+               [(n, _I32) for n in ("dim", "dtype", "kind", "gate_rows")] + [("scale", _F32), ("eps", _F32)]
+
+
+def _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate, scale, eps, kind):
+    """Device, type, description, and the pointers of x, its exps, b and its exps."""
+    dtype = getattr(x, "dtype", None)
+    dev = x.codes.device if isinstance(x, Checkpoint) else getattr(x, "device", None)
+    if kind not in _NORMS:
+        raise ValueError(f"kind must be one of {', '.join(_NORMS)}, got {kind!r}")
+    if b is not None and isinstance(x, Checkpoint) != isinstance(b, Checkpoint):
+        raise TypeError("x and b must both be tensors or both be Checkpoints")
+    x_ptr, x_exps, x_row, shape = _rows_or_checkpoint(x, "x", dtype, dev)
+    if dtype not in _HALF_TYPES:
+        raise TypeError(f"x must be bfloat16 or float16, got {dtype}")
+    n, dim = shape
+    b_ptr = b_exps = None
+    b_row = 0
+    if b is not None:
+        b_ptr, b_exps, b_row, b_shape = _rows_or_checkpoint(b, "b", dtype, dev)
+        if b_shape != shape:
+            raise ValueError(f"b must be {shape}, got {b_shape}")
+    elif post_weight is not None or post_bias is not None or gate is not None:
+        raise ValueError("post_weight, post_bias and gate need b")
+    for t, name in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight"), (post_bias, "post_bias")):
+        if t is None:
+            continue
+        _need(t, name, dtype, 1, dev)
+        if t.numel() != dim:
+            raise ValueError(f"{name} must hold {dim} values, got {t.numel()}")
+    if kind != "layer" and (bias is not None or post_bias is not None):
+        raise ValueError("a bias needs kind \"layer\"")
+    if (bias is not None and weight is None) or (post_bias is not None and post_weight is None):
+        raise ValueError("a bias needs its weight")
+    gate_rows = 0
+    if gate is not None:
+        gate_rows = int(getattr(gate, "dim", int)() == 2)
+        _need(gate, "gate", dtype, 2 if gate_rows else 1, dev)
+        if tuple(gate.shape) != (shape if gate_rows else (dim,)):
+            raise ValueError(f"gate must be {(dim,)} or {shape}, got {tuple(gate.shape)}")
+    d = _NormDesc(n, x_row, b_row, dim, _HALF_TYPES[dtype], _NORMS[kind], gate_rows, float(scale), float(eps))
+    return dev, dtype, d, (x_ptr, x_exps, b_ptr, b_exps)
+
+
+def residual_norm_fwd(x, b=None, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, scale=1.0,
+                      eps=1e-6, kind="rms"):
+    """The norm after a block, its gate and residual scale, the residual sum and the norm before the next block:
+
+        p = N(b; post_weight, post_bias)   (b itself without post_weight)
+        r = x + scale * gate * p           (x itself without b)
+        y = N(r; weight, bias)             (None without weight)
+
+    dict(r, y).  x (the residual stream) and b (the block's output) [n, dim], rows may be strided; weights and
+    biases [dim]; gate [dim] or [n, dim] or None; kind "rms" or "layer" (biases are the latter's).
+    """
+    dev, dtype, d, (x_ptr, x_exps, b_ptr, _) = _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate, scale,
+                                                            eps, kind)
+    if x_exps is not None:
+        raise TypeError("x and b must be tensors")
+    r = torch.empty((d.n, d.dim), dtype=dtype, device=dev) if b is not None else None
+    y = torch.empty((d.n, d.dim), dtype=dtype, device=dev) if weight is not None else None
+    _launch(lib().residual_norm_fwd, dev, ctypes.byref(d), x_ptr, b_ptr, _ptr(weight), _ptr(bias),
+            _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(r), _ptr(y))
+    return {"r": x if b is None else r, "y": y}
+
+
+def residual_norm_bwd(dr, dy, x, b=None, weight=None, bias=None, post_weight=None, post_bias=None, gate=None,
+                      scale=1.0, eps=1e-6, kind="rms", need_dx=True, need_db=True, need_dw=True, need_dgate=True,
+                      ws=None):
+    """Gradients of residual_norm_fwd's r and y: dict(dx, db, dweight, dbias, dpost_weight, dpost_bias, dgate),
+    dense and of the inputs' type, None where there is nothing that they are the gradient of or where not needed
+    (need_dw: the weights' and biases').  dr and dy [n, dim], either may be None.  x and b: the forward's, or
+    Checkpoints of them (the gradients are those at the values that they stand for)."""
+    dev, dtype, d, (x_ptr, x_exps, b_ptr, b_exps) = _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate,
+                                                                 scale, eps, kind)
+    for t, name in ((dr, "dr"), (dy, "dy")):
+        if t is None:
+            continue
+        _need(t, name, dtype, 2, dev)
+        if t.shape != (d.n, d.dim):
+            raise ValueError(f"{name} must be {(d.n, d.dim)}")
+    if dy is not None and weight is None:
+        raise ValueError("dy needs weight")
+
+    def like(t, need):
+        return torch.empty(t.shape, dtype=dtype, device=dev) if need and t is not None else None
+
+    rows = (d.n, d.dim)
+    dx = torch.empty(rows, dtype=dtype, device=dev) if need_dx else None
+    db = torch.empty(rows, dtype=dtype, device=dev) if need_db and b is not None else None
+    dw, dc, dpw, dpc = [like(t, need_dw) for t in (weight, bias, post_weight, post_bias)]
+    dgate = like(gate, need_dgate)
+    L = lib()
+    need = L.residual_norm_bwd_workspace_size(ctypes.byref(d))
+    ws = ws if ws is not None and ws.numel() >= need else _workspace(need, dev)
+    _launch(L.residual_norm_bwd, dev, ctypes.byref(d), _ptr(dr), _ptr(dy), x_ptr, x_exps, b_ptr, b_exps,
+            _ptr(weight), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(dx), _ptr(db), _ptr(dw), _ptr(dc),
+            _ptr(dpw), _ptr(dpc), _ptr(dgate), _ptr(ws), ws.numel())
+    return {"dx": dx, "db": db, "dweight": dw, "dbias": dc, "dpost_weight": dpw, "dpost_bias": dpc, "dgate": dgate}
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, b, weight, bias, post_weight, post_bias, gate, scale, eps, kind, checkpoint):
+        of = [None if t is None else t.detach() for t in (x, b, weight, bias, post_weight, post_bias, gate)]
+        r = residual_norm_fwd(*of, scale=scale, eps=eps, kind=kind)
+        ctx.how = dict(scale=scale, eps=eps, kind=kind)
+        ctx.packed, ctx.has_b = None, b is not None
+        ctx.set_materialize_grads(False)
+        if checkpoint and any(ctx.needs_input_grad[:7]):
+            c = [checkpoint_pack(t) for t in of[:2] if t is not None]
+            ctx.packed = c[0].dtype
+            ctx.save_for_backward(weight, bias, post_weight, post_bias, gate, *(t for p in c for t in p[:2]))
+        else:
+            ctx.save_for_backward(weight, bias, post_weight, post_bias, gate, x, b)
+        # (without a block r is x, which the caller has)
+        return r["r"] if ctx.has_b else None, r["y"]
+
+    @staticmethod
+    def backward(ctx, grad_r, grad_y):
+        weight, bias, post_weight, post_bias, gate, *rows = ctx.saved_tensors
+        if ctx.packed is not None:
+            _no_second("residual_norm")
+        if grad_r is None and grad_y is None:
+            return (None,) * 11
+        need = ctx.needs_input_grad
+        if ctx.packed is None:
+            x, b = [None if t is None else t.detach() for t in rows]
+            inputs = [t for t in rows if t is not None]
+        else:
+            x, *b = [Checkpoint(*rows[i:i + 2], ctx.packed) for i in range(0, len(rows), 2)]
+            b, inputs = (b[0] if b else None), []
+        vectors = [None if t is None else t.detach() for t in (weight, bias, post_weight, post_bias, gate)]
+        g = residual_norm_bwd(*(None if t is None else t.contiguous() for t in (grad_r, grad_y)), x, b, *vectors,
+                              **ctx.how, need_dx=need[0], need_db=need[1], need_dw=any(need[2:6]),
+                              need_dgate=need[6])
+        names = ("dx", "db", "dweight", "dbias", "dpost_weight", "dpost_bias", "dgate")
+        of = [t for t in (grad_r, grad_y, *inputs, weight, bias, post_weight, post_bias, gate) if t is not None]
+        grads = _first_order("residual_norm", [g[t] if wanted else None for t, wanted in zip(names, need)], *of)
+        return (*grads, None, None, None, None)
+
+
+def residual_norm(x, b=None, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, scale=1.0,
+                  eps=1e-6, kind="rms", checkpoint=False):
+    """residual_norm_fwd's (r, y), differentiable once (gradients reach every tensor; scale and eps are frozen).
+    Of the forward it keeps x and b alone, with checkpoint in 8 bits."""
+    _frozen(scale=scale, eps=eps)
+    if b is None and weight is None:
+        raise ValueError("there is nothing to do without b and without weight")
+    r, y = _ResidualNorm.apply(x, b, weight, bias, post_weight, post_bias, gate, float(scale), float(eps), kind,
+                               bool(checkpoint))
+    return (x if b is None else r), y
 
 
 def calibrate(device="cuda:0", mfma_iters=20000, read_bytes=16 << 30, reps=3):

@@ -21,7 +21,8 @@ LIB_NAME = "libhiperrag.so"
 ARCH = "gfx950"
 
 SOURCES = ["abi.hip", "maxsim.hip", "maxsim_argmax.hip", "topk.hip", "loss.hip", "contrastive.hip",
-           "dense.hip", "chunking.hip", "calibration.hip", "attention.hip", "adapters.hip", "rotary.hip"]
+           "dense.hip", "chunking.hip", "calibration.hip", "attention.hip", "adapters.hip", "rotary.hip",
+           "gated.hip", "norm.hip", "checkpoint.hip"]
 
 
 def _hipcc():

@@ -412,6 +412,85 @@ hpr_status check_adapters(const uint16_t* x, int64_t n, int32_t k, const uint16_
 
 }  // namespace
 
+namespace {
+
+// Shared checks of tensors [n, dim] with a row stride.
+hpr_status check_rows(const char* what, int64_t n, int32_t dim, int64_t row, int32_t dtype) {
+  if (n < 0 || n >= (int64_t(1) << 31))
+    return fail(HPR_ERR_INVALID_ARG, "n (%lld) must satisfy 0 <= n < 2^31", (long long)n);
+  if (dtype != HPR_BF16 && dtype != HPR_F16)
+    return fail(HPR_ERR_INVALID_ARG, "dtype (%d) must be HPR_BF16 or HPR_F16", dtype);
+  if (dim < 8 || dim % 8 != 0 || dim > 65536)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%s needs rows of 8 to 65536 values, a multiple of 8 (got %d)", what, dim);
+  if (row < 0 || row % 8 != 0 || row >= (int64_t(1) << 20))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%s: a row stride (%lld) must be a multiple of 8 below 2^20", what,
+                (long long)row);
+  return HPR_OK;
+}
+
+bool checkpoint_fits(int64_t n, int32_t dim) {
+  return launch_fits((n * ((dim + 31) / 32 * 4) + 255) / 256, 256);
+}
+
+hpr_status check_gated(int64_t n, int32_t k, int32_t f, int64_t x_row, int32_t act, int32_t dtype, const void* x,
+                       const uint16_t* w_gate, const uint16_t* w_up) {
+  const hpr_status st = check_rows("gated_linear", n, k, x_row, dtype);
+  if (st != HPR_OK) return st;
+  if (f < 8 || f % 8 != 0 || f > 65536)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "gated_linear needs f %% 8 == 0 and 8 <= f <= 65536 (f=%d)", f);
+  if (act != HPR_SILU && act != HPR_GELU && act != HPR_GELU_TANH)
+    return fail(HPR_ERR_INVALID_ARG, "act (%d) must be HPR_SILU, HPR_GELU or HPR_GELU_TANH", act);
+  if (!w_gate || !w_up || (n > 0 && !x))
+    return fail(HPR_ERR_INVALID_ARG, "x, w_gate and w_up must be non-NULL");
+  if (!aligned16(x) || !aligned16(w_gate) || !aligned16(w_up))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  return HPR_OK;
+}
+
+// Where the pieces of the gradients' workspace lie.
+struct GatedCarve {
+  uint16_t *wt, *d, *dt, *xt, *plain;
+  uint32_t* words;  // maxima of rows, then of columns
+  size_t bytes;
+};
+GatedCarve gated_carve(void* ws, int64_t n, int32_t k, int32_t f, bool packed, bool need_dx, bool need_dw) {
+  const size_t np = (size_t)(n + 7) / 8 * 8;
+  GatedCarve g = {};
+  char* at = static_cast<char*>(ws);
+  auto take = [&](size_t bytes) {
+    char* p = at ? at + g.bytes : nullptr;
+    g.bytes += align_up(bytes);
+    return p;
+  };
+  if (need_dx) g.wt = reinterpret_cast<uint16_t*>(take((size_t)k * 2 * f * 2));
+  if (need_dx) g.d = reinterpret_cast<uint16_t*>(take((size_t)n * 2 * f * 2));
+  if (need_dw) g.dt = reinterpret_cast<uint16_t*>(take(np * 2 * f * 2));
+  if (need_dw) g.xt = reinterpret_cast<uint16_t*>(take(np * k * 2));
+  if (packed) g.plain = reinterpret_cast<uint16_t*>(take((size_t)n * k * 2));
+  g.words = reinterpret_cast<uint32_t*>(take(((size_t)n + f) * sizeof(uint32_t)));
+  return g;
+}
+
+hpr_status check_norm(const hpr_norm* d, bool packed) {
+  if (!d) return fail(HPR_ERR_INVALID_ARG, "the description must be non-NULL");
+  hpr_status st = check_rows("residual_norm", d->n, d->dim, packed ? 0 : d->x_row, d->dtype);
+  if (st == HPR_OK && !packed) st = check_rows("residual_norm", d->n, d->dim, d->b_row, d->dtype);
+  if (st != HPR_OK) return st;
+  if (d->dim > kMaxNormDim)
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "residual_norm needs dim <= %d (dim=%d)", kMaxNormDim, d->dim);
+  if (d->kind != HPR_RMS_NORM && d->kind != HPR_LAYER_NORM)
+    return fail(HPR_ERR_INVALID_ARG, "kind (%d) must be HPR_RMS_NORM or HPR_LAYER_NORM", d->kind);
+  if (d->gate_rows != 0 && d->gate_rows != 1)
+    return fail(HPR_ERR_INVALID_ARG, "gate_rows (%d) must be 0 or 1", d->gate_rows);
+  if (!(d->eps > 0.f) || !(d->eps < 3.0e38f) || !(d->scale > -3.0e38f) || !(d->scale < 3.0e38f))
+    return fail(HPR_ERR_INVALID_ARG, "eps must be positive, scale and eps finite");
+  if (!norm_fits(d->n, d->dim))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%lld rows of %d are more than one launch holds", (long long)d->n, d->dim);
+  return HPR_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 size_t maxsim_score_workspace_size(int32_t nq, int32_t lq, int64_t n_docs, int64_t n_tok,
@@ -832,6 +911,253 @@ hpr_status rotary_apply(const uint16_t* q, int64_t q_row, int64_t q_head, int32_
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = timed("rotary", s, [&] { return launch_rotary(a, s); });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "rotary launch");
+}
+
+hpr_status checkpoint_pack(const uint16_t* x, int64_t x_row, int64_t n, int32_t dim, int32_t dtype, int8_t* codes,
+                           uint8_t* exps, void* stream) {
+  const hpr_status st = check_rows("checkpoint_pack", n, dim, x_row, dtype);
+  if (st != HPR_OK) return st;
+  if (!checkpoint_fits(n, dim))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%lld rows of %d are more than one launch holds", (long long)n, dim);
+  if (n == 0) return HPR_OK;
+  if (!x || !codes || !exps) return fail(HPR_ERR_INVALID_ARG, "x, codes and exps must be non-NULL");
+  if (!aligned16(x) || !aligned16(codes) || !aligned16(exps))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = timed("checkpoint", s, [&] {
+    return launch_checkpoint_pack(x, x_row, n, dim, dtype == HPR_F16, codes, exps, s);
+  });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "checkpoint launch");
+}
+
+hpr_status checkpoint_unpack(const int8_t* codes, const uint8_t* exps, int64_t n, int32_t dim, int32_t dtype,
+                             uint16_t* x, void* stream) {
+  const hpr_status st = check_rows("checkpoint_unpack", n, dim, 0, dtype);
+  if (st != HPR_OK) return st;
+  if (!checkpoint_fits(n, dim))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%lld rows of %d are more than one launch holds", (long long)n, dim);
+  if (n == 0) return HPR_OK;
+  if (!x || !codes || !exps) return fail(HPR_ERR_INVALID_ARG, "codes, exps and x must be non-NULL");
+  if (!aligned16(x) || !aligned16(codes) || !aligned16(exps))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = timed("checkpoint", s, [&] {
+    return launch_checkpoint_unpack(codes, exps, n, dim, dtype == HPR_F16, x, s);
+  });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "checkpoint launch");
+}
+
+hpr_status gated_linear_fwd(const uint16_t* x, int64_t x_row, int64_t n, int32_t k, const uint16_t* w_gate,
+                            const uint16_t* w_up, int32_t f, int32_t act, int32_t dtype, uint16_t* h, void* stream) {
+  const hpr_status st = check_gated(n, k, f, x_row, act, dtype, x, w_gate, w_up);
+  if (st != HPR_OK) return st;
+  if (!gated_fits(n, k, f, false))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%lld rows of %d are more than one launch holds", (long long)n, f);
+  if (n == 0) return HPR_OK;
+  if (!h || !aligned16(h)) return fail(HPR_ERR_INVALID_ARG, "h must be non-NULL and 16-byte aligned");
+  GatedArgs a = {};
+  a.x = x;
+  a.wg = w_gate;
+  a.wu = w_up;
+  a.n = n;
+  a.x_ld = x_row;
+  a.k = k;
+  a.f = f;
+  a.act = act;
+  a.f16 = dtype == HPR_F16;
+  a.h = h;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = timed("gated", s, [&] { return launch_gated(a, false, s); });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "gated projections launch");
+}
+
+size_t gated_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t f, int32_t packed, int32_t need_dx,
+                                       int32_t need_dw) {
+  if (n < 0 || n >= (int64_t(1) << 31) || k < 8 || k > 65536 || f < 8 || f > 65536) return 0;
+  return gated_carve(nullptr, n, k, f, packed != 0, need_dx != 0, need_dw != 0).bytes;
+}
+
+hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_exps, int64_t x_row, int64_t n,
+                            int32_t k, const uint16_t* w_gate, const uint16_t* w_up, int32_t f, int32_t act,
+                            int32_t dtype, uint16_t* dx, uint16_t* dw_gate, uint16_t* dw_up, void* ws,
+                            size_t ws_bytes, void* stream) {
+  const bool packed = x_exps != nullptr, narrow = dtype == HPR_F16;
+  const hpr_status st = check_gated(n, k, f, packed ? 0 : x_row, act, dtype, x, w_gate, w_up);
+  if (st != HPR_OK) return st;
+  if (!dw_gate != !dw_up)
+    return fail(HPR_ERR_INVALID_ARG, "dw_gate and dw_up are computed together: both or neither");
+  const bool need_dx = dx != nullptr, need_dw = dw_gate != nullptr;
+  if (!gated_fits(n, k, f, true) || (need_dw && n > (int64_t(1) << 21)))
+    return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%lld rows of %d are more than the gradients' launches hold", (long long)n,
+                f);
+  if (n > 0 && !dh) return fail(HPR_ERR_INVALID_ARG, "dh must be non-NULL");
+  if (!aligned16(dh) || !aligned16(x_exps) || !aligned16(dx) || !aligned16(dw_gate) || !aligned16(dw_up))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  if (!need_dx && !need_dw) return HPR_OK;
+  const GatedCarve g = gated_carve(ws, n, k, f, packed, need_dx, need_dw);
+  if (!ws || ws_bytes < g.bytes)
+    return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, g.bytes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t np = (n + 7) / 8 * 8;
+  uint32_t *const row_max = g.words, *const col_max = g.words + n;
+  hipError_t e = hipSuccess;
+  if (n > 0) {
+    const uint16_t* const x16 = packed ? nullptr : static_cast<const uint16_t*>(x);
+    const int8_t* const codes = packed ? static_cast<const int8_t*>(x) : nullptr;
+    GatedPrepare p = {};
+    if (need_dx) {
+      p.job[0] = {w_gate, k, nullptr, nullptr, f, k, g.wt, 2 * (int64_t)f, nullptr, 0};
+      p.job[1] = {w_up, k, nullptr, nullptr, f, k, g.wt + f, 2 * (int64_t)f, nullptr, 0};
+    }
+    if (need_dw || packed) p.job[2] = {x16, x_row, codes, x_exps, n, k, g.xt, np, g.plain, 0};
+    if (narrow) {
+      p.clear = g.words;
+      p.words = n + f;
+    }
+    e = timed("gated_prepare", s, [&] {
+      hipError_t q = launch_gated_prepare(p, narrow, s);
+      if (q == hipSuccess && narrow) q = launch_gated_max(dh, n, f, row_max, col_max, s);
+      return q;
+    });
+    GatedArgs a = {};
+    a.x = packed ? g.plain : x16;
+    a.wg = w_gate;
+    a.wu = w_up;
+    a.n = n;
+    a.x_ld = packed ? k : x_row;
+    a.k = k;
+    a.f = f;
+    a.act = act;
+    a.f16 = narrow;
+    a.dh = dh;
+    a.d = g.d;
+    a.dt = g.dt;
+    a.np = np;
+    a.row_max = row_max;
+    a.col_max = col_max;
+    if (e == hipSuccess) e = timed("gated", s, [&] { return launch_gated(a, true, s); });
+  }
+  if (e == hipSuccess && need_dx && n > 0)
+    e = timed("gated_product", s, [&] {
+      const ProductArgs q = {g.d, g.wt, n, k, 2 * f, 2 * f, {dx, nullptr}, n, row_max, 0};
+      return launch_rows_product(q, narrow, s);
+    });
+  if (e == hipSuccess && need_dw)  // (without a row the sums are empty, and the product writes zeros)
+    e = timed("gated_product", s, [&] {
+      const ProductArgs q = {g.dt, g.xt, 2 * (int64_t)f, k, (int)np, (int)np, {dw_gate, dw_up}, f, col_max, 0};
+      return launch_rows_product(q, narrow, s);
+    });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "gated gradient launch");
+}
+
+hpr_status residual_norm_fwd(const hpr_norm* d, const uint16_t* x, const uint16_t* b, const uint16_t* weight,
+                             const uint16_t* bias, const uint16_t* post_weight, const uint16_t* post_bias,
+                             const uint16_t* gate, uint16_t* r, uint16_t* y, void* stream) {
+  const hpr_status st = check_norm(d, false);
+  if (st != HPR_OK) return st;
+  const bool layer = d->kind == HPR_LAYER_NORM;
+  if (d->n > 0 && !b && (post_weight || gate || r))
+    return fail(HPR_ERR_INVALID_ARG, "without b there is no post_weight, gate or r");
+  if (!weight && y) return fail(HPR_ERR_INVALID_ARG, "y needs weight");
+  if ((bias && (!weight || !layer)) || (post_bias && (!post_weight || !layer)))
+    return fail(HPR_ERR_INVALID_ARG, "a bias needs its weight and HPR_LAYER_NORM");
+  if (!aligned16(x) || !aligned16(b) || !aligned16(weight) || !aligned16(bias) || !aligned16(post_weight) ||
+      !aligned16(post_bias) || !aligned16(gate) || !aligned16(r) || !aligned16(y))
+    return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  if (d->n == 0 || (!r && !y)) return HPR_OK;
+  if (!x) return fail(HPR_ERR_INVALID_ARG, "x must be non-NULL");
+  NormArgs a = {};
+  a.x = x;
+  a.b = b;
+  a.x_ld = d->x_row;
+  a.b_ld = d->b_row;
+  a.w = weight;
+  a.c = bias;
+  a.pw = post_weight;
+  a.pc = post_bias;
+  a.gate = gate;
+  a.gate_rows = gate && d->gate_rows;
+  a.layer = layer;
+  a.f16 = d->dtype == HPR_F16;
+  a.scale = d->scale;
+  a.eps = d->eps;
+  a.n = d->n;
+  a.d = d->dim;
+  a.r = r;
+  a.y = y;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = timed("norm_fwd", s, [&] { return launch_norm_fwd(a, s); });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "norm launch");
+}
+
+size_t residual_norm_bwd_workspace_size(const hpr_norm* d) {
+  if (!d || d->n < 0 || d->n >= (int64_t(1) << 31) || d->dim < 8 || d->dim > kMaxNormDim) return 0;
+  return align_up((size_t)norm_parts(d->n, d->dim) * norm_sums(d->kind == HPR_LAYER_NORM) * d->dim * sizeof(float));
+}
+
+hpr_status residual_norm_bwd(const hpr_norm* d, const uint16_t* dr, const uint16_t* dy, const void* x,
+                             const uint8_t* x_exps, const void* b, const uint8_t* b_exps, const uint16_t* weight,
+                             const uint16_t* post_weight, const uint16_t* post_bias, const uint16_t* gate,
+                             uint16_t* dx, uint16_t* db, uint16_t* dweight, uint16_t* dbias, uint16_t* dpost_weight,
+                             uint16_t* dpost_bias, uint16_t* dgate, void* ws, size_t ws_bytes, void* stream) {
+  const bool packed = x_exps != nullptr;
+  const hpr_status st = check_norm(d, packed);
+  if (st != HPR_OK) return st;
+  const bool layer = d->kind == HPR_LAYER_NORM;
+  if (b && packed != (b_exps != nullptr))
+    return fail(HPR_ERR_INVALID_ARG, "x and b are both 16-bit rows or both checkpoints");
+  if (d->n > 0 && !b && (post_weight || gate || db))
+    return fail(HPR_ERR_INVALID_ARG, "without b there is no post_weight, gate or db");
+  if (!weight && (dy || dweight || dbias)) return fail(HPR_ERR_INVALID_ARG, "dy, dweight and dbias need weight");
+  if ((!post_weight && dpost_weight) || (!gate && dgate))
+    return fail(HPR_ERR_INVALID_ARG, "dpost_weight and dgate need post_weight and gate");
+  if ((dbias && !layer) || ((post_bias || dpost_bias) && (!post_weight || !layer)))
+    return fail(HPR_ERR_INVALID_ARG, "a bias needs its weight and HPR_LAYER_NORM");
+  for (const void* p : {(const void*)dr, (const void*)dy, x, (const void*)x_exps, b, (const void*)b_exps,
+                        (const void*)weight, (const void*)post_weight, (const void*)post_bias, (const void*)gate,
+                        (const void*)dx, (const void*)db, (const void*)dweight, (const void*)dbias,
+                        (const void*)dpost_weight, (const void*)dpost_bias, (const void*)dgate})
+    if (!aligned16(p)) return fail(HPR_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  if (d->n > 0 && !x) return fail(HPR_ERR_INVALID_ARG, "x must be non-NULL");
+  const size_t need = residual_norm_bwd_workspace_size(d);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+  NormArgs a = {};
+  if (packed) {
+    a.x_codes = static_cast<const int8_t*>(x);
+    a.x_exps = x_exps;
+    a.b_codes = static_cast<const int8_t*>(b);
+    a.b_exps = b_exps;
+  } else {
+    a.x = static_cast<const uint16_t*>(x);
+    a.b = static_cast<const uint16_t*>(b);
+    a.x_ld = d->x_row;
+    a.b_ld = d->b_row;
+  }
+  a.w = weight;
+  a.pw = post_weight;
+  a.pc = post_bias;
+  a.gate = gate;
+  a.gate_rows = gate && d->gate_rows;
+  a.layer = layer;
+  a.f16 = d->dtype == HPR_F16;
+  a.scale = d->scale;
+  a.eps = d->eps;
+  a.n = d->n;
+  a.d = d->dim;
+  a.dr = dr;
+  a.dy = dy;
+  a.dx = dx;
+  a.db = db;
+  a.dw = dweight;
+  a.dc = dbias;
+  a.dpw = dpost_weight;
+  a.dpc = dpost_bias;
+  (a.gate_rows ? a.dgate_rows : a.dgate) = dgate;
+  a.part = static_cast<float*>(ws);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = timed("norm_bwd", s, [&] { return launch_norm_bwd(a, s); });
+  return e == hipSuccess ? HPR_OK : hip_fail(e, "norm gradient launch");
 }
 
 hpr_status hpr_mfma_calibration(int64_t iters, int32_t operands, float* sink, double* flops,

@@ -1,0 +1,604 @@
+// The gated feed-forward projections and their gradients.
+//
+//   g_t = Wg x_t,  u_t = Wu x_t,  h_t = act(g_t) u_t
+// and for a gradient dh
+//   dg = dh u act'(g),  du = dh act(g),
+//   dx = Wg^T dg + Wu^T du,  dWg = sum_t dg_t x_t^T,  dWu = sum_t du_t x_t^T.
+//
+// Forward: one product whose tiles hold the same columns of Wg and of Wu (PAIR in product.h), so that g and u
+// of a value of h meet in one lane's registers, and the activation and the product are its epilogue: g and u
+// never reach memory.  Backward: the same product again, whose epilogue reads dh and writes d = (dg | du); x is
+// all that it needs of the forward, and g and u are those of 32 bits, not a rounding of them kept over the
+// pass (which would cost 2 k / f of a row more memory, and the exactness of d).  dx is one product of d's rows
+// with the weights' columns, and dW one of d's columns with x's: the weights and x are transposed
+// first (prepare_kernel), d is written both ways round by the epilogue.
+#include "checkpoint.h"
+#include "common.h"
+#include "half.h"
+#include "kernels.h"
+#include "product.h"
+#include "tiles.h"
+
+namespace hpr {
+
+namespace {
+
+// ---- activations ------------------------------------------------------------------------------
+
+// exp of a 32-bit number, relative error (|x| + 2) 2^-24: far below the rounding of what it goes into.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+struct Silu {
+  // (exp overflows to infinity below -88, where the value is 0 to within 1e-36)
+  static __device__ __forceinline__ float sigmoid(float g) {
+    return __builtin_amdgcn_rcpf(1.f + exp_of(-g));
+  }
+  static __device__ __forceinline__ float value(float g) { return g * sigmoid(g); }
+  static __device__ __forceinline__ void both(float g, float& v, float& slope) {
+    const float s = sigmoid(g);
+    v = g * s;
+    slope = s * (1.f + g * (1.f - s));
+  }
+};
+
+// g Phi(g); erfc keeps the lower tail's digits.
+struct Gelu {
+  static __device__ __forceinline__ float cdf(float g) { return 0.5f * erfcf(g * -0.70710678f); }
+  static __device__ __forceinline__ float value(float g) { return g * cdf(g); }
+  static __device__ __forceinline__ void both(float g, float& v, float& slope) {
+    const float p = cdf(g);
+    v = g * p;
+    slope = p + g * 0.39894228f * exp_of(-0.5f * g * g);
+  }
+};
+
+// g (1 + tanh z) / 2 = g / (1 + exp(-2 z)), z = sqrt(2 / pi) (g + 0.044715 g^3)
+struct GeluTanh {
+  static __device__ __forceinline__ float part(float g) {
+    return __builtin_amdgcn_rcpf(1.f + exp_of(-1.59576912f * g * (1.f + 0.044715f * g * g)));
+  }
+  static __device__ __forceinline__ float value(float g) { return g * part(g); }
+  static __device__ __forceinline__ void both(float g, float& v, float& slope) {
+    const float s = part(g);
+    v = g * s;
+    // (s (1 - s) is 0 in 32 bits long before g^2 passes them)
+    const float q = s * (1.f - s);
+    slope = s + (q > 0.f ? g * q * 1.59576912f * (1.f + 0.134145f * g * g) : 0.f);
+  }
+};
+
+// ---- powers of two of fp16 --------------------------------------------------------------------
+
+// dg and du are products' operands in 16 bits.  fp16 has few exponents: where dh is small (a loss that is
+// not scaled), they would lose bits below 2^-14.  So a row of d is written for dx times the power of two that
+// brings the row's largest |dh| into [1, 2), a column for dW times that of its column, and the products'
+// results are multiplied back in 32 bits: exactly undone, whatever the size of dh.  What is left are factors
+// act(g) and u act'(g) as small as the forward's own h, which fp16 rounds as coarsely; and they overflow where
+// they pass 2^15, as a finite h all but excludes.
+// bits: the largest |value| of fp16 as a whole number (max_kernel); 0 and infinities stay as they are.
+__device__ __forceinline__ int up_of(uint32_t bits) {
+  if (bits == 0 || bits >= 0x7c00) return 0;
+  const float v = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+  return 127 - (int)(__float_as_uint(v) >> 23);
+}
+__device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Largest |dh| of every row and column: 64 rows of 512 columns per workgroup, a row per wave at a time.  The
+// maxima of workgroups meet in atomic maxima of whole numbers, which have no order.
+__global__ __launch_bounds__(256) void max_kernel(const uint16_t* dh, int64_t n, int f, uint32_t* rows,
+                                                  uint32_t* cols) {
+  __shared__ uint32_t part[4][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t n_c = (uint32_t)(f + 511) / 512u;
+  const int c = (int)(blockIdx.x % n_c) * 512 + 8 * lane;
+  const int64_t t0 = (int64_t)(blockIdx.x / n_c) * 64;
+  uint32_t most[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int i = wave; i < 64 && t0 + i < n; i += 4) {
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (c < f) v = load16(dh + (t0 + i) * f + c);
+    uint32_t row = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t b = (v[e >> 1] >> (16 * (e & 1))) & 0x7fffu;
+      most[e] = most[e] > b ? most[e] : b;
+      row = row > b ? row : b;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const uint32_t o = (uint32_t)__shfl_xor((int)row, d);
+      row = row > o ? row : o;
+    }
+    if (lane == 0) atomicMax(rows + t0 + i, row);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) part[wave][8 * lane + e] = most[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 512; i += 256) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = m > part[w][i] ? m : part[w][i];
+    const int col = (int)(blockIdx.x % n_c) * 512 + i;
+    if (col < f) atomicMax(cols + col, m);
+  }
+}
+
+// ---- h, and d -----------------------------------------------------------------------------------
+
+// dg and du of one value.
+template <class A>
+__device__ __forceinline__ void gradients(float g, float u, float dh, float& dg, float& du) {
+  float v, slope;
+  A::both(g, v, slope);
+  dg = dh * u * slope;
+  du = dh * v;
+}
+
+template <class T, class A, int BT, int BM, int WT, int WM, int NST, bool GRAD>
+__device__ __forceinline__ void gated_tile(const GatedArgs& a) {
+  using P = TileProduct<T, BT, BM, WT, WM, NST, true>;
+  constexpr int kTb = P::kTb, kMb = P::kMb, kHb = kMb / 2;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // P::kLds
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wt = wave % WT, wm = wave / WT;
+  const int n_m = (a.f + P::kCols - 1) / P::kCols;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + BT - 1) / BT), n_m);
+  const int64_t t0 = a.row0 + (int64_t)at.t * BT;
+  const int m0 = at.m * P::kCols;
+  const int64_t left_t = a.n - t0;
+  const int last_t = left_t < BT ? (int)left_t - 1 : BT - 1;
+  const int last_m = a.f - m0 < P::kCols ? a.f - m0 - 1 : P::kCols - 1;
+  typename P::Acc acc;
+  const int64_t w0 = (int64_t)m0 * a.k;
+  P::run(a.x + t0 * a.x_ld, (int)a.x_ld, last_t, {{a.wg + w0, a.wu + w0}, a.k, last_m}, a.k, smem, wave, lane,
+         acc, [](typename P::Acc&) {});
+
+  const int mw = m0 + wm * P::kWaveCols;       // the wave's first column
+  const int64_t tw = t0 + wt * kTb * 32;       // and row
+  constexpr int kOwn = 32 * 64 * (kHb > kTb ? kHb : kTb);
+  static_assert(P::kW * kOwn <= P::kLds, "the waves' blocks fit the ring");
+  unsigned char* own = smem + wave * kOwn;
+  if constexpr (!GRAD) {
+#pragma unroll
+    for (int j = 0; j < kTb; ++j)
+      store_rows<T, kHb>(a.h + (tw + 32 * j) * a.f + mw, a.f, a.n - tw - 32 * j, a.f - mw, own, lane,
+                         [&](int i, int r) { return A::value(acc[i][j][r]) * acc[i + kHb][j][r]; });
+    return;
+  } else {
+    // d in the place of g and u; 0 past the last row
+#pragma unroll
+    for (int j = 0; j < kTb; ++j) {
+      const int64_t t = tw + 32 * j + col;
+#pragma unroll
+      for (int i = 0; i < kHb; ++i) {
+        uint2 w[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int m = mw + 32 * i + 8 * g + 4 * half;
+          w[g] = uint2{0u, 0u};
+          if (t < a.n && m < a.f) w[g] = *reinterpret_cast<const uint2*>(a.dh + t * a.f + m);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t b = e < 2 ? w[g].x : w[g].y;
+            float dg, du;
+            gradients<A>(acc[i][j][4 * g + e], acc[i + kHb][j][4 * g + e], e & 1 ? T::hi(b) : T::lo(b), dg, du);
+            acc[i][j][4 * g + e] = t < a.n ? dg : 0.f;
+            acc[i + kHb][j][4 * g + e] = t < a.n ? du : 0.f;
+          }
+      }
+    }
+    if (a.d) {
+#pragma unroll
+      for (int j = 0; j < kTb; ++j) {
+        const int64_t t = tw + 32 * j + col;
+        float up = 1.f;
+        if constexpr (T::kNarrow) up = power_of(up_of(a.row_max[t < a.n ? t : a.n - 1]));
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          store_rows<T, kHb>(a.d + (tw + 32 * j) * 2 * a.f + (int64_t)s * a.f + mw, 2 * (int64_t)a.f,
+                             a.n - tw - 32 * j, a.f - mw, own, lane,
+                             [&](int i, int r) { return acc[s * kHb + i][j][r] * up; });
+      }
+    }
+    if (a.dt) {  // 32 columns of d at a time, 32 kTb values of each
+      constexpr int kRow = 64 * kTb, kCh = kRow / 16, kPer = 64 / kCh;
+#pragma unroll
+      for (int i = 0; i < kMb; ++i) {
+        const int m_first = mw + 32 * (i % kHb);
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int r0 = 8 * g + 4 * half;
+          float up[4] = {1.f, 1.f, 1.f, 1.f};
+          if constexpr (T::kNarrow) {
+            if (m_first + r0 < a.f) {
+              const u32x4 bits = *reinterpret_cast<const u32x4*>(a.col_max + m_first + r0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) up[e] = power_of(up_of(bits[e]));
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kTb; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = r0 + e;
+              *reinterpret_cast<uint16_t*>(own + r * kRow + (((4 * j + (col >> 3)) ^ (r % kCh)) << 4) +
+                                           2 * (col & 7)) = (uint16_t)T::pack(acc[i][j][4 * g + e] * up[e], 0.f);
+            }
+        }
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+        for (int q = 0; q < 32 / kPer; ++q) {
+          const int r = q * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh);
+          const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
+          const int m = m_first + r;
+          if (m < a.f && tw + 8 * c < a.np)
+            *reinterpret_cast<u32x4*>(a.dt + ((int64_t)(i < kHb ? 0 : a.f) + m) * a.np + tw + 8 * c) = v;
+        }
+      }
+    }
+  }
+}
+
+template <class T, class A, int BT, int BM, int WT, int WM, int NST, int MINB, bool GRAD>
+__global__ __launch_bounds__(64 * WT * WM, MINB) void gated_kernel(GatedArgs a) {
+  gated_tile<T, A, BT, BM, WT, WM, NST, GRAD>(a);
+}
+
+// Few rows: 32 rows of x by 16 columns of h per workgroup.  Eight waves split k and sum in LDS.
+constexpr int kFewWaves = 8;
+template <class T>
+using GatedFew = WaveProduct<T, 1, 1, 2, 32, true>;
+template <class T>
+constexpr int kGatedFewLds = kFewWaves * GatedFew<T>::kBytes;
+
+template <class T, class A, bool GRAD>
+__device__ __forceinline__ void gated_few(const GatedArgs& a) {
+  using P = GatedFew<T>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t n_m = (uint32_t)(a.f + 15) / 16u;
+  const int m0 = (int)(blockIdx.x % n_m) * 16;
+  const int64_t t0 = (int64_t)(blockIdx.x / n_m) * 32;
+  const int nk = (a.k + 63) / 64;
+  f32x16 acc[1][1];
+  unsigned char* own = smem + wave * P::kBytes;
+  const int64_t w0 = (int64_t)m0 * a.k;
+  P::run(a.x + t0 * a.x_ld, (int)a.x_ld, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31,
+         {{a.wg + w0, a.wu + w0}, a.k, a.f - m0 < 16 ? a.f - m0 - 1 : 15}, a.k, nk * wave / kFewWaves,
+         nk * (wave + 1) / kFewWaves, own, lane, acc);
+  float* part = reinterpret_cast<float*>(own);  // [16][64]
+#pragma unroll
+  for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];
+  __syncthreads();
+  // thread: two columns of a row.  Column m < 16 of wg is entry e = 4 (m / 8) + m % 4 of lane
+  // (row, half (m / 4) % 2), that of wu entry e + 8.
+  if (threadIdx.x >= 256) return;
+  const int row = threadIdx.x & 31, m = 2 * (threadIdx.x >> 5);
+  const int e = 4 * (m >> 3) + (m & 3), from = row + 32 * ((m >> 2) & 1);
+  float g[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    const float* p = reinterpret_cast<const float*>(smem + w * P::kBytes) + from;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      g[c] += p[(e + c) * 64];
+      u[c] += p[(e + 8 + c) * 64];
+    }
+  }
+  const int64_t t = t0 + row;
+  if (m0 + m >= a.f) return;
+  if constexpr (!GRAD) {
+    if (t < a.n)
+      *reinterpret_cast<uint32_t*>(a.h + t * a.f + m0 + m) =
+          T::pack(A::value(g[0]) * u[0], A::value(g[1]) * u[1]);
+  } else {
+    float dg[2] = {0.f, 0.f}, du[2] = {0.f, 0.f};
+    if (t < a.n) {
+      const uint32_t b = *reinterpret_cast<const uint32_t*>(a.dh + t * a.f + m0 + m);
+      gradients<A>(g[0], u[0], T::lo(b), dg[0], du[0]);
+      gradients<A>(g[1], u[1], T::hi(b), dg[1], du[1]);
+      if (a.d) {
+        float up = 1.f;
+        if constexpr (T::kNarrow) up = power_of(up_of(a.row_max[t]));
+        uint16_t* d = a.d + t * 2 * a.f + m0 + m;
+        *reinterpret_cast<uint32_t*>(d) = T::pack(dg[0] * up, dg[1] * up);
+        *reinterpret_cast<uint32_t*>(d + a.f) = T::pack(du[0] * up, du[1] * up);
+      }
+    }
+    if (a.dt && t < a.np) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float up = 1.f;
+        if constexpr (T::kNarrow) up = power_of(up_of(a.col_max[m0 + m + c]));
+        uint16_t* d = a.dt + (int64_t)(m0 + m + c) * a.np + t;
+        d[0] = (uint16_t)T::pack(dg[c] * up, 0.f);
+        d[(int64_t)a.f * a.np] = (uint16_t)T::pack(du[c] * up, 0.f);
+      }
+    }
+  }
+}
+
+template <class T, class A, bool GRAD>
+__global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(GatedArgs a) {
+  gated_few<T, A, GRAD>(a);
+}
+
+// ---- dx, dW -------------------------------------------------------------------------------------
+
+// y[r][c] = 2^-up(r) <x_r, w_c>, rows [0, split) to y[0], the others to y[1].
+template <class T, int BT, int BM, int WT, int WM, int NST>
+__device__ __forceinline__ void rows_tile(const ProductArgs& a) {
+  using P = TileProduct<T, BT, BM, WT, WM, NST>;
+  constexpr int kTb = P::kTb, kMb = P::kMb;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // P::kLds
+  const int lane = threadIdx.x & 63, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wt = wave % WT, wm = wave / WT;
+  const int n_m = (a.m + BM - 1) / BM;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + BT - 1) / BT), n_m);
+  const int64_t t0 = a.row0 + (int64_t)at.t * BT;
+  const int m0 = at.m * BM;
+  const int64_t left_t = a.n - t0;
+  const int last_t = left_t < BT ? (int)left_t - 1 : BT - 1;
+  const int last_m = a.m - m0 < BM ? a.m - m0 - 1 : BM - 1;
+  typename P::Acc acc;
+  P::run(a.x + t0 * a.ld, a.ld, last_t, {{a.w + (int64_t)m0 * a.ld, nullptr}, a.ld, last_m}, a.k, smem, wave,
+         lane, acc, [](typename P::Acc&) {});
+  static_assert(P::kW * 32 * 64 * kMb <= P::kLds, "the waves' blocks fit the ring");
+  unsigned char* own = smem + wave * 32 * 64 * kMb;
+  const int mw = m0 + wm * kMb * 32;
+#pragma unroll
+  for (int j = 0; j < kTb; ++j) {
+    const int64_t r0 = t0 + (wt * kTb + j) * 32;
+    float down = 1.f;
+    if constexpr (T::kNarrow) {
+      const int64_t t = r0 + col < a.n ? r0 + col : a.n - 1;
+      down = power_of(-up_of(a.max_bits[t < a.split ? t : t - a.split]));
+    }
+    auto value = [&](int i, int r) { return acc[i][j][r] * down; };
+    // (the split may lie inside a tile: every row goes to the output that it is of)
+    const int64_t n_first = a.n < a.split ? a.n : a.split;
+    if (r0 < a.split) store_rows<T, kMb>(a.y[0] + r0 * a.m + mw, a.m, n_first - r0, a.m - mw, own, lane, value);
+    if (r0 + 32 > a.split && a.n > a.split)
+      store_rows<T, kMb>(a.y[1] + (r0 - a.split) * a.m + mw, a.m, a.n - r0, a.m - mw, own, lane, value,
+                         a.split - r0);
+  }
+}
+
+template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
+__global__ __launch_bounds__(64 * WT * WM, MINB) void rows_kernel(ProductArgs a) {
+  rows_tile<T, BT, BM, WT, WM, NST>(a);
+}
+
+// Few tiles: 32 rows by 32 columns, eight waves split k.
+template <class T>
+using RowsFew = WaveProduct<T, 1, 1>;
+template <class T>
+constexpr int kRowsFewLds = kFewWaves * RowsFew<T>::kBytes;
+
+template <class T>
+__device__ __forceinline__ void rows_few(const ProductArgs& a) {
+  using P = RowsFew<T>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t n_m = (uint32_t)(a.m + 31) / 32u;
+  const int m0 = (int)(blockIdx.x % n_m) * 32;
+  const int64_t t0 = (int64_t)(blockIdx.x / n_m) * 32;
+  const int nk = (a.k + 63) / 64;
+  f32x16 acc[1][1];
+  unsigned char* own = smem + wave * P::kBytes;
+  P::run(a.x + t0 * a.ld, a.ld, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31,
+         {{a.w + (int64_t)m0 * a.ld, nullptr}, a.ld, a.m - m0 < 32 ? a.m - m0 - 1 : 31}, a.k,
+         nk * wave / kFewWaves, nk * (wave + 1) / kFewWaves, own, lane, acc);
+  float* part = reinterpret_cast<float*>(own);  // [16][64]
+#pragma unroll
+  for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];
+  __syncthreads();
+  // thread: two columns of a row; column m < 32 is entry 4 (m / 8) + m % 4 of lane (row, half (m / 4) % 2)
+  const int row = threadIdx.x & 31, m = 2 * (threadIdx.x >> 5);
+  const int e = 4 * (m >> 3) + (m & 3), from = row + 32 * ((m >> 2) & 1);
+  float v[2] = {0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    const float* p = reinterpret_cast<const float*>(smem + w * P::kBytes) + from;
+    v[0] += p[e * 64];
+    v[1] += p[(e + 1) * 64];
+  }
+  const int64_t t = t0 + row;
+  if (t >= a.n || m0 + m >= a.m) return;
+  const bool first = t < a.split;
+  const int64_t at = first ? t : t - a.split;
+  float down = 1.f;
+  if constexpr (T::kNarrow) down = power_of(-up_of(a.max_bits[at]));
+  *reinterpret_cast<uint32_t*>(a.y[first ? 0 : 1] + at * a.m + m0 + m) = T::pack(v[0] * down, v[1] * down);
+}
+
+template <class T>
+__global__ __launch_bounds__(64 * kFewWaves) void rows_few_kernel(ProductArgs a) {
+  rows_few<T>(a);
+}
+
+// ---- transposes ---------------------------------------------------------------------------------
+
+// Up to three matrices [rows, cols] (multiples of 8 columns) in one launch, a 64 x 64 tile per workgroup:
+// out[c][r] (rows of `ld`, zero from `rows` to the next multiple of 8), of 16-bit values or of a checkpoint's
+// codes, whose values then go to `plain` as well.  And clears `words` for max_kernel.
+template <class T>
+__global__ __launch_bounds__(256) void prepare_kernel(GatedPrepare a) {
+  __shared__ __attribute__((aligned(16))) uint16_t tile[64][72];
+  uint32_t b = blockIdx.x;
+  if (b < a.clear_blocks) {
+    const int64_t i = (int64_t)b * 256 + threadIdx.x;
+    if (i < a.words) a.clear[i] = 0;
+    return;
+  }
+  b -= a.clear_blocks;
+  int w = 0;
+  while (w < 2 && b >= a.job[w].blocks) b -= a.job[w++].blocks;
+  const GatedTranspose& q = a.job[w];
+  const uint32_t n_c = (uint32_t)(q.cols + 63) / 64u;
+  const int64_t r0 = (int64_t)(b / n_c) * 64;
+  const int c0 = (int)(b % n_c) * 64;
+  const int x = 8 * (threadIdx.x & 7), y = threadIdx.x >> 3;
+#pragma unroll
+  for (int i = y; i < 64; i += 32) {
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (r0 + i < q.rows && c0 + x < q.cols) {
+      if (q.codes) {
+        v = unpack8<T>(*reinterpret_cast<const uint2*>(q.codes + (r0 + i) * q.cols + c0 + x),
+                       q.exps[(r0 + i) * ((q.cols + 31) / 32) + (c0 + x) / 32]);
+        if (q.plain) *reinterpret_cast<u32x4*>(q.plain + (r0 + i) * q.cols + c0 + x) = v;
+      } else {
+        v = load16(q.in + (r0 + i) * q.in_ld + c0 + x);
+      }
+    }
+    *reinterpret_cast<u32x4*>(&tile[i][x]) = v;
+  }
+  if (!q.out) return;
+  __syncthreads();
+  // thread: 8 rows of one column; a wave's 64 columns of the same rows read LDS without conflicts
+  const int c = threadIdx.x & 63;
+#pragma unroll
+  for (int k = threadIdx.x >> 6; k < 8; k += 4) {
+    if (c0 + c >= q.cols || r0 + 8 * k >= q.rows) continue;
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      v[e] = (uint32_t)tile[8 * k + 2 * e][c] | (uint32_t)tile[8 * k + 2 * e + 1][c] << 16;
+    *reinterpret_cast<u32x4*>(q.out + (int64_t)(c0 + c) * q.ld + r0 + 8 * k) = v;
+  }
+}
+
+// ---- launches -----------------------------------------------------------------------------------
+
+// The dynamic LDS of a kernel beyond the default limit.
+hipError_t allow_lds(const void* fn, int lds) {
+  return lds > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) : hipSuccess;
+}
+
+template <class T, class A, int BT, int BM, int WT, int WM, int NST, int MINB, bool GRAD>
+hipError_t gated_as(const GatedArgs& a, hipStream_t s) {
+  using P = TileProduct<T, BT, BM, WT, WM, NST, true>;
+  const int64_t grid = (a.n - a.row0 + BT - 1) / BT * ((a.f + P::kCols - 1) / P::kCols);
+  const auto kernel = gated_kernel<T, A, BT, BM, WT, WM, NST, MINB, GRAD>;
+  const hipError_t e = allow_lds((const void*)kernel, P::kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WT * WM), P::kLds, s, a);
+  return hipGetLastError();
+}
+
+template <class T, class A, bool GRAD>
+hipError_t gated_few_as(const GatedArgs& a, hipStream_t s) {
+  const auto kernel = gated_few_kernel<T, A, GRAD>;
+  const hipError_t e = allow_lds((const void*)kernel, kGatedFewLds<T>);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((a.n + 31) / 32 * ((a.f + 15) / 16))), dim3(64 * kFewWaves),
+                     kGatedFewLds<T>, s, a);
+  return hipGetLastError();
+}
+
+template <class T, class A, bool GRAD>
+hipError_t gated(GatedArgs a, hipStream_t s) {
+  auto tiles = [&](int t, int m) { return (a.n - a.row0 + t - 1) / t * ((a.f + m - 1) / m); };
+  if (tiles(32, 16) <= 1024 && a.n <= 64) return gated_few_as<T, A, GRAD>(a, s);
+  if (tiles(256, 128) >= 144) return gated_as<T, A, 256, 256, 4, 2, 2, 1, GRAD>(a, s);
+  if (tiles(128, 64) >= 160) return gated_as<T, A, 128, 128, 4, 2, 4, 1, GRAD>(a, s);
+  return gated_as<T, A, 64, 128, 2, 2, 4, 1, GRAD>(a, s);
+}
+
+template <class T, bool GRAD>
+hipError_t gated_act(const GatedArgs& a, hipStream_t s) {
+  switch (a.act) {
+    case 0: return gated<T, Silu, GRAD>(a, s);
+    case 1: return gated<T, Gelu, GRAD>(a, s);
+    default: return gated<T, GeluTanh, GRAD>(a, s);
+  }
+}
+
+template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
+hipError_t rows_as(const ProductArgs& a, hipStream_t s) {
+  using P = TileProduct<T, BT, BM, WT, WM, NST>;
+  const int64_t grid = (a.n - a.row0 + BT - 1) / BT * ((a.m + BM - 1) / BM);
+  const auto kernel = rows_kernel<T, BT, BM, WT, WM, NST, MINB>;
+  const hipError_t e = allow_lds((const void*)kernel, P::kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WT * WM), P::kLds, s, a);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t rows(ProductArgs a, hipStream_t s) {
+  auto tiles = [&](int b) { return (a.n - a.row0 + b - 1) / b * ((a.m + b - 1) / b); };
+  if (tiles(32) <= 384) {
+    const auto kernel = rows_few_kernel<T>;
+    const hipError_t e = allow_lds((const void*)kernel, kRowsFewLds<T>);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles(32)), dim3(64 * kFewWaves), kRowsFewLds<T>, s, a);
+    return hipGetLastError();
+  }
+  if (tiles(256) >= 144) {
+    const int64_t n_m = (a.m + 255) / 256, rest = tiles(256) % 256;
+    const int64_t whole = (tiles(256) - rest) / n_m * 256;  // rows of the whole rounds
+    ProductArgs w = a;
+    if (rest > 0 && rest <= 112 && whole > 0) w.n = whole;
+    const hipError_t e = rows_as<T, 256, 256, 4, 2, 2, 1>(w, s);
+    if (e != hipSuccess || w.n == a.n) return e;
+    a.row0 = whole;
+  }
+  if (tiles(128) >= 160 || a.row0 > 0) return rows_as<T, 128, 128, 4, 2, 4, 1>(a, s);
+  return rows_as<T, 64, 64, 2, 2, 4, 2>(a, s);
+}
+
+}  // namespace
+
+// (The tiles are 256 x 128 or 256 x 256 by 512 threads in every call of this size.)
+bool gated_fits(int64_t n, int k, int f, bool grads) {
+  auto blocks = [](int64_t size, int of) { return (size + of - 1) / of; };
+  if (!launch_fits(blocks(n, 256) * blocks(f, 128), 512)) return false;
+  if (!grads) return true;
+  const int64_t prepare = blocks(n + f, 256) + 2 * blocks(f, 64) * blocks(k, 64) + blocks(n, 64) * blocks(k, 64);
+  return launch_fits(prepare, 256) && launch_fits(blocks(n, 64) * blocks(f, 512), 256) &&
+         launch_fits(blocks(n, 256) * blocks(k, 256), 512);
+}
+
+hipError_t launch_gated(const GatedArgs& a, bool grad, hipStream_t stream) {
+  if (a.n == 0) return hipSuccess;
+  if (grad) return a.f16 ? gated_act<HalfF16, true>(a, stream) : gated_act<HalfBf16, true>(a, stream);
+  return a.f16 ? gated_act<HalfF16, false>(a, stream) : gated_act<HalfBf16, false>(a, stream);
+}
+
+hipError_t launch_rows_product(const ProductArgs& a, bool f16, hipStream_t stream) {
+  if (a.n == 0) return hipSuccess;
+  return f16 ? rows<HalfF16>(a, stream) : rows<HalfBf16>(a, stream);
+}
+
+hipError_t launch_gated_max(const uint16_t* dh, int64_t n, int f, uint32_t* rows, uint32_t* cols,
+                            hipStream_t stream) {
+  if (n == 0) return hipSuccess;
+  hipLaunchKernelGGL(max_kernel, dim3((unsigned)((n + 63) / 64 * ((f + 511) / 512))), dim3(256), 0, stream, dh, n,
+                     f, rows, cols);
+  return hipGetLastError();
+}
+
+hipError_t launch_gated_prepare(GatedPrepare a, bool f16, hipStream_t stream) {
+  a.clear_blocks = (uint32_t)((a.words + 255) / 256);
+  int64_t blocks = a.clear_blocks;
+  for (GatedTranspose& q : a.job) {
+    q.blocks = (uint32_t)((q.rows + 63) / 64 * ((q.cols + 63) / 64));
+    blocks += q.blocks;
+  }
+  if (blocks == 0) return hipSuccess;
+  if (f16)
+    hipLaunchKernelGGL(prepare_kernel<HalfF16>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL(prepare_kernel<HalfBf16>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace hpr

@@ -378,6 +378,94 @@ bool adapter_ordered(int64_t n, int n_req, int n_ad, int k, int m, int r);
 int64_t adapter_outer_slots(int64_t n, int n_req, int n_ad, int k, int m, int r);
 hipError_t launch_adapter_outer(const AdapterArgs& a, const OuterArgs& o, hipStream_t stream);
 
+// The gated feed-forward projections (gated.hip).  h [n, f] from x [n, k] (rows of x_ld) and wg, wu [f, k];
+// with a gradient dh [n, f], d = (dg | du) [n, 2 f] and its transpose dt [2 f, np] (np: n rounded up to 8, zero
+// past n), either of which may be null.  row_max and col_max: launch_gated_max's, in fp16 alone.
+struct GatedArgs {
+  const uint16_t *x, *wg, *wu;
+  int64_t n, x_ld;
+  int k, f, act;  // HPR_SILU ...
+  bool f16;
+  uint16_t* h;
+  const uint16_t* dh;
+  uint16_t *d, *dt;
+  int64_t np;
+  const uint32_t *row_max, *col_max;
+  int64_t row0 = 0;  // the launcher's
+};
+hipError_t launch_gated(const GatedArgs& a, bool grad, hipStream_t stream);
+// Whether every launch of the forward, or of the gradients, is one that can be made (launch_fits).
+bool gated_fits(int64_t n, int k, int f, bool grads);
+// Largest magnitudes (as fp16 bits) of dh's rows and columns, into zeroed words.
+hipError_t launch_gated_max(const uint16_t* dh, int64_t n, int f, uint32_t* rows, uint32_t* cols,
+                            hipStream_t stream);
+// y = x w^T of x [n, k] and w [m, k], both with rows of ld: rows [0, split) to y[0], the others to y[1] (rows of
+// m).  In fp16 row r is divided by the power of two of max_bits[r], or [r - split].
+struct ProductArgs {
+  const uint16_t *x, *w;
+  int64_t n;
+  int m, k, ld;
+  uint16_t* y[2];
+  int64_t split;
+  const uint32_t* max_bits;
+  int64_t row0 = 0;  // the launcher's
+};
+hipError_t launch_rows_product(const ProductArgs& a, bool f16, hipStream_t stream);
+// Up to three transposes out[c][r] = in[r][c] (out null: none) and words to clear, in one launch.  in: rows of
+// in_ld, or a checkpoint's codes and exps, whose values go to plain [rows, cols] too (null: none).  out's rows are
+// zero from `rows` to the next multiple of 8.  cols % 8 == 0.  The launcher fills `blocks` and clear_blocks.
+struct GatedTranspose {
+  const uint16_t* in;
+  int64_t in_ld;
+  const int8_t* codes;
+  const uint8_t* exps;
+  int64_t rows;
+  int cols;
+  uint16_t* out;
+  int64_t ld;
+  uint16_t* plain;
+  uint32_t blocks;
+};
+struct GatedPrepare {
+  GatedTranspose job[3];
+  uint32_t* clear;
+  int64_t words;
+  uint32_t clear_blocks;
+};
+hipError_t launch_gated_prepare(GatedPrepare a, bool f16, hipStream_t stream);
+
+// Rows in 8 bits (checkpoint.hip): codes [n, d] and exps [n, ceil(d / 32)] of x [n, d] with rows of x_ld, and back.
+hipError_t launch_checkpoint_pack(const uint16_t* x, int64_t x_ld, int64_t n, int d, bool f16, int8_t* codes,
+                                  uint8_t* exps, hipStream_t stream);
+hipError_t launch_checkpoint_unpack(const int8_t* codes, const uint8_t* exps, int64_t n, int d, bool f16,
+                                    uint16_t* x, hipStream_t stream);
+
+// Norms around a block (norm.hip, which states the definition).  x and b are 16-bit rows of x_ld and b_ld or, with
+// x_codes, checkpoints; b may be null (both forms), and so may w (no y), c, pw, pc and gate.
+struct NormArgs {
+  const uint16_t *x, *b;
+  int64_t x_ld, b_ld;
+  const int8_t *x_codes, *b_codes;
+  const uint8_t *x_exps, *b_exps;
+  const uint16_t *w, *c, *pw, *pc, *gate;  // [d]; gate [d], or [n, d] with gate_rows
+  bool gate_rows, layer, f16;
+  float scale, eps;
+  int64_t n;
+  int d;
+  uint16_t *r, *y;                    // [n, d], either may be null
+  const uint16_t *dr, *dy;            // [n, d], either may be null
+  uint16_t *dx, *db, *dgate_rows;     // [n, d], each may be null
+  uint16_t *dw, *dc, *dpw, *dpc, *dgate;  // [d], each may be null
+  float* part;                        // norm_sums(layer) sums of d columns of norm_parts(n, d) groups of rows
+  int64_t parts;                      // the launcher's
+};
+constexpr int kMaxNormDim = 16384;
+inline int norm_sums(bool layer) { return layer ? 4 : 2; }
+int64_t norm_parts(int64_t n, int d);
+bool norm_fits(int64_t n, int d);  // whether the launches can be made (launch_fits)
+hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream);
+hipError_t launch_norm_bwd(NormArgs a, hipStream_t stream);
+
 // Calibration (calibration.hip): a pure-MFMA kernel of mfma_calibration_waves(n_cu) waves, each
 // running `iters` iterations of four v_mfma_f32_32x32x16_bf16 (sink: at least one float per
 // 4-wave workgroup); a pure streaming read of `bytes` (a multiple of 16) with `blocks`
