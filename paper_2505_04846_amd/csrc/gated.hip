@@ -133,119 +133,110 @@ __device__ __forceinline__ void gradients(float g, float u, float dh, float& dg,
   du = dh * v;
 }
 
-template <class T, class A, int BT, int BM, int WT, int WM, int NST, bool GRAD>
+template <class T, class A, class P, bool GRAD>
 __device__ __forceinline__ void gated_tile(const GatedArgs& a) {
-  using P = TileProduct<T, BT, BM, WT, WM, NST, true>;
-  constexpr int kTb = P::kTb, kMb = P::kMb, kHb = kMb / 2;
+  constexpr int kT = P::kT, kM = P::kM, kH = kM / 2;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // P::kLds
-  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int lane = threadIdx.x & 63, row = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wt = wave % WT, wm = wave / WT;
+  const int wt = wave % P::kWt, wm = wave / P::kWt;
   const int n_m = (a.f + P::kCols - 1) / P::kCols;
-  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + BT - 1) / BT), n_m);
-  const int64_t t0 = a.row0 + (int64_t)at.t * BT;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + P::kRows - 1) / P::kRows), n_m);
+  const int64_t t0 = a.row0 + (int64_t)at.t * P::kRows;
   const int m0 = at.m * P::kCols;
   const int64_t left_t = a.n - t0;
-  const int last_t = left_t < BT ? (int)left_t - 1 : BT - 1;
+  const int last_t = left_t < P::kRows ? (int)left_t - 1 : P::kRows - 1;
   const int last_m = a.f - m0 < P::kCols ? a.f - m0 - 1 : P::kCols - 1;
   typename P::Acc acc;
   const int64_t w0 = (int64_t)m0 * a.k;
   P::run(a.x + t0 * a.x_ld, (int)a.x_ld, last_t, {{a.wg + w0, a.wu + w0}, a.k, last_m}, a.k, smem, wave, lane,
-         acc, [](typename P::Acc&) {});
+         acc);
 
-  const int mw = m0 + wm * P::kWaveCols;       // the wave's first column
-  const int64_t tw = t0 + wt * kTb * 32;       // and row
-  constexpr int kOwn = 32 * 64 * (kHb > kTb ? kHb : kTb);
+  const int mw = m0 + wm * P::kWaveCols;  // the wave's first column
+  const int64_t tw = t0 + wt * kT * 16;   // and row
+  constexpr int kOwn = 16 * 32 * (kH > kT ? kH : kT);
   static_assert(P::kW * kOwn <= P::kLds, "the waves' blocks fit the ring");
   unsigned char* own = smem + wave * kOwn;
   if constexpr (!GRAD) {
 #pragma unroll
-    for (int j = 0; j < kTb; ++j)
-      store_rows<T, kHb>(a.h + (tw + 32 * j) * a.f + mw, a.f, a.n - tw - 32 * j, a.f - mw, own, lane,
-                         [&](int i, int r) { return A::value(acc[i][j][r]) * acc[i + kHb][j][r]; });
-    return;
+    for (int j = 0; j < kT; ++j)
+      store_rows16<T, kH>(a.h + (tw + 16 * j) * a.f + mw, a.f, a.n - tw - 16 * j, a.f - mw, own, lane,
+                          [&](int i, int e) { return A::value(acc[i][j][e]) * acc[i + kH][j][e]; });
   } else {
     // d in the place of g and u; 0 past the last row
 #pragma unroll
-    for (int j = 0; j < kTb; ++j) {
-      const int64_t t = tw + 32 * j + col;
+    for (int j = 0; j < kT; ++j) {
+      const int64_t t = tw + 16 * j + row;
+      uint2 w[kH];
 #pragma unroll
-      for (int i = 0; i < kHb; ++i) {
-        uint2 w[4];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int m = mw + 32 * i + 8 * g + 4 * half;
-          w[g] = uint2{0u, 0u};
-          if (t < a.n && m < a.f) w[g] = *reinterpret_cast<const uint2*>(a.dh + t * a.f + m);
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t b = e < 2 ? w[g].x : w[g].y;
-            float dg, du;
-            gradients<A>(acc[i][j][4 * g + e], acc[i + kHb][j][4 * g + e], e & 1 ? T::hi(b) : T::lo(b), dg, du);
-            acc[i][j][4 * g + e] = t < a.n ? dg : 0.f;
-            acc[i + kHb][j][4 * g + e] = t < a.n ? du : 0.f;
-          }
+      for (int i = 0; i < kH; ++i) {
+        const int m = mw + 16 * i + 4 * q;
+        w[i] = uint2{0u, 0u};
+        if (t < a.n && m < a.f) w[i] = *reinterpret_cast<const uint2*>(a.dh + t * a.f + m);
       }
+#pragma unroll
+      for (int i = 0; i < kH; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t b = e < 2 ? w[i].x : w[i].y;
+          float dg, du;
+          gradients<A>(acc[i][j][e], acc[i + kH][j][e], e & 1 ? T::hi(b) : T::lo(b), dg, du);
+          acc[i][j][e] = t < a.n ? dg : 0.f;
+          acc[i + kH][j][e] = t < a.n ? du : 0.f;
+        }
     }
     if (a.d) {
 #pragma unroll
-      for (int j = 0; j < kTb; ++j) {
-        const int64_t t = tw + 32 * j + col;
+      for (int j = 0; j < kT; ++j) {
+        const int64_t t = tw + 16 * j + row;
         float up = 1.f;
         if constexpr (T::kNarrow) up = power_of(up_of(a.row_max[t < a.n ? t : a.n - 1]));
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-          store_rows<T, kHb>(a.d + (tw + 32 * j) * 2 * a.f + (int64_t)s * a.f + mw, 2 * (int64_t)a.f,
-                             a.n - tw - 32 * j, a.f - mw, own, lane,
-                             [&](int i, int r) { return acc[s * kHb + i][j][r] * up; });
+          store_rows16<T, kH>(a.d + (tw + 16 * j) * 2 * a.f + (int64_t)s * a.f + mw, 2 * (int64_t)a.f,
+                              a.n - tw - 16 * j, a.f - mw, own, lane,
+                              [&](int i, int e) { return acc[s * kH + i][j][e] * up; });
       }
     }
-    if (a.dt) {  // 32 columns of d at a time, 32 kTb values of each
-      constexpr int kRow = 64 * kTb, kCh = kRow / 16, kPer = 64 / kCh;
+    if (a.dt) {  // 16 columns of d at a time, 16 kT values of each
+      constexpr int kRow = 32 * kT, kCh = kRow / 16, kPer = 64 / kCh;
 #pragma unroll
-      for (int i = 0; i < kMb; ++i) {
-        const int m_first = mw + 32 * (i % kHb);
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      for (int i = 0; i < kM; ++i) {
+        const int m_first = mw + 16 * (i % kH);
+        float up[4] = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (T::kNarrow) {
+          if (m_first + 4 * q < a.f) {
+            const u32x4 bits = *reinterpret_cast<const u32x4*>(a.col_max + m_first + 4 * q);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int r0 = 8 * g + 4 * half;
-          float up[4] = {1.f, 1.f, 1.f, 1.f};
-          if constexpr (T::kNarrow) {
-            if (m_first + r0 < a.f) {
-              const u32x4 bits = *reinterpret_cast<const u32x4*>(a.col_max + m_first + r0);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) up[e] = power_of(up_of(bits[e]));
-            }
+            for (int e = 0; e < 4; ++e) up[e] = power_of(up_of(bits[e]));
           }
-#pragma unroll
-          for (int j = 0; j < kTb; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int r = r0 + e;
-              *reinterpret_cast<uint16_t*>(own + r * kRow + (((4 * j + (col >> 3)) ^ (r % kCh)) << 4) +
-                                           2 * (col & 7)) = (uint16_t)T::pack(acc[i][j][4 * g + e] * up[e], 0.f);
-            }
         }
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
 #pragma unroll
-        for (int q = 0; q < 32 / kPer; ++q) {
-          const int r = q * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh);
+        for (int j = 0; j < kT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * q + e;
+            *reinterpret_cast<uint16_t*>(own + r * kRow + (((2 * j + (row >> 3)) ^ (r % kCh)) << 4) +
+                                         2 * (row & 7)) = (uint16_t)T::pack(acc[i][j][e] * up[e], 0.f);
+          }
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+        for (int s = 0; s < (16 + kPer - 1) / kPer; ++s) {
+          const int r = s * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh), m = m_first + r;
+          if (kPer > 16 && r >= 16) continue;
           const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
-          const int m = m_first + r;
           if (m < a.f && tw + 8 * c < a.np)
-            *reinterpret_cast<u32x4*>(a.dt + ((int64_t)(i < kHb ? 0 : a.f) + m) * a.np + tw + 8 * c) = v;
+            *reinterpret_cast<u32x4*>(a.dt + ((int64_t)(i < kH ? 0 : a.f) + m) * a.np + tw + 8 * c) = v;
         }
       }
     }
   }
 }
 
-template <class T, class A, int BT, int BM, int WT, int WM, int NST, int MINB, bool GRAD>
-__global__ __launch_bounds__(64 * WT * WM, MINB) void gated_kernel(GatedArgs a) {
-  gated_tile<T, A, BT, BM, WT, WM, NST, GRAD>(a);
+template <class T, class A, class P, bool GRAD>
+__global__ __launch_bounds__(P::kThreads, 1) void gated_kernel(GatedArgs a) {
+  gated_tile<T, A, P, GRAD>(a);
 }
 
 // Few rows: 32 rows of x by 16 columns of h per workgroup.  Eight waves split k and sum in LDS.
@@ -331,48 +322,48 @@ __global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(GatedArgs a) 
 // ---- dx, dW -------------------------------------------------------------------------------------
 
 // y[r][c] = 2^-up(r) <x_r, w_c>, rows [0, split) to y[0], the others to y[1].
-template <class T, int BT, int BM, int WT, int WM, int NST>
+template <class T, class P>
 __device__ __forceinline__ void rows_tile(const ProductArgs& a) {
-  using P = TileProduct<T, BT, BM, WT, WM, NST>;
-  constexpr int kTb = P::kTb, kMb = P::kMb;
+  constexpr int kT = P::kT, kM = P::kM;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // P::kLds
-  const int lane = threadIdx.x & 63, col = lane & 31;
+  const int lane = threadIdx.x & 63, row = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wt = wave % WT, wm = wave / WT;
-  const int n_m = (a.m + BM - 1) / BM;
-  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + BT - 1) / BT), n_m);
-  const int64_t t0 = a.row0 + (int64_t)at.t * BT;
-  const int m0 = at.m * BM;
+  const int wt = wave % P::kWt, wm = wave / P::kWt;
+  const int n_m = (a.m + P::kCols - 1) / P::kCols;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + P::kRows - 1) / P::kRows), n_m);
+  const int64_t t0 = a.row0 + (int64_t)at.t * P::kRows;
+  const int m0 = at.m * P::kCols;
   const int64_t left_t = a.n - t0;
-  const int last_t = left_t < BT ? (int)left_t - 1 : BT - 1;
-  const int last_m = a.m - m0 < BM ? a.m - m0 - 1 : BM - 1;
+  const int last_t = left_t < P::kRows ? (int)left_t - 1 : P::kRows - 1;
+  const int last_m = a.m - m0 < P::kCols ? a.m - m0 - 1 : P::kCols - 1;
   typename P::Acc acc;
   P::run(a.x + t0 * a.ld, a.ld, last_t, {{a.w + (int64_t)m0 * a.ld, nullptr}, a.ld, last_m}, a.k, smem, wave,
-         lane, acc, [](typename P::Acc&) {});
-  static_assert(P::kW * 32 * 64 * kMb <= P::kLds, "the waves' blocks fit the ring");
-  unsigned char* own = smem + wave * 32 * 64 * kMb;
-  const int mw = m0 + wm * kMb * 32;
+         lane, acc);
+  constexpr int kOwn = 16 * 32 * kM;
+  static_assert(P::kW * kOwn <= P::kLds, "the waves' blocks fit the ring");
+  unsigned char* own = smem + wave * kOwn;
+  const int mw = m0 + wm * P::kWaveCols;
 #pragma unroll
-  for (int j = 0; j < kTb; ++j) {
-    const int64_t r0 = t0 + (wt * kTb + j) * 32;
+  for (int j = 0; j < kT; ++j) {
+    const int64_t r0 = t0 + (wt * kT + j) * 16;
     float down = 1.f;
     if constexpr (T::kNarrow) {
-      const int64_t t = r0 + col < a.n ? r0 + col : a.n - 1;
+      const int64_t t = r0 + row < a.n ? r0 + row : a.n - 1;
       down = power_of(-up_of(a.max_bits[t < a.split ? t : t - a.split]));
     }
-    auto value = [&](int i, int r) { return acc[i][j][r] * down; };
+    auto value = [&](int i, int e) { return acc[i][j][e] * down; };
     // (the split may lie inside a tile: every row goes to the output that it is of)
     const int64_t n_first = a.n < a.split ? a.n : a.split;
-    if (r0 < a.split) store_rows<T, kMb>(a.y[0] + r0 * a.m + mw, a.m, n_first - r0, a.m - mw, own, lane, value);
-    if (r0 + 32 > a.split && a.n > a.split)
-      store_rows<T, kMb>(a.y[1] + (r0 - a.split) * a.m + mw, a.m, a.n - r0, a.m - mw, own, lane, value,
-                         a.split - r0);
+    if (r0 < a.split) store_rows16<T, kM>(a.y[0] + r0 * a.m + mw, a.m, n_first - r0, a.m - mw, own, lane, value);
+    if (r0 + 16 > a.split && a.n > a.split)
+      store_rows16<T, kM>(a.y[1] + (r0 - a.split) * a.m + mw, a.m, a.n - r0, a.m - mw, own, lane, value,
+                          a.split - r0);
   }
 }
 
-template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
-__global__ __launch_bounds__(64 * WT * WM, MINB) void rows_kernel(ProductArgs a) {
-  rows_tile<T, BT, BM, WT, WM, NST>(a);
+template <class T, class P>
+__global__ __launch_bounds__(P::kThreads, 1) void rows_kernel(ProductArgs a) {
+  rows_tile<T, P>(a);
 }
 
 // Few tiles: 32 rows by 32 columns, eight waves split k.
@@ -477,19 +468,26 @@ __global__ __launch_bounds__(256) void prepare_kernel(GatedPrepare a) {
 
 // ---- launches -----------------------------------------------------------------------------------
 
+// Tiles of rows by rows of the weights (of a paired tile half of them of each matrix).
+template <class T, bool PAIR>
+using Wide = TileProduct16<T, 256, 256, 4, 2, 3, 2, PAIR>;
+template <class T, bool PAIR>
+using Middle = TileProduct16<T, 128, 128, 4, 2, 4, 4, PAIR>;
+template <class T, bool PAIR>
+using Small = TileProduct16<T, 64, 64, 2, 2, 5, 5, PAIR>;
+
 // The dynamic LDS of a kernel beyond the default limit.
 hipError_t allow_lds(const void* fn, int lds) {
   return lds > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) : hipSuccess;
 }
 
-template <class T, class A, int BT, int BM, int WT, int WM, int NST, int MINB, bool GRAD>
+template <class T, class A, class P, bool GRAD>
 hipError_t gated_as(const GatedArgs& a, hipStream_t s) {
-  using P = TileProduct<T, BT, BM, WT, WM, NST, true>;
-  const int64_t grid = (a.n - a.row0 + BT - 1) / BT * ((a.f + P::kCols - 1) / P::kCols);
-  const auto kernel = gated_kernel<T, A, BT, BM, WT, WM, NST, MINB, GRAD>;
+  const int64_t grid = (a.n - a.row0 + P::kRows - 1) / P::kRows * ((a.f + P::kCols - 1) / P::kCols);
+  const auto kernel = gated_kernel<T, A, P, GRAD>;
   const hipError_t e = allow_lds((const void*)kernel, P::kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WT * WM), P::kLds, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(P::kThreads), P::kLds, s, a);
   return hipGetLastError();
 }
 
@@ -507,9 +505,9 @@ template <class T, class A, bool GRAD>
 hipError_t gated(GatedArgs a, hipStream_t s) {
   auto tiles = [&](int t, int m) { return (a.n - a.row0 + t - 1) / t * ((a.f + m - 1) / m); };
   if (tiles(32, 16) <= 1024 && a.n <= 64) return gated_few_as<T, A, GRAD>(a, s);
-  if (tiles(256, 128) >= 144) return gated_as<T, A, 256, 256, 4, 2, 2, 1, GRAD>(a, s);
-  if (tiles(128, 64) >= 160) return gated_as<T, A, 128, 128, 4, 2, 4, 1, GRAD>(a, s);
-  return gated_as<T, A, 64, 128, 2, 2, 4, 1, GRAD>(a, s);
+  if (tiles(256, 128) >= 144) return gated_as<T, A, Wide<T, true>, GRAD>(a, s);
+  if (tiles(128, 64) >= 160) return gated_as<T, A, Middle<T, true>, GRAD>(a, s);
+  return gated_as<T, A, Small<T, true>, GRAD>(a, s);
 }
 
 template <class T, bool GRAD>
@@ -521,14 +519,13 @@ hipError_t gated_act(const GatedArgs& a, hipStream_t s) {
   }
 }
 
-template <class T, int BT, int BM, int WT, int WM, int NST, int MINB>
+template <class T, class P>
 hipError_t rows_as(const ProductArgs& a, hipStream_t s) {
-  using P = TileProduct<T, BT, BM, WT, WM, NST>;
-  const int64_t grid = (a.n - a.row0 + BT - 1) / BT * ((a.m + BM - 1) / BM);
-  const auto kernel = rows_kernel<T, BT, BM, WT, WM, NST, MINB>;
+  const int64_t grid = (a.n - a.row0 + P::kRows - 1) / P::kRows * ((a.m + P::kCols - 1) / P::kCols);
+  const auto kernel = rows_kernel<T, P>;
   const hipError_t e = allow_lds((const void*)kernel, P::kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WT * WM), P::kLds, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(P::kThreads), P::kLds, s, a);
   return hipGetLastError();
 }
 
@@ -547,12 +544,12 @@ hipError_t rows(ProductArgs a, hipStream_t s) {
     const int64_t whole = (tiles(256) - rest) / n_m * 256;  // rows of the whole rounds
     ProductArgs w = a;
     if (rest > 0 && rest <= 112 && whole > 0) w.n = whole;
-    const hipError_t e = rows_as<T, 256, 256, 4, 2, 2, 1>(w, s);
+    const hipError_t e = rows_as<T, Wide<T, false>>(w, s);
     if (e != hipSuccess || w.n == a.n) return e;
     a.row0 = whole;
   }
-  if (tiles(128) >= 160 || a.row0 > 0) return rows_as<T, 128, 128, 4, 2, 4, 1>(a, s);
-  return rows_as<T, 64, 64, 2, 2, 4, 2>(a, s);
+  if (tiles(128) >= 160 || a.row0 > 0) return rows_as<T, Middle<T, false>>(a, s);
+  return rows_as<T, Small<T, false>>(a, s);
 }
 
 }  // namespace

@@ -1,4 +1,4 @@
-// The two 16-bit types of the encoder's operators, bf16 and fp16: their 32x32x16 product, packing
+// The two 16-bit types of the encoder's operators, bf16 and fp16: their 32x32x16 and 16x16x32 products, packing
 // with rounding to nearest even, and unpacking.
 #pragma once
 
@@ -12,6 +12,9 @@ struct HalfBf16 {
   static constexpr bool kNarrow = false;  // whether fp32 values may lie outside its exponents
   static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     typedef float f2 __attribute__((ext_vector_type(2)));
@@ -27,6 +30,9 @@ struct HalfF16 {
   typedef _Float16 h2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(as_f16x8(a), as_f16x8(b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(a), as_f16x8(b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     typedef float f2 __attribute__((ext_vector_type(2)));

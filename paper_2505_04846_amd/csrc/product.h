@@ -5,6 +5,8 @@
 // (i, j) is row 8 (e / 4) + 4 half + e % 4 of W's block i and row lane & 31 of x's block j.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 #include "half.h"
 #include "tiles.h"
@@ -112,17 +114,13 @@ struct WaveProduct {
 // ---- a workgroup's product ---------------------------------------------------------------------
 
 // Tile of BT rows of x by BM rows of W, WT x WM waves, k in stages of 64 through NST LDS stages.  Wave
-// (wt, wm) holds the rows [32 kTb wt, + 32 kTb) of x and [32 kMb wm, + 32 kMb) of W; of a paired tile the
-// blocks i < kMb / 2 are columns of w[0], the others the same columns of w[1].
-template <class T, int BT, int BM, int WT, int WM, int NST, bool PAIR = false>
+// (wt, wm) holds the rows [32 kTb wt, + 32 kTb) of x and [32 kMb wm, + 32 kMb) of W.
+template <class T, int BT, int BM, int WT, int WM, int NST>
 struct TileProduct {
   static constexpr int kW = WT * WM;
   static constexpr int kTb = BT / 32 / WT, kMb = BM / 32 / WM;  // blocks per wave
   static constexpr int kXBytes = BT * 128, kWBytes = BM * 128, kStage = kXBytes + kWBytes;
   static constexpr int kLds = NST * kStage;
-  static constexpr int kCols = PAIR ? BM / 2 : BM;         // columns of the output
-  static constexpr int kWaveCols = kCols / WM;
-  static_assert(!PAIR || kMb % 2 == 0, "a wave holds both halves of its columns");
   typedef f32x16 Acc[kMb][kTb];
 
   // x: first row of the tile.  `first` is called between the first stages' loads and the products, to add
@@ -136,18 +134,14 @@ struct TileProduct {
     const TileLoad<64, BT, kW> lx(wave, lane, 8);
     const TileLoad<64, BM, kW> lw(wave, lane, 8);
     constexpr int kLoads = lx.kLoads + lw.kLoads;
-    const __amdgpu_buffer_rsrc_t rx = tile_rsrc(xb), rw0 = tile_rsrc(w.w[0]), rw1 = tile_rsrc(w.w[PAIR]);
-    // the eight rows of a wave load are of one half of a wave's rows
-    auto second = [&](int j) { return PAIR && (wave * lw.kLoads + j) * 8 % (BM / WM) >= kWaveCols; };
+    const __amdgpu_buffer_rsrc_t rx = tile_rsrc(xb), rw = tile_rsrc(w.w[0]);
     int ox[lx.kLoads], ow[lw.kLoads];
 #pragma unroll
     for (int j = 0; j < lx.kLoads; ++j)
       ox[j] = (lx.row[j] < last_t ? lx.row[j] : last_t) * ldx * 2 + lx.chunk[j];
 #pragma unroll
-    for (int j = 0; j < lw.kLoads; ++j) {
-      const int row = PAIR ? lw.row[j] / (BM / WM) * kWaveCols + lw.row[j] % kWaveCols : lw.row[j];
-      ow[j] = (row < w.last ? row : w.last) * w.ld * 2 + lw.chunk[j];
-    }
+    for (int j = 0; j < lw.kLoads; ++j)
+      ow[j] = (lw.row[j] < w.last ? lw.row[j] : w.last) * w.ld * 2 + lw.chunk[j];
     const int nk = (k + 63) / 64, nk_full = k / 64;
     // Stage kk into ring buffer buf.  Chunks past the end of k read zeros, so past the last stage too
     // (the ring keeps its number of loads in flight).
@@ -161,8 +155,7 @@ struct TileProduct {
 #pragma unroll
         for (int j = 0; j < lw.kLoads; ++j)
           __builtin_amdgcn_raw_ptr_buffer_load_lds(
-              second(j) ? rw1 : rw0, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, ow[j],
-              kk * 128, 0, 0);
+              rw, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, ow[j], kk * 128, 0, 0);
       } else {
 #pragma unroll
         for (int j = 0; j < lx.kLoads; ++j) {
@@ -174,7 +167,7 @@ struct TileProduct {
 #pragma unroll
         for (int j = 0; j < lw.kLoads; ++j) {
           const bool in = kk * 64 + lw.chunk[j] / 2 < k;
-          const char* wb = (const char*)w.w[second(j)];
+          const char* wb = (const char*)w.w[0];
           const void* p = in ? (const void*)(wb + ow[j] + kk * 128) : (const void*)kZero16;
           __builtin_amdgcn_global_load_lds(
               (glb_void_t*)p, (lds_void_t*)(st + kXBytes + (wave * lw.kLoads + j) * 1024), 16, 0, 0);
@@ -280,6 +273,175 @@ struct TileProduct {
   }
 };
 
+// ---- a workgroup's product, in blocks of 16 ------------------------------------------------------
+
+// The same in 16x16x32 products.  On operands that are not zero the card's power limit holds the clock, and these
+// take less of it than 32x32x16: from registers alone, bf16 normal values, 1.97 PFLOP/s against 1.68 (zeros: 2.44
+// and 2.40).  Wave (wt, wm) holds the rows [16 kT wt, + 16 kT) of x and [16 kM wm, + 16 kM) of W; entry e of block
+// (i, j) is row 4 (lane / 16) + e of W's block i and row lane % 16 of x's block j.  Of a paired tile (PAIR) the
+// blocks i < kM / 2 are columns of w[0], the others the same columns of w[1].
+//
+// k goes in stages of 64 values (whole 128-byte lines: half lines ask the L2 for twice as many) through LDS, x's
+// through a ring of NX, W's through one of NW <= NX.  A stage is two k-steps, whose operands a wave holds in
+// registers: while it multiplies one, it reads the other, and loads what takes the place of the stage before.  One
+// barrier a stage, between its k-steps: from there on nobody reads the stage's LDS.  Reads and loads stand between
+// the products one at a time, because a run of them holds the matrix cores up.
+template <class T, int BT, int BM, int WT, int WM, int NX, int NW, bool PAIR = false>
+struct TileProduct16 {
+  static constexpr int kW = WT * WM;
+  static constexpr int kT = BT / 16 / WT, kM = BM / 16 / WM;  // blocks per wave
+  static constexpr int kX = BT * 128, kStageW = BM * 128;     // bytes of a stage of each
+  static constexpr int kLds = NX * kX + NW * kStageW;
+  static constexpr int kLx = BT / 8 / kW, kLw = BM / 8 / kW;  // loads of a wave for a stage
+  static constexpr int kCols = PAIR ? BM / 2 : BM;            // columns of the output
+  static constexpr int kWaveCols = kCols / WM;
+  static constexpr int kThreads = 64 * kW, kRows = BT, kWt = WT;
+  static_assert(!PAIR || kM % 2 == 0, "a wave holds both halves of its columns");
+  static_assert(NW >= 2 && (NX == NW || NX == NW + 1) && kLds <= 160 * 1024, "the waits below");
+  typedef f32x4 Acc[kM][kT];
+  struct Frags {
+    u32x4 x[kT], w[kM];
+  };
+
+  // x: first row of the tile.  LDS is free for the caller when this returns.
+  static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k,
+                                             unsigned char* smem, int wave, int lane, Acc& acc) {
+    const int wt = wave % WT, wm = wave / WT;
+    const TileLoad<64, BT, kW> lx(wave, lane, 8);
+    const TileLoad<64, BM, kW> lw(wave, lane, 8);
+    const __amdgpu_buffer_rsrc_t rx = tile_rsrc(xb), rw0 = tile_rsrc(w.w[0]), rw1 = tile_rsrc(w.w[PAIR]);
+    // the eight rows of a wave load are of one half of a wave's rows
+    auto second = [&](int j) { return PAIR && (wave * kLw + j) * 8 % (BM / WM) >= kWaveCols; };
+    int ox[kLx], ow[kLw];
+#pragma unroll
+    for (int j = 0; j < kLx; ++j) ox[j] = (lx.row[j] < last_t ? lx.row[j] : last_t) * ldx * 2 + lx.chunk[j];
+#pragma unroll
+    for (int j = 0; j < kLw; ++j) {
+      const int row = PAIR ? lw.row[j] / (BM / WM) * kWaveCols + lw.row[j] % kWaveCols : lw.row[j];
+      ow[j] = (row < w.last ? row : w.last) * w.ld * 2 + lw.chunk[j];
+    }
+    const int nk = (k + 63) / 64, nk_full = k / 64;
+    unsigned char* const ring_w = smem + NX * kX;
+    // Load j of x's or W's stage kk into slot `slot` of its ring.  Chunks past the end of k read zeros, so past the
+    // last stage too (the rings keep their numbers of loads in flight); WHOLE: the stage lies inside k.
+    auto load = [&](auto whole, auto of_x, int slot, int kk, int j) __attribute__((always_inline)) {
+      unsigned char* to;
+      if constexpr (of_x()) to = smem + slot * kX + (wave * kLx + j) * 1024;
+      else to = ring_w + slot * kStageW + (wave * kLw + j) * 1024;
+      if constexpr (whole()) {
+        if constexpr (of_x())
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)to, 16, ox[j], kk * 128, 0, 0);
+        else
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(second(j) ? rw1 : rw0, (lds_void_t*)to, 16, ow[j], kk * 128, 0, 0);
+      } else {
+        const char* from;
+        int chunk;
+        if constexpr (of_x()) from = (const char*)xb + ox[j], chunk = lx.chunk[j];
+        else from = (const char*)w.w[second(j)] + ow[j], chunk = lw.chunk[j];
+        const void* p = kk * 64 + chunk / 2 < k ? (const void*)(from + kk * 128) : (const void*)kZero16;
+        __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)to, 16, 0, 0);
+      }
+    };
+    auto load_all = [&](auto of_x, int slot, int kk) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < (of_x() ? kLx : kLw); ++j) {
+        if (kk < nk_full) load(std::true_type(), of_x, slot, kk, j);
+        else load(std::false_type(), of_x, slot, kk, j);
+      }
+    };
+#pragma unroll
+    for (int s = 0; s < NW; ++s) {
+      load_all(std::false_type(), s, s);
+      if (s < NX - 1) load_all(std::true_type(), s, s);
+    }
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+#pragma unroll
+      for (int j = 0; j < kT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // chunk 4 s + lane / 16 of row lane % 16 of a block of 16 rows, of k-step s
+    const int r = lane & 15, at0 = r * 128 + (((lane >> 4) ^ swz<64>(r)) << 4);
+    const unsigned char* const own_x = smem + wt * kT * 2048;
+    const unsigned char* const own_w = ring_w + wm * kM * 2048;
+    auto read = [&](int slot_x, int slot_w, int s, Frags& f, int b) __attribute__((always_inline)) {
+      const int at = at0 ^ (s << 6);
+      if (b < kT) f.x[b] = *reinterpret_cast<const u32x4*>(own_x + slot_x * kX + at + b * 2048);
+      else f.w[b - kT] = *reinterpret_cast<const u32x4*>(own_w + slot_w * kStageW + at + (b - kT) * 2048);
+    };
+    constexpr int kReads = kT + kM, kProducts = kT * kM;
+    // The products of `now`; between them the reads of k-step s of (slot_x, slot_w), and loads of a stage kk.
+    auto step = [&](auto whole, auto of_x, int slot, int kk, int slot_x, int slot_w, int s, const Frags& now,
+                    Frags& then) __attribute__((always_inline)) {
+      constexpr int kLoads = of_x() ? kLx : kLw;
+#pragma unroll
+      for (int p = 0; p < kProducts; ++p) {
+        const int i = p / kT, j = i & 1 ? kT - 1 - p % kT : p % kT;
+        acc[i][j] = T::mfma16(now.w[i], now.x[j], acc[i][j]);
+        // (loops of constant length, which the compiler unrolls)
+#pragma unroll
+        for (int q = 0; q < kReads; ++q)
+          if (p == q * kProducts / kReads) read(slot_x, slot_w, s, then, q);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+          if (p == l * kProducts / kLoads) load(whole, of_x, slot, kk, l);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // Loads that may be on their way when a stage's have landed: at first, and (of x's and W's last, the older
+    // one's) at a barrier, before which stage kk - 1 + NX of x and kk - 1 + NW of W are the last that were begun.
+    constexpr int kFirst = (NW - 1) * kLw + (NX - 2) * kLx;
+    constexpr int kBehind = NX == NW ? (NX - 2) * (kLx + kLw) : (NW - 1) * kLx + (NW - 2) * kLw;
+    Frags f0, f1;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(kFirst));
+    sync_lds();
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) read(0, 0, 0, f0, q);
+    int kk = 0, sx = 0, sw = 0, before = NX - 1;  // the stage's slots, and that of x's stage before
+    auto turn = [&](auto whole) __attribute__((always_inline)) {
+      step(whole, std::true_type(), before, kk - 1 + NX, sx, sw, 1, f0, f1);
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(kBehind));
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      sync_lds();  // the next stage has landed, and nobody reads this one any more
+      const int slot = sw;
+      before = sx;
+      sx = sx + 1 < NX ? sx + 1 : 0;
+      sw = sw + 1 < NW ? sw + 1 : 0;
+      step(whole, std::false_type(), slot, kk + NW, sx, sw, 0, f1, f0);
+    };
+#pragma unroll 1
+    for (; kk + NX < nk_full; ++kk) turn(std::true_type());
+#pragma unroll 1
+    for (; kk < nk; ++kk) turn(std::false_type());
+    // no load may still target LDS when it is reused or ends, and nobody may still read it
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    sync_lds();
+  }
+};
+
+// A wave's rows of results to memory in whole rows, through LDS of its own (16 rows of 32 BLOCKS bytes): BLOCKS
+// blocks of 16 columns of each of 16 rows.  dst: the first row's first column; value(i, e): entry e of block i of
+// these rows; rows before `from`, from n_rows on and columns from n_cols on are not written.
+template <class T, int BLOCKS, class Value>
+__device__ __forceinline__ void store_rows16(uint16_t* dst, int64_t ld, int64_t n_rows, int n_cols,
+                                             unsigned char* own, int lane, Value&& value, int64_t from = 0) {
+  constexpr int kRow = 32 * BLOCKS, kCh = kRow / 16, kPer = 64 / kCh;  // bytes, chunks; rows of a wave store
+  const int r0 = lane & 15, q = lane >> 4;
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);  // (a wave's LDS operations execute in program order)
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i)
+    *reinterpret_cast<uint2*>(own + r0 * kRow + (((2 * i + (q >> 1)) ^ (r0 % kCh)) << 4) + 8 * (q & 1)) =
+        uint2{T::pack(value(i, 0), value(i, 1)), T::pack(value(i, 2), value(i, 3))};
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+#pragma unroll
+  for (int k = 0; k < (16 + kPer - 1) / kPer; ++k) {
+    const int r = k * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh);
+    if (kPer > 16 && r >= 16) continue;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
+    if (r >= from && r < n_rows && 8 * c < n_cols) *reinterpret_cast<u32x4*>(dst + (int64_t)r * ld + 8 * c) = v;
+  }
+}
+
 // Tile of block b of a grid of n_t row tiles by n_m column tiles.  An XCD walks a contiguous run of tiles,
 // four row tiles abreast: the tiles that it holds at a time (32 of the widest) read 4 row tiles and 8 column
 // tiles, not 1 or 2 and all the columns.
@@ -296,10 +458,10 @@ __device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint3
 
 // A wave's rows of results to memory in whole rows, through LDS of its own: BLOCKS blocks of 32 columns of
 // each of 32 rows at a time.  dst: the first row's first column; value(i, r): entry r of block i of these
-// rows; rows before `from`, from n_rows on and columns from n_cols on are not written.
+// rows; rows from n_rows on and columns from n_cols on are not written.
 template <class T, int BLOCKS, class Value>
 __device__ __forceinline__ void store_rows(uint16_t* dst, int64_t ld, int64_t n_rows, int n_cols,
-                                           unsigned char* own, int lane, Value&& value, int64_t from = 0) {
+                                           unsigned char* own, int lane, Value&& value) {
   constexpr int kRow = 64 * BLOCKS;                             // bytes of a row
   constexpr int kCh = kRow / 16, kPer = 64 / kCh;               // chunks of a row, rows of a wave store
   const int half = lane >> 5, col = lane & 31;
@@ -315,7 +477,7 @@ __device__ __forceinline__ void store_rows(uint16_t* dst, int64_t ld, int64_t n_
   for (int k = 0; k < 32 / kPer; ++k) {
     const int r = k * kPer + lane / kCh, c = (lane % kCh) ^ (r % kCh);
     const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
-    if (r >= from && r < n_rows && 8 * c < n_cols) *reinterpret_cast<u32x4*>(dst + (int64_t)r * ld + 8 * c) = v;
+    if (r < n_rows && 8 * c < n_cols) *reinterpret_cast<u32x4*>(dst + (int64_t)r * ld + 8 * c) = v;
   }
 }
 
