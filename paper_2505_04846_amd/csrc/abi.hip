@@ -482,8 +482,8 @@ hpr_status check_norm(const hpr_norm* d, bool packed) {
     return fail(HPR_ERR_INVALID_ARG, "kind (%d) must be HPR_RMS_NORM or HPR_LAYER_NORM", d->kind);
   if (d->gate_rows != 0 && d->gate_rows != 1)
     return fail(HPR_ERR_INVALID_ARG, "gate_rows (%d) must be 0 or 1", d->gate_rows);
-  if (!(d->eps > 0.f) || !(d->eps < 3.0e38f) || !(d->scale > -3.0e38f) || !(d->scale < 3.0e38f))
-    return fail(HPR_ERR_INVALID_ARG, "eps must be positive, scale and eps finite");
+  if (!(d->eps >= 1.1754944e-38f) || !(d->eps < 3.0e38f) || !(d->scale > -3.0e38f) || !(d->scale < 3.0e38f))
+    return fail(HPR_ERR_INVALID_ARG, "eps must be positive (and normal), scale and eps finite");
   if (!norm_fits(d->n, d->dim))
     return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%lld rows of %d are more than one launch holds", (long long)d->n, d->dim);
   return HPR_OK;

@@ -21,19 +21,23 @@ __device__ __forceinline__ float checkpoint_step(uint32_t e) {
   return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23);
 }
 
-// Value i of eight codes.
-__device__ __forceinline__ float code_value(uint2 codes, int i, float step) {
-  const uint32_t w = i < 4 ? codes.x : codes.y;
-  return (float)(int8_t)(w >> (8 * (i & 3))) * step;
+// Eight codes' values.  A code plus 128 is a byte, which one instruction converts.
+__device__ __forceinline__ void code_values(uint2 codes, uint32_t e, float (&f)[8]) {
+  const float step = checkpoint_step(e);
+  const uint32_t w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    f[i] = ((float)((w[i >> 2] >> (8 * (i & 3))) & 255u) - 128.f) * step;
 }
 
 // Eight values in the 16-bit type, exactly.
 template <class T>
 __device__ __forceinline__ u32x4 unpack8(uint2 codes, uint32_t e) {
-  const float step = checkpoint_step(e);
+  float f[8];
+  code_values(codes, e, f);
   u32x4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = T::pack(code_value(codes, 2 * i, step), code_value(codes, 2 * i + 1, step));
+  for (int i = 0; i < 4; ++i) v[i] = T::pack(f[2 * i], f[2 * i + 1]);
   return v;
 }
 

@@ -456,7 +456,7 @@ struct NormArgs {
   const uint16_t *dr, *dy;            // [n, d], either may be null
   uint16_t *dx, *db, *dgate_rows;     // [n, d], each may be null
   uint16_t *dw, *dc, *dpw, *dpc, *dgate;  // [d], each may be null
-  float* part;                        // norm_sums(layer) sums of d columns of norm_parts(n, d) groups of rows
+  float* part;                        // norm_sums(layer) sums of d columns of norm_parts(n, d) workgroups
   int64_t parts;                      // the launcher's
 };
 constexpr int kMaxNormDim = 16384;

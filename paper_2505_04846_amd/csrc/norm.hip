@@ -124,11 +124,11 @@ __device__ __forceinline__ void statistics(const float (&v)[C][8], const bool (&
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float q = in[c] ? v[c][i] - mean : 0.f;
+      const float q = LAYER ? (in[c] ? v[c][i] - mean : 0.f) : v[c][i];
       s[0] += q * q;
     }
   sums(s);
-  rs = 1.f / __builtin_sqrtf(s[0] * inv_d + eps);
+  rs = __builtin_amdgcn_rsqf(s[0] * inv_d + eps);
 }
 
 template <class T, bool LAYER, int W, int C>
@@ -186,189 +186,294 @@ __global__ __launch_bounds__((Layout<W, C>::kThreads)) void norm_fwd_kernel(Norm
 }
 
 // Rows in turn by a fixed number of workgroups, each of which keeps its rows' sums over columns in registers:
-//   sums 0 and 1: dy s and (of dx, or of dp where the gate is the row's own) times t;  2 and 3: the same without s, t.
-template <class T, bool LAYER, bool PACKED, int W, int C>
-__global__ __launch_bounds__((Layout<W, C>::kThreads)) void norm_bwd_kernel(NormArgs a) {
+//   sums 0 and 1: dy s, and t times dx or, where the gate is the row's own, times scale gate dx;  2 and 3: the same
+//   without s and t.
+// The next row is on its way while one is worked on, and the vectors stay in registers, where there is room for
+// them (C = 1).
+//
+// Rows are read and written through buffers of their own length, 0 for what there is not: values past the row, rows
+// past the last and tensors that are not there read as zeros and are not written, without a branch (with masks and
+// branches a third of the instructions were moves).  Zeros go through the formulas as zeros: of LAYER's mean alone
+// the lanes past the row are kept out.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_of(const void* base, int64_t first, int64_t bytes, bool there) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first, (short)0,
+                                           there && base ? (int)bytes : 0, 0x00020000);
+}
+__device__ __forceinline__ u32x4 read16(__amdgpu_buffer_rsrc_t r, int at) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+}
+__device__ __forceinline__ void write16(__amdgpu_buffer_rsrc_t r, int at, u32x4 v) {
+  typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), r, at, 0, 0);
+}
+
+template <int C>
+struct RowLoads {
+  u32x4 dr[C], dy[C], gate[C];
+  u32x4 x[C], b[C];       // of packed rows the codes alone
+  uint32_t ex[C], eb[C];  // and their exponents
+};
+
+template <class T, bool LAYER, bool PACKED, bool GATE_ROWS, int W, int C>
+__device__ __forceinline__ void norm_bwd_rows(const NormArgs& a) {
   typedef Layout<W, C> L;
   constexpr int kSums = LAYER ? 4 : 2;
+  constexpr bool kHold = C == 1;
   __shared__ float lds[2][L::kWaves][4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowSums<W, L::kWaves> sums = {lds, wave, 0};
   const float inv_d = 1.f / (float)a.d;
   const int blocks = (a.d + 31) / 32;
   const bool has_b = PACKED ? a.b_codes != nullptr : a.b != nullptr;
   int col[C];
+  bool live[C];
   float total[kSums][C][8];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     col[c] = 8 * ((wave % W) * 64 + lane + 64 * W * c);
+    live[c] = col[c] < a.d;
 #pragma unroll
     for (int k = 0; k < kSums; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) total[k][c][i] = 0.f;
   }
+  // w;  scale pw, and scale pc, times the gate where it is shared
+  auto vectors = [&](int c, float (&w)[8], float (&pw)[8], float (&pc)[8]) __attribute__((always_inline)) {
+    float g[8];
+    vector8<T>(live[c] ? a.w : nullptr, col[c], 0.f, w);
+    vector8<T>(live[c] ? a.pw : nullptr, col[c], 1.f, pw);
+    vector8<T>(LAYER && live[c] ? a.pc : nullptr, col[c], 0.f, pc);
+    vector8<T>(!GATE_ROWS && live[c] ? a.gate : nullptr, col[c], 1.f, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float by = a.scale * g[i];
+      pw[i] *= by;
+      pc[i] *= by;
+    }
+  };
+  float w_[kHold ? C : 1][8], pw_[kHold ? C : 1][8], pc_[kHold ? C : 1][8];
+  if constexpr (kHold) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) vectors(c, w_[c], pw_[c], pc_[c]);
+  }
+  const int64_t bytes = 2 * (int64_t)a.d;
+  auto load = [&](int64_t row, RowLoads<C>& l) __attribute__((always_inline)) {
+    const bool there = row < a.n;
+    const auto dr = row_of(a.dr, row * bytes, bytes, there), dy = row_of(a.dy, row * bytes, bytes, there);
+    const auto gate = row_of(GATE_ROWS ? a.gate : nullptr, row * bytes, bytes, there);
+    const void *xp = a.x, *bp = a.b;
+    if constexpr (PACKED) xp = a.x_codes, bp = a.b_codes;
+    const auto x = row_of(xp, PACKED ? row * a.d : 2 * row * a.x_ld, PACKED ? a.d : bytes, there);
+    const auto b = row_of(bp, PACKED ? row * a.d : 2 * row * a.b_ld, PACKED ? a.d : bytes, there);
+    const auto ex = row_of(PACKED ? a.x_exps : nullptr, row * blocks, blocks, there);
+    const auto eb = row_of(PACKED ? a.b_exps : nullptr, row * blocks, blocks, there);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      l.dr[c] = read16(dr, 2 * col[c]);
+      l.dy[c] = read16(dy, 2 * col[c]);
+      if constexpr (GATE_ROWS) l.gate[c] = read16(gate, 2 * col[c]);
+      if constexpr (PACKED) {
+        const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(x, col[c], 0, 0));
+        const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(b, col[c], 0, 0));
+        l.x[c][0] = v.x, l.x[c][1] = v.y;
+        l.b[c][0] = u.x, l.b[c][1] = u.y;
+        l.ex[c] = __builtin_amdgcn_raw_buffer_load_b8(ex, col[c] / 32, 0, 0);
+        l.eb[c] = __builtin_amdgcn_raw_buffer_load_b8(eb, col[c] / 32, 0, 0);
+      } else {
+        l.x[c] = read16(x, 2 * col[c]);
+        l.b[c] = read16(b, 2 * col[c]);
+      }
+    }
+  };
+  auto rows_of = [&](const u32x4& v, uint32_t e, float (&f)[8]) __attribute__((always_inline)) {
+    if constexpr (PACKED) code_values(uint2{v[0], v[1]}, e, f);
+    else widen<T>(v, f);
+  };
+  RowLoads<C> next;
+  const int64_t first = (int64_t)blockIdx.x * L::kRows, stride = (int64_t)gridDim.x * L::kRows;
+  if constexpr (kHold) load(first + wave / W, next);
   // (the same number of turns for every wave of the workgroup: the sums have barriers)
-  for (int64_t row0 = (int64_t)blockIdx.x * L::kRows; row0 < a.n; row0 += (int64_t)gridDim.x * L::kRows) {
+  for (int64_t row0 = first; row0 < a.n; row0 += stride) {
     const int64_t row = row0 + wave / W;
-    bool in[C];
-    float r[C][8], t[C][8], e[C][8], dr[C][8];  // t: b, then its normalised values; e: dy
+    const bool there = row < a.n;
+    if constexpr (!kHold) load(row, next);
+    float r[C][8], t[C][8], e[C][8], dr[C][8], g[GATE_ROWS ? C : 1][8];  // t: b, then its normalised values; e: dy
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      in[c] = col[c] < a.d && row < a.n;
-      const int64_t at = row * a.d + col[c];
-      u32x4 x = {0u, 0u, 0u, 0u}, b = {0u, 0u, 0u, 0u}, vr = {0u, 0u, 0u, 0u}, vy = {0u, 0u, 0u, 0u};
-      if (in[c]) {
-        if constexpr (PACKED) {
-          const int64_t block = row * blocks + col[c] / 32;
-          x = unpack8<T>(*reinterpret_cast<const uint2*>(a.x_codes + at), a.x_exps[block]);
-          if (has_b) b = unpack8<T>(*reinterpret_cast<const uint2*>(a.b_codes + at), a.b_exps[block]);
-        } else {
-          x = load16(a.x + row * a.x_ld + col[c]);
-          if (has_b) b = load16(a.b + row * a.b_ld + col[c]);
-        }
-        if (a.dr) vr = load16(a.dr + at);
-        if (a.dy) vy = load16(a.dy + at);
-      }
-      widen<T>(x, r[c]);
-      widen<T>(b, t[c]);
-      widen<T>(vr, dr[c]);
-      widen<T>(vy, e[c]);
+      rows_of(next.x[c], next.ex[c], r[c]);
+      rows_of(next.b[c], next.eb[c], t[c]);
+      widen<T>(next.dr[c], dr[c]);
+      widen<T>(next.dy[c], e[c]);
+      if constexpr (GATE_ROWS) widen<T>(next.gate[c], g[c]);
     }
+    if constexpr (kHold) load(row + stride, next);
+    auto at_c = [&](int c, float (&w)[8], float (&pw)[8], float (&pc)[8]) __attribute__((always_inline)) {
+      if constexpr (kHold) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = w_[c][i], pw[i] = pw_[c][i], pc[i] = pc_[c][i];
+      } else {
+        vectors(c, w, pw, pc);
+      }
+    };
     float mean_b = 0.f, rs_b = 1.f;
-    if (has_b) {
-      if (a.pw) statistics<LAYER, C>(t, in, inv_d, a.eps, sums, mean_b, rs_b);
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        if (!in[c]) continue;
-        float w[8], o[8], g[8];
-        vector8<T>(a.pw, col[c], 1.f, w);
-        vector8<T>(LAYER ? a.pc : nullptr, col[c], 0.f, o);
-        vector8<T>(a.gate, (a.gate_rows ? row * a.d : 0) + col[c], 1.f, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          t[c][i] = (t[c][i] - mean_b) * rs_b;
-          r[c][i] += a.scale * g[i] * (t[c][i] * w[i] + o[i]);
-        }
-      }
-    }
-    if (a.dy) {
-      float mean = 0.f;
-      if constexpr (LAYER) {
-        float s[1] = {0.f};
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s[0] += r[c][i];
-        sums(s);
-        mean = s[0] * inv_d;
-      }
-      float s[3] = {0.f, 0.f, 0.f};  // of (r - mean)^2, e (r - mean), e
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float w[8];
-        vector8<T>(in[c] ? a.w : nullptr, col[c], 1.f, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float q = in[c] ? r[c][i] - mean : 0.f, v = e[c][i] * w[i];
-          r[c][i] = q;
-          s[0] += q * q;
-          s[1] += v * q;
-          s[2] += v;
-        }
-      }
-      sums(s);
-      const float rs = 1.f / __builtin_sqrtf(s[0] * inv_d + a.eps);
-      const float along = s[1] * inv_d * rs, base = LAYER ? s[2] * inv_d : 0.f;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float w[8];
-        vector8<T>(in[c] ? a.w : nullptr, col[c], 1.f, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float q = r[c][i] * rs;
-          total[0][c][i] += e[c][i] * q;
-          if constexpr (LAYER) total[2][c][i] += e[c][i];
-          dr[c][i] += (e[c][i] * w[i] - base - q * along) * rs;
-        }
-      }
-    }
-    // dr is dx from here on
-    float s[2] = {0.f, 0.f};  // of f t, f
+    if (a.pw) statistics<LAYER, C>(t, live, inv_d, a.eps, sums, mean_b, rs_b);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (!in[c]) continue;
-      const int64_t at = row * a.d + col[c];
-      if (a.dx) *reinterpret_cast<u32x4*>(a.dx + at) = narrow<T>(dr[c]);
-      if (!has_b) continue;
-      float w[8], o[8], g[8], dg[8];
-      vector8<T>(a.pw, col[c], 1.f, w);
-      vector8<T>(LAYER ? a.pc : nullptr, col[c], 0.f, o);
-      vector8<T>(a.gate, (a.gate_rows ? at - col[c] : 0) + col[c], 1.f, g);
+      float w[8], pw[8], pc[8];
+      at_c(c, w, pw, pc);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float dp = a.scale * g[i] * dr[c][i], f = dp * w[i];
-        dg[i] = a.scale * dr[c][i] * (t[c][i] * w[i] + o[i]);
-        const float of = a.gate_rows ? dp : dr[c][i];
-        total[1][c][i] += of * t[c][i];
-        if constexpr (LAYER) total[3][c][i] += of;
-        s[0] += f * t[c][i];
-        s[1] += f;
-        r[c][i] = f;
+        t[c][i] = LAYER ? (live[c] ? (t[c][i] - mean_b) * rs_b : 0.f) : t[c][i] * rs_b;
+        const float p = LAYER ? t[c][i] * pw[i] + pc[i] : t[c][i] * pw[i];
+        r[c][i] += GATE_ROWS ? g[c][i] * p : p;
       }
-      if (a.dgate_rows) *reinterpret_cast<u32x4*>(a.dgate_rows + at) = narrow<T>(dg);
     }
-    if (!has_b) continue;
-    if (a.pw) sums(s);
-    const float along = a.pw ? s[0] * inv_d : 0.f, base = LAYER && a.pw ? s[1] * inv_d : 0.f;
+    float mean = 0.f;
+    if constexpr (LAYER) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[0] += r[c][i];
+      sums(s);
+      mean = s[0] * inv_d;
+    }
+    float s[LAYER ? 3 : 2];  // of (r - mean)^2, e (r - mean), e
+#pragma unroll
+    for (float& v : s) v = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (!in[c] || !a.db) continue;
+      float w[8], pw[8], pc[8];
+      at_c(c, w, pw, pc);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float q = LAYER ? (live[c] ? r[c][i] - mean : 0.f) : r[c][i], v = e[c][i] * w[i];
+        r[c][i] = q;
+        s[0] += q * q;
+        s[1] += v * q;
+        if constexpr (LAYER) s[2] += v;
+      }
+    }
+    sums(s);
+    const float rs = __builtin_amdgcn_rsqf(s[0] * inv_d + a.eps);
+    const float along = s[1] * inv_d * rs;
+    float base = 0.f;
+    if constexpr (LAYER) base = s[2] * inv_d;
+    const auto dx = row_of(a.dx, row * bytes, bytes, there), db = row_of(a.db, row * bytes, bytes, there);
+    const auto dgate = row_of(GATE_ROWS ? a.dgate_rows : nullptr, row * bytes, bytes, there);
+    float back[2] = {0.f, 0.f};  // sums of f t, f
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float w[8], pw[8], pc[8], dg[8];
+      at_c(c, w, pw, pc);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float q = r[c][i] * rs;
+        total[0][c][i] += e[c][i] * q;
+        if constexpr (LAYER) total[2][c][i] += e[c][i];
+        const float d = dr[c][i] + (LAYER ? e[c][i] * w[i] - base - q * along : e[c][i] * w[i] - q * along) * rs;
+        dr[c][i] = d;  // dx from here on
+        float f = d * pw[i], of = d;
+        if constexpr (GATE_ROWS) {
+          f *= g[c][i];
+          of *= a.scale * g[c][i];
+          dg[i] = d * (LAYER ? t[c][i] * pw[i] + pc[i] : t[c][i] * pw[i]);
+        }
+        total[1][c][i] += of * t[c][i];
+        if constexpr (LAYER) total[3][c][i] += of;
+        back[0] += f * t[c][i];
+        if constexpr (LAYER) back[1] += live[c] ? f : 0.f;
+        r[c][i] = f;
+      }
+      write16(dx, 2 * col[c], narrow<T>(dr[c]));
+      if constexpr (GATE_ROWS) write16(dgate, 2 * col[c], narrow<T>(dg));
+    }
+    if (!has_b) continue;
+    if (a.pw) sums(back);
+    const float along_b = a.pw ? back[0] * inv_d : 0.f, base_b = LAYER && a.pw ? back[1] * inv_d : 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
       float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (r[c][i] - base - t[c][i] * along) * rs_b;
-      *reinterpret_cast<u32x4*>(a.db + row * a.d + col[c]) = narrow<T>(v);
+      for (int i = 0; i < 8; ++i)
+        v[i] = LAYER ? (r[c][i] - base_b - t[c][i] * along_b) * rs_b : (r[c][i] - t[c][i] * along_b) * rs_b;
+      write16(db, 2 * col[c], narrow<T>(v));
     }
   }
-  float* part = a.part + ((int64_t)blockIdx.x * L::kRows + wave / W) * kSums * a.d;
+  // the workgroup's rows join in LDS, one wave row after another
+  float* part = a.part + (int64_t)blockIdx.x * kSums * a.d;
+  if constexpr (L::kRows > 1) {
+    __shared__ float joined[kSums][512 * W * C];
+    for (int q = 0; q < L::kRows; ++q) {
+      if (wave / W == q) {
+#pragma unroll
+        for (int k = 0; k < kSums; ++k)
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+              f32x4* to = reinterpret_cast<f32x4*>(&joined[k][col[c] + i]);
+              f32x4 v = {total[k][c][i], total[k][c][i + 1], total[k][c][i + 2], total[k][c][i + 3]};
+              *to = q == 0 ? v : *to + v;
+            }
+      }
+      __syncthreads();
+    }
+    for (int i = 4 * threadIdx.x; i < kSums * 512 * W * C; i += 4 * L::kThreads) {
+      const int k = i / (512 * W * C), c = i % (512 * W * C);
+      if (c < a.d)
+        *reinterpret_cast<f32x4*>(part + (int64_t)k * a.d + c) = *reinterpret_cast<const f32x4*>(&joined[k][c]);
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (col[c] >= a.d) continue;
+      if (!live[c]) continue;
       float* to = part + (int64_t)k * a.d + col[c];
       *reinterpret_cast<f32x4*>(to) = f32x4{total[k][c][0], total[k][c][1], total[k][c][2], total[k][c][3]};
       *reinterpret_cast<f32x4*>(to + 4) = f32x4{total[k][c][4], total[k][c][5], total[k][c][6], total[k][c][7]};
     }
 }
 
-// The groups' sums of 64 columns, in their order within 16 runs of groups, then over the runs; and the gradients
-// that come of them.
+// (Eight waves a row are two workgroups a CU with 128 registers.)
+template <class T, bool LAYER, bool PACKED, bool GATE_ROWS, int W, int C>
+__global__ __launch_bounds__((Layout<W, C>::kThreads), W == 8 ? 4 : 1) void norm_bwd_kernel(NormArgs a) {
+  norm_bwd_rows<T, LAYER, PACKED, GATE_ROWS, W, C>(a);
+}
+
+// The workgroups' sums of 16 columns, in their order within 64 runs of workgroups, then over the runs; and the
+// gradients that come of them.
 template <class T, bool LAYER>
 __global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a) {
   constexpr int kSums = LAYER ? 4 : 2;
-  __shared__ f32x4 lds[16][kSums][16];
-  const int q = threadIdx.x & 15, run = threadIdx.x >> 4;
-  const int c = (int)blockIdx.x * 64 + 4 * q;
+  __shared__ f32x4 lds[64][kSums][4];
+  const int q = threadIdx.x & 3, run = threadIdx.x >> 2;
+  const int c = (int)blockIdx.x * 16 + 4 * q;
   f32x4 v[kSums];
 #pragma unroll
   for (int k = 0; k < kSums; ++k) v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (c < a.d)
-    for (int64_t g = a.parts * run / 16; g < a.parts * (run + 1) / 16; ++g)
+  if (c < a.d) {
+#pragma unroll 4
+    for (int64_t g = a.parts * run / 64; g < a.parts * (run + 1) / 64; ++g)
 #pragma unroll
       for (int k = 0; k < kSums; ++k)
         v[k] += *reinterpret_cast<const f32x4*>(a.part + (g * kSums + k) * a.d + c);
+  }
 #pragma unroll
   for (int k = 0; k < kSums; ++k) lds[run][k][q] = v[k];
   __syncthreads();
-  if (threadIdx.x >= 64) return;
-  const int j = threadIdx.x, to = (int)blockIdx.x * 64 + j;
+  if (threadIdx.x >= 16) return;
+  const int j = threadIdx.x, to = (int)blockIdx.x * 16 + j;
   if (to >= a.d) return;
   float s[kSums];
 #pragma unroll
   for (int k = 0; k < kSums; ++k) {
     s[k] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) s[k] += lds[w][k][j >> 2][j & 3];
+#pragma unroll 8
+    for (int w = 0; w < 64; ++w) s[k] += lds[w][k][j >> 2][j & 3];
   }
   const float none = LAYER ? s[kSums - 1] : 0.f;  // sum 3
   auto one = [&](const uint16_t* p, float other) { return p ? T::lo(p[to]) : other; };
@@ -383,19 +488,31 @@ __global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a) {
   put(a.dgate, a.scale * (one(a.pw, 1.f) * s[1] + one(LAYER ? a.pc : nullptr, 0.f) * none));
 }
 
-// W and C of a row of d values.
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+// W and C of a row of d values in the forward, and in the gradients, which hold more of a column in registers.
 template <class F>
 hipError_t by_dim(int d, F&& f) {
-  if (d <= 512) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-  if (d <= 1024) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
-  if (d <= 2048) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
-  if (d <= 4096) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
-  if (d <= 8192) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
-  return f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+  if (d <= 512) return f(Int<1>(), Int<1>());
+  if (d <= 1024) return f(Int<1>(), Int<2>());
+  if (d <= 2048) return f(Int<2>(), Int<2>());
+  if (d <= 4096) return f(Int<4>(), Int<2>());
+  if (d <= 8192) return f(Int<8>(), Int<2>());
+  return f(Int<8>(), Int<4>());
 }
-int rows_of_group(int d) { return d <= 1024 ? 4 : d <= 2048 ? 2 : 1; }  // Layout::kRows
+template <class F>
+hipError_t by_dim_bwd(int d, F&& f) {
+  if (d <= 512) return f(Int<1>(), Int<1>());
+  if (d <= 1024) return f(Int<2>(), Int<1>());
+  if (d <= 2048) return f(Int<4>(), Int<1>());
+  if (d <= 4096) return f(Int<8>(), Int<1>());
+  if (d <= 8192) return f(Int<16>(), Int<1>());
+  return f(Int<16>(), Int<2>());
+}
+int rows_of_group(int d) { return d <= 512 ? 4 : d <= 1024 ? 2 : 1; }  // Layout::kRows of the gradients
 
-constexpr int kGroups = 1024;  // workgroups of the gradients
+int groups_most(int d) { return d <= 2048 ? 1024 : 512; }  // workgroups of the gradients: four, or two, a CU
 
 template <class T, bool LAYER>
 hipError_t norm_fwd(const NormArgs& a, hipStream_t s) {
@@ -407,36 +524,36 @@ hipError_t norm_fwd(const NormArgs& a, hipStream_t s) {
   });
 }
 
-template <class T, bool LAYER, bool PACKED>
+template <class T, bool LAYER, bool PACKED, bool GATE_ROWS>
 hipError_t norm_bwd(const NormArgs& a, hipStream_t s) {
-  const hipError_t e = by_dim(a.d, [&](auto w, auto c) {
+  const hipError_t e = by_dim_bwd(a.d, [&](auto w, auto c) {
     typedef Layout<w(), c()> L;
     if (a.parts == 0) return hipSuccess;
-    hipLaunchKernelGGL((norm_bwd_kernel<T, LAYER, PACKED, w(), c()>), dim3((unsigned)(a.parts / L::kRows)),
+    hipLaunchKernelGGL((norm_bwd_kernel<T, LAYER, PACKED, GATE_ROWS, w(), c()>), dim3((unsigned)a.parts),
                        dim3(L::kThreads), 0, s, a);
     return hipGetLastError();
   });
   if (e != hipSuccess || !(a.dw || a.dc || a.dpw || a.dpc || a.dgate)) return e;
-  hipLaunchKernelGGL((norm_join_kernel<T, LAYER>), dim3((unsigned)((a.d + 63) / 64)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((norm_join_kernel<T, LAYER>), dim3((unsigned)((a.d + 15) / 16)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-template <class T>
+template <class T, bool LAYER>
 hipError_t norm_bwd_of(const NormArgs& a, hipStream_t s) {
-  if (a.x_codes) return a.layer ? norm_bwd<T, true, true>(a, s) : norm_bwd<T, false, true>(a, s);
-  return a.layer ? norm_bwd<T, true, false>(a, s) : norm_bwd<T, false, false>(a, s);
+  if (a.x_codes) return a.gate_rows ? norm_bwd<T, LAYER, true, true>(a, s) : norm_bwd<T, LAYER, true, false>(a, s);
+  return a.gate_rows ? norm_bwd<T, LAYER, false, true>(a, s) : norm_bwd<T, LAYER, false, false>(a, s);
 }
 
 }  // namespace
 
-// Groups of rows whose sums the gradients keep apart.
+// Workgroups of the gradients, whose sums are kept apart.
 int64_t norm_parts(int64_t n, int d) {
   const int64_t per = rows_of_group(d), groups = (n + per - 1) / per;
-  return (groups < kGroups ? groups : kGroups) * per;
+  return groups < groups_most(d) ? groups : groups_most(d);
 }
 
 bool norm_fits(int64_t n, int d) {
-  const int64_t per = rows_of_group(d);
+  const int64_t per = d <= 1024 ? 4 : d <= 2048 ? 2 : 1;  // Layout::kRows of the forward, which has more workgroups
   return launch_fits((n + per - 1) / per, d <= 4096 ? 256 : 512);
 }
 
@@ -448,7 +565,8 @@ hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) {
 
 hipError_t launch_norm_bwd(NormArgs a, hipStream_t stream) {
   a.parts = norm_parts(a.n, a.d);
-  return a.f16 ? norm_bwd_of<HalfF16>(a, stream) : norm_bwd_of<HalfBf16>(a, stream);
+  if (a.f16) return a.layer ? norm_bwd_of<HalfF16, true>(a, stream) : norm_bwd_of<HalfF16, false>(a, stream);
+  return a.layer ? norm_bwd_of<HalfBf16, true>(a, stream) : norm_bwd_of<HalfBf16, false>(a, stream);
 }
 
 }  // namespace hpr

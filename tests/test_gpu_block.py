@@ -301,9 +301,9 @@ def test_norm_gradients_from_checkpoints(i):
     least = TYPES[ty][3]
     want = norm_oracle(*(B.checkpoint_values(*B.checkpoint_pack(f64(v), least)) for v in (x, b)), t, how, dr, dy, ty)
     for name, v in got.items():
-        if v is not None:
-            assert torch.equal(v, rows[name]), name
+        if v is not None:  # (two kernels, which may contract products and sums in different places)
             hold(v, want[name], want["bound"][name], name)
+            hold(rows[name], want[name], want["bound"][name], name)
 
 
 @pytest.mark.parametrize("i", [2, 4, 5, 11, 13])
