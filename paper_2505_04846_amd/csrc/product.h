@@ -303,8 +303,9 @@ struct TileProduct16 {
     u32x4 x[kT], w[kM];
   };
 
-  // x: first row of the tile.  LDS is free for the caller when this returns.
-  static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k,
+  // x: first row of the tile, of k values.  nk: stages, at least k / 64 (groups of waves that split k call this
+  // with the same number, because of its barriers).  LDS is free for the caller when this returns.
+  static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k, int nk,
                                              unsigned char* smem, int wave, int lane, Acc& acc) {
     const int wt = wave % WT, wm = wave / WT;
     const TileLoad<64, BT, kW> lx(wave, lane, 8);
@@ -320,7 +321,7 @@ struct TileProduct16 {
       const int row = PAIR ? lw.row[j] / (BM / WM) * kWaveCols + lw.row[j] % kWaveCols : lw.row[j];
       ow[j] = (row < w.last ? row : w.last) * w.ld * 2 + lw.chunk[j];
     }
-    const int nk = (k + 63) / 64, nk_full = k / 64;
+    const int nk_full = k / 64;
     unsigned char* const ring_w = smem + NX * kX;
     // Load j of x's or W's stage kk into slot `slot` of its ring.  Chunks past the end of k read zeros, so past the
     // last stage too (the rings keep their numbers of loads in flight); WHOLE: the stage lies inside k.
@@ -396,6 +397,7 @@ struct TileProduct16 {
     sync_lds();
 #pragma unroll
     for (int q = 0; q < kReads; ++q) read(0, 0, 0, f0, q);
+    const int whole = nk_full < nk ? nk_full : nk;
     int kk = 0, sx = 0, sw = 0, before = NX - 1;  // the stage's slots, and that of x's stage before
     auto turn = [&](auto whole) __attribute__((always_inline)) {
       step(whole, std::true_type(), before, kk - 1 + NX, sx, sw, 1, f0, f1);
@@ -409,7 +411,7 @@ struct TileProduct16 {
       step(whole, std::false_type(), slot, kk + NW, sx, sw, 0, f1, f0);
     };
 #pragma unroll 1
-    for (; kk + NX < nk_full; ++kk) turn(std::true_type());
+    for (; kk + NX < whole; ++kk) turn(std::true_type());
 #pragma unroll 1
     for (; kk < nk; ++kk) turn(std::false_type());
     // no load may still target LDS when it is reused or ends, and nobody may still read it
@@ -418,6 +420,40 @@ struct TileProduct16 {
     sync_lds();
   }
 };
+
+// The product of a tile by G groups of waves, each of which has its own rings and a G-th of k's stages.  In the end
+// the sums of all are group 0's (in the groups' order), whose waves go on (true); the others are done.
+template <class P, int G>
+__device__ __forceinline__ bool grouped(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k,
+                                        unsigned char* smem, int wave, int lane, typename P::Acc& acc) {
+  const int stages = (k + 63) / 64, each = (stages + G - 1) / G;
+  const int group = wave / P::kW, in = wave % P::kW, first = group * each * 64;
+  const int left = k - first < each * 64 ? k - first : each * 64;
+  P::run(xb + first, ldx, last_t, {{w.w[0] + first, w.w[1] + first}, w.ld, w.last}, G > 1 ? (left > 0 ? left : 0) : k,
+         each, smem + group * P::kLds, in, lane, acc);
+  if constexpr (G > 1) {
+    constexpr int kOwn = P::kM * P::kT * 1024;  // bytes of a wave's sums
+    static_assert((G - 1) * P::kW * kOwn <= G * P::kLds, "the sums fit the rings");
+    f32x4* mine = reinterpret_cast<f32x4*>(smem + ((group - 1) * P::kW + in) * kOwn);
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < P::kM; ++i)
+#pragma unroll
+        for (int j = 0; j < P::kT; ++j) mine[(i * P::kT + j) * 64 + lane] = acc[i][j];
+    }
+    __syncthreads();
+    if (group > 0) return false;
+#pragma unroll
+    for (int g = 1; g < G; ++g) {
+      const f32x4* from = reinterpret_cast<const f32x4*>(smem + ((g - 1) * P::kW + in) * kOwn);
+#pragma unroll
+      for (int i = 0; i < P::kM; ++i)
+#pragma unroll
+        for (int j = 0; j < P::kT; ++j) acc[i][j] += from[(i * P::kT + j) * 64 + lane];
+    }
+  }
+  return true;
+}
 
 // A wave's rows of results to memory in whole rows, through LDS of its own (16 rows of 32 BLOCKS bytes): BLOCKS
 // blocks of 16 columns of each of 16 rows.  dst: the first row's first column; value(i, e): entry e of block i of
