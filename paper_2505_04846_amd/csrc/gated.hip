@@ -176,8 +176,8 @@ __device__ __forceinline__ void gated_tile(const GatedArgs& a) {
   const int last_m = a.f - m0 < P::kCols ? a.f - m0 - 1 : P::kCols - 1;
   typename P::Acc acc;
   const int64_t w0 = (int64_t)m0 * a.k;
-  if (!grouped<P, G>(a.x + t0 * a.x_ld, (int)a.x_ld, last_t, {{a.wg + w0, a.wu + w0}, a.k, last_m}, a.k, smem, wave,
-                     lane, acc))
+  if (!grouped<P, G>(a.x + t0 * a.x_ld, (int)a.x_ld, last_t, {{a.wg + w0, a.wu + w0}, a.k, last_m}, a.k, at, smem,
+                     wave, lane, acc))
     return;
 
   const int mw = m0 + wm * P::kWaveCols;  // the wave's first column
@@ -268,12 +268,15 @@ __global__ __launch_bounds__(G * P::kThreads, 1) void gated_kernel(GatedArgs a) 
   gated_tile<T, A, P, G, GRAD>(a);
 }
 
-// Few rows: 32 rows of x by 16 columns of h per workgroup.  Eight waves split k and sum in LDS.
-constexpr int kFewWaves = 8;
+// Up to 32 rows by 16 columns of h per workgroup.  Four waves split k and sum in LDS; two workgroups a CU, so that one's
+// loads are on their way while the other starts or ends, and the weights, which the call reads once, go past the
+// caches.  Bound by the weights: 235 MB of 4096 -> 14336 (out of the caches) 1 row 38 us, 6.2 TB/s, 32 rows 45 us (eight
+// waves, one workgroup a CU: 46 and 53; through the caches 42 and 49).
+constexpr int kFewWaves = 8, kGatedWaves = 4;
 template <class T>
-using GatedFew = WaveProduct<T, 1, 1, 2, 32, true>;
+using GatedFew = WaveProduct<T, 1, 1, 2, 32, true, true>;
 template <class T>
-constexpr int kGatedFewLds = kFewWaves * GatedFew<T>::kBytes;
+constexpr int kGatedFewLds = kGatedWaves * GatedFew<T>::kBytes;
 
 template <class T, class A, bool GRAD>
 __device__ __forceinline__ void gated_few(const GatedArgs& a) {
@@ -281,28 +284,25 @@ __device__ __forceinline__ void gated_few(const GatedArgs& a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t n_m = (uint32_t)(a.f + 15) / 16u;
-  const int m0 = (int)(blockIdx.x % n_m) * 16;
-  const int64_t t0 = (int64_t)(blockIdx.x / n_m) * 32;
+  const int m0 = (int)blockIdx.x * 16;
   const int nk = (a.k + 63) / 64;
   f32x16 acc[1][1];
   unsigned char* own = smem + wave * P::kBytes;
   const int64_t w0 = (int64_t)m0 * a.k;
-  P::run(a.x + t0 * a.x_ld, (int)a.x_ld, a.n - t0 < 32 ? (int)(a.n - t0) - 1 : 31,
-         {{a.wg + w0, a.wu + w0}, a.k, a.f - m0 < 16 ? a.f - m0 - 1 : 15}, a.k, nk * wave / kFewWaves,
-         nk * (wave + 1) / kFewWaves, own, lane, acc);
+  P::run(a.x, (int)a.x_ld, (int)a.n - 1,
+         {{a.wg + w0, a.wu + w0}, a.k, a.f - m0 < 16 ? a.f - m0 - 1 : 15}, a.k, nk * wave / kGatedWaves,
+         nk * (wave + 1) / kGatedWaves, own, lane, acc);
   float* part = reinterpret_cast<float*>(own);  // [16][64]
 #pragma unroll
   for (int r = 0; r < 16; ++r) part[r * 64 + lane] = acc[0][0][r];
   __syncthreads();
   // thread: two columns of a row.  Column m < 16 of wg is entry e = 4 (m / 8) + m % 4 of lane
   // (row, half (m / 4) % 2), that of wu entry e + 8.
-  if (threadIdx.x >= 256) return;
   const int row = threadIdx.x & 31, m = 2 * (threadIdx.x >> 5);
   const int e = 4 * (m >> 3) + (m & 3), from = row + 32 * ((m >> 2) & 1);
   float g[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};
 #pragma unroll
-  for (int w = 0; w < kFewWaves; ++w) {
+  for (int w = 0; w < kGatedWaves; ++w) {
     const float* p = reinterpret_cast<const float*>(smem + w * P::kBytes) + from;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -310,7 +310,7 @@ __device__ __forceinline__ void gated_few(const GatedArgs& a) {
       u[c] += p[(e + 8 + c) * 64];
     }
   }
-  const int64_t t = t0 + row;
+  const int64_t t = row;
   if (m0 + m >= a.f) return;
   if constexpr (!GRAD) {
     if (t < a.n)
@@ -344,7 +344,8 @@ __device__ __forceinline__ void gated_few(const GatedArgs& a) {
 }
 
 template <class T, class A, bool GRAD>
-__global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(GatedArgs a) {
+__global__ __launch_bounds__(64 * kGatedWaves) void gated_few_kernel(GatedArgs a) {
+  static_assert(kGatedWaves == 4, "a thread for every two columns of 32 rows");
   gated_few<T, A, GRAD>(a);
 }
 
@@ -367,7 +368,7 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& a) {
   const int last_m = a.m - m0 < P::kCols ? a.m - m0 - 1 : P::kCols - 1;
   typename P::Acc acc;
   const uint16_t* const w0 = a.w + (int64_t)m0 * a.ld;
-  if (!grouped<P, G>(a.x + t0 * a.ld, a.ld, last_t, {{w0, w0}, a.ld, last_m}, a.k, smem, wave, lane, acc)) return;
+  if (!grouped<P, G>(a.x + t0 * a.ld, a.ld, last_t, {{w0, w0}, a.ld, last_m}, a.k, at, smem, wave, lane, acc)) return;
   constexpr int kOwn = 16 * 32 * kM, kSums = (G - 1) * P::kW * kM * kT * 1024;
   static_assert(kSums + P::kW * kOwn <= G * P::kLds, "the waves' blocks fit beside the sums");
   unsigned char* own = smem + kSums + wave * kOwn;
@@ -523,18 +524,18 @@ hipError_t gated_as(const GatedArgs& a, hipStream_t s) {
 
 template <class T, class A, bool GRAD>
 hipError_t gated_few_as(const GatedArgs& a, hipStream_t s) {
+  constexpr int lds = kGatedFewLds<T>;
   const auto kernel = gated_few_kernel<T, A, GRAD>;
-  const hipError_t e = allow_lds((const void*)kernel, kGatedFewLds<T>);
+  const hipError_t e = allow_lds((const void*)kernel, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((a.n + 31) / 32 * ((a.f + 15) / 16))), dim3(64 * kFewWaves),
-                     kGatedFewLds<T>, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(a.f + 15) / 16u), dim3(64 * kGatedWaves), lds, s, a);
   return hipGetLastError();
 }
 
 template <class T, class A, bool GRAD>
 hipError_t gated(GatedArgs a, hipStream_t s) {
   auto tiles = [&](int t, int m) { return (a.n - a.row0 + t - 1) / t * ((a.f + m - 1) / m); };
-  if (tiles(32, 16) <= 1024 && a.n <= 64) return gated_few_as<T, A, GRAD>(a, s);
+  if (a.n <= 32) return gated_few_as<T, A, GRAD>(a, s);
   if (tiles(256, 128) >= 144) return gated_as<T, A, Wide<T, true>, GRAD>(a, s);
   if (tiles(128, 64) >= 160) return gated_as<T, A, Middle<T, true>, GRAD>(a, s);
   return gated_as<T, A, Small<T, true>, GRAD, kSmallGroups>(a, s);

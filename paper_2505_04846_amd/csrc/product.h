@@ -29,8 +29,9 @@ struct PanelW {
 // by one wave: its NST LDS stages are its own, so waves that split k run without a barrier.  Whole 128-byte
 // lines go straight to LDS (operands read from memory by lanes touch twice as many lines a load: a token's
 // projection took 22 us that way).  Of P, ROWS rows are loaded; the results of the rest of its last 32 are
-// not to be used (their operands are what LDS holds past the stage, of this wave's or another's).
-template <class T, int NB, int XB, int NST = 2, int ROWS = 32 * NB, bool PAIR = false>
+// not to be used (their operands are what LDS holds past the stage, of this wave's or another's).  STREAM: P is read
+// once by the whole call, and keeps out of the caches.
+template <class T, int NB, int XB, int NST = 2, int ROWS = 32 * NB, bool PAIR = false, bool STREAM = false>
 struct WaveProduct {
   static constexpr int kStage = XB * 4096 + ROWS * 128;
   static constexpr int kBytes = NST * kStage;
@@ -58,9 +59,13 @@ struct WaveProduct {
       unsigned char* st = lds + buf * kStage;
       if (kk < whole) {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kX ? rx : (second(j) ? rq : rp),
-                                                   (lds_void_t*)(st + j * 1024), 16, off[j], kk * 128, 0, 0);
+        for (int j = 0; j < kLoads; ++j) {
+          if (j < kX)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)(st + j * 1024), 16, off[j], kk * 128, 0, 0);
+          else  // (2: nt)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(second(j) ? rq : rp, (lds_void_t*)(st + j * 1024), 16, off[j],
+                                                     kk * 128, 0, STREAM ? 2 : 0);
+        }
       } else {  // the end of k: chunks past it read zeros
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
@@ -273,6 +278,20 @@ struct TileProduct {
   }
 };
 
+// Tile of block b of a grid of n_t row tiles by n_m column tiles.  An XCD walks a contiguous run of tiles,
+// four row tiles abreast: the tiles that it holds at a time (32 of the widest) read 4 row tiles and 8 column
+// tiles, not 1 or 2 and all the columns.
+struct TileAt {
+  uint32_t t;
+  int m;
+};
+__device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint32_t n_t, int n_m) {
+  const uint32_t lin = (uint32_t)xcd_linear(block, blocks);
+  const uint32_t g0 = lin / (4u * n_m) * 4u, in_g = lin - g0 * n_m;
+  const uint32_t abreast = n_t - g0 < 4u ? n_t - g0 : 4u;
+  return {g0 + in_g % abreast, (int)(in_g / abreast)};
+}
+
 // ---- a workgroup's product, in blocks of 16 ------------------------------------------------------
 
 // The same in 16x16x32 products.  On operands that are not zero the card's power limit holds the clock, and these
@@ -286,6 +305,12 @@ struct TileProduct {
 // registers: while it multiplies one, it reads the other, and loads what takes the place of the stage before.  One
 // barrier a stage, between its k-steps: from there on nobody reads the stage's LDS.  Reads and loads stand between
 // the products one at a time, because a run of them holds the matrix cores up.
+//
+// An XCD's tiles (tile_at) go through k together, so that every stage is new to its L2, and its loads would wait for
+// memory.  In the largest tile one more load a wave touches lines kTouch stages ahead: the four row tiles share the
+// columns' panel, and each touches a quarter of its rows' lines, as the eight column tiles do an eighth of the
+// rows'.  (Zeros as operands 1,990 -> 1,745 us, 13,063 rows, 4096 -> 14336; the gradients of 6,529 rows 4,010 ->
+// 3,890; on random operands the forward is at the power limit without it.)
 template <class T, int BT, int BM, int WT, int WM, int NX, int NW, bool PAIR = false>
 struct TileProduct16 {
   static constexpr int kW = WT * WM;
@@ -296,6 +321,7 @@ struct TileProduct16 {
   static constexpr int kCols = PAIR ? BM / 2 : BM;            // columns of the output
   static constexpr int kWaveCols = kCols / WM;
   static constexpr int kThreads = 64 * kW, kRows = BT, kWt = WT;
+  static constexpr int kTouch = BT == 256 && BM == 256 && kW == 8 ? 4 : 0;  // (0: none)
   static_assert(!PAIR || kM % 2 == 0, "a wave holds both halves of its columns");
   static_assert(NW >= 2 && (NX == NW || NX == NW + 1) && kLds <= 160 * 1024, "the waits below");
   typedef f32x4 Acc[kM][kT];
@@ -306,7 +332,7 @@ struct TileProduct16 {
   // x: first row of the tile, of k values.  nk: stages, at least k / 64 (groups of waves that split k call this
   // with the same number, because of its barriers).  LDS is free for the caller when this returns.
   static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k, int nk,
-                                             unsigned char* smem, int wave, int lane, Acc& acc) {
+                                             TileAt tile, unsigned char* smem, int wave, int lane, Acc& acc) {
     const int wt = wave % WT, wm = wave / WT;
     const TileLoad<64, BT, kW> lx(wave, lane, 8);
     const TileLoad<64, BM, kW> lw(wave, lane, 8);
@@ -360,6 +386,17 @@ struct TileProduct16 {
 #pragma unroll
       for (int j = 0; j < kT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+    // lines to touch: of eight rows of W in the first lanes, of four of x in the next, and those again
+    const char* touch = nullptr;
+    uint32_t touched = 0;
+    if constexpr (kTouch > 0) {
+      auto row_of = [](int row, int last) { return row < last ? row : last; };
+      const int of_w = (int)(tile.t & 3u) * 64 + wave * 8 + (lane & 7);
+      const int of_x = row_of((tile.m & 7) * 32 + wave * 4 + (lane & 3), last_t);
+      const bool up = PAIR && of_w % (BM / WM) >= kWaveCols;
+      const int in_w = row_of(PAIR ? of_w / (BM / WM) * kWaveCols + of_w % kWaveCols : of_w, w.last);
+      touch = lane < 8 ? (const char*)w.w[up] + (int64_t)in_w * w.ld * 2 : (const char*)xb + (int64_t)of_x * ldx * 2;
+    }
     // chunk 4 s + lane / 16 of row lane % 16 of a block of 16 rows, of k-step s
     const int r = lane & 15, at0 = r * 128 + (((lane >> 4) ^ swz<64>(r)) << 4);
     const unsigned char* const own_x = smem + wt * kT * 2048;
@@ -404,6 +441,15 @@ struct TileProduct16 {
       __builtin_amdgcn_s_waitcnt(waitcnt_vm(kBehind));
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       sync_lds();  // the next stage has landed, and nobody reads this one any more
+      if constexpr (kTouch > 0) {
+        // (the one before has arrived: it is older than what the wait above was for)
+        asm volatile("" : : "v"(touched));
+        if constexpr (whole()) {
+          const int stage = kk + kTouch < nk_full ? kk + kTouch : nk_full - 1;
+          touched = *reinterpret_cast<const uint32_t*>(touch + stage * 128);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
       const int slot = sw;
       before = sx;
       sx = sx + 1 < NX ? sx + 1 : 0;
@@ -414,6 +460,7 @@ struct TileProduct16 {
     for (; kk + NX < whole; ++kk) turn(std::true_type());
 #pragma unroll 1
     for (; kk < nk; ++kk) turn(std::false_type());
+    if constexpr (kTouch > 0) asm volatile("" : : "v"(touched));
     // no load may still target LDS when it is reused or ends, and nobody may still read it
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
@@ -424,13 +471,13 @@ struct TileProduct16 {
 // The product of a tile by G groups of waves, each of which has its own rings and a G-th of k's stages.  In the end
 // the sums of all are group 0's (in the groups' order), whose waves go on (true); the others are done.
 template <class P, int G>
-__device__ __forceinline__ bool grouped(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k,
+__device__ __forceinline__ bool grouped(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k, TileAt tile,
                                         unsigned char* smem, int wave, int lane, typename P::Acc& acc) {
   const int stages = (k + 63) / 64, each = (stages + G - 1) / G;
   const int group = wave / P::kW, in = wave % P::kW, first = group * each * 64;
   const int left = k - first < each * 64 ? k - first : each * 64;
   P::run(xb + first, ldx, last_t, {{w.w[0] + first, w.w[1] + first}, w.ld, w.last}, G > 1 ? (left > 0 ? left : 0) : k,
-         each, smem + group * P::kLds, in, lane, acc);
+         each, tile, smem + group * P::kLds, in, lane, acc);
   if constexpr (G > 1) {
     constexpr int kOwn = P::kM * P::kT * 1024;  // bytes of a wave's sums
     static_assert((G - 1) * P::kW * kOwn <= G * P::kLds, "the sums fit the rings");
@@ -476,20 +523,6 @@ __device__ __forceinline__ void store_rows16(uint16_t* dst, int64_t ld, int64_t 
     const u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kRow + (lane % kCh) * 16);
     if (r >= from && r < n_rows && 8 * c < n_cols) *reinterpret_cast<u32x4*>(dst + (int64_t)r * ld + 8 * c) = v;
   }
-}
-
-// Tile of block b of a grid of n_t row tiles by n_m column tiles.  An XCD walks a contiguous run of tiles,
-// four row tiles abreast: the tiles that it holds at a time (32 of the widest) read 4 row tiles and 8 column
-// tiles, not 1 or 2 and all the columns.
-struct TileAt {
-  uint32_t t;
-  int m;
-};
-__device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint32_t n_t, int n_m) {
-  const uint32_t lin = (uint32_t)xcd_linear(block, blocks);
-  const uint32_t g0 = lin / (4u * n_m) * 4u, in_g = lin - g0 * n_m;
-  const uint32_t abreast = n_t - g0 < 4u ? n_t - g0 : 4u;
-  return {g0 + in_g % abreast, (int)(in_g / abreast)};
 }
 
 // A wave's rows of results to memory in whole rows, through LDS of its own: BLOCKS blocks of 32 columns of
