@@ -162,6 +162,9 @@ def _public_raw_stream(index):
 # The raw handle of a device's current stream, without the Stream object around it.  torch's accessor
 # for it is not public: where it is missing, the public way.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _public_raw_stream)
+# The current device's index likewise, without the checks around it (the tensors of a call are on a device
+# already).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(device):
@@ -174,7 +177,7 @@ def _launch(fn, device, *args):
     Entering torch's device guard costs about as much as a kernel launch, so only a call for
     another device than the current one does."""
     index = device.index  # (a tensor's device always has one)
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         status = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
@@ -826,6 +829,11 @@ def rotary(q, k, pos, cos, sin):
 def _need_rows(t, name, dtype, device):
     """Row stride of t [rows, values], with contiguous values and 16-byte aligned rows (columns of a wider
     tensor are fine).  One row is never stepped over: its stride counts as 0."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and dtype in _HALF_TYPES and t.device == device and t.is_cuda
+            and t.is_contiguous()):
+        shape = t.shape
+        if len(shape) == 2 and not (shape[1] & 7 or t.data_ptr() & 15):
+            return shape[1]
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype or dtype not in _HALF_TYPES:
@@ -864,9 +872,21 @@ def _rows_or_checkpoint(t, name, dtype, device):
     """(pointer, exps pointer, row stride, shape) of 16-bit rows or of a checkpoint of them."""
     if isinstance(t, Checkpoint):
         _need_checkpoint(t, name, dtype, device)
-        return _ptr(t.codes), _ptr(t.exps), 0, tuple(t.codes.shape)
+        return t.codes.data_ptr(), t.exps.data_ptr(), 0, t.codes.shape
     row = _need_rows(t, name, dtype, device)
-    return _ptr(t), None, row, tuple(t.shape)
+    return t.data_ptr(), None, row, t.shape
+
+
+def _need_vector(t, name, dtype, dim, device):
+    """Pointer of t [dim], None for None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.is_cuda
+            and t.shape == (dim,) and t.is_contiguous()):
+        _need(t, name, dtype, 1, device)
+        if t.numel() != dim:
+            raise ValueError(f"{name} must hold {dim} values, got {t.numel()}")
+    return t.data_ptr()
 
 
 def checkpoint_pack(x):
@@ -877,9 +897,10 @@ def checkpoint_pack(x):
     dev = getattr(x, "device", None)
     row = _need_rows(x, "x", dtype, dev)
     n, dim = x.shape
-    codes = torch.empty((n, dim), dtype=torch.int8, device=dev)
-    exps = torch.empty((n, (dim + 31) // 32), dtype=torch.uint8, device=dev)
-    _launch(lib().checkpoint_pack, dev, _ptr(x), row, n, dim, _HALF_TYPES[dtype], _ptr(codes), _ptr(exps))
+    codes = torch.empty(n, dim, dtype=torch.int8, device=dev)
+    exps = torch.empty(n, (dim + 31) // 32, dtype=torch.uint8, device=dev)
+    _launch(lib().checkpoint_pack, dev, x.data_ptr(), row, n, dim, _HALF_TYPES[dtype], codes.data_ptr(),
+            exps.data_ptr())
     return Checkpoint(codes, exps, dtype)
 
 
@@ -891,7 +912,7 @@ def checkpoint_unpack(c, out=None):
     dev = c.codes.device
     n, dim = c.codes.shape
     if out is None:
-        out = torch.empty((n, dim), dtype=c.dtype, device=dev)
+        out = torch.empty(n, dim, dtype=c.dtype, device=dev)
     else:
         _need(out, "out", c.dtype, 2, dev)
         if out.shape != (n, dim):
@@ -910,11 +931,12 @@ def _gated_weights(w_gate, w_up, act):
     _need(w_gate, "w_gate", dtype, 2)
     dev = w_gate.device
     _need(w_up, "w_up", dtype, 2, dev)
-    if w_gate.shape != w_up.shape:
-        raise ValueError(f"w_gate and w_up differ in shape: {tuple(w_gate.shape)}, {tuple(w_up.shape)}")
+    shape = w_gate.shape
+    if shape != w_up.shape:
+        raise ValueError(f"w_gate and w_up differ in shape: {tuple(shape)}, {tuple(w_up.shape)}")
     if act not in _ACTIVATIONS:
         raise ValueError(f"act must be one of {', '.join(_ACTIVATIONS)}, got {act!r}")
-    return dev, dtype, *w_gate.shape
+    return dev, dtype, *shape
 
 
 def gated_linear_fwd(x, w_gate, w_up, act="silu", out=None):
@@ -924,17 +946,17 @@ def gated_linear_fwd(x, w_gate, w_up, act="silu", out=None):
     """
     dev, dtype, f, k = _gated_weights(w_gate, w_up, act)
     row = _need_rows(x, "x", dtype, dev)
-    n = x.shape[0]
-    if x.shape[1] != k:
-        raise ValueError(f"x has {x.shape[1]} columns, w_gate {k}")
+    n, cols = x.shape
+    if cols != k:
+        raise ValueError(f"x has {cols} columns, w_gate {k}")
     if out is None:
-        out = torch.empty((n, f), dtype=dtype, device=dev)
+        out = x.new_empty(n, f)
     else:
         _need(out, "out", dtype, 2, dev)
         if out.shape != (n, f):
             raise ValueError(f"out must be {(n, f)}")
-    _launch(lib().gated_linear_fwd, dev, _ptr(x), row, n, k, _ptr(w_gate), _ptr(w_up), f, _ACTIVATIONS[act],
-            _HALF_TYPES[dtype], _ptr(out))
+    _launch(lib().gated_linear_fwd, dev, x.data_ptr(), row, n, k, w_gate.data_ptr(), w_up.data_ptr(), f,
+            _ACTIVATIONS[act], _HALF_TYPES[dtype], out.data_ptr())
     return {"h": out}
 
 
@@ -1009,7 +1031,7 @@ class _NormDesc(ctypes.Structure):
 
 
 def _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate, scale, eps, kind):
-    """Device, type, description, and the pointers of x, its exps, b and its exps."""
+    """Device, type, description, the pointers of x, its exps, b and its exps, and those of the vectors and gate."""
     dtype = getattr(x, "dtype", None)
     dev = x.codes.device if isinstance(x, Checkpoint) else getattr(x, "device", None)
     if kind not in _NORMS:
@@ -1017,35 +1039,34 @@ def _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate, scale, eps, k
     if b is not None and isinstance(x, Checkpoint) != isinstance(b, Checkpoint):
         raise TypeError("x and b must both be tensors or both be Checkpoints")
     x_ptr, x_exps, x_row, shape = _rows_or_checkpoint(x, "x", dtype, dev)
-    if dtype not in _HALF_TYPES:
-        raise TypeError(f"x must be bfloat16 or float16, got {dtype}")
     n, dim = shape
     b_ptr = b_exps = None
     b_row = 0
     if b is not None:
         b_ptr, b_exps, b_row, b_shape = _rows_or_checkpoint(b, "b", dtype, dev)
         if b_shape != shape:
-            raise ValueError(f"b must be {shape}, got {b_shape}")
+            raise ValueError(f"b must be {tuple(shape)}, got {tuple(b_shape)}")
     elif post_weight is not None or post_bias is not None or gate is not None:
         raise ValueError("post_weight, post_bias and gate need b")
-    for t, name in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight"), (post_bias, "post_bias")):
-        if t is None:
-            continue
-        _need(t, name, dtype, 1, dev)
-        if t.numel() != dim:
-            raise ValueError(f"{name} must hold {dim} values, got {t.numel()}")
+    vectors = (_need_vector(weight, "weight", dtype, dim, dev), _need_vector(bias, "bias", dtype, dim, dev),
+               _need_vector(post_weight, "post_weight", dtype, dim, dev),
+               _need_vector(post_bias, "post_bias", dtype, dim, dev))
     if kind != "layer" and (bias is not None or post_bias is not None):
         raise ValueError("a bias needs kind \"layer\"")
     if (bias is not None and weight is None) or (post_bias is not None and post_weight is None):
         raise ValueError("a bias needs its weight")
     gate_rows = 0
-    if gate is not None:
-        gate_rows = int(getattr(gate, "dim", int)() == 2)
-        _need(gate, "gate", dtype, 2 if gate_rows else 1, dev)
-        if tuple(gate.shape) != (shape if gate_rows else (dim,)):
-            raise ValueError(f"gate must be {(dim,)} or {shape}, got {tuple(gate.shape)}")
+    gate_ptr = None
+    if isinstance(gate, torch.Tensor) and gate.dim() == 2:
+        gate_rows = 1
+        _need(gate, "gate", dtype, 2, dev)
+        if gate.shape != shape:
+            raise ValueError(f"gate must be {(dim,)} or {tuple(shape)}, got {tuple(gate.shape)}")
+        gate_ptr = gate.data_ptr()
+    else:
+        gate_ptr = _need_vector(gate, "gate", dtype, dim, dev)
     d = _NormDesc(n, x_row, b_row, dim, _HALF_TYPES[dtype], _NORMS[kind], gate_rows, float(scale), float(eps))
-    return dev, dtype, d, (x_ptr, x_exps, b_ptr, b_exps)
+    return dev, dtype, d, (x_ptr, x_exps, b_ptr, b_exps), (*vectors, gate_ptr)
 
 
 def residual_norm_fwd(x, b=None, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, scale=1.0,
@@ -1059,14 +1080,14 @@ def residual_norm_fwd(x, b=None, weight=None, bias=None, post_weight=None, post_
     dict(r, y).  x (the residual stream) and b (the block's output) [n, dim], rows may be strided; weights and
     biases [dim]; gate [dim] or [n, dim] or None; kind "rms" or "layer" (biases are the latter's).
     """
-    dev, dtype, d, (x_ptr, x_exps, b_ptr, _) = _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate, scale,
-                                                            eps, kind)
-    if x_exps is not None:
+    dev, _, d, (x_ptr, x_exps, b_ptr, _), vectors = _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate,
+                                                                 scale, eps, kind)
+    if isinstance(x, Checkpoint):
         raise TypeError("x and b must be tensors")
-    r = torch.empty((d.n, d.dim), dtype=dtype, device=dev) if b is not None else None
-    y = torch.empty((d.n, d.dim), dtype=dtype, device=dev) if weight is not None else None
-    _launch(lib().residual_norm_fwd, dev, ctypes.byref(d), x_ptr, b_ptr, _ptr(weight), _ptr(bias),
-            _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(r), _ptr(y))
+    n, dim = x.shape
+    r = x.new_empty(n, dim) if b is not None else None
+    y = x.new_empty(n, dim) if weight is not None else None
+    _launch(lib().residual_norm_fwd, dev, ctypes.byref(d), x_ptr, b_ptr, *vectors, _ptr(r), _ptr(y))
     return {"r": x if b is None else r, "y": y}
 
 
@@ -1077,8 +1098,8 @@ def residual_norm_bwd(dr, dy, x, b=None, weight=None, bias=None, post_weight=Non
     dense and of the inputs' type, None where there is nothing that they are the gradient of or where not needed
     (need_dw: the weights' and biases').  dr and dy [n, dim], either may be None.  x and b: the forward's, or
     Checkpoints of them (the gradients are those at the values that they stand for)."""
-    dev, dtype, d, (x_ptr, x_exps, b_ptr, b_exps) = _norm_inputs(x, b, weight, bias, post_weight, post_bias, gate,
-                                                                 scale, eps, kind)
+    dev, dtype, d, (x_ptr, x_exps, b_ptr, b_exps), (w_ptr, _, pw_ptr, pc_ptr, g_ptr) = _norm_inputs(
+        x, b, weight, bias, post_weight, post_bias, gate, scale, eps, kind)
     for t, name in ((dr, "dr"), (dy, "dy")):
         if t is None:
             continue
@@ -1100,7 +1121,7 @@ def residual_norm_bwd(dr, dy, x, b=None, weight=None, bias=None, post_weight=Non
     need = L.residual_norm_bwd_workspace_size(ctypes.byref(d))
     ws = ws if ws is not None and ws.numel() >= need else _workspace(need, dev)
     _launch(L.residual_norm_bwd, dev, ctypes.byref(d), _ptr(dr), _ptr(dy), x_ptr, x_exps, b_ptr, b_exps,
-            _ptr(weight), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(dx), _ptr(db), _ptr(dw), _ptr(dc),
+            w_ptr, pw_ptr, pc_ptr, g_ptr, _ptr(dx), _ptr(db), _ptr(dw), _ptr(dc),
             _ptr(dpw), _ptr(dpc), _ptr(dgate), _ptr(ws), ws.numel())
     return {"dx": dx, "db": db, "dweight": dw, "dbias": dc, "dpost_weight": dpw, "dpost_bias": dpc, "dgate": dgate}
 
