@@ -451,6 +451,7 @@ hpr_status check_gated(int64_t n, int32_t k, int32_t f, int64_t x_row, int32_t a
 struct GatedCarve {
   uint16_t *wt, *d, *dt, *xt, *plain;
   uint32_t* words;  // maxima of rows, then of columns
+  float* part;      // of one product after the other
   size_t bytes;
 };
 GatedCarve gated_carve(void* ws, int64_t n, int32_t k, int32_t f, bool packed, bool need_dx, bool need_dw) {
@@ -468,6 +469,9 @@ GatedCarve gated_carve(void* ws, int64_t n, int32_t k, int32_t f, bool packed, b
   if (need_dw) g.xt = reinterpret_cast<uint16_t*>(take(np * k * 2));
   if (packed) g.plain = reinterpret_cast<uint16_t*>(take((size_t)n * k * 2));
   g.words = reinterpret_cast<uint32_t*>(take(((size_t)n + f) * sizeof(uint32_t)));
+  const size_t of_dx = need_dx ? rows_product_bytes(n, k, 2 * f) : 0;
+  const size_t of_dw = need_dw ? rows_product_bytes(2 * (int64_t)f, k, (int)np) : 0;
+  g.part = reinterpret_cast<float*>(take(of_dx > of_dw ? of_dx : of_dw));
   return g;
 }
 
@@ -1039,12 +1043,12 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
   }
   if (e == hipSuccess && need_dx && n > 0)
     e = timed("gated_product", s, [&] {
-      const ProductArgs q = {g.d, g.wt, n, k, 2 * f, 2 * f, {dx, nullptr}, n, row_max, 0};
+      const ProductArgs q = {g.d, g.wt, n, k, 2 * f, 2 * f, {dx, nullptr}, n, row_max, g.part};
       return launch_rows_product(q, narrow, s);
     });
   if (e == hipSuccess && need_dw)  // (without a row the sums are empty, and the product writes zeros)
     e = timed("gated_product", s, [&] {
-      const ProductArgs q = {g.dt, g.xt, 2 * (int64_t)f, k, (int)np, (int)np, {dw_gate, dw_up}, f, col_max, 0};
+      const ProductArgs q = {g.dt, g.xt, 2 * (int64_t)f, k, (int)np, (int)np, {dw_gate, dw_up}, f, col_max, g.part};
       return launch_rows_product(q, narrow, s);
     });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "gated gradient launch");

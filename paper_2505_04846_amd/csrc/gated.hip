@@ -168,8 +168,8 @@ __device__ __forceinline__ void gated_tile(const GatedArgs& a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wt = wave % P::kWt, wm = wave % P::kW / P::kWt;  // (of group 0, which stores)
   const int n_m = (a.f + P::kCols - 1) / P::kCols;
-  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + P::kRows - 1) / P::kRows), n_m);
-  const int64_t t0 = a.row0 + (int64_t)at.t * P::kRows;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n + P::kRows - 1) / P::kRows), n_m);
+  const int64_t t0 = (int64_t)at.t * P::kRows;
   const int m0 = at.m * P::kCols;
   const int64_t left_t = a.n - t0;
   const int last_t = left_t < P::kRows ? (int)left_t - 1 : P::kRows - 1;
@@ -351,7 +351,8 @@ __global__ __launch_bounds__(64 * kGatedWaves) void gated_few_kernel(GatedArgs a
 
 // ---- dx, dW -------------------------------------------------------------------------------------
 
-// y[r][c] = 2^-up(r) <x_r, w_c>, rows [0, split) to y[0], the others to y[1].
+// y[r][c] = 2^-up(r) <x_r, w_c>, rows [0, split) to y[0], the others to y[1].  Where the tiles are too few for the chip and
+// k is long, `splits` workgroups share a tile's k, and their sums go to memory in 32 bits for join_kernel.
 template <class T, class P, int G>
 __device__ __forceinline__ void rows_tile(const ProductArgs& a) {
   constexpr int kT = P::kT, kM = P::kM;
@@ -360,19 +361,37 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wt = wave % P::kWt, wm = wave % P::kW / P::kWt;  // (of group 0, which stores)
   const int n_m = (a.m + P::kCols - 1) / P::kCols;
-  const TileAt at = tile_at(blockIdx.x, gridDim.x, (uint32_t)((a.n - a.row0 + P::kRows - 1) / P::kRows), n_m);
+  const uint32_t n_t = (uint32_t)((a.n - a.row0 + P::kRows - 1) / P::kRows);
+  // (an XCD's workgroups are tiles of the same part of k, and share its lines)
+  const uint32_t lin = (uint32_t)xcd_linear(blockIdx.x, gridDim.x), part = lin / (n_t * (uint32_t)n_m);
+  const TileAt at = tile_of(lin - part * n_t * n_m, n_t, n_m);
+  const int each = ((a.k + 63) / 64 + a.splits - 1) / a.splits * 64, k0 = (int)part * each;
+  const int left_k = a.k - k0 < each ? a.k - k0 : each;
   const int64_t t0 = a.row0 + (int64_t)at.t * P::kRows;
   const int m0 = at.m * P::kCols;
   const int64_t left_t = a.n - t0;
   const int last_t = left_t < P::kRows ? (int)left_t - 1 : P::kRows - 1;
   const int last_m = a.m - m0 < P::kCols ? a.m - m0 - 1 : P::kCols - 1;
   typename P::Acc acc;
-  const uint16_t* const w0 = a.w + (int64_t)m0 * a.ld;
-  if (!grouped<P, G>(a.x + t0 * a.ld, a.ld, last_t, {{w0, w0}, a.ld, last_m}, a.k, at, smem, wave, lane, acc)) return;
+  const uint16_t* const w0 = a.w + (int64_t)m0 * a.ld + k0;
+  if (!grouped<P, G>(a.x + t0 * a.ld + k0, a.ld, last_t, {{w0, w0}, a.ld, last_m}, left_k > 0 ? left_k : 0, at, smem,
+                     wave, lane, acc))
+    return;
   constexpr int kOwn = 16 * 32 * kM, kSums = (G - 1) * P::kW * kM * kT * 1024;
   static_assert(kSums + P::kW * kOwn <= G * P::kLds, "the waves' blocks fit beside the sums");
   unsigned char* own = smem + kSums + wave * kOwn;
   const int mw = m0 + wm * P::kWaveCols;
+  if (a.splits > 1) {
+#pragma unroll
+    for (int j = 0; j < kT; ++j) {
+      const int64_t r = t0 + (wt * kT + j) * 16 + row;
+      float* to = a.part + ((int64_t)part * a.n + r) * a.m + mw + 4 * (lane >> 4);
+#pragma unroll
+      for (int i = 0; i < kM; ++i)
+        if (r < a.n && mw + 16 * i + 4 * (lane >> 4) < a.m) *reinterpret_cast<f32x4*>(to + 16 * i) = acc[i][j];
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < kT; ++j) {
     const int64_t r0 = t0 + (wt * kT + j) * 16;
@@ -394,6 +413,29 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& a) {
 template <class T, class P, int G>
 __global__ __launch_bounds__(G * P::kThreads, 1) void rows_kernel(ProductArgs a) {
   rows_tile<T, P, G>(a);
+}
+
+// The splits' sums, in their order: eight values a thread.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, all = a.n * a.m;
+  if (i >= all) return;
+  f32x4 v[2] = {};
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    const f32x4* from = reinterpret_cast<const f32x4*>(a.part + s * all + i);
+    v[0] += from[0];
+    v[1] += from[1];
+  }
+  const int64_t t = i / a.m, c = i - t * a.m;
+  const bool first = t < a.split;
+  const int64_t at = first ? t : t - a.split;
+  float down = 1.f;
+  if constexpr (T::kNarrow) down = power_of(-up_of(a.max_bits[at]));
+  u32x4 w;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) w[q] = T::pack(v[q >> 1][2 * (q & 1)] * down, v[q >> 1][2 * (q & 1) + 1] * down);
+  *reinterpret_cast<u32x4*>(a.y[first ? 0 : 1] + at * a.m + c) = w;
 }
 
 // Few tiles: 32 rows by 32 columns, eight waves split k.
@@ -514,7 +556,7 @@ hipError_t allow_lds(const void* fn, int lds) {
 
 template <class T, class A, class P, bool GRAD, int G = 1>
 hipError_t gated_as(const GatedArgs& a, hipStream_t s) {
-  const int64_t grid = (a.n - a.row0 + P::kRows - 1) / P::kRows * ((a.f + P::kCols - 1) / P::kCols);
+  const int64_t grid = (a.n + P::kRows - 1) / P::kRows * ((a.f + P::kCols - 1) / P::kCols);
   const auto kernel = gated_kernel<T, A, P, G, GRAD>;
   const hipError_t e = allow_lds((const void*)kernel, G * P::kLds);
   if (e != hipSuccess) return e;
@@ -532,13 +574,20 @@ hipError_t gated_few_as(const GatedArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The tile of h, or of d, by the number of tiles (h alone, us; rows, k -> f):
+//   one row of tiles of 16 columns   up to 32 rows
+//   64 x 32     up to 256 of these: 146 rows, 768 -> 2304 (216 tiles) 6.8 (128 x 64: 8.2), 96 rows, 4096 -> 4096 (256) 17.5
+//               (26.5); 200 rows, 768 -> 2304 (288) 11.0 (8.1), 48 rows, 4096 -> 14336 (448) 39 (36)
+//   128 x 64    otherwise, until
+//   256 x 128   there are 144 of these: 1,500 rows, 768 -> 2304 (108) 19.6 (16.2), 2,048 rows (144) 20.8 (23.9), 1,024 rows,
+//               4096 -> 4096 (128) 78 (65), 1,500 rows (192) 84 (95)
 template <class T, class A, bool GRAD>
-hipError_t gated(GatedArgs a, hipStream_t s) {
-  auto tiles = [&](int t, int m) { return (a.n - a.row0 + t - 1) / t * ((a.f + m - 1) / m); };
+hipError_t gated(const GatedArgs& a, hipStream_t s) {
+  auto tiles = [&](int t, int m) { return (a.n + t - 1) / t * ((a.f + m - 1) / m); };
   if (a.n <= 32) return gated_few_as<T, A, GRAD>(a, s);
+  if (tiles(64, 32) <= 256) return gated_as<T, A, Small<T, true>, GRAD, kSmallGroups>(a, s);
   if (tiles(256, 128) >= 144) return gated_as<T, A, Wide<T, true>, GRAD>(a, s);
-  if (tiles(128, 64) >= 160) return gated_as<T, A, Middle<T, true>, GRAD>(a, s);
-  return gated_as<T, A, Small<T, true>, GRAD, kSmallGroups>(a, s);
+  return gated_as<T, A, Middle<T, true>, GRAD>(a, s);
 }
 
 template <class T, bool GRAD>
@@ -552,7 +601,7 @@ hipError_t gated_act(const GatedArgs& a, hipStream_t s) {
 
 template <class T, class P, int G = 1>
 hipError_t rows_as(const ProductArgs& a, hipStream_t s) {
-  const int64_t grid = (a.n - a.row0 + P::kRows - 1) / P::kRows * ((a.m + P::kCols - 1) / P::kCols);
+  const int64_t grid = (a.n - a.row0 + P::kRows - 1) / P::kRows * ((a.m + P::kCols - 1) / P::kCols) * a.splits;
   const auto kernel = rows_kernel<T, P, G>;
   const hipError_t e = allow_lds((const void*)kernel, G * P::kLds);
   if (e != hipSuccess) return e;
@@ -560,27 +609,68 @@ hipError_t rows_as(const ProductArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// How a product's tiles are made: the least estimated time, of 256 workgroups at a time, a stage of 64 values of k taking
+// a tile what it took in calls of 1 to 1,000 rows (256 x 256 1.26 us, 128 x 128 0.55, 64 x 64 by four groups of waves 0.29,
+// 32 x 32 by eight waves 0.14), and the splits' sums 8 bytes a value, written and read at 3.5 TB/s, and a launch.
+// The gradients of x alone, us with splits (without): 764 rows, 4096 -> 14336 (k 28672) 476 (578), 300 rows 331 (493),
+// 1,500 rows 738 (936), 764 rows, 768 -> 2304 (k 4608) 35 (39), 450 rows, 1024 -> 4096 45 (54).
+struct RowsPlan {
+  int tile;  // 0: 32 x 32, 1: 64 x 64, 2: 128 x 128, 3: 256 x 256
+  int splits;
+};
+RowsPlan rows_plan(int64_t n, int m, int k) {
+  constexpr int kSize[4] = {32, 64, 128, 256};
+  constexpr double kStage[4] = {0.143, 0.29, 0.55, 1.26};
+  const int64_t stages = k > 0 ? (k + 63) / 64 : 1;
+  RowsPlan best = {3, 1};
+  double least = 0.0;
+  for (int t = 3; t >= 0; --t) {
+    const int64_t tiles = (n + kSize[t] - 1) / kSize[t] * ((m + kSize[t] - 1) / kSize[t]);
+    const int most = t < 2 || tiles >= 256 ? 1 : 16;
+    for (int s = 1; s <= most && (s == 1 || (tiles * s <= 256 && stages / s >= 4)); ++s) {
+      const double rounds = (double)((tiles * s + 255) / 256), part = (double)((stages + s - 1) / s);
+      const double us = rounds * part * kStage[t] + (s > 1 ? 8.0 + (double)s * (double)n * m * 8.0 / 3.5e6 : 0.0);
+      if (t == 3 && s == 1) least = us;
+      if (us < least) {
+        least = us;
+        best = {t, s};
+      }
+    }
+  }
+  return best;
+}
+
 template <class T>
 hipError_t rows(ProductArgs a, hipStream_t s) {
-  auto tiles = [&](int b) { return (a.n - a.row0 + b - 1) / b * ((a.m + b - 1) / b); };
-  if (tiles(32) <= 384) {
+  const RowsPlan plan = rows_plan(a.n, a.m, a.k);
+  a.splits = plan.splits;
+  hipError_t e = hipSuccess;
+  if (plan.tile == 0) {
     const auto kernel = rows_few_kernel<T>;
-    const hipError_t e = allow_lds((const void*)kernel, kRowsFewLds<T>);
+    e = allow_lds((const void*)kernel, kRowsFewLds<T>);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles(32)), dim3(64 * kFewWaves), kRowsFewLds<T>, s, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.n + 31) / 32 * ((a.m + 31) / 32))), dim3(64 * kFewWaves),
+                       kRowsFewLds<T>, s, a);
     return hipGetLastError();
   }
-  if (tiles(256) >= 144) {
-    const int64_t n_m = (a.m + 255) / 256, rest = tiles(256) % 256;
-    const int64_t whole = (tiles(256) - rest) / n_m * 256;  // rows of the whole rounds
+  if (plan.tile == 1) return rows_as<T, Small<T, false>, kSmallGroups>(a, s);
+  if (plan.tile == 2) {
+    e = rows_as<T, Middle<T, false>>(a, s);
+  } else {
+    // a last round of up to 112 tiles (of 256, one a CU) is left to the next size
+    const int64_t n_m = (a.m + 255) / 256, tiles = (a.n + 255) / 256 * n_m, rest = tiles % 256;
+    const int64_t whole = (tiles - rest) / n_m * 256;  // rows of the whole rounds
     ProductArgs w = a;
-    if (rest > 0 && rest <= 112 && whole > 0) w.n = whole;
-    const hipError_t e = rows_as<T, Wide<T, false>>(w, s);
-    if (e != hipSuccess || w.n == a.n) return e;
-    a.row0 = whole;
+    if (a.splits == 1 && rest > 0 && rest <= 112 && whole > 0) w.n = whole;
+    e = rows_as<T, Wide<T, false>>(w, s);
+    if (e == hipSuccess && w.n < a.n) {
+      a.row0 = whole;
+      e = rows_as<T, Middle<T, false>>(a, s);
+    }
   }
-  if (tiles(128) >= 160 || a.row0 > 0) return rows_as<T, Middle<T, false>>(a, s);
-  return rows_as<T, Small<T, false>, kSmallGroups>(a, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)((a.n * a.m / 8 + 255) / 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -599,6 +689,11 @@ hipError_t launch_gated(const GatedArgs& a, bool grad, hipStream_t stream) {
   if (a.n == 0) return hipSuccess;
   if (grad) return a.f16 ? gated_act<HalfF16, true>(a, stream) : gated_act<HalfBf16, true>(a, stream);
   return a.f16 ? gated_act<HalfF16, false>(a, stream) : gated_act<HalfBf16, false>(a, stream);
+}
+
+size_t rows_product_bytes(int64_t n, int m, int k) {
+  const int splits = rows_plan(n, m, k).splits;
+  return splits > 1 ? (size_t)splits * n * m * sizeof(float) : 0;
 }
 
 hipError_t launch_rows_product(const ProductArgs& a, bool f16, hipStream_t stream) {

@@ -391,7 +391,6 @@ struct GatedArgs {
   uint16_t *d, *dt;
   int64_t np;
   const uint32_t *row_max, *col_max;
-  int64_t row0 = 0;  // the launcher's
 };
 hipError_t launch_gated(const GatedArgs& a, bool grad, hipStream_t stream);
 // Whether every launch of the forward, or of the gradients, is one that can be made (launch_fits).
@@ -408,8 +407,11 @@ struct ProductArgs {
   uint16_t* y[2];
   int64_t split;
   const uint32_t* max_bits;
-  int64_t row0 = 0;  // the launcher's
+  float* part;  // workspace of rows_product_bytes(n, m, k)
+  int64_t row0 = 0;  // the launcher's, and
+  int splits = 1;
 };
+size_t rows_product_bytes(int64_t n, int m, int k);
 hipError_t launch_rows_product(const ProductArgs& a, bool f16, hipStream_t stream);
 // Up to three transposes out[c][r] = in[r][c] (out null: none) and words to clear, in one launch.  in: rows of
 // in_ld, or a checkpoint's codes and exps, whose values go to plain [rows, cols] too (null: none).  out's rows are

@@ -285,11 +285,13 @@ struct TileAt {
   uint32_t t;
   int m;
 };
-__device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint32_t n_t, int n_m) {
-  const uint32_t lin = (uint32_t)xcd_linear(block, blocks);
+__device__ __forceinline__ TileAt tile_of(uint32_t lin, uint32_t n_t, int n_m) {
   const uint32_t g0 = lin / (4u * n_m) * 4u, in_g = lin - g0 * n_m;
   const uint32_t abreast = n_t - g0 < 4u ? n_t - g0 : 4u;
   return {g0 + in_g % abreast, (int)(in_g / abreast)};
+}
+__device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint32_t n_t, int n_m) {
+  return tile_of((uint32_t)xcd_linear(block, blocks), n_t, n_m);
 }
 
 // ---- a workgroup's product, in blocks of 16 ------------------------------------------------------
