@@ -463,13 +463,14 @@ GatedCarve gated_carve(void* ws, int64_t n, int32_t k, int32_t f, bool packed, b
     g.bytes += align_up(bytes);
     return p;
   };
-  if (need_dx) g.wt = reinterpret_cast<uint16_t*>(take((size_t)k * 2 * f * 2));
+  const bool columns = gated_by_columns(n);
+  if (need_dx && !columns) g.wt = reinterpret_cast<uint16_t*>(take((size_t)k * 2 * f * 2));
   if (need_dx) g.d = reinterpret_cast<uint16_t*>(take((size_t)n * 2 * f * 2));
   if (need_dw) g.dt = reinterpret_cast<uint16_t*>(take(np * 2 * f * 2));
   if (need_dw) g.xt = reinterpret_cast<uint16_t*>(take(np * k * 2));
   if (packed) g.plain = reinterpret_cast<uint16_t*>(take((size_t)n * k * 2));
   g.words = reinterpret_cast<uint32_t*>(take(((size_t)n + f) * sizeof(uint32_t)));
-  const size_t of_dx = need_dx ? rows_product_bytes(n, k, 2 * f) : 0;
+  const size_t of_dx = !need_dx ? 0 : columns ? gated_columns_bytes(n, k, f) : rows_product_bytes(n, k, 2 * f);
   const size_t of_dw = need_dw ? rows_product_bytes(2 * (int64_t)f, k, (int)np) : 0;
   g.part = reinterpret_cast<float*>(take(of_dx > of_dw ? of_dx : of_dw));
   return g;
@@ -1009,7 +1010,7 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
     const uint16_t* const x16 = packed ? nullptr : static_cast<const uint16_t*>(x);
     const int8_t* const codes = packed ? static_cast<const int8_t*>(x) : nullptr;
     GatedPrepare p = {};
-    if (need_dx) {
+    if (g.wt) {
       p.job[0] = {w_gate, k, nullptr, nullptr, f, k, g.wt, 2 * (int64_t)f, nullptr, 0};
       p.job[1] = {w_up, k, nullptr, nullptr, f, k, g.wt + f, 2 * (int64_t)f, nullptr, 0};
     }
@@ -1043,6 +1044,8 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
   }
   if (e == hipSuccess && need_dx && n > 0)
     e = timed("gated_product", s, [&] {
+      if (gated_by_columns(n))
+        return launch_gated_columns({g.d, w_gate, w_up, n, k, f, g.part, 0}, narrow, dx, row_max, s);
       const ProductArgs q = {g.d, g.wt, n, k, 2 * f, 2 * f, {dx, nullptr}, n, row_max, g.part};
       return launch_rows_product(q, narrow, s);
     });

@@ -487,6 +487,137 @@ __global__ __launch_bounds__(64 * kFewWaves) void rows_few_kernel(ProductArgs a)
   rows_few<T>(a);
 }
 
+// dx of few rows, from the weights as they lie: dx[t][c] = sum_j d[t][j] w[j][c], where the weights' rows j are read in
+// tiles of 64 rows by 64 columns and their columns taken by the LDS reads (tr_frag), so that nothing is transposed
+// first.  A workgroup takes 32 TB rows by 64 columns and a part of the sum, its four waves a quarter of it each, without a
+// barrier; they join in LDS and the parts in join_kernel.  Bound by the weights, which are read once for every 32 TB
+// rows: %COL%
+template <int TB>
+constexpr int kColumnsStages = TB == 1 ? 3 : 2;
+template <int TB>
+constexpr int kColumnsStage = 8192 + TB * 4096;  // bytes: 64 rows of w's 64 columns, 32 TB rows of d's 64 values
+constexpr int kColumnsWaves = 4;
+template <int TB>
+constexpr int kColumnsLds = kColumnsWaves * kColumnsStages<TB> * kColumnsStage<TB>;
+
+template <class T, int TB>
+__device__ __forceinline__ void columns_few(const ColumnsArgs& a) {
+  constexpr int kStages = kColumnsStages<TB>, kStage = kColumnsStage<TB>, kLoads = 8 + 4 * TB;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // kColumnsLds
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t n_c = (uint32_t)(a.k + 63) / 64u, n_t = (uint32_t)((a.n + 32 * TB - 1) / (32 * TB));
+  const int c0 = (int)(blockIdx.x % n_c) * 64;
+  const int64_t t0 = (int64_t)(blockIdx.x / n_c % n_t) * 32 * TB;
+  const int part = (int)(blockIdx.x / n_c / n_t);
+  // stages of wg's rows, then of wu's; this wave's are [s0, s1)
+  const int of_one = (a.f + 63) / 64, unit = part * kColumnsWaves + wave, units = a.splits * kColumnsWaves;
+  const int s0 = (int)((int64_t)2 * of_one * unit / units), s1 = (int)((int64_t)2 * of_one * (unit + 1) / units);
+  const int64_t left_t = a.n - t0;
+  const int last_t = left_t < 32 * TB ? (int)left_t - 1 : 32 * TB - 1;
+  const int last_c = a.k - c0 < 64 ? a.k - c0 - 8 : 56;
+  unsigned char* const own = smem + wave * kStages * kStage;
+  const uint32_t lds = LDS_ADDRESS(smem) + wave * kStages * kStage;
+  const int lr = lane >> 3;  // row of a wave load, 8 rows of 8 chunks
+  // (a row of w past the last repeats it: d is zero there)
+  auto issue = [&](int buf, int s) __attribute__((always_inline)) {
+    const bool up = s >= of_one;
+    const int f0 = (up ? s - of_one : s) * 64, n_f = a.f - f0 < 64 ? a.f - f0 : 64;
+    const rsrc_t rw = rsrc_of((up ? a.wu : a.wg) + (int64_t)f0 * a.k + c0);
+    const uint16_t* const d = a.d + t0 * 2 * a.f + (up ? a.f : 0) + f0;
+    const uint32_t st = lds + buf * kStage;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = 8 * j + lr, c = 8 * ((lane & 7) ^ swz<64>(r)), in = r < n_f ? r : n_f - 1;
+      load_lds16_stream(rw, st + j * 1024, (uint32_t)(in * a.k + (c < last_c ? c : last_c)) * 2u);
+    }
+#pragma unroll
+    for (int j = 0; j < 4 * TB; ++j) {
+      const int r = 8 * j + lr, c = 8 * ((lane & 7) ^ swz<64>(r));
+      const uint16_t* from = d + (int64_t)(r < last_t ? r : last_t) * 2 * a.f + c;
+      load_lds16(c < n_f ? (const void*)from : (const void*)kZero16, st + 8192 + j * 1024);
+    }
+  };
+  f32x16 acc[2][TB];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  const TileReads<64> rd(lane);
+#pragma unroll
+  for (int q = 0; q < kStages - 1; ++q)
+    if (s0 + q < s1) issue(q, s0 + q);
+#pragma unroll 1
+  for (int s = s0, buf = 0; s < s1; ++s, buf = buf + 1 < kStages ? buf + 1 : 0) {
+    if (s + kStages - 1 < s1) {
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // that stage's reads are done
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      issue(buf > 0 ? buf - 1 : kStages - 1, s + kStages - 1);
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm((kStages - 1) * kLoads));
+    } else if (kStages == 3 && s + 1 < s1) {
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
+    } else {
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    }
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    const unsigned char* ws = own + buf * kStage;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        // d's values in tr_frag's order of rows: 8 (e / 4) + 4 half + e % 4 of these 16
+        u32x4 fd[TB];
+#pragma unroll
+        for (int j = 0; j < TB; ++j) {
+          const int r = 32 * j + col, c = 4 * b + 2 * st;
+          const unsigned char* row = ws + 8192 + r * 128 + 8 * half;
+          const uint2 lo = *reinterpret_cast<const uint2*>(row + ((c ^ swz<64>(r)) << 4));
+          const uint2 hi = *reinterpret_cast<const uint2*>(row + (((c + 1) ^ swz<64>(r)) << 4));
+          fd[j] = u32x4{lo.x, lo.y, hi.x, hi.y};
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const u32x4 fw = rd.tr_frag(ws, b, st, i);
+#pragma unroll
+          for (int j = 0; j < TB; ++j) acc[i][j] = T::mfma(fw, fd[j], acc[i][j]);
+        }
+      }
+  }
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  float* const sums = reinterpret_cast<float*>(own);  // [2 TB * 16][64]
+  static_assert(2 * TB * 4096 <= kStages * kStage, "the wave's sums fit its stages");
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sums[(16 * (i * TB + j) + r) * 64 + lane] = acc[i][j][r];
+  __syncthreads();
+  // four columns of a row at a time: entries 4 g .. 4 g + 3 of block (i, j)
+  for (int q = wave; q < 8 * TB; q += kColumnsWaves) {
+    const int g = q & 3, i = (q >> 2) / TB, j = (q >> 2) % TB;
+    const int c = c0 + 32 * i + 8 * g + 4 * half;
+    const int64_t t = t0 + 32 * j + col;
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kColumnsWaves; ++w)
+        v[e] += reinterpret_cast<const float*>(smem + w * kStages * kStage)[(4 * q + e) * 64 + lane];
+    }
+    if (t < a.n && c < a.k) *reinterpret_cast<f32x4*>(a.part + ((int64_t)part * a.n + t) * a.k + c) = v;
+  }
+}
+
+template <class T, int TB>
+__global__ __launch_bounds__(64 * kColumnsWaves) void columns_kernel(ColumnsArgs a) {
+  columns_few<T, TB>(a);
+}
+
 // ---- transposes ---------------------------------------------------------------------------------
 
 // Up to three matrices [rows, cols] (multiples of 8 columns) in one launch, a 64 x 64 tile per workgroup:
@@ -673,7 +804,50 @@ hipError_t rows(ProductArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <class T, int TB>
+hipError_t columns_as(const ColumnsArgs& a, hipStream_t s) {
+  const auto kernel = columns_kernel<T, TB>;
+  const hipError_t e = allow_lds((const void*)kernel, kColumnsLds<TB>);
+  if (e != hipSuccess) return e;
+  const int64_t grid = (a.k + 63) / 64 * ((a.n + 32 * TB - 1) / (32 * TB)) * a.splits;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kColumnsWaves), kColumnsLds<TB>, s, a);
+  return hipGetLastError();
+}
+
+// Parts of the sum: two rounds of workgroups, of two stages a wave at least.
+int columns_splits(int64_t n, int k, int f) {
+  const int64_t tiles = (k + 63) / 64 * (n <= 32 ? 1 : (n + 63) / 64);
+  int64_t s = 512 / tiles;
+  const int64_t most = (f + 63) / 64 * 2 / (2 * kColumnsWaves);
+  s = s < most ? s : most;
+  return s < 1 ? 1 : (int)s;
+}
+
+template <class T>
+hipError_t columns(ColumnsArgs a, uint16_t* dx, const uint32_t* row_max, hipStream_t s) {
+  a.splits = columns_splits(a.n, a.k, a.f);
+  const hipError_t e = a.n <= 32 ? columns_as<T, 1>(a, s) : columns_as<T, 2>(a, s);
+  if (e != hipSuccess) return e;
+  ProductArgs q = {nullptr, nullptr, a.n, a.k, 0, 0, {dx, nullptr}, a.n, row_max, a.part};
+  q.splits = a.splits;
+  hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)((a.n * a.k / 8 + 255) / 256)), dim3(256), 0, s, q);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+// dx by columns_kernel up to here: %RULE%
+bool gated_by_columns(int64_t n) { return n <= 128; }
+
+size_t gated_columns_bytes(int64_t n, int k, int f) {
+  return (size_t)columns_splits(n, k, f) * n * k * sizeof(float);
+}
+
+hipError_t launch_gated_columns(const ColumnsArgs& a, bool f16, uint16_t* dx, const uint32_t* row_max,
+                                hipStream_t stream) {
+  if (a.n == 0) return hipSuccess;
+  return f16 ? columns<HalfF16>(a, dx, row_max, stream) : columns<HalfBf16>(a, dx, row_max, stream);
+}
 
 // (The tiles are 256 x 128 or 256 x 256 by 512 threads in every call of this size.)
 bool gated_fits(int64_t n, int k, int f, bool grads) {

@@ -413,6 +413,19 @@ struct ProductArgs {
 };
 size_t rows_product_bytes(int64_t n, int m, int k);
 hipError_t launch_rows_product(const ProductArgs& a, bool f16, hipStream_t stream);
+// dx [n, k] of few rows (gated_by_columns) from d [n, 2 f] and the weights [f, k], without a transpose; part: workspace of
+// gated_columns_bytes.  The launcher fills splits.
+struct ColumnsArgs {
+  const uint16_t *d, *wg, *wu;
+  int64_t n;
+  int k, f;
+  float* part;
+  int splits;
+};
+bool gated_by_columns(int64_t n);
+size_t gated_columns_bytes(int64_t n, int k, int f);
+hipError_t launch_gated_columns(const ColumnsArgs& a, bool f16, uint16_t* dx, const uint32_t* row_max,
+                                hipStream_t stream);
 // Up to three transposes out[c][r] = in[r][c] (out null: none) and words to clear, in one launch.  in: rows of
 // in_ld, or a checkpoint's codes and exps, whose values go to plain [rows, cols] too (null: none).  out's rows are
 // zero from `rows` to the next multiple of 8.  cols % 8 == 0.  The launcher fills `blocks` and clear_blocks.
