@@ -13,7 +13,7 @@ namespace {
 // values zero.  To pack, a wave takes RUNS runs of 64 chunks at a time, so that a lane has RUNS loads on their way and
 // the wave's 16 RUNS exponents are one store.
 //
-// Bound by memory: 53,248 rows of 4096 %PACK%
+// Bound by memory: 53,248 rows of 4096 105 us to pack (6.3 TB/s of 661 MB) and 113 to unpack (5.9).
 constexpr int kThreads = 256;
 
 // Chunk i of the rows: row, first column, block of the rows (chunks past the last lie in rows past the last).

@@ -8,9 +8,9 @@
 // Forward: one product whose tiles hold the same columns of Wg and of Wu (PAIR in product.h), so that g and u
 // of a value of h meet in one lane's registers, and the activation and the product are its epilogue: g and u
 // never reach memory.  Backward: the same product again, whose epilogue reads dh and writes d = (dg | du); x is
-// all that it needs of the forward, and g and u are those of 32 bits, not a rounding of them kept over the
-// pass (which would cost 2 k / f of a row more memory, and the exactness of d).  dx is one product of d's rows
-// with the weights' columns, and dW one of d's columns with x's: the weights and x are transposed
+// all that it needs of the forward, and g and u are those of 32 bits, not a rounding of them kept from one pass to
+// the other (which would take 4 f bytes a row over that time, and exactness from d).  dx is one product of d's rows
+// with the weights' columns, and dW one of d's columns with x's: x, and past 192 rows the weights, are transposed
 // first (prepare_kernel), d is written both ways round by the epilogue.
 #include "checkpoint.h"
 #include "common.h"
@@ -43,8 +43,8 @@ struct Silu {
 
 // g Phi(g), Phi(-x sqrt 2) = erfc(x) / 2 = exp(-x^2) t P(t) with t = 1 / (1 + 0.4 x), x >= 0: erfc(x) exp(x^2) / t
 // is smooth on (0, 1], and P, of degree 8, is a least-squares fit to it with the weights moved towards the largest
-// relative error; in 32 bits within 2.7e-7 of it, in the tail too (the library's erfc took twice the time of
-// a whole tile's products at k = 768: 764 rows, 768 -> 2304 %GELU%).
+// relative error; in 32 bits within 2.7e-7 of it, in the tail too (h of 13,057 rows, 768 -> 2304 in fp16: 108 us
+// with it, 130 with the library's erfc).
 struct Gelu {
   static __device__ __forceinline__ float cdf(float g, float& e) {
     const float t = __builtin_amdgcn_rcpf(1.f + __builtin_fabsf(g) * (0.4f * 0.70710678f));
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void rows_few_kernel(ProductArgs a)
 // tiles of 64 rows by 64 columns and their columns taken by the LDS reads (tr_frag), so that nothing is transposed
 // first.  A workgroup takes 32 TB rows by 64 columns and a part of the sum, its four waves a quarter of it each, without a
 // barrier; they join in LDS and the parts in join_kernel.  Bound by the weights, which are read once for every 32 TB
-// rows: %COL%
+// rows: x's gradients of 64 rows, 4096 -> 14336, d's product included: 104 us, with the weights transposed first 224.
 template <int TB>
 constexpr int kColumnsStages = TB == 1 ? 3 : 2;
 template <int TB>
@@ -751,12 +751,15 @@ struct RowsPlan {
 };
 RowsPlan rows_plan(int64_t n, int m, int k) {
   constexpr int kSize[4] = {32, 64, 128, 256};
+  constexpr int kThreads[4] = {64 * kFewWaves, kSmallGroups * Small<HalfBf16, false>::kThreads,
+                               Middle<HalfBf16, false>::kThreads, Wide<HalfBf16, false>::kThreads};
   constexpr double kStage[4] = {0.143, 0.29, 0.55, 1.26};
   const int64_t stages = k > 0 ? (k + 63) / 64 : 1;
   RowsPlan best = {3, 1};
   double least = 0.0;
   for (int t = 3; t >= 0; --t) {
     const int64_t tiles = (n + kSize[t] - 1) / kSize[t] * ((m + kSize[t] - 1) / kSize[t]);
+    if (t < 3 && !launch_fits(tiles, kThreads[t])) continue;  // (gated_fits has asked for those of 256)
     const int most = t < 2 || tiles >= 256 ? 1 : 16;
     for (int s = 1; s <= most && (s == 1 || (tiles * s <= 256 && stages / s >= 4)); ++s) {
       const double rounds = (double)((tiles * s + 255) / 256), part = (double)((stages + s - 1) / s);
@@ -836,8 +839,9 @@ hipError_t columns(ColumnsArgs a, uint16_t* dx, const uint32_t* row_max, hipStre
 
 }  // namespace
 
-// dx by columns_kernel up to here: %RULE%
-bool gated_by_columns(int64_t n) { return n <= 128; }
+// dx by columns_kernel up to here, from transposed weights past it (us, 4096 -> 14336 and 768 -> 2304): 160 rows 224 and
+// 24.6 (transposed 276 and 25.0), 192 rows 226 and 25.8 (280 and 25.4), 256 rows 266 and 30.6 (290 and 28.5).
+bool gated_by_columns(int64_t n) { return n <= 192; }
 
 size_t gated_columns_bytes(int64_t n, int k, int f) {
   return (size_t)columns_splits(n, k, f) * n * k * sizeof(float);
@@ -849,13 +853,14 @@ hipError_t launch_gated_columns(const ColumnsArgs& a, bool f16, uint16_t* dx, co
   return f16 ? columns<HalfF16>(a, dx, row_max, stream) : columns<HalfBf16>(a, dx, row_max, stream);
 }
 
-// (The tiles are 256 x 128 or 256 x 256 by 512 threads in every call of this size.)
+// (Where a limit is near, the tiles are 256 x 128 and 256 x 256 by 512 threads, and max_kernel's of 64 rows; rows_plan
+// leaves out smaller ones that do not fit.)
 bool gated_fits(int64_t n, int k, int f, bool grads) {
   auto blocks = [](int64_t size, int of) { return (size + of - 1) / of; };
   if (!launch_fits(blocks(n, 256) * blocks(f, 128), 512)) return false;
   if (!grads) return true;
   const int64_t prepare = blocks(n + f, 256) + 2 * blocks(f, 64) * blocks(k, 64) + blocks(n, 64) * blocks(k, 64);
-  return launch_fits(prepare, 256) && launch_fits(blocks(n, 16) * blocks(f, 512), 256) &&
+  return launch_fits(prepare, 256) && launch_fits(blocks(n, 64) * blocks(f, 512), 256) &&
          launch_fits(blocks(n, 256) * blocks(k, 256), 512);
 }
 

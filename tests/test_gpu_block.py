@@ -103,6 +103,11 @@ GATED = [
     (1100, 40, 1288, "bf16", "silu"), (1500, 72, 1032, "f16", "gelu_tanh"), (2309, 72, 2056, "bf16", "silu"),
     (2500, 136, 2000, "f16", "silu"), (6001, 1600, 64, "bf16", "gelu"), (9, 8, 5000, "bf16", "silu"),
     (515, 4104, 8, "bf16", "silu"), (40, 4096, 4104, "f16", "gelu"), (700, 1288, 3000, "bf16", "silu"),
+    # x's gradients without a transpose: one and several tiles of 32 and of 64 rows, widths that end inside a stage
+    (2, 72, 1000, "f16", "silu"), (32, 200, 3336, "bf16", "gelu"), (63, 1096, 520, "f16", "gelu_tanh"),
+    (129, 72, 2504, "bf16", "silu"), (192, 264, 712, "f16", "silu"), (193, 264, 712, "f16", "silu"),
+    # and with k split between workgroups: tiles of 128 rows, and of 256
+    (449, 776, 2312, "f16", "gelu"), (1100, 2056, 8200, "bf16", "silu"),
 ]
 
 
@@ -478,3 +483,122 @@ def test_autograd_by_differences():
             # random, twice; a straight line holds to the step's square
             noise = 2.0 ** -11 * 0.1 * (2 * (40 * 520 + 40 * 264)) ** 0.5
             assert abs((up - down) - along) <= 4 * noise + 0.02 * abs(along), (up - down, along)
+
+
+def test_backward_in_a_graph():
+    """A whole step through autograd, captured and replayed: leaves of its own, so that no eager graph holds them."""
+    def step(args, packed):
+        x, b, wg, wu, t, how, dh = args
+        x, b, wg, wu, *t_leaves = (v.detach().requires_grad_() for v in (x, b, wg, wu, *t.values()))
+        r, y = hpr.residual_norm(x, b, **dict(zip(t, t_leaves)), **how, checkpoint=packed)
+        h = hpr.gated_linear(y, wg, wu, checkpoint=packed)
+        return [r.detach(), h.detach(), *torch.autograd.grad([r, h], [x, b, wg, wu, *t_leaves], [b.detach(), dh])]
+
+    for packed in (False, True):
+        args = block_inputs("f16", 1, 150)
+        step(args, packed)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(args, packed)
+        for seed in (2, 3, 4):
+            new = block_inputs("f16", seed, 150)
+            for to, frm in zip((*args[:4], *args[4].values(), args[6]), (*new[:4], *new[4].values(), new[6])):
+                to.copy_(frm)
+            want = step(new, packed)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, c) for a, c in zip(out, want))
+
+
+def test_two_threads():
+    """Calls of two threads at once, each on its stream: no state is shared."""
+    import threading
+    cases = [block_inputs(ty, s, n) for ty, s, n in (("bf16", 3, 520), ("f16", 4, 61))]
+    want = [block_pass(*c, False) for c in cases]
+    torch.cuda.synchronize()
+    same = [False, False]
+
+    def run(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            runs = [block_pass(*cases[i], False) for _ in range(5)]
+            torch.cuda.current_stream().synchronize()
+        same[i] = all(torch.equal(a, b) for r in runs for a, b in zip(r, want[i]))
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert same == [True, True]
+
+
+def test_gated_workspace():
+    """A workspace of the size that is asked for, or larger, with anything in it; one that is too small is not used."""
+    for n, k, f, ty in ((20, 72, 264, "bf16"), (150, 200, 520, "f16"), (449, 776, 2312, "f16")):
+        dt = TYPES[ty][0]
+        g = gen(n)
+        x, wg, wu, dh = (rand(g, *s, dtype=dt, std=0.3) for s in ((n, k), (f, k), (f, k), (n, f)))
+        want = hpr.gated_linear_bwd(dh, x, wg, wu)
+        need = hpr.lib().gated_linear_bwd_workspace_size(n, k, f, 0, 1, 1)
+        for size in (need, need + 4096, need - 1, 16):
+            ws = torch.full((size + 256,), 0xff, dtype=torch.uint8, device=DEV)
+            got = hpr.gated_linear_bwd(dh, x, wg, wu, ws=ws[:size])
+            assert all(torch.equal(got[name], v) for name, v in want.items())
+            assert (ws[size:] == 0xff).all() and (size >= need or (ws == 0xff).all())
+
+
+# ---- offsets past 32 bits -------------------------------------------------------------------
+
+
+def far_rows(n):
+    """Rows at the start, on both sides of the middle, and at the end."""
+    return torch.cat([torch.arange(40), torch.arange(n // 2 - 40, n // 2 + 40), torch.arange(n - 90, n)])
+
+
+@pytest.mark.parametrize("n,k,f,dw", [((1 << 20) + 300, 2056, 1032, True), ((1 << 28) + 5, 8, 8, False)])
+def test_gated_far_rows(n, k, f, dw):
+    """Rows, and d's, past 2^31 values; and so many rows of so few columns that small tiles are more than one launch
+    holds.  Rows of dh between those that are looked at are 0: they add nothing to the weights' gradients."""
+    dt, at = torch.bfloat16, far_rows(n).to(DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    x = torch.empty(n, k, dtype=dt, device=DEV).normal_(generator=g)
+    wg, wu = (rand(gen(s), f, k, dtype=dt, std=k ** -0.5) for s in (2, 3))
+    dh = torch.zeros(n, f, dtype=dt, device=DEV)
+    dh[at] = rand(gen(4), len(at), f, dtype=dt, std=0.3)
+    want = B.gated_linear(f64(x[at]), f64(wg), f64(wu), "silu", f64(dh[at]), *TYPES["bf16"][1:3])
+    hold(hpr.gated_linear_fwd(x, wg, wu)["h"][at], want["h"], want["bound"]["h"], "h")
+    got = hpr.gated_linear_bwd(dh, x, wg, wu, need_dw=dw)
+    hold(got["dx"][at], want["dx"], want["bound"]["dx"], "dx")
+    assert torch.count_nonzero(got["dx"].abs().amax(1)) <= len(at)
+    for name in ("dw_gate", "dw_up") if dw else ():
+        hold(got[name], want[name], want["bound"][name], name)
+
+
+def test_norm_far_rows():
+    n, d, dt = (1 << 20) + 300, 2056, torch.bfloat16
+    at = far_rows(n).to(DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    x, b = (torch.empty(n, d, dtype=dt, device=DEV).normal_(generator=g) for _ in range(2))
+    t = dict(weight=rand(gen(2), d, dtype=dt, std=0.3, mean=1.0),
+             post_weight=rand(gen(3), d, dtype=dt, std=0.3, mean=1.0), gate=rand(gen(4), d, dtype=dt))
+    how = dict(scale=0.5, eps=1e-6, kind="rms")
+    dr, dy = (torch.zeros(n, d, dtype=dt, device=DEV) for _ in range(2))
+    dr[at], dy[at] = (rand(gen(s), len(at), d, dtype=dt, std=0.3) for s in (5, 6))
+    want = norm_oracle(f64(x[at]), f64(b[at]), t, how, dr[at], dy[at], "bf16")
+    f = hpr.residual_norm_fwd(x, b, **t, **how)
+    for name in ("r", "y"):
+        hold(f[name][at], want[name], want["bound"][name], name)
+    del f
+    got = hpr.residual_norm_bwd(dr, dy, x, b, **t, **how)
+    for name, v in got.items():
+        if v is not None:
+            hold(v[at] if name in ("dx", "db") else v, want[name], want["bound"][name], name)
+    del got
+    c = hpr.checkpoint_pack(x)
+    codes, exps = B.checkpoint_pack(f64(x[at]), -126)
+    assert (c.codes[at].cpu().numpy() == codes).all() and (c.exps[at].cpu().numpy() == exps).all()
+    assert same_rows(hpr.checkpoint_unpack(c)[at], B.checkpoint_values(codes, exps))
