@@ -131,6 +131,9 @@ __device__ __forceinline__ void statistics(const float (&v)[C][8], const bool (&
   rs = __builtin_amdgcn_rsqf(s[0] * inv_d + eps);
 }
 
+// A row per W waves, read once: x and b in, r and y out.  Bound by memory: 53,248 rows of 4096 (1.74 GB) 296 us, 5.9 TB/s
+// (304 with stores that stay in the caches; with 13,057 rows, whose inputs still lie in the last cache, 60 and 82).  Small
+// calls wait for two dependent sums: 64 rows 4.5 us.
 template <class T, bool LAYER, int W, int C>
 __global__ __launch_bounds__((Layout<W, C>::kThreads)) void norm_fwd_kernel(NormArgs a) {
   typedef Layout<W, C> L;
@@ -166,7 +169,7 @@ __global__ __launch_bounds__((Layout<W, C>::kThreads)) void norm_fwd_kernel(Norm
       vector8<T>(a.gate, (a.gate_rows ? row * a.d : 0) + col[c], 1.f, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) r[c][i] += a.scale * g[i] * ((b[c][i] - mean) * rs * w[i] + o[i]);
-      if (a.r) *reinterpret_cast<u32x4*>(a.r + row * a.d + col[c]) = narrow<T>(r[c]);
+      if (a.r) store16_stream(a.r + row * a.d + col[c], narrow<T>(r[c]));
     }
   }
   if (a.y) {
@@ -180,7 +183,7 @@ __global__ __launch_bounds__((Layout<W, C>::kThreads)) void norm_fwd_kernel(Norm
       vector8<T>(LAYER ? a.c : nullptr, col[c], 0.f, o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = (r[c][i] - mean) * rs * w[i] + o[i];
-      *reinterpret_cast<u32x4*>(a.y + row * a.d + col[c]) = narrow<T>(y);
+      store16_stream(a.y + row * a.d + col[c], narrow<T>(y));
     }
   }
 }
@@ -190,6 +193,10 @@ __global__ __launch_bounds__((Layout<W, C>::kThreads)) void norm_fwd_kernel(Norm
 //   without s and t.
 // The next row is on its way while one is worked on, and the vectors stay in registers, where there is room for
 // them (C = 1).
+//
+// Bound by memory, with vector instructions for two fifths of the time: 53,248 rows of 4096 (2.6 GB) 525 to 540 us, 4.9 TB/s
+// (a copy reaches 5.1), from checkpoints 475.  More waves a row, not more chunks a lane: two rows' tensors and the sums
+// fill the registers of C = 1.
 //
 // Rows are read and written through buffers of their own length, 0 for what there is not: values past the row, rows
 // past the last and tensors that are not there read as zeros and are not written, without a branch (with masks and
@@ -204,7 +211,7 @@ __device__ __forceinline__ u32x4 read16(__amdgpu_buffer_rsrc_t r, int at) {
 }
 __device__ __forceinline__ void write16(__amdgpu_buffer_rsrc_t r, int at, u32x4 v) {
   typedef unsigned int v4u __attribute__((ext_vector_type(4)));
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), r, at, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), r, at, 0, 2);  // nt, as store16_stream
 }
 
 template <int C>
@@ -445,7 +452,8 @@ __global__ __launch_bounds__((Layout<W, C>::kThreads), W == 8 ? 4 : 1) void norm
 }
 
 // The workgroups' sums of 16 columns, in their order within 64 runs of workgroups, then over the runs; and the
-// gradients that come of them.
+// gradients that come of them.  Reads 8 or 16 bytes a column and workgroup of the gradients' kernel: 4096 columns of 512
+// workgroups (17 MB) 10 us, most of it the start and the reads' latency.
 template <class T, bool LAYER>
 __global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a) {
   constexpr int kSums = LAYER ? 4 : 2;
