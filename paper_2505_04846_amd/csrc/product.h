@@ -336,8 +336,8 @@ struct TileProduct16 {
   static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k, int nk,
                                              TileAt tile, unsigned char* smem, int wave, int lane, Acc& acc) {
     const int wt = wave % WT, wm = wave / WT;
-    const TileLoad<64, BT, kW> lx(wave, lane, 8);
-    const TileLoad<64, BM, kW> lw(wave, lane, 8);
+    const TileLoad<64, BT, kW, true> lx(wave, lane, 8);
+    const TileLoad<64, BM, kW, true> lw(wave, lane, 8);
     const __amdgpu_buffer_rsrc_t rx = tile_rsrc(xb), rw0 = tile_rsrc(w.w[0]), rw1 = tile_rsrc(w.w[PAIR]);
     // the eight rows of a wave load are of one half of a wave's rows
     auto second = [&](int j) { return PAIR && (wave * kLw + j) * 8 % (BM / WM) >= kWaveCols; };
@@ -400,7 +400,7 @@ struct TileProduct16 {
       touch = lane < 8 ? (const char*)w.w[up] + (int64_t)in_w * w.ld * 2 : (const char*)xb + (int64_t)of_x * ldx * 2;
     }
     // chunk 4 s + lane / 16 of row lane % 16 of a block of 16 rows, of k-step s
-    const int r = lane & 15, at0 = r * 128 + (((lane >> 4) ^ swz<64>(r)) << 4);
+    const int r = lane & 15, at0 = r * 128 + (((lane >> 4) ^ swz16(r)) << 4);
     const unsigned char* const own_x = smem + wt * kT * 2048;
     const unsigned char* const own_w = ring_w + wm * kM * 2048;
     auto read = [&](int slot_x, int slot_w, int s, Frags& f, int b) __attribute__((always_inline)) {

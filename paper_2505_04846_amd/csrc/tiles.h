@@ -16,6 +16,12 @@ __device__ __forceinline__ int swz(int r) {
   return D >= 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
+// The same of rows of 64 values that are read 16 at a time, each in the four chunks of half a row by lanes 16 apart
+// (operands of 16x16x32 products).  Of such a read LDS serves in a cycle rows 0-3 and 12-15 of one chunk with rows 4-11
+// of its neighbour: with swz, which is for 32 rows of one chunk, each would take two (3 million cycles of conflicts in
+// 13,063 rows, 4096 -> 14336, with swz 291 million, half of the reads' time).
+__device__ __forceinline__ int swz16(int r) { return (r >> 1) & 7; }
+
 // Offsets of a lane's reads from an LDS tile.
 template <int D>
 struct TileReads {
@@ -113,7 +119,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const void* base) {
 // Loads a tile of ROWS rows of D values straight into LDS, NW waves sharing it: every wave load
 // fills 1 KiB.  Rows past the last valid one repeat it, chunks past the row's `chunks` repeat the
 // last (the products' other operand is zero there).
-template <int D, int ROWS, int NW>
+template <int D, int ROWS, int NW, bool BY16 = false>
 struct TileLoad {
   static constexpr int kCh = D / 8;                       // chunks of a row
   static constexpr int kRows = 64 / kCh;                  // rows of a wave load
@@ -124,7 +130,7 @@ struct TileLoad {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       row[j] = (wave * kLoads + j) * kRows + lane / kCh;
-      const int c = (lane % kCh) ^ swz<D>(row[j]);
+      const int c = (lane % kCh) ^ (BY16 ? swz16(row[j]) : swz<D>(row[j]));
       chunk[j] = (c < chunks ? c : chunks - 1) * 16;
     }
   }
