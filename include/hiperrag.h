@@ -515,9 +515,9 @@ hpr_status gated_linear_fwd(const uint16_t* x, int64_t x_row, int64_t n, int32_t
  *   dh [n, f] dense; x [n, k] with row stride x_row or, with x_exps, checkpoint_pack's codes (dense; the
  *   gradients are those at the values that they stand for); dx [n, k] and dw_gate, dw_up [f, k], dense; dx, or
  *   dw_gate and dw_up together, may be NULL
- *   ws     workspace of gated_linear_bwd_workspace_size(...) bytes: transposed operands, dg and du each way that
- *          is needed (8 n f bytes for both), partial sums; packed, need_dx, need_dw: 0 or 1.  (Other sizes take
- *          other ways: more rows may need less.)  With dw_gate and dw_up n is at most 2^21
+ *   ws     workspace of gated_linear_bwd_workspace_size(...) bytes: dg and du each way that is needed (8 n f bytes
+ *          for both), a checkpoint's rows, partial sums (of few rows, so that more rows may need less); packed,
+ *          need_dx, need_dw: 0 or 1.  With dw_gate and dw_up n is at most 2^21
  * ------------------------------------------------------------------------------------------- */
 size_t gated_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t f, int32_t packed, int32_t need_dx,
                                        int32_t need_dw);
@@ -602,7 +602,7 @@ hpr_status hpr_read_calibration(const void* buf, int64_t bytes, uint32_t* sink, 
  * stored), "dense_scan", "dense_merge", "dense_fallback", "semantic_chunk", "retrieval_metrics",
  * "attn_fwd" and "attn_bwd" (all launches of a call), "adapter_shrink", "adapter_expand",
  * "adapter_transpose", "adapter_outer", "rotary", "checkpoint", "gated" (h, or dg and du),
- * "gated_prepare" (the gradients' transposes, and fp16's maxima), "gated_product" (dx, dw_gate and
+ * "gated_prepare" (a checkpoint's rows, and fp16's maxima), "gated_product" (dx, dw_gate and
  * dw_up), "norm_fwd", "norm_bwd", "mfma_calibration", "read_calibration"), returns the sum of their
  * durations in milliseconds and the launch count (0 and 0 for any other name, such as "pool", which
  * is no launch of its own any more), and forgets them. */

@@ -449,7 +449,7 @@ hpr_status check_gated(int64_t n, int32_t k, int32_t f, int64_t x_row, int32_t a
 
 // Where the pieces of the gradients' workspace lie.
 struct GatedCarve {
-  uint16_t *wt, *d, *dt, *xt, *plain;
+  uint16_t *d, *dt, *plain;
   uint32_t* words;  // maxima of rows, then of columns
   float* part;      // of one product after the other
   size_t bytes;
@@ -463,15 +463,12 @@ GatedCarve gated_carve(void* ws, int64_t n, int32_t k, int32_t f, bool packed, b
     g.bytes += align_up(bytes);
     return p;
   };
-  const bool columns = gated_by_columns(n);
-  if (need_dx && !columns) g.wt = reinterpret_cast<uint16_t*>(take((size_t)k * 2 * f * 2));
   if (need_dx) g.d = reinterpret_cast<uint16_t*>(take((size_t)n * 2 * f * 2));
   if (need_dw) g.dt = reinterpret_cast<uint16_t*>(take(np * 2 * f * 2));
-  if (need_dw) g.xt = reinterpret_cast<uint16_t*>(take(np * k * 2));
   if (packed) g.plain = reinterpret_cast<uint16_t*>(take((size_t)n * k * 2));
   g.words = reinterpret_cast<uint32_t*>(take(((size_t)n + f) * sizeof(uint32_t)));
-  const size_t of_dx = !need_dx ? 0 : columns ? gated_columns_bytes(n, k, f) : rows_product_bytes(n, k, 2 * f);
-  const size_t of_dw = need_dw ? rows_product_bytes(2 * (int64_t)f, k, (int)np) : 0;
+  const size_t of_dx = need_dx ? rows_product_bytes(n, k, 2 * f) : 0;
+  const size_t of_dw = need_dw ? rows_product_bytes(2 * (int64_t)f, k, (int)n) : 0;
   g.part = reinterpret_cast<float*>(take(of_dx > of_dw ? of_dx : of_dw));
   return g;
 }
@@ -992,7 +989,7 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
   if (!dw_gate != !dw_up)
     return fail(HPR_ERR_INVALID_ARG, "dw_gate and dw_up are computed together: both or neither");
   const bool need_dx = dx != nullptr, need_dw = dw_gate != nullptr;
-  if (!gated_fits(n, k, f, true) || (need_dw && n > (int64_t(1) << 21)))
+  if (!gated_fits(n, k, f, true) || (packed && !checkpoint_fits(n, k)) || (need_dw && n > (int64_t(1) << 21)))
     return fail(HPR_ERR_UNSUPPORTED_SHAPE, "%lld rows of %d are more than the gradients' launches hold", (long long)n,
                 f);
   if (n > 0 && !dh) return fail(HPR_ERR_INVALID_ARG, "dh must be non-NULL");
@@ -1004,32 +1001,24 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
     return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, g.bytes);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t np = (n + 7) / 8 * 8;
-  uint32_t *const row_max = g.words, *const col_max = g.words + n;
+  const uint16_t* const rows = packed ? g.plain : static_cast<const uint16_t*>(x);
+  const int64_t row = packed ? k : x_row;
+  const uint32_t *const row_max = g.words, *const col_max = g.words + n;
   hipError_t e = hipSuccess;
   if (n > 0) {
-    const uint16_t* const x16 = packed ? nullptr : static_cast<const uint16_t*>(x);
-    const int8_t* const codes = packed ? static_cast<const int8_t*>(x) : nullptr;
-    GatedPrepare p = {};
-    if (g.wt) {
-      p.job[0] = {w_gate, k, nullptr, nullptr, f, k, g.wt, 2 * (int64_t)f, nullptr, 0};
-      p.job[1] = {w_up, k, nullptr, nullptr, f, k, g.wt + f, 2 * (int64_t)f, nullptr, 0};
-    }
-    if (need_dw || packed) p.job[2] = {x16, x_row, codes, x_exps, n, k, g.xt, np, g.plain, 0};
-    if (narrow) {
-      p.clear = g.words;
-      p.words = n + f;
-    }
-    e = timed("gated_prepare", s, [&] {
-      hipError_t q = launch_gated_prepare(p, narrow, s);
-      if (q == hipSuccess && narrow) q = launch_gated_max(dh, n, f, row_max, col_max, s);
-      return q;
-    });
+    if (packed || narrow)
+      e = timed("gated_prepare", s, [&] {
+        hipError_t q = hipSuccess;
+        if (packed) q = launch_checkpoint_unpack(static_cast<const int8_t*>(x), x_exps, n, k, narrow, g.plain, s);
+        if (q == hipSuccess && narrow) q = launch_gated_max(dh, n, f, g.words, s);
+        return q;
+      });
     GatedArgs a = {};
-    a.x = packed ? g.plain : x16;
+    a.x = rows;
     a.wg = w_gate;
     a.wu = w_up;
     a.n = n;
-    a.x_ld = packed ? k : x_row;
+    a.x_ld = row;
     a.k = k;
     a.f = f;
     a.act = act;
@@ -1044,14 +1033,13 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
   }
   if (e == hipSuccess && need_dx && n > 0)
     e = timed("gated_product", s, [&] {
-      if (gated_by_columns(n))
-        return launch_gated_columns({g.d, w_gate, w_up, n, k, f, g.part, 0}, narrow, dx, row_max, s);
-      const ProductArgs q = {g.d, g.wt, n, k, 2 * f, 2 * f, {dx, nullptr}, n, row_max, g.part};
+      const ProductArgs q = {g.d, 2 * f, {w_gate, w_up}, k, f, n, k, 2 * f, {dx, nullptr}, n, row_max, g.part};
       return launch_rows_product(q, narrow, s);
     });
   if (e == hipSuccess && need_dw)  // (without a row the sums are empty, and the product writes zeros)
     e = timed("gated_product", s, [&] {
-      const ProductArgs q = {g.dt, g.xt, 2 * (int64_t)f, k, (int)np, (int)np, {dw_gate, dw_up}, f, col_max, g.part};
+      const ProductArgs q = {g.dt, (int)np, {rows, rows}, (int)row, (int)np, 2 * (int64_t)f, k, (int)n, {dw_gate, dw_up}, f,
+                             col_max, g.part};
       return launch_rows_product(q, narrow, s);
     });
   return e == hipSuccess ? HPR_OK : hip_fail(e, "gated gradient launch");

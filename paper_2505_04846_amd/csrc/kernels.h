@@ -395,15 +395,18 @@ struct GatedArgs {
 hipError_t launch_gated(const GatedArgs& a, bool grad, hipStream_t stream);
 // Whether every launch of the forward, or of the gradients, is one that can be made (launch_fits).
 bool gated_fits(int64_t n, int k, int f, bool grads);
-// Largest magnitudes (as fp16 bits) of dh's rows and columns, into zeroed words.
-hipError_t launch_gated_max(const uint16_t* dh, int64_t n, int f, uint32_t* rows, uint32_t* cols,
-                            hipStream_t stream);
-// y = x w^T of x [n, k] and w [m, k], both with rows of ld: rows [0, split) to y[0], the others to y[1] (rows of
-// m).  In fp16 row r is divided by the power of two of max_bits[r], or [r - split].
+// Largest magnitudes (as fp16 bits) of dh's rows and columns, into words [n + f].
+hipError_t launch_gated_max(const uint16_t* dh, int64_t n, int f, uint32_t* words, hipStream_t stream);
+// y = x w of x [n, k] with rows of ld and w [k, m] with rows of w_ld, whose rows from `half` on are w[1]'s: rows
+// [0, split) of y to y[0], the others to y[1] (rows of m).  In fp16 row r is divided by the power of two of
+// max_bits[r], or [r - split].  x's values from k to the next multiple of 8 are zero.
 struct ProductArgs {
-  const uint16_t *x, *w;
+  const uint16_t* x;
+  int ld;
+  const uint16_t* w[2];
+  int w_ld, half;
   int64_t n;
-  int m, k, ld;
+  int m, k;
   uint16_t* y[2];
   int64_t split;
   const uint32_t* max_bits;
@@ -413,41 +416,6 @@ struct ProductArgs {
 };
 size_t rows_product_bytes(int64_t n, int m, int k);
 hipError_t launch_rows_product(const ProductArgs& a, bool f16, hipStream_t stream);
-// dx [n, k] of few rows (gated_by_columns) from d [n, 2 f] and the weights [f, k], without a transpose; part: workspace of
-// gated_columns_bytes.  The launcher fills splits.
-struct ColumnsArgs {
-  const uint16_t *d, *wg, *wu;
-  int64_t n;
-  int k, f;
-  float* part;
-  int splits;
-};
-bool gated_by_columns(int64_t n);
-size_t gated_columns_bytes(int64_t n, int k, int f);
-hipError_t launch_gated_columns(const ColumnsArgs& a, bool f16, uint16_t* dx, const uint32_t* row_max,
-                                hipStream_t stream);
-// Up to three transposes out[c][r] = in[r][c] (out null: none) and words to clear, in one launch.  in: rows of
-// in_ld, or a checkpoint's codes and exps, whose values go to plain [rows, cols] too (null: none).  out's rows are
-// zero from `rows` to the next multiple of 8.  cols % 8 == 0.  The launcher fills `blocks` and clear_blocks.
-struct GatedTranspose {
-  const uint16_t* in;
-  int64_t in_ld;
-  const int8_t* codes;
-  const uint8_t* exps;
-  int64_t rows;
-  int cols;
-  uint16_t* out;
-  int64_t ld;
-  uint16_t* plain;
-  uint32_t blocks;
-};
-struct GatedPrepare {
-  GatedTranspose job[3];
-  uint32_t* clear;
-  int64_t words;
-  uint32_t clear_blocks;
-};
-hipError_t launch_gated_prepare(GatedPrepare a, bool f16, hipStream_t stream);
 
 // Rows in 8 bits (checkpoint.hip): codes [n, d] and exps [n, ceil(d / 32)] of x [n, d] with rows of x_ld, and back.
 hipError_t launch_checkpoint_pack(const uint16_t* x, int64_t x_ld, int64_t n, int d, bool f16, int8_t* codes,

@@ -23,6 +23,18 @@ struct PanelW {
   int last;              // last valid row, which the rows past it repeat
 };
 
+// A right operand by columns: value c of k is row c of w[0] below `half`, row c - half of w[1] from there; the tile's
+// columns begin at those rows' own.
+struct PanelT {
+  const uint16_t* w[2];
+  int ld;           // elements from a row to the next
+  int last;         // last valid column, whose chunk of 8 the chunks past it repeat
+  int first, half;  // k begins at value `first`
+  __device__ __forceinline__ const uint16_t* row(int c) const {
+    return c < half ? w[0] + (int64_t)c * ld : w[1] + (int64_t)(c - half) * ld;
+  }
+};
+
 // ---- a wave's own product ----------------------------------------------------------------------
 
 // acc[b][c] = rows [32 b, 32 b + 32) of P times rows [32 c, + 32) of X, over stages [kk0, kk1) of 64 values,
@@ -313,6 +325,13 @@ __device__ __forceinline__ TileAt tile_at(uint32_t block, uint32_t blocks, uint3
 // columns' panel, and each touches a quarter of its rows' lines, as the eight column tiles do an eighth of the
 // rows'.  (Zeros as operands 1,990 -> 1,745 us, 13,063 rows, 4096 -> 14336; the gradients of 6,529 rows 4,010 ->
 // 3,890; on random operands the forward is at the power limit without it.)
+//
+// W by columns (PanelT): a stage is 64 rows of BM values, and the matrix cores' operands, eight rows of a column a
+// lane, are read with two transposing reads.  Such a read takes 32 bytes of eight rows a cycle (four, and the four
+// that are eight or so further): their chunks are placed (by_rows) so that these are all of the banks.  Its loads are
+// written out (load_lds16): before a transposing read the compiler waits for every load to LDS that it knows of (x's
+// gradients of 6,529 rows, 4096 -> 14336 3,450 us, without the waits 2,393).  It touches no lines ahead: the touched
+// value's wait would be for all of those loads too.
 template <class T, int BT, int BM, int WT, int WM, int NX, int NW, bool PAIR = false>
 struct TileProduct16 {
   static constexpr int kW = WT * WM;
@@ -323,6 +342,9 @@ struct TileProduct16 {
   static constexpr int kCols = PAIR ? BM / 2 : BM;            // columns of the output
   static constexpr int kWaveCols = kCols / WM;
   static constexpr int kThreads = 64 * kW, kRows = BT, kWt = WT;
+  static __device__ __forceinline__ int in_stage(int load, int lane) {  // row of a lane's chunk, by columns
+    return load * (512 / BM) + lane / (BM / 8);
+  }
   static constexpr int kTouch = BT == 256 && BM == 256 && kW == 8 ? 4 : 0;  // (0: none)
   static_assert(!PAIR || kM % 2 == 0, "a wave holds both halves of its columns");
   static_assert(NW >= 2 && (NX == NW || NX == NW + 1) && kLds <= 160 * 1024, "the waits below");
@@ -331,10 +353,17 @@ struct TileProduct16 {
     u32x4 x[kT], w[kM];
   };
 
+  // Chunk c of row r of a stage by columns is stored at position c ^ by_rows(r) of its row.
+  static __device__ __forceinline__ int by_rows(int r) { return ((r & 3) | (((r >> 3) ^ (r >> 4)) & 1) << 2) << 1; }
+
   // x: first row of the tile, of k values.  nk: stages, at least k / 64 (groups of waves that split k call this
   // with the same number, because of its barriers).  LDS is free for the caller when this returns.
-  static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const PanelW& w, int k, int nk,
+  template <class Panel>
+  static __device__ __forceinline__ void run(const uint16_t* xb, int ldx, int last_t, const Panel& w, int k, int nk,
                                              TileAt tile, unsigned char* smem, int wave, int lane, Acc& acc) {
+    constexpr bool kByCols = std::is_same<Panel, PanelT>::value;
+    static_assert(!kByCols || (!PAIR && BM >= 128), "by_rows needs 16 chunks a row");
+    constexpr int kTouches = kByCols ? 0 : kTouch;
     const int wt = wave % WT, wm = wave / WT;
     const TileLoad<64, BT, kW, true> lx(wave, lane, 8);
     const TileLoad<64, BM, kW, true> lw(wave, lane, 8);
@@ -346,10 +375,21 @@ struct TileProduct16 {
     for (int j = 0; j < kLx; ++j) ox[j] = (lx.row[j] < last_t ? lx.row[j] : last_t) * ldx * 2 + lx.chunk[j];
 #pragma unroll
     for (int j = 0; j < kLw; ++j) {
+      if constexpr (kByCols) {
+        constexpr int kCh = BM / 8;
+        const int r = in_stage(wave * kLw + j, lane), c = (lane % kCh) ^ by_rows(r), last = w.last / 8;
+        ow[j] = r * w.ld * 2 + (c < last ? c : last) * 16;
+        continue;
+      }
       const int row = PAIR ? lw.row[j] / (BM / WM) * kWaveCols + lw.row[j] % kWaveCols : lw.row[j];
       ow[j] = (row < w.last ? row : w.last) * w.ld * 2 + lw.chunk[j];
     }
-    const int nk_full = k / 64;
+    // stages that lie inside k, and (by columns) in one matrix, which those before the first that does not do
+    int nk_full = k / 64;
+    if constexpr (kByCols) {
+      const int left = w.half - w.first;
+      if (left > 0 && left % 64 != 0 && left / 64 < nk_full) nk_full = left / 64;
+    }
     unsigned char* const ring_w = smem + NX * kX;
     // Load j of x's or W's stage kk into slot `slot` of its ring.  Chunks past the end of k read zeros, so past the
     // last stage too (the rings keep their numbers of loads in flight); WHOLE: the stage lies inside k.
@@ -357,18 +397,28 @@ struct TileProduct16 {
       unsigned char* to;
       if constexpr (of_x()) to = smem + slot * kX + (wave * kLx + j) * 1024;
       else to = ring_w + slot * kStageW + (wave * kLw + j) * 1024;
-      if constexpr (whole()) {
+      if constexpr (kByCols && whole()) {
+        const uint32_t at = (uint32_t)(uintptr_t)(lds_void_t*)to;
+        if constexpr (of_x()) load_lds16(rsrc_of(xb), at, (uint32_t)(ox[j] + kk * 128));
+        else if constexpr (kByCols) load_lds16(rsrc_of(w.row(w.first + kk * 64)), at, (uint32_t)ow[j]);
+      } else if constexpr (whole()) {
         if constexpr (of_x())
           __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void_t*)to, 16, ox[j], kk * 128, 0, 0);
         else
           __builtin_amdgcn_raw_ptr_buffer_load_lds(second(j) ? rw1 : rw0, (lds_void_t*)to, 16, ow[j], kk * 128, 0, 0);
       } else {
-        const char* from;
-        int chunk;
-        if constexpr (of_x()) from = (const char*)xb + ox[j], chunk = lx.chunk[j];
-        else from = (const char*)w.w[second(j)] + ow[j], chunk = lw.chunk[j];
-        const void* p = kk * 64 + chunk / 2 < k ? (const void*)(from + kk * 128) : (const void*)kZero16;
-        __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)to, 16, 0, 0);
+        const void* p = nullptr;
+        if constexpr (of_x()) {
+          p = kk * 64 + lx.chunk[j] / 2 < k ? (const void*)((const char*)xb + ox[j] + kk * 128) : (const void*)kZero16;
+        } else if constexpr (kByCols) {
+          const int r = in_stage(wave * kLw + j, lane), c = kk * 64 + r;
+          p = c < k ? (const void*)((const char*)w.row(w.first + c) + (ow[j] - r * w.ld * 2)) : (const void*)kZero16;
+        } else {
+          p = kk * 64 + lw.chunk[j] / 2 < k ? (const void*)((const char*)w.w[second(j)] + ow[j] + kk * 128)
+                                            : (const void*)kZero16;
+        }
+        if constexpr (kByCols) load_lds16(p, (uint32_t)(uintptr_t)(lds_void_t*)to);
+        else __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)to, 16, 0, 0);
       }
     };
     auto load_all = [&](auto of_x, int slot, int kk) __attribute__((always_inline)) {
@@ -391,7 +441,7 @@ struct TileProduct16 {
     // lines to touch: of eight rows of W in the first lanes, of four of x in the next, and those again
     const char* touch = nullptr;
     uint32_t touched = 0;
-    if constexpr (kTouch > 0) {
+    if constexpr (kTouches > 0) {
       auto row_of = [](int row, int last) { return row < last ? row : last; };
       const int of_w = (int)(tile.t & 3u) * 64 + wave * 8 + (lane & 7);
       const int of_x = row_of((tile.m & 7) * 32 + wave * 4 + (lane & 3), last_t);
@@ -402,11 +452,22 @@ struct TileProduct16 {
     // chunk 4 s + lane / 16 of row lane % 16 of a block of 16 rows, of k-step s
     const int r = lane & 15, at0 = r * 128 + (((lane >> 4) ^ swz16(r)) << 4);
     const unsigned char* const own_x = smem + wt * kT * 2048;
-    const unsigned char* const own_w = ring_w + wm * kM * 2048;
+    const unsigned char* const own_w = kByCols ? ring_w : ring_w + wm * kM * 2048;
+    // by columns: of block b the rows 8 (lane / 16) + lane % 16 / 4, and four further, of k-step s
+    const int rt = 8 * (lane >> 4) + ((lane & 15) >> 2);
+    const int at_t = rt * BM * 2 + ((((2 * wm * kM) ^ by_rows(rt)) | ((lane & 3) >> 1)) << 4) + ((lane & 1) << 3);
     auto read = [&](int slot_x, int slot_w, int s, Frags& f, int b) __attribute__((always_inline)) {
       const int at = at0 ^ (s << 6);
       if (b < kT) f.x[b] = *reinterpret_cast<const u32x4*>(own_x + slot_x * kX + at + b * 2048);
-      else f.w[b - kT] = *reinterpret_cast<const u32x4*>(own_w + slot_w * kStageW + at + (b - kT) * 2048);
+      else if constexpr (kByCols) {
+        typedef short v4s __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) v4s lds_v4s;
+        typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+        const unsigned char* p = own_w + slot_w * kStageW + (at_t ^ ((b - kT) << 5)) + s * 64 * BM;
+        const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p));
+        const v2u hi = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 8 * BM)));
+        f.w[b - kT] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      } else f.w[b - kT] = *reinterpret_cast<const u32x4*>(own_w + slot_w * kStageW + at + (b - kT) * 2048);
     };
     constexpr int kReads = kT + kM, kProducts = kT * kM;
     // The products of `now`; between them the reads of k-step s of (slot_x, slot_w), and loads of a stage kk.
@@ -443,7 +504,7 @@ struct TileProduct16 {
       __builtin_amdgcn_s_waitcnt(waitcnt_vm(kBehind));
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       sync_lds();  // the next stage has landed, and nobody reads this one any more
-      if constexpr (kTouch > 0) {
+      if constexpr (kTouches > 0) {
         // (the one before has arrived: it is older than what the wait above was for)
         asm volatile("" : : "v"(touched));
         if constexpr (whole()) {
@@ -462,7 +523,7 @@ struct TileProduct16 {
     for (; kk + NX < whole; ++kk) turn(std::true_type());
 #pragma unroll 1
     for (; kk < nk; ++kk) turn(std::false_type());
-    if constexpr (kTouch > 0) asm volatile("" : : "v"(touched));
+    if constexpr (kTouches > 0) asm volatile("" : : "v"(touched));
     // no load may still target LDS when it is reused or ends, and nobody may still read it
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
@@ -478,7 +539,7 @@ __device__ __forceinline__ bool grouped(const uint16_t* xb, int ldx, int last_t,
   const int stages = (k + 63) / 64, each = (stages + G - 1) / G;
   const int group = wave / P::kW, in = wave % P::kW, first = group * each * 64;
   const int left = k - first < each * 64 ? k - first : each * 64;
-  P::run(xb + first, ldx, last_t, {{w.w[0] + first, w.w[1] + first}, w.ld, w.last}, G > 1 ? (left > 0 ? left : 0) : k,
+  P::run(xb + first, ldx, last_t, PanelW{{w.w[0] + first, w.w[1] + first}, w.ld, w.last}, G > 1 ? (left > 0 ? left : 0) : k,
          each, tile, smem + group * P::kLds, in, lane, acc);
   if constexpr (G > 1) {
     constexpr int kOwn = P::kM * P::kT * 1024;  // bytes of a wave's sums

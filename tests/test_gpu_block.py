@@ -103,11 +103,13 @@ GATED = [
     (1100, 40, 1288, "bf16", "silu"), (1500, 72, 1032, "f16", "gelu_tanh"), (2309, 72, 2056, "bf16", "silu"),
     (2500, 136, 2000, "f16", "silu"), (6001, 1600, 64, "bf16", "gelu"), (9, 8, 5000, "bf16", "silu"),
     (515, 4104, 8, "bf16", "silu"), (40, 4096, 4104, "f16", "gelu"), (700, 1288, 3000, "bf16", "silu"),
-    # x's gradients without a transpose: one and several tiles of 32 and of 64 rows, widths that end inside a stage
+    # few rows, odd columns, widths that end inside a stage
     (2, 72, 1000, "f16", "silu"), (32, 200, 3336, "bf16", "gelu"), (63, 1096, 520, "f16", "gelu_tanh"),
     (129, 72, 2504, "bf16", "silu"), (192, 264, 712, "f16", "silu"), (193, 264, 712, "f16", "silu"),
-    # and with k split between workgroups: tiles of 128 rows, and of 256
+    # k split between workgroups: tiles of 128 rows, and of 256
     (449, 776, 2312, "f16", "gelu"), (1100, 2056, 8200, "bf16", "silu"),
+    # large tiles whose stages of 64 rows of the weights end with the first matrix, and do not
+    (900, 2048, 8256, "f16", "silu"), (2000, 4096, 1088, "bf16", "gelu"), (4200, 4104, 520, "f16", "silu"),
 ]
 
 
