@@ -212,6 +212,13 @@ def _workspace(nbytes, device):
     return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
 
 
+def _given_workspace(ws, nbytes, device):
+    """ws where it can serve, or a new one."""
+    fits = ws is not None and ws.device == device and ws.is_contiguous() and ws.numel() >= nbytes \
+        and ws.data_ptr() % 256 == 0
+    return ws if fits else _workspace(nbytes, device)
+
+
 def _maxsim_inputs(Q, D, off):
     _need(Q, "Q", torch.bfloat16, 3)
     dev = Q.device
@@ -963,7 +970,7 @@ def gated_linear_fwd(x, w_gate, w_up, act="silu", out=None):
 def gated_linear_bwd(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=True, ws=None):
     """Gradients of gated_linear_fwd's h: dict(dx, dw_gate, dw_up), dense and of the inputs' type, None where
     not needed.  x: the forward's, or a Checkpoint of it (the gradients are those at the values that it stands
-    for).  A ws that is too small is not used."""
+    for).  A ws that is too small, not aligned or not dense on x's device is not used."""
     dev, dtype, f, k = _gated_weights(w_gate, w_up, act)
     x_ptr, exps, row, shape = _rows_or_checkpoint(x, "x", dtype, dev)
     n = shape[0]
@@ -974,7 +981,7 @@ def gated_linear_bwd(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=True
         raise ValueError(f"dh must be {(n, f)}")
     L = lib()
     need = L.gated_linear_bwd_workspace_size(n, k, f, exps is not None, bool(need_dx), bool(need_dw))
-    ws = ws if ws is not None and ws.numel() >= need else _workspace(need, dev)
+    ws = _given_workspace(ws, need, dev)
     dx = torch.empty((n, k), dtype=dtype, device=dev) if need_dx else None
     dw = [torch.empty((f, k), dtype=dtype, device=dev) if need_dw else None for _ in range(2)]
     _launch(L.gated_linear_bwd, dev, _ptr(dh), x_ptr, exps, row, n, k, _ptr(w_gate), _ptr(w_up), f,
@@ -1119,7 +1126,7 @@ def residual_norm_bwd(dr, dy, x, b=None, weight=None, bias=None, post_weight=Non
     dgate = like(gate, need_dgate)
     L = lib()
     need = L.residual_norm_bwd_workspace_size(ctypes.byref(d))
-    ws = ws if ws is not None and ws.numel() >= need else _workspace(need, dev)
+    ws = _given_workspace(ws, need, dev)
     _launch(L.residual_norm_bwd, dev, ctypes.byref(d), _ptr(dr), _ptr(dy), x_ptr, x_exps, b_ptr, b_exps,
             w_ptr, pw_ptr, pc_ptr, g_ptr, _ptr(dx), _ptr(db), _ptr(dw), _ptr(dc),
             _ptr(dpw), _ptr(dpc), _ptr(dgate), _ptr(ws), ws.numel())

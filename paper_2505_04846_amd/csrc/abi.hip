@@ -999,6 +999,7 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
   const GatedCarve g = gated_carve(ws, n, k, f, packed, need_dx, need_dw);
   if (!ws || ws_bytes < g.bytes)
     return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, g.bytes);
+  if (!aligned16(ws)) return fail(HPR_ERR_INVALID_ARG, "the workspace must be aligned");
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t np = (n + 7) / 8 * 8;
   const uint16_t* const rows = packed ? g.plain : static_cast<const uint16_t*>(x);
@@ -1117,6 +1118,7 @@ hpr_status residual_norm_bwd(const hpr_norm* d, const uint16_t* dr, const uint16
   const size_t need = residual_norm_bwd_workspace_size(d);
   if (need > 0 && (!ws || ws_bytes < need))
     return fail(HPR_ERR_WORKSPACE_TOO_SMALL, "workspace %zu < %zu bytes", ws ? ws_bytes : (size_t)0, need);
+  if (!aligned16(ws)) return fail(HPR_ERR_INVALID_ARG, "the workspace must be aligned");
   NormArgs a = {};
   if (packed) {
     a.x_codes = static_cast<const int8_t*>(x);

@@ -52,6 +52,7 @@ def test_gated_rejects_more():
     # each half of the gradients needs no more than both, and nothing is asked for sizes that are refused
     assert size(100, 64, 40, 0, 1, 0) < need and size(100, 64, 40, 0, 0, 1) < need
     assert size(-1, 64, 40, 0, 1, 1) == 0 and size(100, 0, 40, 0, 1, 1) == 0 and size(100, 64, 70000, 0, 1, 1) == 0
+    assert _gated("bwd", ws=FAKE_ODD) == INVALID and _norm("bwd", ws=FAKE_ODD) == INVALID
     # nothing to do
     assert _gated("fwd", n=0, x=None, h=None) == 0
     assert _gated("bwd", dx=None, dwg=None, dwu=None, ws=None, ws_bytes=0) == 0

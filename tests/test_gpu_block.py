@@ -110,6 +110,8 @@ GATED = [
     (449, 776, 2312, "f16", "gelu"), (1100, 2056, 8200, "bf16", "silu"),
     # large tiles whose stages of 64 rows of the weights end with the first matrix, and do not
     (900, 2048, 8256, "f16", "silu"), (2000, 4096, 1088, "bf16", "gelu"), (4200, 4104, 520, "f16", "silu"),
+    # the weights' gradients with their rows split between workgroups, the two matrices' edge inside a tile
+    (9001, 264, 328, "f16", "gelu"), (5003, 520, 136, "bf16", "silu"),
 ]
 
 
@@ -549,6 +551,10 @@ def test_gated_workspace():
             got = hpr.gated_linear_bwd(dh, x, wg, wu, ws=ws[:size])
             assert all(torch.equal(got[name], v) for name, v in want.items())
             assert (ws[size:] == 0xff).all() and (size >= need or (ws == 0xff).all())
+        odd = torch.full((2 * need + 512,), 0xff, dtype=torch.uint8, device=DEV)
+        for ws in (odd[8:], odd[::2], odd.cpu()):  # not aligned, not dense, elsewhere: not used
+            got = hpr.gated_linear_bwd(dh, x, wg, wu, ws=ws)
+            assert all(torch.equal(got[name], v) for name, v in want.items()) and (odd == 0xff).all()
 
 
 # ---- offsets past 32 bits -------------------------------------------------------------------
