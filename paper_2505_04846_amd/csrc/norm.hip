@@ -88,6 +88,10 @@ __device__ __forceinline__ u32x4 narrow(const float (&f)[8]) {
   for (int i = 0; i < 4; ++i) v[i] = T::pack(f[2 * i], f[2 * i + 1]);
   return v;
 }
+// 16 bytes that are not read again soon: past the caches, which keep what is.
+__device__ __forceinline__ void store16_stream(void* p, u32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+}
 // Eight values of a vector of d at col, `other` without one.
 template <class T>
 __device__ __forceinline__ void vector8(const uint16_t* p, int64_t at, float other, float (&f)[8]) {

@@ -585,6 +585,26 @@ def test_gated_far_rows(n, k, f, dw):
         hold(got[name], want[name], want["bound"][name], name)
 
 
+@pytest.mark.parametrize("n", [5, 300])
+def test_gated_far_columns(n):
+    """Weights past 2^31 values.  Columns of dh between those that are looked at are 0."""
+    k, f, dt = 40960, 65536, torch.bfloat16
+    at = far_rows(f).to(DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    wg, wu = (torch.empty(f, k, dtype=dt, device=DEV).normal_(std=k ** -0.5, generator=g) for _ in range(2))
+    x = rand(gen(1), n, k, dtype=dt)
+    dh = torch.zeros(n, f, dtype=dt, device=DEV)
+    dh[:, at] = rand(gen(2), n, len(at), dtype=dt, std=0.3)
+    want = B.gated_linear(f64(x), f64(wg[at]), f64(wu[at]), "silu", f64(dh[:, at]), *TYPES["bf16"][1:3])
+    hold(hpr.gated_linear_fwd(x, wg, wu)["h"][:, at], want["h"], want["bound"]["h"], "h")
+    got = hpr.gated_linear_bwd(dh, x, wg, wu)
+    hold(got["dx"], want["dx"], want["bound"]["dx"], "dx")
+    for name in ("dw_gate", "dw_up"):
+        hold(got[name][at], want[name], want["bound"][name], name)
+        assert torch.count_nonzero(got[name].abs().amax(1)) <= len(at)
+
+
 def test_norm_far_rows():
     n, d, dt = (1 << 20) + 300, 2056, torch.bfloat16
     at = far_rows(n).to(DEV)
