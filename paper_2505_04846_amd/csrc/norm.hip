@@ -455,13 +455,14 @@ __global__ __launch_bounds__((Layout<W, C>::kThreads), W == 8 ? 4 : 1) void norm
   norm_bwd_rows<T, LAYER, PACKED, GATE_ROWS, W, C>(a);
 }
 
-// The workgroups' sums of 16 columns, in their order within 64 runs of workgroups, then over the runs; and the
+// The workgroups' sums of 16 columns, in their order within 256 runs of workgroups, then over the runs; and the
 // gradients that come of them.  Reads 8 or 16 bytes a column and workgroup of the gradients' kernel: 4096 columns of 512
-// workgroups (17 MB) 10 us, most of it the start and the reads' latency.
+// workgroups (17 MB) 8.9 us, 768 columns of 1,024 (13 MB) 10.7 (in 64 runs: 9.0 and 13.1), most of it start and latency.
+constexpr int kJoinRuns = 256;
 template <class T, bool LAYER>
-__global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a) {
-  constexpr int kSums = LAYER ? 4 : 2;
-  __shared__ f32x4 lds[64][kSums][4];
+__global__ __launch_bounds__(4 * kJoinRuns) void norm_join_kernel(NormArgs a) {
+  constexpr int kSums = LAYER ? 4 : 2, kParts = 4 * kJoinRuns / (16 * kSums), kOf = kJoinRuns / kParts;
+  __shared__ float lds[kJoinRuns][kSums][16];
   const int q = threadIdx.x & 3, run = threadIdx.x >> 2;
   const int c = (int)blockIdx.x * 16 + 4 * q;
   f32x4 v[kSums];
@@ -469,23 +470,29 @@ __global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a) {
   for (int k = 0; k < kSums; ++k) v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (c < a.d) {
 #pragma unroll 4
-    for (int64_t g = a.parts * run / 64; g < a.parts * (run + 1) / 64; ++g)
+    for (int64_t g = a.parts * run / kJoinRuns; g < a.parts * (run + 1) / kJoinRuns; ++g)
 #pragma unroll
       for (int k = 0; k < kSums; ++k)
         v[k] += *reinterpret_cast<const f32x4*>(a.part + (g * kSums + k) * a.d + c);
   }
 #pragma unroll
-  for (int k = 0; k < kSums; ++k) lds[run][k][q] = v[k];
+  for (int k = 0; k < kSums; ++k) *reinterpret_cast<f32x4*>(&lds[run][k][4 * q]) = v[k];
   __syncthreads();
-  if (threadIdx.x >= 16) return;
-  const int j = threadIdx.x, to = (int)blockIdx.x * 16 + j;
-  if (to >= a.d) return;
+  const int j = threadIdx.x & 15, of = (threadIdx.x >> 4) % kSums, part = threadIdx.x / (16 * kSums);
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kOf; ++w) sum += lds[part * kOf + w][of][j];
+  __syncthreads();
+  lds[part][of][j] = sum;
+  __syncthreads();
+  const int to = (int)blockIdx.x * 16 + j;
+  if (threadIdx.x >= 16 || to >= a.d) return;
   float s[kSums];
 #pragma unroll
   for (int k = 0; k < kSums; ++k) {
     s[k] = 0.f;
-#pragma unroll 8
-    for (int w = 0; w < 64; ++w) s[k] += lds[w][k][j >> 2][j & 3];
+#pragma unroll
+    for (int w = 0; w < kParts; ++w) s[k] += lds[w][k][j];
   }
   const float none = LAYER ? s[kSums - 1] : 0.f;  // sum 3
   auto one = [&](const uint16_t* p, float other) { return p ? T::lo(p[to]) : other; };
@@ -546,7 +553,7 @@ hipError_t norm_bwd(const NormArgs& a, hipStream_t s) {
     return hipGetLastError();
   });
   if (e != hipSuccess || !(a.dw || a.dc || a.dpw || a.dpc || a.dgate)) return e;
-  hipLaunchKernelGGL((norm_join_kernel<T, LAYER>), dim3((unsigned)((a.d + 15) / 16)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((norm_join_kernel<T, LAYER>), dim3((unsigned)((a.d + 15) / 16)), dim3(4 * kJoinRuns), 0, s, a);
   return hipGetLastError();
 }
 
