@@ -528,7 +528,7 @@ struct RowsPlan {
 };
 RowsPlan rows_plan(int64_t n, int m, int k) {
   constexpr double kStage[2] = {0.55, 1.26};
-  const int64_t stages = k > 0 ? (k + 63) / 64 : 1;
+  const int64_t stages = k > 0 ? ((int64_t)k + 63) / 64 : 1;
   RowsPlan best = {true, 1};
   double least = 0.0;
   for (int wide = 1; wide >= 0; --wide) {

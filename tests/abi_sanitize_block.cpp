@@ -97,6 +97,8 @@ int main() {
     expect("row", gated_linear_fwd(p, row, 10, 64, p, p, 64, 0, 0, p, nullptr), HPR_ERR_UNSUPPORTED_SHAPE);
     expect("row", checkpoint_pack(p, row, 10, 64, 0, codes, exps, nullptr), HPR_ERR_UNSUPPORTED_SHAPE);
   }
+  // the most rows of the widest rows
+  if (!gated_linear_bwd_workspace_size(INT32_MAX, 65536, 65536, 1, 1, 1)) ++failures;
   std::printf("ok: %d failures\n", failures);
   return failures != 0;
 }
