@@ -384,7 +384,7 @@ struct TileProduct16 {
       const int row = PAIR ? lw.row[j] / (BM / WM) * kWaveCols + lw.row[j] % kWaveCols : lw.row[j];
       ow[j] = (row < w.last ? row : w.last) * w.ld * 2 + lw.chunk[j];
     }
-    // stages that lie inside k, and (by columns) in one matrix, which those before the first that does not do
+    // the stages before the first that leaves k or (by columns) has rows of both matrices
     int nk_full = k / 64;
     if constexpr (kByCols) {
       const int left = w.half - w.first;
@@ -392,7 +392,7 @@ struct TileProduct16 {
     }
     unsigned char* const ring_w = smem + NX * kX;
     // Load j of x's or W's stage kk into slot `slot` of its ring.  Chunks past the end of k read zeros, so past the
-    // last stage too (the rings keep their numbers of loads in flight); WHOLE: the stage lies inside k.
+    // last stage too (the rings keep their numbers of loads in flight); WHOLE: the stage is one of nk_full.
     auto load = [&](auto whole, auto of_x, int slot, int kk, int j) __attribute__((always_inline)) {
       unsigned char* to;
       if constexpr (of_x()) to = smem + slot * kX + (wave * kLx + j) * 1024;
