@@ -466,7 +466,7 @@ GatedCarve gated_carve(void* ws, int64_t n, int32_t k, int32_t f, bool packed, b
   if (need_dx) g.d = reinterpret_cast<uint16_t*>(take((size_t)n * 2 * f * 2));
   if (need_dw) g.dt = reinterpret_cast<uint16_t*>(take(np * 2 * f * 2));
   if (packed) g.plain = reinterpret_cast<uint16_t*>(take((size_t)n * k * 2));
-  g.words = reinterpret_cast<uint32_t*>(take(((size_t)n + f) * sizeof(uint32_t)));
+  g.words = reinterpret_cast<uint32_t*>(take(((size_t)gated_cols_at(n) + f) * sizeof(uint32_t)));
   const size_t of_dx = need_dx ? rows_product_bytes(n, k, 2 * f) : 0;
   const size_t of_dw = need_dw ? rows_product_bytes(2 * (int64_t)f, k, (int)n) : 0;
   g.part = reinterpret_cast<float*>(take(of_dx > of_dw ? of_dx : of_dw));
@@ -1004,7 +1004,7 @@ hpr_status gated_linear_bwd(const uint16_t* dh, const void* x, const uint8_t* x_
   const int64_t np = (n + 7) / 8 * 8;
   const uint16_t* const rows = packed ? g.plain : static_cast<const uint16_t*>(x);
   const int64_t row = packed ? k : x_row;
-  const uint32_t *const row_max = g.words, *const col_max = g.words + n;
+  const uint32_t *const row_max = g.words, *const col_max = g.words + gated_cols_at(n);
   hipError_t e = hipSuccess;
   if (n > 0) {
     if (packed || narrow)

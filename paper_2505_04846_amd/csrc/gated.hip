@@ -581,7 +581,7 @@ bool gated_fits(int64_t n, int k, int f, bool grads) {
   auto blocks = [](int64_t size, int of) { return (size + of - 1) / of; };
   if (!launch_fits(blocks(n, 256) * blocks(f, 128), 512)) return false;
   if (!grads) return true;
-  return launch_fits(blocks(n + f, 256), 256) && launch_fits(blocks(n, 64) * blocks(f, 512), 256) &&
+  return launch_fits(blocks(gated_cols_at(n) + f, 256), 256) && launch_fits(blocks(n, 64) * blocks(f, 512), 256) &&
          launch_fits(blocks(n, 256) * blocks(k, 256), 512);
 }
 
@@ -603,8 +603,9 @@ hipError_t launch_rows_product(const ProductArgs& a, bool f16, hipStream_t strea
 
 hipError_t launch_gated_max(const uint16_t* dh, int64_t n, int f, uint32_t* words, hipStream_t stream) {
   if (n == 0) return hipSuccess;
-  hipLaunchKernelGGL(clear_kernel, dim3((unsigned)((n + f + 255) / 256)), dim3(256), 0, stream, words, n + f);
-  uint32_t *const rows = words, *const cols = words + n;
+  const int64_t all = gated_cols_at(n) + f;
+  hipLaunchKernelGGL(clear_kernel, dim3((unsigned)((all + 255) / 256)), dim3(256), 0, stream, words, all);
+  uint32_t *const rows = words, *const cols = words + gated_cols_at(n);
   // fewer atomics where there are workgroups enough
   const int64_t n_c = (f + 511) / 512;
   if ((n + 63) / 64 * n_c >= 1024)

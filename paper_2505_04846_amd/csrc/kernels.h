@@ -395,7 +395,9 @@ struct GatedArgs {
 hipError_t launch_gated(const GatedArgs& a, bool grad, hipStream_t stream);
 // Whether every launch of the forward, or of the gradients, is one that can be made (launch_fits).
 bool gated_fits(int64_t n, int k, int f, bool grads);
-// Largest magnitudes (as fp16 bits) of dh's rows and columns, into words [n + f].
+// Largest magnitudes (as fp16 bits) of dh's rows, and from word gated_cols_at(n) on of its columns (read four at a
+// time, at a multiple of 16 bytes), into words [gated_cols_at(n) + f].
+inline int64_t gated_cols_at(int64_t n) { return (n + 3) / 4 * 4; }
 hipError_t launch_gated_max(const uint16_t* dh, int64_t n, int f, uint32_t* words, hipStream_t stream);
 // y = x w of x [n, k] with rows of ld and w [k, m] with rows of w_ld, whose rows from `half` on are w[1]'s: rows
 // [0, split) of y to y[0], the others to y[1] (rows of m).  In fp16 row r is divided by the power of two of
