@@ -509,8 +509,9 @@ hpr_status gated_linear_fwd(const uint16_t* x, int64_t x_row, int64_t n, int32_t
  * With g = w_gate x[t] and u = w_up x[t], formed again, dg = dh u act'(g) and du = dh act(g):
  *     dx[t] = w_gate^T dg[t] + w_up^T du[t];  dw_gate = sum_t dg[t] x[t]^T;  dw_up = sum_t du[t] x[t]^T
  * dg and du are rounded once to 16 bits as operands, in fp16 times powers of two that bring every row's (for
- * dx) or column's (for dw_gate and dw_up) largest |dh| to [1, 2), exactly undone in the fp32 sums (products
- * of act(g) or u act'(g) past 32752 overflow).  All sums are fp32 with a fixed order.
+ * dx) or column's (for dw_gate and dw_up) largest |dh| to [1/4, 1/2), exactly undone in the fp32 sums: act(g) and
+ * u act'(g) overflow from 131040 on, which no g and u that are numbers of fp16 reach, and below 2^-12 they lose
+ * bits.  All sums are fp32 with a fixed order.
  *
  *   dh [n, f] dense; x [n, k] with row stride x_row or, with x_exps, checkpoint_pack's codes (dense; the
  *   gradients are those at the values that they stand for); dx [n, k] and dw_gate, dw_up [f, k], dense; dx, or

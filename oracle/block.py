@@ -85,11 +85,13 @@ def gated_linear(x, w_gate, w_up, act, dh=None, u=0.0, tiny=0.0):
     if dh is not None:
         adh = np.abs(dh)
         dg, du = dh * v * slope, dh * a
-        # (as operands: rounded to u, in fp16 below the normal range at the size of the row or column)
+        # (as operands: rounded to u, in fp16 below the normal range at the size of the row or column: they are
+        # multiplied by the power of two that brings its largest |dh| to [1/4, 1/2), rounded to within `tiny` there,
+        # and divided by it again, which makes it 4 tiny times the power of two of that |dh|)
         e_g = adh * (np.abs(slope) * ev + es * (np.abs(v) + ev)) + (3 * F32 + u) * np.abs(dg) + LEAST
         e_u = adh * ea + (2 * F32 + u) * np.abs(du) + LEAST
-        row = tiny * _power(adh.max(1, initial=0.0))[:, None]
-        col = tiny * _power(adh.max(0, initial=0.0))[None]
+        row = 4 * tiny * _power(adh.max(1, initial=0.0))[:, None]
+        col = 4 * tiny * _power(adh.max(0, initial=0.0))[None]
         r.update(dx=dg @ w_gate + du @ w_up, dw_gate=dg.T @ x, dw_up=du.T @ x)
         b["dx"] = 1.01 * ((e_g + row) @ ag + (e_u + row) @ au
                           + 2 * f * F32 * (np.abs(dg) @ ag + np.abs(du) @ au))

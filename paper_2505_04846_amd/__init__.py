@@ -970,7 +970,10 @@ def gated_linear_fwd(x, w_gate, w_up, act="silu", out=None):
 def gated_linear_bwd(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dw=True, ws=None):
     """Gradients of gated_linear_fwd's h: dict(dx, dw_gate, dw_up), dense and of the inputs' type, None where
     not needed.  x: the forward's, or a Checkpoint of it (the gradients are those at the values that it stands
-    for).  A ws that is too small, not aligned or not dense on x's device is not used."""
+    for).  The gradients of the two projections, dh u act'(g) and dh act(g), are rounded once to the type, as the
+    products' operands; in fp16 times powers of two that hold them for every g and u that are numbers of it (from
+    131,040 on, act(g) and u act'(g) overflow; below 2^-12 they lose bits).  A ws that is too small, not aligned or not
+    dense on x's device is not used."""
     dev, dtype, f, k = _gated_weights(w_gate, w_up, act)
     x_ptr, exps, row, shape = _rows_or_checkpoint(x, "x", dtype, dev)
     n = shape[0]

@@ -89,15 +89,17 @@ struct GeluTanh {
 
 // dg and du are products' operands in 16 bits.  fp16 has few exponents: where dh is small (a loss that is
 // not scaled), they would lose bits below 2^-14.  So a row of d is written for dx times the power of two that
-// brings the row's largest |dh| into [1, 2), a column for dW times that of its column, and the products'
-// results are multiplied back in 32 bits: exactly undone, whatever the size of dh.  What is left are factors
-// act(g) and u act'(g) as small as the forward's own h, which fp16 rounds as coarsely; and they overflow where
-// they pass 2^15, as a finite h all but excludes.
+// brings the row's largest |dh| into [1/4, 1/2), a column for dW times that of its column, and the products'
+// results are multiplied back in 32 bits: exactly undone, whatever the size of dh.  What is left are the factors act(g)
+// and u act'(g).  Where g and u are numbers of fp16 they are at most 1.13 times 65504, and half of that is one too: no
+// larger power would do, whatever h is (g of 0.5 and u of 60,000 have h of 18,700 and u act'(g) of 44,400; brought to
+// [1, 2), as it was, dx of that row was infinite).  They overflow from 131,040 on, which g or u has to pass 65504
+// for, and lose bits below 2^-12, where h is about as small and fp16 rounds it as coarsely.
 // bits: the largest |value| of fp16 as a whole number (max_kernel); 0 and infinities stay as they are.
 __device__ __forceinline__ int up_of(uint32_t bits) {
   if (bits == 0 || bits >= 0x7c00) return 0;
   const float v = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-  return 127 - (int)(__float_as_uint(v) >> 23);
+  return 125 - (int)(__float_as_uint(v) >> 23);
 }
 __device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
