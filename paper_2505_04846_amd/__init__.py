@@ -650,6 +650,13 @@ def _first_order(name, grads, *of):
     return [g if g is None else next(tied) for g in grads]
 
 
+def _dense(grad):
+    """A gradient as the library reads it: dense, at a multiple of 16 bytes.  autograd may hand over a part of a larger
+    buffer (the backward pass of torch.cat), which can begin anywhere."""
+    grad = grad.contiguous()
+    return grad if grad.data_ptr() % 16 == 0 else grad.clone()
+
+
 class _PackedAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, q_off, k_off, k_len, causal, window, scale):
@@ -665,7 +672,7 @@ class _PackedAttention(torch.autograd.Function):
     def backward(ctx, grad_out):
         q, k, v, out, lse, q_off, k_off, k_len = ctx.saved_tensors
         need = ctx.needs_input_grad
-        g = packed_attention_bwd(grad_out.contiguous(), q, k, v, out, lse, q_off, k_off, k_len,
+        g = packed_attention_bwd(_dense(grad_out), q, k, v, out, lse, q_off, k_off, k_len,
                                  *ctx.how, need_dq=need[0], need_dkv=need[1] or need[2])
         dq, dk, dv = _first_order("packed_attention", [g["dq"], g["dk"] if need[1] else None,
                                                        g["dv"] if need[2] else None],
@@ -760,7 +767,7 @@ class _AdapterLinear(torch.autograd.Function):
     def backward(ctx, grad_y):
         need = ctx.needs_input_grad
         saved = ctx.saved_tensors
-        g = adapter_linear_bwd(grad_y.contiguous(), *saved, need_dx=need[0], need_da=need[2],
+        g = adapter_linear_bwd(_dense(grad_y), *saved, need_dx=need[0], need_da=need[2],
                                need_db=need[3])
         x, _, A, B = saved[:4]
         dx, da, db = _first_order("adapter_linear", [g["dx"], g["da"], g["db"]], grad_y, x, A, B)
@@ -815,7 +822,7 @@ class _Rotary(torch.autograd.Function):
     @staticmethod
     def backward(ctx, gq, gk):
         need_q, need_k = ctx.needs_input_grad[:2]
-        a, b = [g.contiguous() if g is not None and need else None
+        a, b = [_dense(g) if g is not None and need else None
                 for g, need in ((gq, need_q), (gk, need_k))]
         back = (*ctx.saved_tensors, not ctx.inverse)
         # (a rotation too, and differentiable as one)
@@ -1018,7 +1025,7 @@ class _GatedLinear(torch.autograd.Function):
             _no_second("gated_linear")
         need = ctx.needs_input_grad
         of = x[0].detach() if ctx.packed is None else Checkpoint(*x, ctx.packed)
-        g = gated_linear_bwd(grad_h.contiguous(), of, w_gate.detach(), w_up.detach(), ctx.act, need_dx=need[0],
+        g = gated_linear_bwd(_dense(grad_h), of, w_gate.detach(), w_up.detach(), ctx.act, need_dx=need[0],
                              need_dw=need[1] or need[2])
         dx, dg, du = _first_order("gated_linear", [g["dx"], g["dw_gate"] if need[1] else None,
                                                    g["dw_up"] if need[2] else None],
@@ -1168,7 +1175,7 @@ class _ResidualNorm(torch.autograd.Function):
             x, *b = [Checkpoint(*rows[i:i + 2], ctx.packed) for i in range(0, len(rows), 2)]
             b, inputs = (b[0] if b else None), []
         vectors = [None if t is None else t.detach() for t in (weight, bias, post_weight, post_bias, gate)]
-        g = residual_norm_bwd(*(None if t is None else t.contiguous() for t in (grad_r, grad_y)), x, b, *vectors,
+        g = residual_norm_bwd(*(None if t is None else _dense(t) for t in (grad_r, grad_y)), x, b, *vectors,
                               **ctx.how, need_dx=need[0], need_db=need[1], need_dw=any(need[2:6]),
                               need_dgate=need[6])
         names = ("dx", "db", "dweight", "dbias", "dpost_weight", "dpost_bias", "dgate")

@@ -37,3 +37,23 @@ def test_gradients_where_a_factor_is_large(n, f, act, ty, g, u):
     for name in got:
         hold(got[name], want[name], want["bound"][name], name)
         assert (np.abs(f64(got[name]) - want[name]) <= 2.1 * TYPES[ty][1] * np.abs(want[name])).all(), name
+
+
+def test_gradients_that_are_parts_of_a_larger_buffer():
+    """torch.cat's backward pass gives views that begin anywhere."""
+    dt = torch.bfloat16
+    x, b, wg, wu, w = (torch.randn(s, generator=gen(i)).to(dt).to(DEV).requires_grad_()
+                       for i, s in enumerate([(9, 64), (9, 64), (40, 64), (40, 64), (64,)]))
+    one = torch.ones(3, dtype=dt, device=DEV, requires_grad=True)
+
+    def grads(join):
+        r, y = hpr.residual_norm(x, b, w)
+        h = hpr.gated_linear(y, wg, wu)
+        out = join(r, h)
+        weight = torch.linspace(-1, 1, r.numel() + h.numel(), device=DEV).to(dt)
+        return torch.autograd.grad((out * weight).sum(), [x, b, wg, wu, w])
+
+    want = grads(lambda *t: torch.cat([v.flatten() for v in t]))
+    got = grads(lambda *t: torch.cat([one] + [v.flatten() for v in t])[3:])
+    for a, c in zip(got, want):
+        assert torch.equal(a, c)
