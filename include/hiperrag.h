@@ -518,7 +518,8 @@ hpr_status gated_linear_fwd(const uint16_t* x, int64_t x_row, int64_t n, int32_t
  *   dw_gate and dw_up together, may be NULL
  *   ws     workspace of gated_linear_bwd_workspace_size(...) bytes: dg and du each way that is needed (8 n f bytes
  *          for both), a checkpoint's rows, partial sums (of few rows, so that more rows may need less); packed,
- *          need_dx, need_dw: 0 or 1.  With dw_gate and dw_up n is at most 2^21
+ *          need_dx, need_dw: 0 or 1 (the size is 0 for k or f that no call takes).  With dw_gate and dw_up n is at
+ *          most 2^21
  * ------------------------------------------------------------------------------------------- */
 size_t gated_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t f, int32_t packed, int32_t need_dx,
                                        int32_t need_dw);
@@ -567,7 +568,8 @@ hpr_status residual_norm_fwd(const hpr_norm* d, const uint16_t* x, const uint16_
  * stand for).  dx, db [n, dim]; dweight, dbias, dpost_weight, dpost_bias [dim]; dgate [dim] or [n, dim], as gate:
  * each may be NULL, and is, where what it is the gradient of is (dbias apart, which needs weight alone).
  * In fp32 throughout, each output rounded once; the sums over rows have a fixed order (no atomics).
- *   ws     workspace of residual_norm_bwd_workspace_size(d) bytes: partial sums over the rows
+ *   ws     workspace of residual_norm_bwd_workspace_size(d) bytes (0 for a dim that no call takes): partial sums over
+ *          the rows
  * ------------------------------------------------------------------------------------------- */
 size_t residual_norm_bwd_workspace_size(const hpr_norm* d);
 hpr_status residual_norm_bwd(const hpr_norm* d, const uint16_t* dr, const uint16_t* dy, const void* x,

@@ -975,7 +975,7 @@ hpr_status gated_linear_fwd(const uint16_t* x, int64_t x_row, int64_t n, int32_t
 
 size_t gated_linear_bwd_workspace_size(int64_t n, int32_t k, int32_t f, int32_t packed, int32_t need_dx,
                                        int32_t need_dw) {
-  if (n < 0 || n >= (int64_t(1) << 31) || k < 8 || k > 65536 || f < 8 || f > 65536) return 0;
+  if (n < 0 || n >= (int64_t(1) << 31) || k < 8 || k > 65536 || k % 8 || f < 8 || f > 65536 || f % 8) return 0;
   return gated_carve(nullptr, n, k, f, packed != 0, need_dx != 0, need_dw != 0).bytes;
 }
 
@@ -1087,7 +1087,7 @@ hpr_status residual_norm_fwd(const hpr_norm* d, const uint16_t* x, const uint16_
 }
 
 size_t residual_norm_bwd_workspace_size(const hpr_norm* d) {
-  if (!d || d->n < 0 || d->n >= (int64_t(1) << 31) || d->dim < 8 || d->dim > kMaxNormDim) return 0;
+  if (!d || d->n < 0 || d->n >= (int64_t(1) << 31) || d->dim < 8 || d->dim > kMaxNormDim || d->dim % 8) return 0;
   return align_up((size_t)norm_parts(d->n, d->dim) * norm_sums(d->kind == HPR_LAYER_NORM) * d->dim * sizeof(float));
 }
 
