@@ -559,11 +559,14 @@ hipError_t rows(ProductArgs a, hipStream_t s) {
   if (!plan.wide) {
     e = rows_as<T, Middle<T, false>>(a, s);
   } else {
-    // a last round of up to 112 tiles (of 256, one a CU) is left to the next size
+    // A last round of up to 112 tiles (of 256, one a CU) is left to the next size, where these are at most 448: two rounds.
+    // (They may be more, because the rows are cut at whole tile rows: 2,048 rows, 11000 -> 4096, x's gradients 643 us in
+    // one launch, 679 with 516 of them.)
     const int64_t n_m = (a.m + 255) / 256, tiles = (a.n + 255) / 256 * n_m, rest = tiles % 256;
     const int64_t whole = (tiles - rest) / n_m * 256;  // rows of the whole rounds
+    const int64_t small = (a.n - whole + 127) / 128 * ((a.m + 127) / 128);
     ProductArgs w = a;
-    if (a.splits == 1 && rest > 0 && rest <= 112 && whole > 0) w.n = whole;
+    if (a.splits == 1 && rest > 0 && rest <= 112 && whole > 0 && small <= 448) w.n = whole;
     e = rows_as<T, Wide<T, false>>(w, s);
     if (e == hipSuccess && w.n < a.n) {
       a.row0 = whole;
