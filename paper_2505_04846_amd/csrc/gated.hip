@@ -25,7 +25,8 @@ namespace {
 
 // ---- activations ------------------------------------------------------------------------------
 
-// exp of a 32-bit number, relative error (|x| + 2) 2^-24: far below the rounding of what it goes into.
+// exp of a 32-bit number, relative error (1.25 |x| + 2) 2^-24 (the product's rounding, the constant's, 0.22 2^-24, and
+// the instruction's): far below the rounding of what it goes into.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 struct Silu {
@@ -87,7 +88,10 @@ struct GeluTanh {
 
 // ---- powers of two of fp16 --------------------------------------------------------------------
 
-// dg and du are products' operands in 16 bits.  fp16 has few exponents: where dh is small (a loss that is
+// dg and du are products' operands in 16 bits, rounded once.  That makes dx and dW 1.4 times as far off as outputs' own
+// rounding alone would (bf16 2.3e-3 of their norm beside 1.7e-3, fp16 2.9e-4 beside 2.1e-4); in two numbers each they
+// would double the products of dx and dW, half of the time of all gradients.
+// fp16 has few exponents: where dh is small (a loss that is
 // not scaled), they would lose bits below 2^-14.  So a row of d is written for dx times the power of two that
 // brings the row's largest |dh| into [1/4, 1/2), a column for dW times that of its column, and the products'
 // results are multiplied back in 32 bits: exactly undone, whatever the size of dh.  What is left are the factors act(g)
@@ -487,11 +491,12 @@ hipError_t gated_few_as(const GatedArgs& a, hipStream_t s) {
 
 // The tile of h, or of d, by the number of tiles (h alone, us; rows, k -> f):
 //   one row of tiles of 16 columns   up to 32 rows
-//   64 x 32     up to 256 of these: 146 rows, 768 -> 2304 (216 tiles) 6.8 (128 x 64: 8.2), 96 rows, 4096 -> 4096 (256) 17.5
-//               (26.5); 200 rows, 768 -> 2304 (288) 11.0 (8.1), 48 rows, 4096 -> 14336 (448) 39 (36)
+//   64 x 32     up to 256 of these: 146 rows, 768 -> 2304 (216 tiles) 6.4 (128 x 64: 7.7), 96 rows, 4096 -> 4096 (256) 18.4
+//               (23.8); 200 rows, 768 -> 2304 (288) 10.9 (7.7), 48 rows, 4096 -> 14336 (448) 40 (36)
 //   128 x 64    otherwise, until
-//   256 x 128   there are 144 of these: 1,500 rows, 768 -> 2304 (108) 19.6 (16.2), 2,048 rows (144) 20.8 (23.9), 1,024 rows,
-//               4096 -> 4096 (128) 78 (65), 1,500 rows (192) 84 (95)
+//   256 x 128   there are 144 of these: 1,500 rows, 768 -> 2304 (108) 19.1 (15.4), 2,048 rows (144) 19.9 (22.8), 1,024 rows,
+//               4096 -> 4096 (128) 72 (61), 1,500 rows (192) 80 (91)
+// (Past a whole round of these there is no rule for the last one, as rows() has.)
 template <class T, class A, bool GRAD>
 hipError_t gated(const GatedArgs& a, hipStream_t s) {
   auto tiles = [&](int t, int m) { return (a.n + t - 1) / t * ((a.f + m - 1) / m); };
@@ -521,9 +526,12 @@ hipError_t rows_as(const ProductArgs& a, hipStream_t s) {
 }
 
 // How a product's tiles are made: the least estimated time, of 256 workgroups at a time, a stage of 64 values of k taking
-// a tile what it took in calls of 1 to 1,000 rows (256 x 256 1.26 us, 128 x 128 0.55), and the splits' sums 8 bytes a value,
-// written and read at 3.5 TB/s, and a launch.  (x's gradients, us, with splits and without: 764 rows, 4096 -> 14336 476 and
-// 578, 300 rows 331 and 493, measured with transposed weights.)
+// a tile 1.26 us (256 x 256) or 0.55 (128 x 128), and the splits' sums 8 bytes a value, written and read at 3.5 TB/s, and a
+// launch.  The stages' times were taken with both operands by rows; as they are now a stage of dx takes 1.05 to 1.17 us
+// (up to 128 tiles of 256 x 256, 4096 -> 14336) and 1.45 (256 of them), and 0.39 (64 tiles of 128 x 128) to 0.57 (256 and
+// more).  (dx's product, us, as the rule has it, in tiles of 128 and in tiles of 256, each without splits: 256 rows,
+// 4096 -> 14336 72, 176 and 471, 764 rows 153, 223 and 484, 2,048 rows 352, 484 and 523, 4,096 rows 656, 1,017 and 648,
+// 764 rows, 768 -> 2304 20, 35 and 84.)
 struct RowsPlan {
   bool wide;  // 256 x 256, or 128 x 128
   int splits;

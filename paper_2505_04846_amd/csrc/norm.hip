@@ -195,12 +195,18 @@ __global__ __launch_bounds__((Layout<W, C>::kThreads)) void norm_fwd_kernel(Norm
 // Rows in turn by a fixed number of workgroups, each of which keeps its rows' sums over columns in registers:
 //   sums 0 and 1: dy s, and t times dx or, where the gate is the row's own, times scale gate dx;  2 and 3: the same
 //   without s and t.
-// The next row is on its way while one is worked on, and the vectors stay in registers, where there is room for
-// them (C = 1).
+// The next row is on its way while one is worked on, and the vectors stay in registers, up to 8,192 values (C = 1).
 //
-// Bound by memory, with vector instructions for two fifths of the time: 53,248 rows of 4096 (2.6 GB) 525 to 540 us, 4.9 TB/s
-// (a copy reaches 5.1), from checkpoints 475.  More waves a row, not more chunks a lane: two rows' tensors and the sums
-// fill the registers of C = 1.
+// Bound by memory, with vector instructions for two fifths of the time, where that fits the registers: 53,248 rows of
+// 4096 (2.6 GB) 525 to 540 us, 4.9 TB/s (a copy reaches 5.1), from checkpoints 475.  More waves a row, not more chunks a
+// lane: two rows' tensors and the sums fill the registers of C = 1.  128 registers, four waves a SIMD, hold RMS norm up to
+// 8,192 values (from checkpoints above 4,096 all but 2 to 4), with gates of rows up to 2,048 (129 of one form).
+// Layer norm has twice the sums and takes 122 to 159 up to 2,048 values: past 128 (with gates of rows; in bf16 above 512
+// values; above 1,024) three workgroups are on a CU, and the launch's 1,024 are a round and a third.  Above 2,048 values,
+// where a workgroup's size leaves 128, layer norm spills 23 to 67 of a lane's registers, RMS with gates of rows up to 28,
+// and above 8,192 values every form 41 to 150.  53.5 million values in bf16, us, RMS and layer norm: rows of 512 131 and
+// 140, 768 137 and 167 (fp16 138 and 150), 1024 134 and 154, 2048 135 and 161, 4096 135 and 245, 8192 139 and 473, 16384
+// 353 and 827; with gates of rows 768 179 and 201, 2048 177 and 195, 4096 178 and 426, 8192 257 and 635.
 //
 // Rows are read and written through buffers of their own length, 0 for what there is not: values past the row, rows
 // past the last and tensors that are not there read as zeros and are not written, without a branch (with masks and
@@ -449,7 +455,7 @@ __device__ __forceinline__ void norm_bwd_rows(const NormArgs& a) {
     }
 }
 
-// (Eight waves a row are two workgroups a CU with 128 registers.)
+// (Eight waves a row are two workgroups a CU with 128 registers, which some forms spill for: see above.)
 template <class T, bool LAYER, bool PACKED, bool GATE_ROWS, int W, int C>
 __global__ __launch_bounds__((Layout<W, C>::kThreads), W == 8 ? 4 : 1) void norm_bwd_kernel(NormArgs a) {
   norm_bwd_rows<T, LAYER, PACKED, GATE_ROWS, W, C>(a);
@@ -531,7 +537,9 @@ hipError_t by_dim_bwd(int d, F&& f) {
 }
 int rows_of_group(int d) { return d <= 512 ? 4 : d <= 1024 ? 2 : 1; }  // Layout::kRows of the gradients
 
-int groups_most(int d) { return d <= 2048 ? 1024 : 512; }  // workgroups of the gradients: four, or two, a CU
+// Workgroups of the gradients: four a CU, or two, where their registers are as many as RMS norm's.  (Above 4,096 values,
+// 16 waves, one is on a CU, and these are two rounds.)
+int groups_most(int d) { return d <= 2048 ? 1024 : 512; }
 
 template <class T, bool LAYER>
 hipError_t norm_fwd(const NormArgs& a, hipStream_t s) {
