@@ -91,14 +91,13 @@ struct GeluTanh {
 // dg and du are products' operands in 16 bits, rounded once.  That makes dx and dW 1.4 times as far off as outputs' own
 // rounding alone would (bf16 2.3e-3 of their norm beside 1.7e-3, fp16 2.9e-4 beside 2.1e-4); in two numbers each they
 // would double the products of dx and dW, half of the time of all gradients.
-// fp16 has few exponents: where dh is small (a loss that is
-// not scaled), they would lose bits below 2^-14.  So a row of d is written for dx times the power of two that
-// brings the row's largest |dh| into [1/4, 1/2), a column for dW times that of its column, and the products'
-// results are multiplied back in 32 bits: exactly undone, whatever the size of dh.  What is left are the factors act(g)
-// and u act'(g).  Where g and u are numbers of fp16 they are at most 1.13 times 65504, and half of that is one too: no
-// larger power would do, whatever h is (g of 0.5 and u of 60,000 have h of 18,700 and u act'(g) of 44,400; brought to
-// [1, 2), as it was, dx of that row was infinite).  They overflow from 131,040 on, which g or u has to pass 65504
-// for, and lose bits below 2^-12, where h is about as small and fp16 rounds it as coarsely.
+// fp16 has few exponents: where dh is small (a loss that is not scaled), they would lose bits below 2^-14.  So a row of
+// d is written for dx times the power of two that brings the row's largest |dh| into [1/4, 1/2), a column for dW times
+// that of its column, and the products' results are multiplied back in 32 bits: exactly undone, whatever the size of
+// dh.  What is left are the factors act(g) and u act'(g).  Where g and u are numbers of fp16 these are at most 1.13 times
+// 65504, and half of that is a number of fp16 too; a larger power would not do, finite as h may be (g of 0.5 and u of
+// 60,000: h of 18,700, u act'(g) of 44,400, which [1, 2) makes infinite).  They overflow from 131,040 on, which g or u
+// passes 65504 for, and lose bits below 2^-12 (h, as a number of fp16, does below 2^-14).
 // bits: the largest |value| of fp16 as a whole number (max_kernel); 0 and infinities stay as they are.
 __device__ __forceinline__ int up_of(uint32_t bits) {
   if (bits == 0 || bits >= 0x7c00) return 0;
